@@ -272,6 +272,83 @@ int qnn_bconv2d_backward_weights(const float *g, const uint32_t *a_planes, int a
                                  size_t workspace_bytes, void *stream);
 
 /*
+ * Group-scaled 4-bit weights.  The layers above give a weight tensor ONE grid step; the calls below keep the same odd
+ * codes (Eq. 7 with 4 bits: q = 2t - 15, t = 0..15, plane i of q is bit i of t) but give every `group` consecutive
+ * weights of a row their own step, and leave the activations as real numbers.  Weight (j, i) of matrix e is
+ *   W_e[j][i] = alpha[e] * scale_e[j][i / group] * q_e[j][i],
+ * scale an 8-bit float (1 sign, 4 exponent, 3 mantissa bits, bias 7; finite, sign 0), alpha fp32.  A scale has 4
+ * significant bits and a code 4, so scale * q is exact in bf16 and in fp16: no kernel below rounds a weight.
+ *
+ * Storage, in tiles of 128 rows x 128 columns (TN = ceil(n/128), TK = ceil(k/128)), all padding 0:
+ *   codes   uint32 [experts][TN][TK][4 (c)][128 (row)][4 (w)]: the word holds t of the eight columns
+ *           128*tile + 32*w + 8*c + j, element j = 2p + h at bits 4p + 16h.  16-byte aligned.
+ *   scales  uint8 [experts][TN][TK][128 / group][128 (row)].  16-byte aligned.
+ *   alpha   fp32 [experts]
+ * group is 32, 64 or 128.  Sizes: n, k, experts in 1..65535*16, 1..65535*16, 1..65535.
+ *
+ * Element types of real operands: QNN_F32, QNN_BF16, QNN_F16.  Every product is accumulated in fp32 and rounded once to
+ * the result's type.  bf16 and fp16 operands enter exactly; an fp32 operand enters as the exact sum of three bf16 numbers
+ * (24 significant bits = 8 + 8 + 8), one tensor-core product each.
+ */
+#define QNN_F32 0
+#define QNN_BF16 1
+#define QNN_F16 2
+
+/* Bytes of the two arrays above (0 = arguments out of range). */
+size_t qnn_g4_codes_bytes(int experts, int n, int k);
+size_t qnn_g4_scales_bytes(int experts, int n, int k, int group);
+
+/*
+ * Real weights -> codes, scales, alpha.  Per matrix alpha = max|w| / (15 * 448); per group scale = max|w| / (15 * alpha)
+ * rounded to nearest even (448 is the largest scale); per weight the odd code nearest to w / (alpha * scale), a value
+ * half-way between two codes going to the one farther from zero, 0 to -1, values outside to the end codes, NaN to -15
+ * (the encoder's rules).  All in binary32.  A group whose scale rounds to 0 decodes to zeros.  Infinities give alpha =
+ * infinity and are not meaningful.
+ *   w   [experts][n][ldw] of `type`, ldw >= k, any alignment of its element size
+ */
+int qnn_g4_pack_weights(const void *w, int type, int experts, int n, int k, int64_t ldw, int group, uint32_t *codes,
+                        uint8_t *scales, float *alpha, void *stream);
+
+/*
+ * Few rows times one matrix: y[r][j] = sum_i x[r][i] * W[j][i].  The single-token form of a layer: it reads the codes
+ * once and is meant for up to about 32 rows; more rows give the right result but belong to qnn_g4_expert_gemm.
+ *   x  [rows][ldx] (ldx >= k), y [rows][ldy] (ldy >= n), both of `type`; rows = 0 is allowed and does nothing.
+ */
+int qnn_g4_matvec(const void *x, int type, int64_t rows, int64_t ldx, const uint32_t *codes, const uint8_t *scales,
+                  const float *alpha, int n, int k, int group, void *y, int64_t ldy, void *stream);
+
+/*
+ * Products grouped by expert.  Rows are sorted by expert: expert e owns rows offsets[e] .. offsets[e + 1] - 1
+ * (offsets: device int32 [experts + 1], not decreasing, read by the kernels only, so the split may change between
+ * replays of a captured call).  Experts may have no rows; rows in front of offsets[0] or from offsets[experts] on belong
+ * to nobody and their results are not written.  Offsets outside 0 .. rows are clamped.
+ *   forward           y[r][j]  = sum_i x[r][i] * W_e[j][i]             x [rows][ldx], y [rows][ldy]
+ *   backward_data     dx[r][i] = sum_j dy[r][j] * W_e[j][i]            dy [rows][lddy], dx [rows][lddx]
+ *   backward_weights  gw[e][j][i] = sum over e's rows of dy[r][j] * x[r][i]     gw fp32 [experts][n][k], fully written
+ *                     (zeros for an expert without rows): the gradient of W_e, which a straight-through training step
+ *                     applies to the real weights that were packed.
+ * rows = 0 is allowed (backward_weights then writes zeros).  rows < 2^31 / 256.
+ *   workspace  device scratch owned by the caller, 256-byte aligned, of at least qnn_g4_expert_*_workspace(...) bytes
+ *              (which may be 0; workspace may then be NULL).  It holds real operands that the tensor cores cannot read
+ *              where they lie: the three parts of fp32 rows, and rows whose address or stride is not a multiple of 16
+ *              bytes.  The query looks at the addresses for their alignment only.
+ * Waits inside the kernels are bounded and reported by qnn_tensor_path_status.
+ */
+size_t qnn_g4_expert_gemm_workspace(const void *x, int type, int64_t rows, int64_t ldx, int experts, int n, int k);
+int qnn_g4_expert_gemm(const void *x, int type, int64_t rows, int64_t ldx, const int32_t *offsets, int experts,
+                       const uint32_t *codes, const uint8_t *scales, const float *alpha, int n, int k, int group, void *y,
+                       int64_t ldy, void *workspace, size_t workspace_bytes, void *stream);
+size_t qnn_g4_expert_backward_data_workspace(const void *dy, int type, int64_t rows, int64_t lddy, int experts, int n, int k);
+int qnn_g4_expert_backward_data(const void *dy, int type, int64_t rows, int64_t lddy, const int32_t *offsets, int experts,
+                                const uint32_t *codes, const uint8_t *scales, const float *alpha, int n, int k, int group,
+                                void *dx, int64_t lddx, void *workspace, size_t workspace_bytes, void *stream);
+size_t qnn_expert_backward_weights_workspace(const void *dy, const void *x, int type, int64_t rows, int64_t lddy, int64_t ldx,
+                                             int experts, int n, int k);
+int qnn_expert_backward_weights(const void *dy, const void *x, int type, int64_t rows, int64_t lddy, int64_t ldx,
+                                const int32_t *offsets, int experts, int n, int k, float *gw, void *workspace,
+                                size_t workspace_bytes, void *stream);
+
+/*
  * Planes [rows][bits][qnn_row_words(k)] -> the odd codes q = sum_i 2^(i-1) * plane_i (Eq. 8) as fp32:
  * out[row*ld + col] (transpose = 0, ld >= k) or out[col*ld + row] (transpose != 0, ld >= rows).
  */

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 from pathlib import Path
+from typing import NamedTuple
 
 import torch
 
@@ -24,10 +25,15 @@ EXPORTS = [
     "qnn_mbit_encoder_backward", "qnn_bgemm_backward_data_workspace", "qnn_bgemm_backward_data",
     "qnn_bgemm_backward_weights_workspace", "qnn_bgemm_backward_weights", "qnn_bconv2d_backward_data_workspace",
     "qnn_bconv2d_backward_data", "qnn_bconv2d_backward_weights_workspace", "qnn_bconv2d_backward_weights", "qnn_unpack_codes_f32",
+    "qnn_g4_codes_bytes", "qnn_g4_scales_bytes", "qnn_g4_pack_weights", "qnn_g4_matvec", "qnn_g4_expert_gemm_workspace",
+    "qnn_g4_expert_gemm", "qnn_g4_expert_backward_data_workspace", "qnn_g4_expert_backward_data",
+    "qnn_expert_backward_weights_workspace", "qnn_expert_backward_weights",
     "qnn_tensor_path_status", "qnn_last_device_status", "qnn_selftest_bounded_wait", "qnn_bgemm_int8_tensor_workspace", "qnn_bgemm_int8_tensor",
     "qnn_absmax_f32", "qnn_fc_forward_host", "qnn_fc_forward_host_pipelined", "qnn_fc_forward_noalloc", "qnn_probe_bitops", "qnn_probe_naive_sgemm", "qnn_probe_copy", "qnn_popcounts_per_output",
 ]
 NOALLOC_SCRATCH_BYTES = 8 << 20
+F32, BF16, F16 = 0, 1, 2                      # element types of the real operands of the 4-bit-weight calls
+REAL_TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
 
 class QnnError(RuntimeError):
@@ -75,6 +81,21 @@ def _load() -> C.CDLL:
     lib.qnn_bconv2d_backward_weights_workspace.restype = sz
     lib.qnn_bconv2d_backward_weights_workspace.argtypes = [i] * 9
     lib.qnn_bconv2d_backward_weights.argtypes = [p, p, i] + [i] * 9 + [f, p, p, sz, p]
+    lib.qnn_g4_codes_bytes.restype = sz
+    lib.qnn_g4_codes_bytes.argtypes = [i, i, i]
+    lib.qnn_g4_scales_bytes.restype = sz
+    lib.qnn_g4_scales_bytes.argtypes = [i] * 4
+    lib.qnn_g4_pack_weights.argtypes = [p, i, i, i, i, i64, i, p, p, p, p]
+    lib.qnn_g4_matvec.argtypes = [p, i, i64, i64, p, p, p, i, i, i, p, i64, p]
+    lib.qnn_g4_expert_gemm_workspace.restype = sz
+    lib.qnn_g4_expert_gemm_workspace.argtypes = [p, i, i64, i64, i, i, i]
+    lib.qnn_g4_expert_gemm.argtypes = [p, i, i64, i64, p, i, p, p, p, i, i, i, p, i64, p, sz, p]
+    lib.qnn_g4_expert_backward_data_workspace.restype = sz
+    lib.qnn_g4_expert_backward_data_workspace.argtypes = [p, i, i64, i64, i, i, i]
+    lib.qnn_g4_expert_backward_data.argtypes = [p, i, i64, i64, p, i, p, p, p, i, i, i, p, i64, p, sz, p]
+    lib.qnn_expert_backward_weights_workspace.restype = sz
+    lib.qnn_expert_backward_weights_workspace.argtypes = [p, p, i, i64, i64, i64, i, i, i]
+    lib.qnn_expert_backward_weights.argtypes = [p, p, i, i64, i64, i64, p, i, i, i, p, p, sz, p]
     lib.qnn_tensor_path_status.argtypes = [C.POINTER(C.c_uint)]
     lib.qnn_last_device_status.argtypes = [C.POINTER(C.c_uint)]
     lib.qnn_selftest_bounded_wait.argtypes = [u, p]
@@ -339,6 +360,169 @@ def bconv2d_backward_weights(g: torch.Tensor, a_planes: torch.Tensor, ab: int, H
     _check(lib.qnn_bconv2d_backward_weights(_ptr(g), _ptr(a_planes), ab, N, H, W, C, Cout, R, S, stride, pad, float(alpha),
                                             _ptr(gw), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)),
            "qnn_bconv2d_backward_weights")
+    return gw
+
+
+class G4Weights(NamedTuple):
+    """Group-scaled 4-bit weights of one matrix or of several experts' (the storage of include/qnn.h)."""
+    codes: torch.Tensor      # int32 [experts, ceil(n/128), ceil(k/128), 4, 128, 4]
+    scales: torch.Tensor     # uint8 [experts, ceil(n/128), ceil(k/128), 128 // group, 128], 1-4-3 floats
+    alpha: torch.Tensor      # fp32 [experts]
+    n: int                   # output features
+    k: int                   # reduction length
+    group: int               # weights of a row that share a scale: 32, 64 or 128
+
+
+def _real_rows(t: torch.Tensor, width: int, name: str) -> int:
+    """Checks a [rows, width] operand whose rows may be strided; returns its type code."""
+    if t.dim() != 2 or t.shape[1] != width:
+        raise ValueError(f"{name} must be [rows, {width}]")
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current CUDA device")
+    if t.stride(1) != 1 and width > 1 and t.shape[0] > 0 or t.stride(0) < width and t.shape[0] > 1:
+        raise ValueError(f"{name} must have contiguous rows that do not overlap")
+    code = REAL_TYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16")
+    return code
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _g4_check(w: G4Weights, device: torch.device) -> int:
+    """Checks the three arrays of a handle against its sizes; returns the number of matrices."""
+    if w.group not in (32, 64, 128):
+        raise ValueError("group must be 32, 64 or 128")
+    shape = w.codes.shape
+    if (w.codes.dtype is not torch.int32 or w.scales.dtype is not torch.uint8 or w.alpha.dtype is not torch.float32
+            or not w.codes.is_contiguous() or not w.scales.is_contiguous() or not w.alpha.is_contiguous()):
+        raise ValueError("codes, scales and alpha must be contiguous int32, uint8 and float32")
+    tiles = ((w.n + 127) // 128, (w.k + 127) // 128)
+    if len(shape) != 6 or shape[1:] != tiles + (4, 128, 4):
+        raise ValueError("codes do not have the shape of an n x k matrix")
+    if w.scales.shape != (shape[0],) + tiles + (128 // w.group, 128) or w.alpha.shape != (shape[0],):
+        raise ValueError("scales or alpha do not have the shape that goes with the codes")
+    if w.codes.device != device or w.scales.device != device or w.alpha.device != device:
+        raise ValueError("the weights must be on the device of the rows")
+    return shape[0]
+
+
+def _expert_offsets(offsets: torch.Tensor, device: torch.device) -> int:
+    if offsets.dtype is not torch.int32 or offsets.dim() != 1 or not offsets.is_contiguous() or offsets.device != device:
+        raise ValueError("offsets must be contiguous int32 [experts + 1] on the device of the rows")
+    if offsets.shape[0] < 2:
+        raise ValueError("offsets must have experts + 1 entries")
+    return offsets.shape[0] - 1
+
+
+def _out_rows(out, rows: int, width: int, like: torch.Tensor, name: str, stream):
+    """A given result is checked; a missing one is allocated for the stream that will write it."""
+    if out is None:
+        return _on_stream(stream, lambda: torch.empty((rows, width), dtype=like.dtype, device=like.device))
+    if out.dtype is not like.dtype or out.shape[0] != rows:
+        raise ValueError(f"{name} must be [{rows}, {width}] {like.dtype}")
+    _real_rows(out, width, name)
+    return out
+
+
+def _on_stream(stream, make):
+    """Runs an allocation so that its memory belongs to `stream` (a block freed early is then reused in that stream's order)."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        return make()
+
+
+def _scratch(nbytes: int, device, workspace, stream):
+    if nbytes == 0 or workspace is not None:
+        return workspace
+    return _on_stream(stream, lambda: torch.empty(nbytes, dtype=torch.uint8, device=device))
+
+
+def _scratch_bytes(ws) -> int:
+    return 0 if ws is None else ws.numel() * ws.element_size()
+
+
+def g4_pack_weights(w: torch.Tensor, group: int = 128, stream=None) -> G4Weights:
+    """Real weights [n, k] or [experts, n, k] -> 4-bit odd codes with a scale for every `group` weights of a row."""
+    if w.dim() not in (2, 3) or not w.is_cuda or w.dtype not in REAL_TYPES or not w.is_contiguous():
+        raise ValueError("w must be a contiguous CUDA tensor [n, k] or [experts, n, k] of float32, bfloat16 or float16")
+    n, k = w.shape[-2:]
+    experts = w.shape[0] if w.dim() == 3 else 1
+    if group not in (32, 64, 128) or experts < 1 or n < 1 or k < 1:
+        raise QnnError(E_ARG, "qnn_g4_pack_weights")
+    shape = (experts, (n + 127) // 128, (k + 127) // 128)
+    codes, scales, alpha = _on_stream(stream, lambda: (
+        torch.empty(shape + (4, 128, 4), dtype=torch.int32, device=w.device),
+        torch.empty(shape + (128 // group, 128), dtype=torch.uint8, device=w.device),
+        torch.empty(experts, dtype=torch.float32, device=w.device)))
+    _check(lib.qnn_g4_pack_weights(_ptr(w), REAL_TYPES[w.dtype], experts, n, k, k, group, _ptr(codes), _ptr(scales), _ptr(alpha),
+                                   _stream(stream)), "qnn_g4_pack_weights")
+    return G4Weights(codes, scales, alpha, n, k, group)
+
+
+def g4_matvec(x: torch.Tensor, w: G4Weights, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """x [rows, k] (few rows; their stride is free) times one 4-bit matrix -> [rows, n] of x's type."""
+    code = _real_rows(x, w.k, "x")
+    if _g4_check(w, x.device) != 1:
+        raise ValueError("g4_matvec takes one matrix")
+    out = _out_rows(out, x.shape[0], w.n, x, "out", stream)
+    _check(lib.qnn_g4_matvec(_ptr(x), code, x.shape[0], _row_stride(x), _ptr(w.codes), _ptr(w.scales), _ptr(w.alpha), w.n, w.k,
+                             w.group, _ptr(out), _row_stride(out), _stream(stream)), "qnn_g4_matvec")
+    return out
+
+
+def g4_expert_gemm(x: torch.Tensor, w: G4Weights, offsets: torch.Tensor, out: torch.Tensor | None = None,
+                   workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """x [rows, k], rows sorted by expert (expert e owns rows offsets[e] .. offsets[e+1]) -> [rows, n] of x's type."""
+    code = _real_rows(x, w.k, "x")
+    experts, rows, ldx = _g4_check(w, x.device), x.shape[0], _row_stride(x)
+    if _expert_offsets(offsets, x.device) != experts:
+        raise ValueError("offsets must have experts + 1 entries")
+    out = _out_rows(out, rows, w.n, x, "out", stream)
+    need = lib.qnn_g4_expert_gemm_workspace(_ptr(x), code, rows, ldx, experts, w.n, w.k)
+    ws = _scratch(need, x.device, workspace, stream)
+    _check(lib.qnn_g4_expert_gemm(_ptr(x), code, rows, ldx, _ptr(offsets), experts, _ptr(w.codes), _ptr(w.scales), _ptr(w.alpha),
+                                  w.n, w.k, w.group, _ptr(out), _row_stride(out), _ptr(ws), _scratch_bytes(ws),
+                                  _stream(stream)), "qnn_g4_expert_gemm")
+    return out
+
+
+def g4_expert_gemm_backward_data(dy: torch.Tensor, w: G4Weights, offsets: torch.Tensor, out: torch.Tensor | None = None,
+                                 workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Gradient of g4_expert_gemm with respect to x: dy [rows, n] -> [rows, k] of dy's type."""
+    code = _real_rows(dy, w.n, "dy")
+    experts, rows, lddy = _g4_check(w, dy.device), dy.shape[0], _row_stride(dy)
+    if _expert_offsets(offsets, dy.device) != experts:
+        raise ValueError("offsets must have experts + 1 entries")
+    out = _out_rows(out, rows, w.k, dy, "out", stream)
+    need = lib.qnn_g4_expert_backward_data_workspace(_ptr(dy), code, rows, lddy, experts, w.n, w.k)
+    ws = _scratch(need, dy.device, workspace, stream)
+    _check(lib.qnn_g4_expert_backward_data(_ptr(dy), code, rows, lddy, _ptr(offsets), experts, _ptr(w.codes), _ptr(w.scales),
+                                           _ptr(w.alpha), w.n, w.k, w.group, _ptr(out), _row_stride(out), _ptr(ws),
+                                           _scratch_bytes(ws), _stream(stream)), "qnn_g4_expert_backward_data")
+    return out
+
+
+def expert_gemm_backward_weights(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Tensor, gw: torch.Tensor | None = None,
+                                 workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Gradient of g4_expert_gemm with respect to the decoded weights: dy [rows, n], x [rows, k] -> fp32 [experts, n, k]."""
+    n, k = dy.shape[-1], x.shape[-1]
+    code = _real_rows(dy, n, "dy")
+    if _real_rows(x, k, "x") != code or x.shape[0] != dy.shape[0]:
+        raise ValueError("dy and x must have the same type and number of rows")
+    experts, rows = _expert_offsets(offsets, dy.device), x.shape[0]
+    if gw is None:
+        gw = _on_stream(stream, lambda: torch.empty((experts, n, k), dtype=torch.float32, device=dy.device))
+    elif _dev(gw, torch.float32, "gw").shape != (experts, n, k):
+        raise ValueError("gw must be [experts, n, k]")
+    lddy, ldx = _row_stride(dy), _row_stride(x)
+    need = lib.qnn_expert_backward_weights_workspace(_ptr(dy), _ptr(x), code, rows, lddy, ldx, experts, n, k)
+    ws = _scratch(need, dy.device, workspace, stream)
+    _check(lib.qnn_expert_backward_weights(_ptr(dy), _ptr(x), code, rows, lddy, ldx, _ptr(offsets), experts, n, k, _ptr(gw),
+                                           _ptr(ws), _scratch_bytes(ws), _stream(stream)), "qnn_expert_backward_weights")
     return gw
 
 
