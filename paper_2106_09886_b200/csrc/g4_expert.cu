@@ -1,5 +1,5 @@
 // Products with group-scaled 4-bit weights, grouped by expert: entry points and kernels.
-#include "g4_format.cuh"
+#include "g4_rows.cuh"
 
 namespace {
 
@@ -114,7 +114,7 @@ extern "C" int qnn_g4_matvec(const void *x, int type, int64_t rows, int64_t ldx,
     if (rc == QNN_OK) rc = check_rows(y, type, rows, ldy, n);
     if (rc != QNN_OK || rows == 0) return rc;
     const G4Weights w{codes, scales, alpha, n, k, group, g4_tiles(n), g4_tiles(k)};
-    return by_type<0>(type, x, ldx, nullptr, 0, rows, nullptr, 1, w, y, ldy, static_cast<cudaStream_t>(stream));
+    return qnn_g4_rows(x, type, ldx, (int)rows, nullptr, 1, w, y, ldy, rows < 32 ? (int)rows : 32, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" size_t qnn_g4_expert_gemm_workspace(const void *, int, int64_t, int64_t, int, int, int) { return 0; }
@@ -130,6 +130,8 @@ extern "C" int qnn_g4_expert_gemm(const void *x, int type, int64_t rows, int64_t
     if (rc == QNN_OK) rc = check_workspace(workspace, workspace_bytes, qnn_g4_expert_gemm_workspace(x, type, rows, ldx, experts, n, k));
     if (rc != QNN_OK || rows == 0) return rc;
     const G4Weights w{codes, scales, alpha, n, k, group, g4_tiles(n), g4_tiles(k)};
+    if (rows <= 8 * (int64_t)experts)
+        return qnn_g4_rows(x, type, ldx, (int)rows, offsets, experts, w, y, ldy, 8, static_cast<cudaStream_t>(stream));
     return by_type<0>(type, x, ldx, nullptr, 0, rows, offsets, experts, w, y, ldy, static_cast<cudaStream_t>(stream));
 }
 
