@@ -284,7 +284,7 @@ int qnn_bconv2d_backward_weights(const float *g, const uint32_t *a_planes, int a
  *           128*tile + 32*w + 8*c + j, element j = 2p + h at bits 4p + 16h.  16-byte aligned.
  *   scales  uint8 [experts][TN][TK][128 / group][128 (row)].  16-byte aligned.
  *   alpha   fp32 [experts]
- * group is 32, 64 or 128.  Sizes: n, k, experts in 1..65535*16, 1..65535*16, 1..65535.
+ * group is 32, 64 or 128; n and k are at most 65535*16, experts at most 4096.
  *
  * Element types of real operands: QNN_F32, QNN_BF16, QNN_F16.  Every product is accumulated in fp32 and rounded once to
  * the result's type.  bf16 and fp16 operands enter exactly; an fp32 operand enters as the exact sum of three bf16 numbers

@@ -1,5 +1,6 @@
 // Products with group-scaled 4-bit weights, grouped by expert: entry points and kernels.
-#include "g4_rows.cuh"
+#include "g4_stage.cuh"
+#include "g4_tensor_api.cuh"
 
 namespace {
 
@@ -117,7 +118,13 @@ extern "C" int qnn_g4_matvec(const void *x, int type, int64_t rows, int64_t ldx,
     return qnn_g4_rows(x, type, ldx, (int)rows, nullptr, 1, w, y, ldy, rows < 32 ? (int)rows : 32, static_cast<cudaStream_t>(stream));
 }
 
-extern "C" size_t qnn_g4_expert_gemm_workspace(const void *, int, int64_t, int64_t, int, int, int) { return 0; }
+// Few rows for each expert: the form that reads the codes once for a handful of rows and splits the contraction.
+static bool g4_few_rows(int64_t rows, int experts) { return rows <= 8 * (int64_t)experts; }
+
+extern "C" size_t qnn_g4_expert_gemm_workspace(const void *x, int type, int64_t rows, int64_t ldx, int experts, int n, int k) {
+    if (!g4_type_ok(type) || !g4_dims_ok(experts, n, k) || rows <= 0 || rows >= G4_MAX_ROWS) return 0;
+    return g4_few_rows(rows, experts) || g4_rows_in_place(x, type, ldx) ? 0 : g4_staged_bytes(type, rows, k);
+}
 
 extern "C" int qnn_g4_expert_gemm(const void *x, int type, int64_t rows, int64_t ldx, const int32_t *offsets, int experts,
                                   const uint32_t *codes, const uint8_t *scales, const float *alpha, int n, int k, int group,
@@ -130,12 +137,19 @@ extern "C" int qnn_g4_expert_gemm(const void *x, int type, int64_t rows, int64_t
     if (rc == QNN_OK) rc = check_workspace(workspace, workspace_bytes, qnn_g4_expert_gemm_workspace(x, type, rows, ldx, experts, n, k));
     if (rc != QNN_OK || rows == 0) return rc;
     const G4Weights w{codes, scales, alpha, n, k, group, g4_tiles(n), g4_tiles(k)};
-    if (rows <= 8 * (int64_t)experts)
-        return qnn_g4_rows(x, type, ldx, (int)rows, offsets, experts, w, y, ldy, 8, static_cast<cudaStream_t>(stream));
-    return by_type<0>(type, x, ldx, nullptr, 0, rows, offsets, experts, w, y, ldy, static_cast<cudaStream_t>(stream));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (g4_few_rows(rows, experts)) return qnn_g4_rows(x, type, ldx, (int)rows, offsets, experts, w, y, ldy, 8, st);
+    const G4TensorArgs a{w, offsets, experts, (int)rows, y, ldy};
+    if (g4_rows_in_place(x, type, ldx)) return qnn_g4_tensor_fwd(x, type, ldx, a, st);
+    rc = qnn_stage_rows(x, type, ldx, (int)rows, k, workspace, st);
+    return rc != QNN_OK ? rc : qnn_g4_tensor_fwd(workspace, type, g4_padded_width(k), a, st);
 }
 
-extern "C" size_t qnn_g4_expert_backward_data_workspace(const void *, int, int64_t, int64_t, int, int, int) { return 0; }
+extern "C" size_t qnn_g4_expert_backward_data_workspace(const void *dy, int type, int64_t rows, int64_t lddy, int experts, int n,
+                                                        int k) {
+    if (!g4_type_ok(type) || !g4_dims_ok(experts, n, k) || rows <= 0 || rows >= G4_MAX_ROWS) return 0;
+    return g4_rows_in_place(dy, type, lddy) ? 0 : g4_staged_bytes(type, rows, n);
+}
 
 extern "C" int qnn_g4_expert_backward_data(const void *dy, int type, int64_t rows, int64_t lddy, const int32_t *offsets,
                                            int experts, const uint32_t *codes, const uint8_t *scales, const float *alpha, int n,
@@ -150,7 +164,11 @@ extern "C" int qnn_g4_expert_backward_data(const void *dy, int type, int64_t row
         rc = check_workspace(workspace, workspace_bytes, qnn_g4_expert_backward_data_workspace(dy, type, rows, lddy, experts, n, k));
     if (rc != QNN_OK || rows == 0) return rc;
     const G4Weights w{codes, scales, alpha, n, k, group, g4_tiles(n), g4_tiles(k)};
-    return by_type<1>(type, dy, lddy, nullptr, 0, rows, offsets, experts, w, dx, lddx, static_cast<cudaStream_t>(stream));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const G4TensorArgs a{w, offsets, experts, (int)rows, dx, lddx};
+    if (g4_rows_in_place(dy, type, lddy)) return qnn_g4_tensor_data(dy, type, lddy, a, st);
+    rc = qnn_stage_rows(dy, type, lddy, (int)rows, n, workspace, st);
+    return rc != QNN_OK ? rc : qnn_g4_tensor_data(workspace, type, g4_padded_width(n), a, st);
 }
 
 extern "C" size_t qnn_expert_backward_weights_workspace(const void *, const void *, int, int64_t, int64_t, int64_t, int, int, int) {

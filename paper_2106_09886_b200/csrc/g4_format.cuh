@@ -10,6 +10,7 @@ constexpr int G4_TILE = 128;                       // rows and columns of a stor
 constexpr int G4_TILE_WORDS = 128 * 128 / 8;       // its codes: 8 KB
 constexpr float G4_SCALE_MAX = 448.0f;             // largest 1-4-3 float
 constexpr int G4_MAX_DIM = 65535 * 16;
+constexpr int G4_MAX_EXPERTS = 4096;               // blocks of rows stay countable in 31 bits whatever the offsets hold
 constexpr int64_t G4_MAX_ROWS = (1ll << 31) / 256; // row tiles stay far inside 32-bit tile arithmetic
 
 struct G4Weights {
@@ -23,7 +24,7 @@ struct G4Weights {
 static inline bool g4_type_ok(int t) { return t == QNN_F32 || t == QNN_BF16 || t == QNN_F16; }
 static inline int g4_type_bytes(int t) { return t == QNN_F32 ? 4 : 2; }
 static inline bool g4_dims_ok(int experts, int n, int k) {
-    return experts >= 1 && experts <= 65535 && n >= 1 && n <= G4_MAX_DIM && k >= 1 && k <= G4_MAX_DIM;
+    return experts >= 1 && experts <= G4_MAX_EXPERTS && n >= 1 && n <= G4_MAX_DIM && k >= 1 && k <= G4_MAX_DIM;
 }
 static inline bool g4_group_ok(int g) { return g == 32 || g == 64 || g == 128; }
 static inline int g4_tiles(int v) { return (v + G4_TILE - 1) / G4_TILE; }

@@ -1,0 +1,576 @@
+// Products grouped by expert on the fifth-generation tensor cores: result = weights x rows, accumulated in tensor memory
+// with the weight features as the 128 lanes of an accumulator and the rows (tokens) as its columns, so that a stored
+// 128 x 128 tile of codes is unpacked once and multiplied with up to 256 tokens, and a ragged number of tokens only
+// narrows the columns.
+//
+//   G4_FWD   y[r][j]  = alpha sum_i W[j][i] x[r][i]:  lanes j, contraction over i.  A thread owns a lane and unpacks the
+//            64 codes of its row straight into the A operand in tensor memory: no shared-memory round trip, one group
+//            scale per thread.
+//   G4_DATA  dx[r][i] = alpha sum_j W[j][i] dy[r][j]: lanes i, contraction over j.  The same stored tile is needed
+//            transposed; it is unpacked row by row into shared memory and read as an MN-major operand, which transposes.
+//
+// W / alpha = scale * (2t - 15) has at most 8 significant bits: exact in bf16 and fp16, so the only roundings are the
+// fp32 additions and the last one to the result's type.  fp32 rows come as three bf16 parts; A is unpacked once for them.
+//
+// CG = 2: a pair of thread blocks (cluster) works on 256 lanes x TN tokens with cta_group::2 instructions, each block
+// holding its 128 lanes of weights and half of the tokens, which halves what is read per product.
+#pragma once
+#include "tc_ptx.cuh"
+#include "g4_rows.cuh"
+
+namespace {
+
+enum G4Mode { G4_FWD = 0, G4_DATA = 1 };
+
+template <class T> struct G4Type;                       // operand type, parts of a row, instruction-descriptor format
+template <> struct G4Type<float> { typedef __nv_bfloat16 Op; static constexpr int PARTS = 3; static constexpr uint32_t FMT = 1; };
+template <> struct G4Type<__nv_bfloat16> { typedef __nv_bfloat16 Op; static constexpr int PARTS = 1; static constexpr uint32_t FMT = 1; };
+template <> struct G4Type<__half> { typedef __half Op; static constexpr int PARTS = 1; static constexpr uint32_t FMT = 0; };
+
+// ------------------------------------------------------------------------------------------------ pair-aware PTX
+
+template <int CG> __device__ __forceinline__ uint32_t pair_rank() {
+    uint32_t r = 0;
+    if constexpr (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+template <int CG> __device__ __forceinline__ void pair_sync() {       // every thread of both blocks
+    if constexpr (CG == 1) {
+        __syncthreads();
+    } else {
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+}
+// Address of the leading block's copy of a barrier (the two blocks lay out their shared memory alike).
+template <int CG> __device__ __forceinline__ uint32_t leader_addr(const void *p) {
+    uint32_t a = smem_u32(p);
+    if constexpr (CG == 2) asm volatile("mapa.shared::cluster.u32 %0, %0, 0;" : "+r"(a));
+    return a;
+}
+template <int CG> __device__ __forceinline__ void arrive_leader(uint64_t *bar) {
+    if constexpr (CG == 1)
+        asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+    else
+        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_addr<2>(bar)) : "memory");
+}
+__device__ __forceinline__ void arrive_local(uint64_t *bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t *bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+    return ok != 0;
+}
+// mbar_wait for barriers on which the other block's threads arrive.
+template <int CG>
+__device__ __forceinline__ bool pair_wait(uint64_t *bar, uint32_t parity, volatile uint32_t *abort_flag, unsigned id,
+                                          unsigned int *err, uint32_t limit) {
+    if constexpr (CG == 1) {
+        return mbar_wait(bar, parity, abort_flag, id, err, limit);
+    } else {
+        for (uint32_t it = 0; it < limit; ++it) {
+            if (mbar_try_wait_cluster(bar, parity)) return true;
+            if ((it & 1023u) == 1023u && *abort_flag) return false;
+        }
+        *abort_flag = 1;
+        atomicCAS(err, 0u, 1u + id);
+        return false;
+    }
+}
+// 2-D box into this block's shared memory, its bytes counted on the leading block's barrier.
+template <int CG>
+__device__ __forceinline__ void pair_load_2d(void *dst, const CUtensorMap *map, uint64_t *bar, int x, int y) {
+    if constexpr (CG == 1)
+        tma_load_2d(dst, map, bar, x, y);
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+            ::"r"(smem_u32(dst)), "l"(map), "r"(leader_addr<2>(bar)), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
+template <int CG> __device__ __forceinline__ void pair_tmem_alloc(uint32_t *slot, uint32_t ncols) {   // one whole warp per block
+    if constexpr (CG == 1) {
+        tmem_alloc(slot, ncols);
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(ncols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+}
+template <int CG> __device__ __forceinline__ void pair_tmem_dealloc(uint32_t taddr, uint32_t ncols) {
+    if constexpr (CG == 1) tmem_dealloc(taddr, ncols);
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
+}
+// Arrives on the barrier (of both blocks) when the instructions issued so far have completed.
+template <int CG> __device__ __forceinline__ void pair_commit(uint64_t *bar) {
+    if constexpr (CG == 1)
+        tc_commit(bar);
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
+}
+// D (+)= A * B^T, 16 steps of the contraction; A in tensor memory (TS) or shared memory (SS), B in shared memory.
+template <int CG>
+__device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    if constexpr (CG == 1)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                     ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                     ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void mma_f16_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    if constexpr (CG == 1)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// 32 columns of this thread's lane.
+__device__ __forceinline__ void tmem_store_32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+        ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+          "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+          "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
+        : "memory");
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
+// Shared-memory descriptor of an MN-major tile with the 128-byte swizzle: blocks of 64 elements of the M (or N) dimension
+// (128 bytes) x the contraction's rows; rows in groups of 8 (1024 bytes apart, the stride offset), the next 64 elements
+// `block_bytes` further (the leading offset).  16 steps of the contraction are 2048 bytes.
+__device__ __forceinline__ uint64_t smem_desc_mn_sw128(uint32_t saddr, uint32_t block_bytes) {
+    return (uint64_t)((saddr >> 4) & 0x3FFFu) | ((uint64_t)(block_bytes >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+// Instruction descriptor of kind::f16 with fp32 accumulation: formats (0 fp16, 1 bf16) at bits 7 and 10, transposition of
+// A and B (MN-major) at bits 15 and 16, N/8 at bit 17, M/16 at bit 24.
+__host__ __device__ constexpr uint32_t idesc_f16(uint32_t fmt, int m, int n, bool a_mn, bool b_mn) {
+    return (1u << 4) | (fmt << 7) | (fmt << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
+           ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+
+struct Ring {                                            // position in a ring of stages and the parity of its round
+    int s = 0;
+    uint32_t ph = 0;
+    __device__ __forceinline__ void next(int stages) {
+        if (++s == stages) { s = 0; ph ^= 1u; }
+    }
+};
+
+// Blocks of TN rows, counted expert by expert, visited in increasing order by a whole warp.
+struct SlotCursor {
+    const int32_t *offsets;
+    int experts, rows, tile;
+    int base = 0, before = 0, a = 0, b = 0, mine = 0, incl = 0;
+    __device__ __forceinline__ SlotCursor(const int32_t *o, int e, int r, int t) : offsets(o), experts(e), rows(r), tile(t) { load(); }
+    __device__ __forceinline__ void load() {
+        const int lane = threadIdx.x & 31;
+        a = b = 0;
+        if (base + lane < experts) expert_rows(offsets, base + lane, rows, a, b);
+        mine = b > a ? (b - a + tile - 1) / tile : 0;
+        incl = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, incl, d);
+            if (lane >= d) incl += o;
+        }
+    }
+    __device__ __forceinline__ ExpertSlot seek(int slot) {
+        while (base < experts) {
+            const unsigned hit = __ballot_sync(0xffffffffu, slot < before + incl);
+            if (hit) {
+                const int src = __ffs(hit) - 1;
+                const int first = __shfl_sync(0xffffffffu, a, src) + (slot - before - __shfl_sync(0xffffffffu, incl - mine, src)) * tile;
+                return {base + src, first, min(__shfl_sync(0xffffffffu, b, src), first + tile)};
+            }
+            before += __shfl_sync(0xffffffffu, incl, 31);
+            base += 32;
+            if (base < experts) load();
+        }
+        return {-1, 0, 0};
+    }
+};
+
+struct G4TensorParams {
+    G4Weights w;
+    const int32_t *offsets;
+    int experts, rows;
+    void *out;
+    int64_t ldo;
+    int features;                         // width of the result
+    int ftiles;                           // tiles of 128 * CG features
+    int steps;                            // stored tiles along the contraction
+    unsigned int *err;
+    unsigned int wait_limit;
+};
+
+constexpr int G4_THREADS = 512;           // warps: 0 rows by TMA, 1 matrix instructions, 2 codes by bulk copies (and owner of
+                                          // the tensor memory), 3 idle, 4-7 results, 8-15 unpacking
+constexpr int G4_UNPACK_WARPS = 8;
+
+template <int CG, int TN, int MODE>
+struct G4Shape {
+    static constexpr int XROWS = TN / CG;                       // tokens whose rows this block stages
+    static constexpr int X_SUB = XROWS * 128;                   // 64 columns of them, 128-byte swizzle
+    static constexpr int X_STAGE = 2 * X_SUB;                   // a stored tile's 128
+    static constexpr int C_STAGE = G4_TILE_WORDS * 4 + 512;     // codes and up to four rows of scales
+    static constexpr int A_STAGE = MODE == G4_DATA ? 128 * 128 * 2 : 0;
+    static constexpr int A_SMEM_STAGES = 2;
+    static constexpr int ACC_BUFS = TN <= 128 ? 2 : 1;
+    static constexpr int A_STAGES = MODE == G4_DATA ? A_SMEM_STAGES : 4;     // (64 tensor-memory columns each)
+    static constexpr int C_STAGES = 4;
+    static constexpr int FIXED = C_STAGES * C_STAGE + (MODE == G4_DATA ? A_SMEM_STAGES * A_STAGE : 0);
+    static constexpr int X_FIT = (220 * 1024 - FIXED) / X_STAGE;
+    static constexpr int X_STAGES = X_FIT > 8 ? 8 : X_FIT;
+    static constexpr int X_OFF = 0;
+    static constexpr int A_OFF = X_STAGES * X_STAGE;
+    static constexpr int C_OFF = A_OFF + (MODE == G4_DATA ? A_SMEM_STAGES * A_STAGE : 0);
+    static constexpr int BAR_OFF = C_OFF + C_STAGES * C_STAGE;
+    static constexpr int TOTAL = BAR_OFF + (2 * (X_STAGES + C_STAGES + A_STAGES) + 4) * 8 + 16 + 1024;
+    static constexpr int ACC_COLS = ACC_BUFS * TN;
+    static_assert(ACC_COLS + (MODE == G4_FWD ? 64 * A_STAGES : 0) <= 512, "tensor memory");
+    static_assert(X_STAGES >= 2 && TOTAL <= 227 * 1024, "shared memory");
+};
+
+// Eight codes of a word -> four packed pairs of scale * q.
+template <class Op>
+__device__ __forceinline__ void unpack_word(uint32_t word, uint32_t scale2, uint32_t *out) {
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const uint32_t s = p == 0 ? word << 3 : word >> (4 * p - 3);
+        if constexpr (std::is_same<Op, __half>::value) {
+            const uint32_t u = (s & 0x00780078u) | 0x64006400u;                       // 1024 + 8t
+            __half2 v = __hfma2(*reinterpret_cast<const __half2 *>(&u), __half2half2(__ushort_as_half(0x3400)),
+                                __half2half2(__ushort_as_half(0xDC3C)));              // * 0.25 - 271 = 2t - 15
+            v = __hmul2(v, *reinterpret_cast<const __half2 *>(&scale2));
+            out[p] = *reinterpret_cast<const uint32_t *>(&v);
+        } else {
+            const uint32_t u = (s & 0x00780078u) | 0x3F803F80u;                       // 1 + t/16
+            __nv_bfloat162 v = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&u), __bfloat162bfloat162(__ushort_as_bfloat16(0x4200)),
+                                       __bfloat162bfloat162(__ushort_as_bfloat16(0xC23C)));   // * 32 - 47 = 2t - 15
+            v = __hmul2(v, *reinterpret_cast<const __nv_bfloat162 *>(&scale2));
+            out[p] = *reinterpret_cast<const uint32_t *>(&v);
+        }
+    }
+}
+template <class Op> __device__ __forceinline__ uint32_t scale_pair(uint8_t b) {
+    if constexpr (std::is_same<Op, __half>::value) {
+        const __half2 v = __float2half2_rn(g4_scale_f32(b));
+        return *reinterpret_cast<const uint32_t *>(&v);
+    } else {
+        const __nv_bfloat162 v = __float2bfloat162_rn(g4_scale_f32(b));
+        return *reinterpret_cast<const uint32_t *>(&v);
+    }
+}
+
+template <int CG, int TN, int MODE, class T>
+__global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_constant__ CUtensorMap map_x, const G4TensorParams p) {
+    using L = G4Shape<CG, TN, MODE>;
+    using Op = typename G4Type<T>::Op;
+    constexpr int PARTS = G4Type<T>::PARTS;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint64_t *x_full = reinterpret_cast<uint64_t *>(smem + L::BAR_OFF);     // leader: both blocks' rows have landed
+    uint64_t *x_empty = x_full + L::X_STAGES;                               // each block: the instructions have read them
+    uint64_t *c_full = x_empty + L::X_STAGES;                               // each block: its codes have landed
+    uint64_t *c_empty = c_full + L::C_STAGES;
+    uint64_t *a_full = c_empty + L::C_STAGES;                               // leader: both blocks have unpacked a tile
+    uint64_t *a_empty = a_full + L::A_STAGES;
+    uint64_t *acc_full = a_empty + L::A_STAGES;                             // each block
+    uint64_t *acc_empty = acc_full + 2;                                     // leader: both blocks have read an accumulator out
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(acc_empty + 2);
+    volatile uint32_t *abort_flag = tmem_slot + 1;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = (int)pair_rank<CG>();
+    const int first_work = blockIdx.x / CG, work_stride = gridDim.x / CG;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < L::X_STAGES; ++s) { mbar_init(&x_full[s], 1); mbar_init(&x_empty[s], 1); }
+        for (int s = 0; s < L::C_STAGES; ++s) { mbar_init(&c_full[s], 1); mbar_init(&c_empty[s], G4_UNPACK_WARPS); }
+        for (int s = 0; s < L::A_STAGES; ++s) { mbar_init(&a_full[s], G4_UNPACK_WARPS * CG); mbar_init(&a_empty[s], 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 4 * CG); }
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 2) pair_tmem_alloc<CG>(tmem_slot, 512);
+    tc_fence_before();
+    __syncthreads();
+    pair_sync<CG>();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    auto stop = [&]() { return __any_sync(0xffffffffu, *abort_flag != 0); };       // the same answer for a whole warp
+    int committed = 0;                    // matrix-instruction thread: accumulators committed
+
+    if (warp == 0) {                      // ------------------------------------------------ rows
+        SlotCursor cur(p.offsets, p.experts, p.rows, TN);
+        Ring x;
+        long long it = 0;
+        for (int t = first_work; !stop(); t += work_stride) {
+            const ExpertSlot slot = cur.seek(t / p.ftiles);
+            if (slot.expert < 0) break;
+            if (lane == 0) {
+                const int row = slot.first + rank * L::XROWS;
+                for (int kt = 0; kt < p.steps && !*abort_flag; ++kt)
+                    for (int part = 0; part < PARTS; ++part) {
+                        if (!mbar_wait(&x_empty[x.s], x.ph ^ 1u, abort_flag, 0, p.err, p.wait_limit)) break;
+                        if (rank == 0) mbar_expect_tx(&x_full[x.s], CG * L::X_STAGE);
+                        uint8_t *dst = smem + L::X_OFF + x.s * L::X_STAGE;
+                        pair_load_2d<CG>(dst, &map_x, &x_full[x.s], kt * 128, part * p.rows + row);
+                        pair_load_2d<CG>(dst + L::X_SUB, &map_x, &x_full[x.s], kt * 128 + 64, part * p.rows + row);
+                        x.next(L::X_STAGES);
+                        ++it;
+                    }
+            }
+            __syncwarp();
+        }
+        if (*abort_flag && lane == 0) {
+            if (rank == 0) drain_copies_in_flight(x_full, it, L::X_STAGES, p.wait_limit);
+            else for (int i = 0; i < 1000; ++i) __nanosleep(1000);            // its copies count on the leader's barriers
+        }
+    } else if (warp == 2) {               // ------------------------------------------------ codes and scales
+        SlotCursor cur(p.offsets, p.experts, p.rows, TN);
+        Ring c;
+        long long it = 0;
+        const int groups = G4_TILE / p.w.group;
+        for (int t = first_work; !stop(); t += work_stride) {
+            const ExpertSlot slot = cur.seek(t / p.ftiles);
+            if (slot.expert < 0) break;
+            if (lane == 0) {
+                // a block whose features lie past the end repeats the last tile; its results are not stored
+                const int f = min((t % p.ftiles) * CG + rank, (MODE == G4_FWD ? p.w.tiles_n : p.w.tiles_k) - 1);
+                const int64_t e0 = (int64_t)slot.expert * p.w.tiles_n * p.w.tiles_k;
+                for (int kt = 0; kt < p.steps; ++kt) {
+                    if (!mbar_wait(&c_empty[c.s], c.ph ^ 1u, abort_flag, 0, p.err, p.wait_limit)) break;
+                    const int64_t tile = e0 + (MODE == G4_FWD ? (int64_t)f * p.w.tiles_k + kt : (int64_t)kt * p.w.tiles_k + f);
+                    mbar_expect_tx(&c_full[c.s], G4_TILE_WORDS * 4 + groups * G4_TILE);
+                    uint8_t *dst = smem + L::C_OFF + c.s * L::C_STAGE;
+                    bulk_load(dst, p.w.codes + tile * G4_TILE_WORDS, G4_TILE_WORDS * 4, &c_full[c.s]);
+                    bulk_load(dst + G4_TILE_WORDS * 4, p.w.scales + tile * (groups * G4_TILE), groups * G4_TILE, &c_full[c.s]);
+                    c.next(L::C_STAGES);
+                    ++it;
+                }
+            }
+            __syncwarp();
+        }
+        if (*abort_flag && lane == 0) drain_copies_in_flight(c_full, it, L::C_STAGES, p.wait_limit);
+    } else if (warp == 1) {               // ------------------------------------------------ matrix instructions
+        if (rank == 0) {
+            SlotCursor cur(p.offsets, p.experts, p.rows, TN);
+            Ring x, a;
+            constexpr uint32_t idesc = idesc_f16(G4Type<T>::FMT, 128 * CG, TN, MODE == G4_DATA, false);
+            int local = 0;
+            for (int t = first_work; !stop(); t += work_stride, ++local) {
+                const ExpertSlot slot = cur.seek(t / p.ftiles);
+                if (slot.expert < 0) break;
+                if (lane == 0) {
+                    const int buf = local % L::ACC_BUFS;
+                    const bool ok = pair_wait<CG>(&acc_empty[buf], ((uint32_t)(local / L::ACC_BUFS) & 1u) ^ 1u, abort_flag, 3, p.err, p.wait_limit);
+                    tc_fence_after();
+                    const uint32_t d = tmem_base + (uint32_t)(buf * TN);
+                    for (int kt = 0; ok && kt < p.steps; ++kt) {
+                        if (!pair_wait<CG>(&a_full[a.s], a.ph, abort_flag, 1, p.err, p.wait_limit)) break;
+                        bool went = true;
+                        for (int part = 0; part < PARTS; ++part) {
+                            if (!(went = mbar_wait(&x_full[x.s], x.ph, abort_flag, 1, p.err, p.wait_limit))) break;
+                            tc_fence_after();
+                            const uint32_t xs = smem_u32(smem + L::X_OFF + x.s * L::X_STAGE);
+                            const uint64_t b0 = smem_desc_k_sw128(xs), b1 = smem_desc_k_sw128(xs + L::X_SUB);
+                            if constexpr (MODE == G4_FWD) {
+                                const uint32_t at = tmem_base + L::ACC_COLS + a.s * 64;
+#pragma unroll
+                                for (int j = 0; j < 8; ++j)
+                                    mma_f16_ts<CG>(d, at + 8 * j, (j < 4 ? b0 : b1) + 2 * (j & 3), idesc, (kt | part | j) != 0 ? 1u : 0u);
+                            } else {
+                                const uint64_t ad = smem_desc_mn_sw128(smem_u32(smem + L::A_OFF + a.s * L::A_STAGE), 128 * 128);
+#pragma unroll
+                                for (int j = 0; j < 8; ++j)
+                                    mma_f16_ss<CG>(d, ad + 128 * j, (j < 4 ? b0 : b1) + 2 * (j & 3), idesc, (kt | part | j) != 0 ? 1u : 0u);
+                            }
+                            pair_commit<CG>(&x_empty[x.s]);
+                            x.next(L::X_STAGES);
+                        }
+                        if (!went) break;
+                        pair_commit<CG>(&a_empty[a.s]);
+                        a.next(L::A_STAGES);
+                    }
+                    if (ok) {
+                        pair_commit<CG>(&acc_full[buf]);
+                        committed = local + 1;
+                    }
+                }
+                __syncwarp();
+            }
+        }
+    } else if (warp >= 8) {               // ------------------------------------------------ unpacking
+        SlotCursor cur(p.offsets, p.experts, p.rows, TN);
+        Ring c, a;
+        const int q = warp & 3, half = (warp - 8) >> 2;
+        const int r = q * 32 + lane;
+        const int log_group = p.w.group == 32 ? 5 : p.w.group == 64 ? 6 : 7;
+        for (int t = first_work; !stop(); t += work_stride) {
+            const ExpertSlot slot = cur.seek(t / p.ftiles);
+            if (slot.expert < 0) break;
+            bool ok = true;
+            for (int kt = 0; kt < p.steps; ++kt) {
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait(&c_full[c.s], c.ph, abort_flag, 1, p.err, p.wait_limit)))) break;
+                const uint8_t *src = smem + L::C_OFF + c.s * L::C_STAGE;
+                const uint8_t *sc = src + G4_TILE_WORDS * 4 + r;
+                if constexpr (MODE == G4_FWD) {
+                    // lane r, columns 64 * half .. + 63 of the tile: words 2 * half and 2 * half + 1 of the four units
+                    uint2 w2[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) w2[u] = *reinterpret_cast<const uint2 *>(src + u * 2048 + r * 16 + half * 8);
+                    const uint32_t s0 = scale_pair<Op>(sc[((64 * half) >> log_group) * G4_TILE]);
+                    const uint32_t s1 = scale_pair<Op>(sc[((64 * half + 32) >> log_group) * G4_TILE]);
+                    __syncwarp();
+                    if (lane == 0) arrive_local(&c_empty[c.s]);
+                    uint32_t v[32];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        unpack_word<Op>(w2[u].x, s0, v + 4 * u);
+                        unpack_word<Op>(w2[u].y, s1, v + 16 + 4 * u);
+                    }
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(&a_empty[a.s], a.ph ^ 1u, abort_flag, 0, p.err, p.wait_limit)))) break;
+                    tc_fence_after();
+                    tmem_store_32(tmem_base + ((uint32_t)(q * 32) << 16) + L::ACC_COLS + a.s * 64 + half * 32, v);
+                    tc_fence_before();
+                } else {
+                    // row r of the contraction, units 2 * half and 2 * half + 1: word w of unit u holds lanes 32w + 8u .. + 7
+                    uint4 w4[2];
+                    w4[0] = *reinterpret_cast<const uint4 *>(src + (2 * half) * 2048 + r * 16);
+                    w4[1] = *reinterpret_cast<const uint4 *>(src + (2 * half + 1) * 2048 + r * 16);
+                    uint32_t s[4];
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) s[w] = scale_pair<Op>(sc[((32 * w) >> log_group) * G4_TILE]);
+                    __syncwarp();
+                    if (lane == 0) arrive_local(&c_empty[c.s]);
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(&a_empty[a.s], a.ph ^ 1u, abort_flag, 0, p.err, p.wait_limit)))) break;
+                    uint8_t *dst = smem + L::A_OFF + a.s * L::A_STAGE + r * 128;
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const uint32_t word[4] = {w4[u].x, w4[u].y, w4[u].z, w4[u].w};
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            uint32_t v[4];
+                            unpack_word<Op>(word[w], s[w], v);
+                            const int chunk = (w & 1) * 4 + 2 * half + u;
+                            *reinterpret_cast<uint4 *>(dst + (w >> 1) * (128 * 128) + ((chunk ^ (r & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+                        }
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+                __syncwarp();
+                if (lane == 0) arrive_leader<CG>(&a_full[a.s]);
+                c.next(L::C_STAGES);
+                a.next(L::A_STAGES);
+            }
+            if (!ok) break;
+        }
+    } else if (warp >= 4) {               // ------------------------------------------------ results
+        SlotCursor cur(p.offsets, p.experts, p.rows, TN);
+        const int q = warp & 3;
+        int local = 0;
+        for (int t = first_work; !stop(); t += work_stride, ++local) {
+            const ExpertSlot slot = cur.seek(t / p.ftiles);
+            if (slot.expert < 0) break;
+            const int buf = local % L::ACC_BUFS;
+            if (!__all_sync(0xffffffffu, mbar_wait(&acc_full[buf], (uint32_t)(local / L::ACC_BUFS) & 1u, abort_flag, 2, p.err, p.wait_limit))) break;
+            tc_fence_after();
+            const int f = ((t % p.ftiles) * CG + rank) * 128 + q * 32 + lane;
+            const float alpha = __ldg(p.w.alpha + slot.expert);
+            T *dst = static_cast<T *>(p.out) + (int64_t)slot.first * p.ldo + f;
+            const int have = slot.last - slot.first;
+#pragma unroll 1
+            for (int c0 = 0; c0 < have; c0 += 32) {
+                uint32_t v[32];
+                tmem_load_32(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * TN + c0), v);
+                if (f < p.features) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (c0 + i < have) real_store(dst + (int64_t)(c0 + i) * p.ldo, __fmul_rn(__uint_as_float(v[i]), alpha));
+                }
+                __syncwarp();
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_leader<CG>(&acc_empty[buf]);
+        }
+    }
+    __syncwarp();
+    if (warp == 1 && rank == 0 && lane == 0 && committed > 0) {
+        // every instruction issued has completed once the last commit has arrived (an abort's tiles are committed too)
+        const int last = committed - 1;
+        for (uint32_t w = 0; w < p.wait_limit && !mbar_try_wait(&acc_full[last % L::ACC_BUFS], (uint32_t)(last / L::ACC_BUFS) & 1u); ++w) {}
+    }
+    tc_fence_before();
+    __syncthreads();
+    pair_sync<CG>();
+    if (warp == 2) {
+        tc_fence_after();
+        pair_tmem_dealloc<CG>(tmem_base, 512);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ host side
+
+// Tensor map of a row-major matrix of 2-byte elements: boxes of 64 columns x box_rows rows, 128-byte swizzle, zeros outside.
+inline bool make_map_16(CUtensorMap *map, bool fp16, const void *base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
+    cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+    cuuint32_t estr[2] = {1, 1};
+    return fn(map, fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), dims,
+              strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// x: operand rows of G4Type<T>::Op, [PARTS * rows][ldx], 16-byte aligned rows, `width` columns.
+template <int CG, int TN, int MODE, class T>
+int g4_tensor_launch(const void *x, int64_t ldx, int width, G4TensorParams p, int sms, cudaStream_t st) {
+    using L = G4Shape<CG, TN, MODE>;
+    auto kernel = g4_tensor_kernel<CG, TN, MODE, T>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::TOTAL) != cudaSuccess) return QNN_E_CUDA;
+    CUtensorMap map;
+    if (!make_map_16(&map, std::is_same<T, __half>::value, x, (int64_t)p.rows * G4Type<T>::PARTS, width, ldx, L::XROWS)) return QNN_E_CUDA;
+    p.ftiles = (g4_tiles(p.features) + CG - 1) / CG;
+    const int64_t work = expert_slots_most(p.rows, p.experts, TN) * p.ftiles;
+    if (work > 0x3FFFFFFFll) return QNN_E_RANGE;
+    const int most = sms / CG;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((work < most ? work : most) * CG));
+    cfg.blockDim = dim3(G4_THREADS);
+    cfg.dynamicSmemBytes = L::TOTAL;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CG;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = CG > 1 ? 1 : 0;
+    if (cudaLaunchKernelEx(&cfg, kernel, map, p) != cudaSuccess) {
+        cudaGetLastError();
+        return QNN_E_CUDA;
+    }
+    return QNN_OK;
+}
+
+}  // namespace

@@ -1,0 +1,32 @@
+// Choice of the tile for a grouped product.
+#pragma once
+#include "g4_tensor.cuh"
+#include "g4_tensor_api.cuh"
+
+namespace {
+
+template <int MODE, class T>
+int g4_tensor_pick(const void *x, int64_t ldx, const G4TensorArgs &a, cudaStream_t st) {
+    G4TensorParams p = {};
+    p.w = a.w; p.offsets = a.offsets; p.experts = a.experts; p.rows = a.rows; p.out = a.out; p.ldo = a.ldo;
+    p.features = MODE == G4_FWD ? a.w.n : a.w.k;
+    p.steps = MODE == G4_FWD ? a.w.tiles_k : a.w.tiles_n;
+    p.wait_limit = WAIT_LIMIT;
+    if (!(p.err = qnn_tc_error_word())) return QNN_E_CUDA;
+    const int sms = sm_count();
+    if (sms <= 0) return QNN_E_CUDA;
+    const int width = MODE == G4_FWD ? a.w.k : a.w.n;
+    const int64_t each = (a.rows + a.experts - 1) / a.experts;              // rows an expert has on average
+    if (each <= 48) return g4_tensor_launch<1, 32, MODE, T>(x, ldx, width, p, sms, st);
+    if (each <= 96) return g4_tensor_launch<1, 64, MODE, T>(x, ldx, width, p, sms, st);
+    return g4_tensor_launch<1, 128, MODE, T>(x, ldx, width, p, sms, st);
+}
+
+template <int MODE>
+int g4_tensor_run(const void *x, int type, int64_t ldx, const G4TensorArgs &a, cudaStream_t st) {
+    if (type == QNN_F32) return g4_tensor_pick<MODE, float>(x, ldx, a, st);
+    if (type == QNN_BF16) return g4_tensor_pick<MODE, __nv_bfloat16>(x, ldx, a, st);
+    return g4_tensor_pick<MODE, __half>(x, ldx, a, st);
+}
+
+}  // namespace

@@ -30,7 +30,7 @@ def test_sizes(qnn):
         for group in (32, 64, 128):
             assert g(2, n, k, group) == 2 * ref.tiles(n) * ref.tiles(k) * 128 * 128 // group
     assert f(1, 4096, 4096) * 2 == 4096 * 4096
-    assert f(0, 4, 4) == 0 and f(1, 0, 4) == 0 and f(1, 4, -1) == 0 and f(65536, 4, 4) == 0 and f(1, 65535 * 16 + 1, 4) == 0
+    assert f(0, 4, 4) == 0 and f(1, 0, 4) == 0 and f(1, 4, -1) == 0 and f(4097, 4, 4) == 0 and f(1, 65535 * 16 + 1, 4) == 0
     assert g(1, 4, 4, 16) == 0 and g(1, 4, 4, 0) == 0 and g(1, 4, 0, 32) == 0
 
 
@@ -61,7 +61,7 @@ def test_pack_refusals(qnn, p):
     for bad in ({"codes": mis}, {"scales": mis}, {"w": ctypes.c_void_p(p.value + 2)}, {"alpha": ctypes.c_void_p(p.value + 1)},
                 {"type": 1, "w": ctypes.c_void_p(p.value + 1)}):
         assert call(**bad) == qnn.E_ALIGN, bad
-    assert call(experts=65535, n=65535 * 16, k=65535 * 16, ldw=65535 * 16) == qnn.E_RANGE
+    assert call(experts=4096, n=65535 * 16, k=65535 * 16, ldw=65535 * 16) == qnn.E_RANGE
 
 
 def test_matvec_refusals(qnn, p):
@@ -97,7 +97,7 @@ def test_expert_refusals(qnn, p, name):
         return f(*[kw.get(key, v) for key, v in zip(names, ok)])
 
     for bad in ({"x": None}, {"y": None}, {"codes": None}, {"scales": None}, {"alpha": None}, {"offsets": None}, {"type": 3},
-                {"rows": -1}, {"experts": 0}, {"experts": 65536}, {"ldx": width - 1}, {"ldy": other - 1}, {"group": 1},
+                {"rows": -1}, {"experts": 0}, {"experts": 4097}, {"ldx": width - 1}, {"ldy": other - 1}, {"group": 1},
                 {"n": 0}, {"k": 0}):
         assert call(**bad) == qnn.E_ARG, bad
     for bad in ({"codes": mis}, {"scales": mis}, {"offsets": ctypes.c_void_p(p.value + 2)}, {"x": ctypes.c_void_p(p.value + 1)},
@@ -146,12 +146,12 @@ def test_binding_refusals(qnn):
                  lambda: qnn.g4_pack_weights(torch.zeros((8, 64)))):
         with pytest.raises(ValueError):
             call()
-    assert qnn._g4_check(w, cpu.device) == 1
+    assert qnn._g4_check(w, -1) == 1
     for bad in (w._replace(group=16), w._replace(n=129), w._replace(k=129), w._replace(codes=w.codes.float()),
                 w._replace(scales=w.scales[..., :64]), w._replace(alpha=torch.ones(2)),
                 w._replace(codes=w.codes.expand(2, -1, -1, -1, -1, -1))):
         with pytest.raises(ValueError):
-            qnn._g4_check(bad, cpu.device)
+            qnn._g4_check(bad, -1)
     for bad in (torch.tensor([0, 2]), torch.tensor([0], dtype=torch.int32), torch.zeros((2, 2), dtype=torch.int32)):
         with pytest.raises(ValueError):
-            qnn._expert_offsets(bad, cpu.device)
+            qnn._expert_offsets(bad, -1)
