@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(acc_empty + 2);
     volatile uint32_t *abort_flag = tmem_slot + 1;
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = warp_index(), lane = threadIdx.x & 31;
     const int rank = (int)pair_rank<CG>();
     const int first_work = blockIdx.x / CG, work_stride = gridDim.x / CG;
     const int per_expert = p.itiles * p.jtiles, work = p.experts * per_expert;
@@ -74,21 +74,28 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
     pair_sync<CG>();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+    auto warp_wait = [&](uint64_t *bar, uint32_t parity, unsigned id) {
+        return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, id, p.err, p.wait_limit));
+    };
+    auto pair_warp_wait = [&](uint64_t *bar, uint32_t parity, unsigned id) {
+        return __all_sync(0xffffffffu, pair_wait<CG>(bar, parity, abort_flag, id, p.err, p.wait_limit));
+    };
     auto stop = [&]() { return __any_sync(0xffffffffu, *abort_flag != 0); };
     int committed = 0;
 
     if (warp == 0) {
         Ring g;
         long long it = 0;
-        if (lane == 0) {
-            for (int t = first_work; t < work && !*abort_flag; t += work_stride) {
-                const int e = t / per_expert, in = t - e * per_expert;
-                int first, last;
-                expert_rows(p.offsets, e, p.rows, first, last);
-                const int i0 = ((in % p.itiles) * CG + rank) * 128, j0 = (in / p.itiles) * TN + rank * L::B_COLS;
-                for (int r = first; r < last && !*abort_flag; r += L::ROWS)
-                    for (int q = 0; q < PAIRS; ++q) {
-                        if (!mbar_wait(&empty[g.s], g.ph ^ 1u, abort_flag, 0, p.err, p.wait_limit)) break;
+        for (int t = first_work; t < work && !stop(); t += work_stride) {
+            const int e = t / per_expert, in = t - e * per_expert;
+            int first, last;
+            expert_rows(p.offsets, e, p.rows, first, last);
+            const int i0 = ((in % p.itiles) * CG + rank) * 128, j0 = (in / p.itiles) * TN + rank * L::B_COLS;
+            bool ok = true;
+            for (int r = first; ok && r < last; r += L::ROWS)
+                for (int q = 0; q < PAIRS; ++q) {
+                    if (!(ok = warp_wait(&empty[g.s], g.ph ^ 1u, 0))) break;
+                    if (elect_one()) {
                         mbar_expect_tx(&landed[g.s], L::STAGE);
                         uint8_t *dst = smem + g.s * L::STAGE;
                         const int rx = (PAIRS == 1 ? 0 : pair_x(q) * p.rows) + r, rd = (PAIRS == 1 ? 0 : pair_dy(q) * p.rows) + r;
@@ -97,12 +104,14 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
 #pragma unroll
                         for (int b = 0; b < L::B_COLS / 64; ++b)
                             tma_load_2d(dst + L::A_BYTES + b * L::BLOCK, &map_dy, &landed[g.s], j0 + b * 64, rd);
-                        g.next(L::STAGES);
-                        ++it;
                     }
-            }
-            if (*abort_flag) drain_copies_in_flight(landed, it, L::STAGES, p.wait_limit);
+                    __syncwarp();
+                    g.next(L::STAGES);
+                    ++it;
+                }
+            if (!ok) break;
         }
+        if (*abort_flag && lane == 0) drain_copies_in_flight(landed, it, L::STAGES, p.wait_limit);
     } else if (warp == 2) {               // stages whose rows all belong to the expert pass through
         Ring g;
         for (int t = first_work; t < work && !stop(); t += work_stride) {
@@ -112,7 +121,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
             bool ok = true;
             for (int r = first; ok && r < last; r += L::ROWS)
                 for (int q = 0; q < PAIRS; ++q) {
-                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(&landed[g.s], g.ph, abort_flag, 1, p.err, p.wait_limit)))) break;
+                    if (!(ok = warp_wait(&landed[g.s], g.ph, 1))) break;
                     const int valid = last - r;
                     if (valid < L::ROWS) {
                         uint8_t *stage = smem + g.s * L::STAGE;
@@ -128,31 +137,36 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
             if (!ok) break;
         }
     } else if (warp == 1) {
-        if (rank == 0 && lane == 0) {
+        if (rank == 0) {
             Ring g;
             constexpr uint32_t idesc = idesc_f16(G4Type<T>::FMT, 128 * CG, TN, true, true);
             int local = 0;
-            for (int t = first_work; t < work && !*abort_flag; t += work_stride) {
+            for (int t = first_work; t < work && !stop(); t += work_stride) {
                 int first, last;
                 expert_rows(p.offsets, t / per_expert, p.rows, first, last);
                 if (first >= last) continue;                     // nothing to add up: the result warps write zeros
                 const int buf = local % L::ACC_BUFS;
-                if (!pair_wait<CG>(&acc_empty[buf], ((uint32_t)(local / L::ACC_BUFS) & 1u) ^ 1u, abort_flag, 3, p.err, p.wait_limit)) break;
+                if (!pair_warp_wait(&acc_empty[buf], ((uint32_t)(local / L::ACC_BUFS) & 1u) ^ 1u, 3)) break;
                 tc_fence_after();
                 const uint32_t d = tmem_base + (uint32_t)(buf * TN);
-                for (int r = first; r < last && !*abort_flag; r += L::ROWS)
+                bool ok = true;
+                for (int r = first; ok && r < last; r += L::ROWS)
                     for (int q = 0; q < PAIRS; ++q) {
-                        if (!pair_wait<CG>(&ready[g.s], g.ph, abort_flag, 1, p.err, p.wait_limit)) break;
+                        if (!(ok = pair_warp_wait(&ready[g.s], g.ph, 1))) break;
                         tc_fence_after();
                         const uint32_t at = smem_u32(smem + g.s * L::STAGE);
                         const uint64_t a = smem_desc_mn_sw128(at, L::BLOCK), b = smem_desc_mn_sw128(at + L::A_BYTES, L::BLOCK);
+                        if (elect_one()) {
 #pragma unroll
-                        for (int j = 0; j < L::ROWS / 16; ++j)
-                            mma_f16_ss<CG>(d, a + 128 * j, b + 128 * j, idesc, ((r - first) | q | j) != 0 ? 1u : 0u);
-                        pair_commit<CG>(&empty[g.s]);
+                            for (int j = 0; j < L::ROWS / 16; ++j)
+                                mma_f16_ss<CG>(d, a + 128 * j, b + 128 * j, idesc, ((r - first) | q | j) != 0 ? 1u : 0u);
+                            pair_commit<CG>(&empty[g.s]);
+                        }
+                        __syncwarp();
                         g.next(L::STAGES);
                     }
-                pair_commit<CG>(&acc_full[buf]);
+                if (elect_one()) pair_commit<CG>(&acc_full[buf]);            // also after a wait that gave up: see the end
+                __syncwarp();
                 committed = ++local;
             }
         }
@@ -172,7 +186,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
                 continue;
             }
             const int buf = local % L::ACC_BUFS;
-            if (!__all_sync(0xffffffffu, mbar_wait(&acc_full[buf], (uint32_t)(local / L::ACC_BUFS) & 1u, abort_flag, 2, p.err, p.wait_limit))) break;
+            if (!warp_wait(&acc_full[buf], (uint32_t)(local / L::ACC_BUFS) & 1u, 2)) break;
             tc_fence_after();
 #pragma unroll 1
             for (int c0 = 0; c0 < have; c0 += 32) {

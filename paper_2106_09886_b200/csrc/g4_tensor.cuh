@@ -164,6 +164,15 @@ __host__ __device__ constexpr uint32_t idesc_f16(uint32_t fmt, int m, int n, boo
            ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 
+// One lane of a converged warp, chosen so that the compiler knows the branch for a single-thread region of uniform values
+// (instructions that take uniform registers are then issued straight; behind lane == 0 each operand is moved over first).
+__device__ __forceinline__ bool elect_one() {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
+    return ok != 0;
+}
+__device__ __forceinline__ int warp_index() { return __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0); }
+
 struct Ring {                                            // position in a ring of stages and the parity of its round
     int s = 0;
     uint32_t ph = 0;
@@ -296,7 +305,7 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(acc_empty + 2);
     volatile uint32_t *abort_flag = tmem_slot + 1;
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = warp_index(), lane = threadIdx.x & 31;
     const int rank = (int)pair_rank<CG>();
     const int first_work = blockIdx.x / CG, work_stride = gridDim.x / CG;
 
@@ -315,6 +324,13 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
     pair_sync<CG>();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+    // waits of a whole warp: every lane polls (each needs the barrier's acquire), all go on or all give up
+    auto warp_wait = [&](uint64_t *bar, uint32_t parity, unsigned id) {
+        return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, id, p.err, p.wait_limit));
+    };
+    auto pair_warp_wait = [&](uint64_t *bar, uint32_t parity, unsigned id) {
+        return __all_sync(0xffffffffu, pair_wait<CG>(bar, parity, abort_flag, id, p.err, p.wait_limit));
+    };
     auto stop = [&]() { return __any_sync(0xffffffffu, *abort_flag != 0); };       // the same answer for a whole warp
     int committed = 0;                    // matrix-instruction thread: accumulators committed
 
@@ -325,20 +341,22 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
         for (int t = first_work; !stop(); t += work_stride) {
             const ExpertSlot slot = cur.seek(t / p.ftiles);
             if (slot.expert < 0) break;
-            if (lane == 0) {
-                const int row = slot.first + rank * L::XROWS;
-                for (int kt = 0; kt < p.steps && !*abort_flag; ++kt)
-                    for (int part = 0; part < PARTS; ++part) {
-                        if (!mbar_wait(&x_empty[x.s], x.ph ^ 1u, abort_flag, 0, p.err, p.wait_limit)) break;
+            const int row = slot.first + rank * L::XROWS;
+            bool ok = true;
+            for (int kt = 0; ok && kt < p.steps; ++kt)
+                for (int part = 0; part < PARTS; ++part) {
+                    if (!(ok = warp_wait(&x_empty[x.s], x.ph ^ 1u, 0))) break;
+                    if (elect_one()) {
                         if (rank == 0) mbar_expect_tx(&x_full[x.s], CG * L::X_STAGE);
                         uint8_t *dst = smem + L::X_OFF + x.s * L::X_STAGE;
                         pair_load_2d<CG>(dst, &map_x, &x_full[x.s], kt * 128, part * p.rows + row);
                         pair_load_2d<CG>(dst + L::X_SUB, &map_x, &x_full[x.s], kt * 128 + 64, part * p.rows + row);
-                        x.next(L::X_STAGES);
-                        ++it;
                     }
-            }
-            __syncwarp();
+                    __syncwarp();
+                    x.next(L::X_STAGES);
+                    ++it;
+                }
+            if (!ok) break;
         }
         if (*abort_flag && lane == 0) {
             if (rank == 0) drain_copies_in_flight(x_full, it, L::X_STAGES, p.wait_limit);
@@ -352,22 +370,24 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
         for (int t = first_work; !stop(); t += work_stride) {
             const ExpertSlot slot = cur.seek(t / p.ftiles);
             if (slot.expert < 0) break;
-            if (lane == 0) {
-                // a block whose features lie past the end repeats the last tile; its results are not stored
-                const int f = min((t % p.ftiles) * CG + rank, (MODE == G4_FWD ? p.w.tiles_n : p.w.tiles_k) - 1);
-                const int64_t e0 = (int64_t)slot.expert * p.w.tiles_n * p.w.tiles_k;
-                for (int kt = 0; kt < p.steps; ++kt) {
-                    if (!mbar_wait(&c_empty[c.s], c.ph ^ 1u, abort_flag, 0, p.err, p.wait_limit)) break;
-                    const int64_t tile = e0 + (MODE == G4_FWD ? (int64_t)f * p.w.tiles_k + kt : (int64_t)kt * p.w.tiles_k + f);
+            // a block whose features lie past the end repeats the last tile; its results are not stored
+            const int f = min((t % p.ftiles) * CG + rank, (MODE == G4_FWD ? p.w.tiles_n : p.w.tiles_k) - 1);
+            const int64_t e0 = (int64_t)slot.expert * p.w.tiles_n * p.w.tiles_k;
+            bool ok = true;
+            for (int kt = 0; kt < p.steps; ++kt) {
+                if (!(ok = warp_wait(&c_empty[c.s], c.ph ^ 1u, 0))) break;
+                const int64_t tile = e0 + (MODE == G4_FWD ? (int64_t)f * p.w.tiles_k + kt : (int64_t)kt * p.w.tiles_k + f);
+                if (elect_one()) {
                     mbar_expect_tx(&c_full[c.s], G4_TILE_WORDS * 4 + groups * G4_TILE);
                     uint8_t *dst = smem + L::C_OFF + c.s * L::C_STAGE;
                     bulk_load(dst, p.w.codes + tile * G4_TILE_WORDS, G4_TILE_WORDS * 4, &c_full[c.s]);
                     bulk_load(dst + G4_TILE_WORDS * 4, p.w.scales + tile * (groups * G4_TILE), groups * G4_TILE, &c_full[c.s]);
-                    c.next(L::C_STAGES);
-                    ++it;
                 }
+                __syncwarp();
+                c.next(L::C_STAGES);
+                ++it;
             }
-            __syncwarp();
+            if (!ok) break;
         }
         if (*abort_flag && lane == 0) drain_copies_in_flight(c_full, it, L::C_STAGES, p.wait_limit);
     } else if (warp == 1) {               // ------------------------------------------------ matrix instructions
@@ -379,19 +399,18 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
             for (int t = first_work; !stop(); t += work_stride, ++local) {
                 const ExpertSlot slot = cur.seek(t / p.ftiles);
                 if (slot.expert < 0) break;
-                if (lane == 0) {
-                    const int buf = local % L::ACC_BUFS;
-                    const bool ok = pair_wait<CG>(&acc_empty[buf], ((uint32_t)(local / L::ACC_BUFS) & 1u) ^ 1u, abort_flag, 3, p.err, p.wait_limit);
-                    tc_fence_after();
-                    const uint32_t d = tmem_base + (uint32_t)(buf * TN);
-                    for (int kt = 0; ok && kt < p.steps; ++kt) {
-                        if (!pair_wait<CG>(&a_full[a.s], a.ph, abort_flag, 1, p.err, p.wait_limit)) break;
-                        bool went = true;
-                        for (int part = 0; part < PARTS; ++part) {
-                            if (!(went = mbar_wait(&x_full[x.s], x.ph, abort_flag, 1, p.err, p.wait_limit))) break;
-                            tc_fence_after();
-                            const uint32_t xs = smem_u32(smem + L::X_OFF + x.s * L::X_STAGE);
-                            const uint64_t b0 = smem_desc_k_sw128(xs), b1 = smem_desc_k_sw128(xs + L::X_SUB);
+                const int buf = local % L::ACC_BUFS;
+                if (!pair_warp_wait(&acc_empty[buf], ((uint32_t)(local / L::ACC_BUFS) & 1u) ^ 1u, 3)) break;
+                const uint32_t d = tmem_base + (uint32_t)(buf * TN);
+                bool ok = true;
+                for (int kt = 0; ok && kt < p.steps; ++kt) {
+                    if (!(ok = pair_warp_wait(&a_full[a.s], a.ph, 1))) break;
+                    for (int part = 0; part < PARTS; ++part) {
+                        if (!(ok = warp_wait(&x_full[x.s], x.ph, 1))) break;
+                        tc_fence_after();
+                        const uint32_t xs = smem_u32(smem + L::X_OFF + x.s * L::X_STAGE);
+                        const uint64_t b0 = smem_desc_k_sw128(xs), b1 = smem_desc_k_sw128(xs + L::X_SUB);
+                        if (elect_one()) {
                             if constexpr (MODE == G4_FWD) {
                                 const uint32_t at = tmem_base + L::ACC_COLS + a.s * 64;
 #pragma unroll
@@ -404,18 +423,16 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
                                     mma_f16_ss<CG>(d, ad + 128 * j, (j < 4 ? b0 : b1) + 2 * (j & 3), idesc, (kt | part | j) != 0 ? 1u : 0u);
                             }
                             pair_commit<CG>(&x_empty[x.s]);
-                            x.next(L::X_STAGES);
+                            if (part == PARTS - 1) pair_commit<CG>(&a_empty[a.s]);
                         }
-                        if (!went) break;
-                        pair_commit<CG>(&a_empty[a.s]);
-                        a.next(L::A_STAGES);
+                        __syncwarp();
+                        x.next(L::X_STAGES);
                     }
-                    if (ok) {
-                        pair_commit<CG>(&acc_full[buf]);
-                        committed = local + 1;
-                    }
+                    a.next(L::A_STAGES);
                 }
+                if (elect_one()) pair_commit<CG>(&acc_full[buf]);            // also after a wait that gave up: see the end
                 __syncwarp();
+                committed = local + 1;
             }
         }
     } else if (warp >= 8) {               // ------------------------------------------------ unpacking
@@ -429,7 +446,7 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
             if (slot.expert < 0) break;
             bool ok = true;
             for (int kt = 0; kt < p.steps; ++kt) {
-                if (!(ok = __all_sync(0xffffffffu, mbar_wait(&c_full[c.s], c.ph, abort_flag, 1, p.err, p.wait_limit)))) break;
+                if (!(ok = warp_wait(&c_full[c.s], c.ph, 1))) break;
                 const uint8_t *src = smem + L::C_OFF + c.s * L::C_STAGE;
                 const uint8_t *sc = src + G4_TILE_WORDS * 4 + r;
                 if constexpr (MODE == G4_FWD) {
@@ -447,7 +464,7 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
                         unpack_word<Op>(w2[u].x, s0, v + 4 * u);
                         unpack_word<Op>(w2[u].y, s1, v + 16 + 4 * u);
                     }
-                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(&a_empty[a.s], a.ph ^ 1u, abort_flag, 0, p.err, p.wait_limit)))) break;
+                    if (!(ok = warp_wait(&a_empty[a.s], a.ph ^ 1u, 0))) break;
                     tc_fence_after();
                     tmem_store_32(tmem_base + ((uint32_t)(q * 32) << 16) + L::ACC_COLS + a.s * 64 + half * 32, v);
                     tc_fence_before();
@@ -461,7 +478,7 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
                     for (int w = 0; w < 4; ++w) s[w] = scale_pair<Op>(sc[((32 * w) >> log_group) * G4_TILE]);
                     __syncwarp();
                     if (lane == 0) arrive_local(&c_empty[c.s]);
-                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(&a_empty[a.s], a.ph ^ 1u, abort_flag, 0, p.err, p.wait_limit)))) break;
+                    if (!(ok = warp_wait(&a_empty[a.s], a.ph ^ 1u, 0))) break;
                     uint8_t *dst = smem + L::A_OFF + a.s * L::A_STAGE + r * 128;
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
@@ -491,7 +508,7 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
             const ExpertSlot slot = cur.seek(t / p.ftiles);
             if (slot.expert < 0) break;
             const int buf = local % L::ACC_BUFS;
-            if (!__all_sync(0xffffffffu, mbar_wait(&acc_full[buf], (uint32_t)(local / L::ACC_BUFS) & 1u, abort_flag, 2, p.err, p.wait_limit))) break;
+            if (!warp_wait(&acc_full[buf], (uint32_t)(local / L::ACC_BUFS) & 1u, 2)) break;
             tc_fence_after();
             const int f = ((t % p.ftiles) * CG + rank) * 128 + q * 32 + lane;
             const float alpha = __ldg(p.w.alpha + slot.expert);
