@@ -3,8 +3,8 @@
 // Bound: reading the codes once (n*k/2 bytes).  At HBM speed a B200 streams 13e12 weights a second, 2.8 lane
 // instructions each, which one fused multiply-add per weight and row does not fit; so the products run as warp-level
 // m16n8k16 matrix instructions with 16 features as the rows and up to 8 x-columns per instruction, and a weight costs
-// only its unpacking: per pair one shift, one three-input logic operation that drops the 4-bit code into the mantissa of
-// 1.0 (bf16: 1 + t/16) or 1024.0 (fp16: 1024 + 8t), and one fused multiply-add that makes the odd integer 2t - 15, exact.
+// only its unpacking: per pair a shift, a logic operation that leaves the 4-bit code as a small multiple of the type's
+// smallest step, and one fused multiply-add that makes the odd integer 2t - 15 (times a power of two) exactly.
 // Group scales multiply the fp32 sums of a group, not the weights.  (The tensor memory path needs 128 features and a
 // pipeline per thread block; with a few rows its fixed cost is the larger part.)
 //
@@ -21,21 +21,25 @@ template <> struct RowType<__nv_bfloat16> { static constexpr int PARTS = 1; };
 template <> struct RowType<__half> { static constexpr int PARTS = 1; };
 template <> struct RowType<float> { static constexpr int PARTS = 3; };
 
-// Four pairs of a code word -> q of pair p in both halves (bf16, or fp16 for fp16 rows).
+// Pair p of a code word as numbers of the operand's type, exact:
+//   bf16  the bare nibble is the subnormal t * 2^-133; times 2^127 minus 15 * 2^-7 it is q / 128;
+//   fp16  the nibble under the exponent of 1024 is 1024 + 16t; an eighth of it minus 143 is q.
+template <class T> struct CodeScale { static constexpr float UNDO = 128.0f; };
+template <> struct CodeScale<__half> { static constexpr float UNDO = 1.0f; };
 template <class T>
 __device__ __forceinline__ uint32_t code_pair(uint32_t word, int p) {
-    const uint32_t s = p == 0 ? word << 3 : word >> (4 * p - 3);
     uint32_t r;
-    if constexpr (sizeof(T) == 2 && !std::is_same<T, __nv_bfloat16>::value) {
-        const uint32_t u = (s & 0x00780078u) | 0x64006400u;                       // 1024 + 8t
-        const __half2 v = __hfma2(*reinterpret_cast<const __half2 *>(&u), __half2half2(__ushort_as_half(0x3400)),
-                                  __half2half2(__ushort_as_half(0xDC3C)));        // * 0.25 - 271
+    if constexpr (std::is_same<T, __half>::value) {
+        const uint32_t s = p == 0 ? word << 4 : word >> (4 * p - 4);
+        uint32_t u;
+        asm("lop3.b32 %0, %1, 0x00F000F0, 0x64006400, 0xEA;" : "=r"(u) : "r"(s));
+        const __half2 v = __hfma2(*reinterpret_cast<const __half2 *>(&u), __half2half2(__ushort_as_half(0x3000)),
+                                  __half2half2(__ushort_as_half(0xD878)));
         r = *reinterpret_cast<const uint32_t *>(&v);
     } else {
-        const uint32_t u = (s & 0x00780078u) | 0x3F803F80u;                       // 1 + t/16
-        const __nv_bfloat162 v = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&u),
-                                         __bfloat162bfloat162(__ushort_as_bfloat16(0x4200)),
-                                         __bfloat162bfloat162(__ushort_as_bfloat16(0xC23C)));   // * 32 - 47
+        const uint32_t u = (word >> (4 * p)) & 0x000F000Fu;
+        const __nv_bfloat162 v = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&u), __bfloat162bfloat162(__ushort_as_bfloat16(0x7F00)),
+                                         __bfloat162bfloat162(__ushort_as_bfloat16(0xBDF0)));
         r = *reinterpret_cast<const uint32_t *>(&v);
     }
     return r;
@@ -118,8 +122,8 @@ __global__ void __launch_bounds__(WARPS * 32) g4_rows_kernel(const T *__restrict
                 if (at < w.tiles_k) {
                     lo[u] = __ldcs(codes + (int64_t)at * (G4_TILE_WORDS / 4));
                     hi[u] = __ldcs(codes + (int64_t)at * (G4_TILE_WORDS / 4) + 8);
-                    slo[u] = g4_scale_f32(__ldg(scales + (int64_t)at * (GROUPS * G4_TILE)));
-                    shi[u] = g4_scale_f32(__ldg(scales + (int64_t)at * (GROUPS * G4_TILE) + 8));
+                    slo[u] = __fmul_rn(g4_scale_f32(__ldg(scales + (int64_t)at * (GROUPS * G4_TILE))), CodeScale<T>::UNDO);
+                    shi[u] = __fmul_rn(g4_scale_f32(__ldg(scales + (int64_t)at * (GROUPS * G4_TILE) + 8)), CodeScale<T>::UNDO);
                 } else {
                     lo[u] = hi[u] = make_uint4(0u, 0u, 0u, 0u);
                     slo[u] = shi[u] = 0.0f;

@@ -148,8 +148,8 @@ __device__ __forceinline__ void tmem_store_32(uint32_t taddr, const uint32_t (&r
           "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
           "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
         : "memory");
-    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
+__device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Shared-memory descriptor of an MN-major tile with the 128-byte swizzle: blocks of 64 elements of the M (or N) dimension
 // (128 bytes) x the contraction's rows; rows in groups of 8 (1024 bytes apart, the stride offset), the next 64 elements
@@ -230,7 +230,7 @@ struct G4TensorParams {
 
 constexpr int G4_THREADS = 512;           // warps: 0 rows by TMA, 1 matrix instructions, 2 codes by bulk copies (and owner of
                                           // the tensor memory), 3 idle, 4-7 results, 8-15 unpacking
-constexpr int G4_UNPACK_WARPS = 8;
+constexpr int G4_UNPACK_WARPS = 4;        // that unpack one stored tile
 
 template <int CG, int TN, int MODE>
 struct G4Shape {
@@ -256,34 +256,51 @@ struct G4Shape {
     static_assert(X_STAGES >= 2 && TOTAL <= 227 * 1024, "shared memory");
 };
 
-// Eight codes of a word -> four packed pairs of scale * q.
-template <class Op>
-__device__ __forceinline__ void unpack_word(uint32_t word, uint32_t scale2, uint32_t *out) {
+// A group's scale as the unpacking needs it.  A masked nibble is an integer multiple of the smallest step of its format:
+//   bf16  the bare nibble is the subnormal t * 2^-133, and one fused multiply-add by s * 2^119 makes s * (2t - 15) * 2^-15
+//         (the power of two that keeps the factor finite; the results are multiplied by 2^15);
+//   fp16  the nibble under the exponent of 1024 is 1024 + t or 1024 + 16t; less 1024, times 2s or s/8, minus 15s.
+// Every step is exact: s has 4 significant bits, 15s and s * q have 8.
+template <class Op> struct GroupScale;
+template <> struct GroupScale<__nv_bfloat16> {
+    static constexpr float UNDO = 32768.0f;
+    __nv_bfloat162 mul, add;
+    __device__ __forceinline__ explicit GroupScale(uint8_t b) {
+        const float s = g4_scale_f32(b);
+        mul = __float2bfloat162_rn(__fmul_rn(s, 6.646139978924579e+35f));          // 2^119
+        add = __float2bfloat162_rn(__fmul_rn(s, -15.0f / 32768.0f));
+    }
+};
+template <> struct GroupScale<__half> {
+    static constexpr float UNDO = 1.0f;
+    __half2 mul0, mul1, add;
+    __device__ __forceinline__ explicit GroupScale(uint8_t b) {
+        const __half2 s = __float2half2_rn(g4_scale_f32(b));
+        mul0 = __hadd2(s, s);
+        mul1 = __hmul2(s, __half2half2(__ushort_as_half(0x3000)));                  // 1/8
+        add = __hmul2(s, __half2half2(__ushort_as_half(0xCB80)));                   // -15
+    }
+};
+
+// Eight codes of a word -> four packed pairs of scale * q (times 1 / UNDO).
+__device__ __forceinline__ void unpack_word(uint32_t word, const GroupScale<__nv_bfloat16> &s, uint32_t *out) {
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
-        const uint32_t s = p == 0 ? word << 3 : word >> (4 * p - 3);
-        if constexpr (std::is_same<Op, __half>::value) {
-            const uint32_t u = (s & 0x00780078u) | 0x64006400u;                       // 1024 + 8t
-            __half2 v = __hfma2(*reinterpret_cast<const __half2 *>(&u), __half2half2(__ushort_as_half(0x3400)),
-                                __half2half2(__ushort_as_half(0xDC3C)));              // * 0.25 - 271 = 2t - 15
-            v = __hmul2(v, *reinterpret_cast<const __half2 *>(&scale2));
-            out[p] = *reinterpret_cast<const uint32_t *>(&v);
-        } else {
-            const uint32_t u = (s & 0x00780078u) | 0x3F803F80u;                       // 1 + t/16
-            __nv_bfloat162 v = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&u), __bfloat162bfloat162(__ushort_as_bfloat16(0x4200)),
-                                       __bfloat162bfloat162(__ushort_as_bfloat16(0xC23C)));   // * 32 - 47 = 2t - 15
-            v = __hmul2(v, *reinterpret_cast<const __nv_bfloat162 *>(&scale2));
-            out[p] = *reinterpret_cast<const uint32_t *>(&v);
-        }
+        const uint32_t u = (word >> (4 * p)) & 0x000F000Fu;
+        const __nv_bfloat162 v = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&u), s.mul, s.add);
+        out[p] = *reinterpret_cast<const uint32_t *>(&v);
     }
 }
-template <class Op> __device__ __forceinline__ uint32_t scale_pair(uint8_t b) {
-    if constexpr (std::is_same<Op, __half>::value) {
-        const __half2 v = __float2half2_rn(g4_scale_f32(b));
-        return *reinterpret_cast<const uint32_t *>(&v);
-    } else {
-        const __nv_bfloat162 v = __float2bfloat162_rn(g4_scale_f32(b));
-        return *reinterpret_cast<const uint32_t *>(&v);
+__device__ __forceinline__ void unpack_word(uint32_t word, const GroupScale<__half> &s, uint32_t *out) {
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        uint32_t u;
+        const uint32_t w = p < 2 ? word : word >> 8;
+        if (p & 1) asm("lop3.b32 %0, %1, 0x00F000F0, 0x64006400, 0xEA;" : "=r"(u) : "r"(w));
+        else asm("lop3.b32 %0, %1, 0x000F000F, 0x64006400, 0xEA;" : "=r"(u) : "r"(w));
+        const __half2 d = __hadd2(*reinterpret_cast<const __half2 *>(&u), __half2half2(__ushort_as_half(0xE400)));    // -1024
+        const __half2 v = __hfma2(d, (p & 1) ? s.mul1 : s.mul0, s.add);
+        out[p] = *reinterpret_cast<const uint32_t *>(&v);
     }
 }
 
@@ -437,57 +454,59 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
         }
     } else if (warp >= 8) {               // ------------------------------------------------ unpacking
         SlotCursor cur(p.offsets, p.experts, p.rows, TN);
+        // The two groups of four warps take stored tiles in turn, a thread unpacks a whole row of one: with both in flight,
+        // the waits and the latencies of one are covered by the other's arithmetic.
         Ring c, a;
-        const int q = warp & 3, half = (warp - 8) >> 2;
+        const int q = warp & 3, group = (warp - 8) >> 2;
         const int r = q * 32 + lane;
         const int log_group = p.w.group == 32 ? 5 : p.w.group == 64 ? 6 : 7;
+        int turn = 0;
         for (int t = first_work; !stop(); t += work_stride) {
             const ExpertSlot slot = cur.seek(t / p.ftiles);
             if (slot.expert < 0) break;
             bool ok = true;
-            for (int kt = 0; kt < p.steps; ++kt) {
+            for (int kt = 0; kt < p.steps; ++kt, c.next(L::C_STAGES), a.next(L::A_STAGES), turn ^= 1) {
+                if (turn != group) continue;
                 if (!(ok = warp_wait(&c_full[c.s], c.ph, 1))) break;
                 const uint8_t *src = smem + L::C_OFF + c.s * L::C_STAGE;
                 const uint8_t *sc = src + G4_TILE_WORDS * 4 + r;
+                uint4 u4[4];                                   // word w of unit u: columns 32w + 8u .. + 7 of row r
+#pragma unroll
+                for (int u = 0; u < 4; ++u) u4[u] = *reinterpret_cast<const uint4 *>(src + u * 2048 + r * 16);
+                uint8_t sb[4];
+#pragma unroll
+                for (int w = 0; w < 4; ++w) sb[w] = sc[((32 * w) >> log_group) * G4_TILE];
+                __syncwarp();
+                if (lane == 0) arrive_local(&c_empty[c.s]);
+                if (!(ok = warp_wait(&a_empty[a.s], a.ph ^ 1u, 0))) break;
                 if constexpr (MODE == G4_FWD) {
-                    // lane r, columns 64 * half .. + 63 of the tile: words 2 * half and 2 * half + 1 of the four units
-                    uint2 w2[4];
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) w2[u] = *reinterpret_cast<const uint2 *>(src + u * 2048 + r * 16 + half * 8);
-                    const uint32_t s0 = scale_pair<Op>(sc[((64 * half) >> log_group) * G4_TILE]);
-                    const uint32_t s1 = scale_pair<Op>(sc[((64 * half + 32) >> log_group) * G4_TILE]);
-                    __syncwarp();
-                    if (lane == 0) arrive_local(&c_empty[c.s]);
-                    uint32_t v[32];
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        unpack_word<Op>(w2[u].x, s0, v + 4 * u);
-                        unpack_word<Op>(w2[u].y, s1, v + 16 + 4 * u);
-                    }
-                    if (!(ok = warp_wait(&a_empty[a.s], a.ph ^ 1u, 0))) break;
+                    // lane r of the A operand, 32 tensor-memory columns (64 codes) at a time
                     tc_fence_after();
-                    tmem_store_32(tmem_base + ((uint32_t)(q * 32) << 16) + L::ACC_COLS + a.s * 64 + half * 32, v);
+                    const uint32_t at = tmem_base + ((uint32_t)(q * 32) << 16) + L::ACC_COLS + a.s * 64;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t v[32];
+                        const GroupScale<Op> s0(sb[2 * h]), s1(sb[2 * h + 1]);
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            unpack_word(h == 0 ? u4[u].x : u4[u].z, s0, v + 4 * u);
+                            unpack_word(h == 0 ? u4[u].y : u4[u].w, s1, v + 16 + 4 * u);
+                        }
+                        tmem_store_32(at + 32 * h, v);
+                    }
+                    tmem_store_wait();
                     tc_fence_before();
                 } else {
-                    // row r of the contraction, units 2 * half and 2 * half + 1: word w of unit u holds lanes 32w + 8u .. + 7
-                    uint4 w4[2];
-                    w4[0] = *reinterpret_cast<const uint4 *>(src + (2 * half) * 2048 + r * 16);
-                    w4[1] = *reinterpret_cast<const uint4 *>(src + (2 * half + 1) * 2048 + r * 16);
-                    uint32_t s[4];
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) s[w] = scale_pair<Op>(sc[((32 * w) >> log_group) * G4_TILE]);
-                    __syncwarp();
-                    if (lane == 0) arrive_local(&c_empty[c.s]);
-                    if (!(ok = warp_wait(&a_empty[a.s], a.ph ^ 1u, 0))) break;
+                    // row r of the contraction: eight lanes a word, 16 bytes of the MN-major operand
                     uint8_t *dst = smem + L::A_OFF + a.s * L::A_STAGE + r * 128;
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const uint32_t word[4] = {w4[u].x, w4[u].y, w4[u].z, w4[u].w};
+                    for (int w = 0; w < 4; ++w) {
+                        const GroupScale<Op> s(sb[w]);
 #pragma unroll
-                        for (int w = 0; w < 4; ++w) {
+                        for (int u = 0; u < 4; ++u) {
                             uint32_t v[4];
-                            unpack_word<Op>(word[w], s[w], v);
-                            const int chunk = (w & 1) * 4 + 2 * half + u;
+                            unpack_word(w == 0 ? u4[u].x : w == 1 ? u4[u].y : w == 2 ? u4[u].z : u4[u].w, s, v);
+                            const int chunk = (w & 1) * 4 + u;
                             *reinterpret_cast<uint4 *>(dst + (w >> 1) * (128 * 128) + ((chunk ^ (r & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
                         }
                     }
@@ -495,8 +514,6 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
                 }
                 __syncwarp();
                 if (lane == 0) arrive_leader<CG>(&a_full[a.s]);
-                c.next(L::C_STAGES);
-                a.next(L::A_STAGES);
             }
             if (!ok) break;
         }
@@ -511,7 +528,7 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
             if (!warp_wait(&acc_full[buf], (uint32_t)(local / L::ACC_BUFS) & 1u, 2)) break;
             tc_fence_after();
             const int f = ((t % p.ftiles) * CG + rank) * 128 + q * 32 + lane;
-            const float alpha = __ldg(p.w.alpha + slot.expert);
+            const float alpha = __ldg(p.w.alpha + slot.expert), undo = GroupScale<Op>::UNDO;
             T *dst = static_cast<T *>(p.out) + (int64_t)slot.first * p.ldo + f;
             const int have = slot.last - slot.first;
 #pragma unroll 1
@@ -521,7 +538,7 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
                 if (f < p.features) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
-                        if (c0 + i < have) real_store(dst + (int64_t)(c0 + i) * p.ldo, __fmul_rn(__uint_as_float(v[i]), alpha));
+                        if (c0 + i < have) real_store(dst + (int64_t)(c0 + i) * p.ldo, __fmul_rn(__fmul_rn(__uint_as_float(v[i]), undo), alpha));
                 }
                 __syncwarp();
             }
