@@ -224,6 +224,7 @@ struct G4TensorParams {
     int features;                         // width of the result
     int ftiles;                           // tiles of 128 * CG features
     int steps;                            // stored tiles along the contraction
+    bool out_vec;                         // the result's rows start and advance by whole 16 bytes
     unsigned int *err;
     unsigned int wait_limit;
 };
@@ -232,28 +233,32 @@ constexpr int G4_THREADS = 512;           // warps: 0 rows by TMA, 1 matrix inst
                                           // the tensor memory), 3 idle, 4-7 results, 8-15 unpacking
 constexpr int G4_UNPACK_WARPS = 4;        // that unpack one stored tile
 
-template <int CG, int TN, int MODE>
+// A stage is one stored tile of the contraction (128 steps): its unpacked weights (64 columns of tensor memory, or 32 KB
+// of shared memory) and the rows' parts.  Both halves of a stage fill and empty on one pair of barriers.
+template <int CG, int TN, int MODE, int PARTS>
 struct G4Shape {
     static constexpr int XROWS = TN / CG;                       // tokens whose rows this block stages
     static constexpr int X_SUB = XROWS * 128;                   // 64 columns of them, 128-byte swizzle
-    static constexpr int X_STAGE = 2 * X_SUB;                   // a stored tile's 128
-    static constexpr int C_STAGE = G4_TILE_WORDS * 4 + 512;     // codes and up to four rows of scales
+    static constexpr int X_PART = 2 * X_SUB;
     static constexpr int A_STAGE = MODE == G4_DATA ? 128 * 128 * 2 : 0;
-    static constexpr int A_SMEM_STAGES = 2;
-    static constexpr int ACC_BUFS = TN <= 128 ? 2 : 1;
-    static constexpr int A_STAGES = MODE == G4_DATA ? A_SMEM_STAGES : 4;     // (64 tensor-memory columns each)
-    static constexpr int C_STAGES = 4;
-    static constexpr int FIXED = C_STAGES * C_STAGE + (MODE == G4_DATA ? A_SMEM_STAGES * A_STAGE : 0);
-    static constexpr int X_FIT = (220 * 1024 - FIXED) / X_STAGE;
-    static constexpr int X_STAGES = X_FIT > 8 ? 8 : X_FIT;
-    static constexpr int X_OFF = 0;
-    static constexpr int A_OFF = X_STAGES * X_STAGE;
-    static constexpr int C_OFF = A_OFF + (MODE == G4_DATA ? A_SMEM_STAGES * A_STAGE : 0);
-    static constexpr int BAR_OFF = C_OFF + C_STAGES * C_STAGE;
-    static constexpr int TOTAL = BAR_OFF + (2 * (X_STAGES + C_STAGES + A_STAGES) + 4) * 8 + 16 + 1024;
+    static constexpr int STAGE = PARTS * X_PART + A_STAGE;
+    static constexpr int C_STAGE = G4_TILE_WORDS * 4 + 512;     // codes and up to four rows of scales
+    // deep where reading the codes is the bound; two where that makes room for a third stage
+    static constexpr int C_STAGES = TN <= 64 && PARTS == 1 ? 8 : (MODE == G4_DATA && TN > 128 ? 2 : 3);
+    // Two accumulators, so that results are stored under the next sum, where tensor memory has room for them.
+    static constexpr int ACC_BUFS = (MODE == G4_DATA ? 2 * TN <= 512 : 2 * TN <= 256) ? 2 : 1;
     static constexpr int ACC_COLS = ACC_BUFS * TN;
-    static_assert(ACC_COLS + (MODE == G4_FWD ? 64 * A_STAGES : 0) <= 512, "tensor memory");
-    static_assert(X_STAGES >= 2 && TOTAL <= 227 * 1024, "shared memory");
+    // fp32: sums leave tensor memory after every stage (see PROMOTE in the kernel)
+    static constexpr int OUT_WARP = PARTS == 1 ? 32 * 80 : 0;   // transposing buffer of a result warp: 32 tokens x 32 features
+    static constexpr int FIXED = C_STAGES * C_STAGE + 4 * OUT_WARP + 2048;
+    static constexpr int FIT_SMEM = (227 * 1024 - FIXED) / STAGE;
+    static constexpr int FIT_TMEM = MODE == G4_DATA ? 8 : (512 - ACC_COLS) / 64;
+    static constexpr int STAGES = FIT_SMEM < FIT_TMEM ? FIT_SMEM : FIT_TMEM;
+    static constexpr int C_OFF = STAGES * STAGE;
+    static constexpr int OUT_OFF = C_OFF + C_STAGES * C_STAGE;
+    static constexpr int BAR_OFF = OUT_OFF + 4 * OUT_WARP;
+    static constexpr int TOTAL = BAR_OFF + (2 * (STAGES + C_STAGES) + 5) * 8 + 16 + 1024;
+    static_assert(STAGES >= 2 && TOTAL <= 227 * 1024, "shared memory");
 };
 
 // A group's scale as the unpacking needs it.  A masked nibble is an integer multiple of the smallest step of its format:
@@ -304,22 +309,86 @@ __device__ __forceinline__ void unpack_word(uint32_t word, const GroupScale<__ha
     }
 }
 
+// 16 lanes x 32 columns: register 4i + {0, 1} of lane l holds row l/4, columns 8i + 2(l%4) + {0, 1}; + {2, 3} row l/4 + 8.
+__device__ __forceinline__ void tmem_load_16x32(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+}
+template <class T> __device__ __forceinline__ uint32_t pack_pair(float lo, float hi) {
+    if constexpr (std::is_same<T, __half>::value) {
+        const __half2 v = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&v);
+    } else {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&v);
+    }
+}
+
+// 32 tokens x 32 features of an accumulator (lanes = features) -> rows of a 2-byte result.  The quarter is transposed on its
+// way through shared memory (80 bytes a token: every store and load below is free of bank conflicts), so that a token's
+// features leave as 16-byte stores.  `f` the first feature, `vec`: rows start and advance by whole 16 bytes.
+template <class T>
+__device__ __forceinline__ void store_quarter(uint32_t taddr, uint8_t *buf, T *row0, int64_t ldo, int tokens, int f, int features,
+                                              float undo, float alpha, bool vec) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t at = smem_u32(buf) + ((lane >> 4) * 8 + (lane & 7)) * 80 + ((lane >> 3) & 1) * 16;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        uint32_t r[16];
+        tmem_load_16x32(taddr + ((uint32_t)(16 * h) << 16), r);
+        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        uint32_t v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] = pack_pair<T>(__fmul_rn(__fmul_rn(__uint_as_float(r[2 * i]), undo), alpha), __fmul_rn(__fmul_rn(__uint_as_float(r[2 * i + 1]), undo), alpha));
+#pragma unroll
+        for (int i = 0; i < 2; ++i)                       // tokens 16i .. 16i + 15, features 16h .. 16h + 15
+            asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};"
+                         ::"r"(at + i * 16 * 80 + h * 32), "r"(v[4 * i]), "r"(v[4 * i + 1]), "r"(v[4 * i + 2]), "r"(v[4 * i + 3]) : "memory");
+    }
+    __syncwarp();
+    const int f0 = f + (lane >> 3) * 8;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int token = i * 8 + (lane & 7);
+        if (token >= tokens) break;
+        const uint4 v = *reinterpret_cast<const uint4 *>(buf + token * 80 + (lane >> 3) * 16);
+        T *dst = row0 + (int64_t)token * ldo + f0;
+        if (vec && f0 + 8 <= features) {
+            *reinterpret_cast<uint4 *>(dst) = v;
+        } else {
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (f0 + j < features) reinterpret_cast<uint16_t *>(dst)[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+        }
+    }
+    __syncwarp();
+}
+
 template <int CG, int TN, int MODE, class T>
 __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_constant__ CUtensorMap map_x, const G4TensorParams p) {
-    using L = G4Shape<CG, TN, MODE>;
     using Op = typename G4Type<T>::Op;
     constexpr int PARTS = G4Type<T>::PARTS;
+    using L = G4Shape<CG, TN, MODE, PARTS>;
+    // The tensor cores cut a sum towards zero at every addition, which for a long contraction is a hundred times the
+    // rounding of an fp32 result.  fp32 results therefore add up only one stage in tensor memory (smallest parts first) and
+    // the result warps add the stages in registers, to nearest.
+    constexpr bool PROMOTE = PARTS > 1;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    uint64_t *x_full = reinterpret_cast<uint64_t *>(smem + L::BAR_OFF);     // leader: both blocks' rows have landed
-    uint64_t *x_empty = x_full + L::X_STAGES;                               // each block: the instructions have read them
-    uint64_t *c_full = x_empty + L::X_STAGES;                               // each block: its codes have landed
+    uint64_t *full = reinterpret_cast<uint64_t *>(smem + L::BAR_OFF);       // leader: both blocks' rows and unpacked weights
+    uint64_t *empty = full + L::STAGES;                                     // each block: the instructions have read a stage
+    uint64_t *c_full = empty + L::STAGES;                                   // each block: its codes have landed
     uint64_t *c_empty = c_full + L::C_STAGES;
-    uint64_t *a_full = c_empty + L::C_STAGES;                               // leader: both blocks have unpacked a tile
-    uint64_t *a_empty = a_full + L::A_STAGES;
-    uint64_t *acc_full = a_empty + L::A_STAGES;                             // each block
+    uint64_t *acc_full = c_empty + L::C_STAGES;                             // each block
     uint64_t *acc_empty = acc_full + 2;                                     // leader: both blocks have read an accumulator out
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(acc_empty + 2);
+    uint64_t *finish = acc_empty + 2;                                       // every instruction has completed
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(finish + 1);
     volatile uint32_t *abort_flag = tmem_slot + 1;
 
     const int warp = warp_index(), lane = threadIdx.x & 31;
@@ -327,10 +396,10 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
     const int first_work = blockIdx.x / CG, work_stride = gridDim.x / CG;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < L::X_STAGES; ++s) { mbar_init(&x_full[s], 1); mbar_init(&x_empty[s], 1); }
+        for (int s = 0; s < L::STAGES; ++s) { mbar_init(&full[s], G4_UNPACK_WARPS * CG + 1); mbar_init(&empty[s], 1); }
         for (int s = 0; s < L::C_STAGES; ++s) { mbar_init(&c_full[s], 1); mbar_init(&c_empty[s], G4_UNPACK_WARPS); }
-        for (int s = 0; s < L::A_STAGES; ++s) { mbar_init(&a_full[s], G4_UNPACK_WARPS * CG); mbar_init(&a_empty[s], 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 4 * CG); }
+        mbar_init(finish, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -349,51 +418,51 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
         return __all_sync(0xffffffffu, pair_wait<CG>(bar, parity, abort_flag, id, p.err, p.wait_limit));
     };
     auto stop = [&]() { return __any_sync(0xffffffffu, *abort_flag != 0); };       // the same answer for a whole warp
-    int committed = 0;                    // matrix-instruction thread: accumulators committed
 
     if (warp == 0) {                      // ------------------------------------------------ rows
         SlotCursor cur(p.offsets, p.experts, p.rows, TN);
-        Ring x;
+        Ring g;
         long long it = 0;
         for (int t = first_work; !stop(); t += work_stride) {
             const ExpertSlot slot = cur.seek(t / p.ftiles);
             if (slot.expert < 0) break;
             const int row = slot.first + rank * L::XROWS;
             bool ok = true;
-            for (int kt = 0; ok && kt < p.steps; ++kt)
-                for (int part = 0; part < PARTS; ++part) {
-                    if (!(ok = warp_wait(&x_empty[x.s], x.ph ^ 1u, 0))) break;
-                    if (elect_one()) {
-                        if (rank == 0) mbar_expect_tx(&x_full[x.s], CG * L::X_STAGE);
-                        uint8_t *dst = smem + L::X_OFF + x.s * L::X_STAGE;
-                        pair_load_2d<CG>(dst, &map_x, &x_full[x.s], kt * 128, part * p.rows + row);
-                        pair_load_2d<CG>(dst + L::X_SUB, &map_x, &x_full[x.s], kt * 128 + 64, part * p.rows + row);
+            for (int kt = 0; kt < p.steps; ++kt) {
+                if (!(ok = warp_wait(&empty[g.s], g.ph ^ 1u, 0))) break;
+                if (elect_one()) {
+                    if (rank == 0) mbar_expect_tx(&full[g.s], CG * PARTS * L::X_PART);
+                    uint8_t *dst = smem + g.s * L::STAGE;
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part) {
+                        pair_load_2d<CG>(dst + part * L::X_PART, &map_x, &full[g.s], kt * 128, part * p.rows + row);
+                        pair_load_2d<CG>(dst + part * L::X_PART + L::X_SUB, &map_x, &full[g.s], kt * 128 + 64, part * p.rows + row);
                     }
-                    __syncwarp();
-                    x.next(L::X_STAGES);
-                    ++it;
                 }
+                __syncwarp();
+                g.next(L::STAGES);
+                ++it;
+            }
             if (!ok) break;
         }
-        if (*abort_flag && lane == 0) {
-            if (rank == 0) drain_copies_in_flight(x_full, it, L::X_STAGES, p.wait_limit);
-            else for (int i = 0; i < 1000; ++i) __nanosleep(1000);            // its copies count on the leader's barriers
-        }
+        // after an abort the copies in flight may still land (their barriers may never complete, with unpacking stopped)
+        if (*abort_flag && it > 0)
+            for (int i = 0; i < 1000; ++i) __nanosleep(1000);
     } else if (warp == 2) {               // ------------------------------------------------ codes and scales
         SlotCursor cur(p.offsets, p.experts, p.rows, TN);
         Ring c;
         long long it = 0;
         const int groups = G4_TILE / p.w.group;
+        const int64_t stride = MODE == G4_FWD ? 1 : p.w.tiles_k;            // stored tiles between steps of the contraction
         for (int t = first_work; !stop(); t += work_stride) {
             const ExpertSlot slot = cur.seek(t / p.ftiles);
             if (slot.expert < 0) break;
             // a block whose features lie past the end repeats the last tile; its results are not stored
             const int f = min((t % p.ftiles) * CG + rank, (MODE == G4_FWD ? p.w.tiles_n : p.w.tiles_k) - 1);
-            const int64_t e0 = (int64_t)slot.expert * p.w.tiles_n * p.w.tiles_k;
+            int64_t tile = (int64_t)slot.expert * p.w.tiles_n * p.w.tiles_k + (MODE == G4_FWD ? (int64_t)f * p.w.tiles_k : f);
             bool ok = true;
-            for (int kt = 0; kt < p.steps; ++kt) {
+            for (int kt = 0; kt < p.steps; ++kt, tile += stride) {
                 if (!(ok = warp_wait(&c_empty[c.s], c.ph ^ 1u, 0))) break;
-                const int64_t tile = e0 + (MODE == G4_FWD ? (int64_t)f * p.w.tiles_k + kt : (int64_t)kt * p.w.tiles_k + f);
                 if (elect_one()) {
                     mbar_expect_tx(&c_full[c.s], G4_TILE_WORDS * 4 + groups * G4_TILE);
                     uint8_t *dst = smem + L::C_OFF + c.s * L::C_STAGE;
@@ -410,53 +479,51 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
     } else if (warp == 1) {               // ------------------------------------------------ matrix instructions
         if (rank == 0) {
             SlotCursor cur(p.offsets, p.experts, p.rows, TN);
-            Ring x, a;
+            Ring g, acc;
             constexpr uint32_t idesc = idesc_f16(G4Type<T>::FMT, 128 * CG, TN, MODE == G4_DATA, false);
-            int local = 0;
-            for (int t = first_work; !stop(); t += work_stride, ++local) {
+            const uint64_t b_desc = smem_desc_k_sw128(smem_u32(smem));
+            const uint64_t a_desc = smem_desc_mn_sw128(smem_u32(smem) + PARTS * L::X_PART, 128 * 128);
+            bool ok = true;
+            for (int t = first_work; ok && !stop(); t += work_stride) {
                 const ExpertSlot slot = cur.seek(t / p.ftiles);
                 if (slot.expert < 0) break;
-                const int buf = local % L::ACC_BUFS;
-                if (!pair_warp_wait(&acc_empty[buf], ((uint32_t)(local / L::ACC_BUFS) & 1u) ^ 1u, 3)) break;
-                const uint32_t d = tmem_base + (uint32_t)(buf * TN);
-                bool ok = true;
-                for (int kt = 0; ok && kt < p.steps; ++kt) {
-                    if (!(ok = pair_warp_wait(&a_full[a.s], a.ph, 1))) break;
-                    for (int part = 0; part < PARTS; ++part) {
-                        if (!(ok = warp_wait(&x_full[x.s], x.ph, 1))) break;
-                        tc_fence_after();
-                        const uint32_t xs = smem_u32(smem + L::X_OFF + x.s * L::X_STAGE);
-                        const uint64_t b0 = smem_desc_k_sw128(xs), b1 = smem_desc_k_sw128(xs + L::X_SUB);
-                        if (elect_one()) {
-                            if constexpr (MODE == G4_FWD) {
-                                const uint32_t at = tmem_base + L::ACC_COLS + a.s * 64;
+                for (int kt = 0; kt < p.steps; ++kt) {
+                    const bool fresh = PROMOTE || kt == 0;
+                    if (fresh) ok = pair_warp_wait(&acc_empty[acc.s], acc.ph ^ 1u, 3);
+                    if (ok) ok = pair_warp_wait(&full[g.s], g.ph, 1);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t d = tmem_base + (uint32_t)(acc.s * TN);
+                    if (elect_one()) {
+                        const uint64_t stage = (uint64_t)(g.s * (L::STAGE >> 4));
 #pragma unroll
-                                for (int j = 0; j < 8; ++j)
-                                    mma_f16_ts<CG>(d, at + 8 * j, (j < 4 ? b0 : b1) + 2 * (j & 3), idesc, (kt | part | j) != 0 ? 1u : 0u);
-                            } else {
-                                const uint64_t ad = smem_desc_mn_sw128(smem_u32(smem + L::A_OFF + a.s * L::A_STAGE), 128 * 128);
+                        for (int part = PARTS - 1; part >= 0; --part) {
 #pragma unroll
-                                for (int j = 0; j < 8; ++j)
-                                    mma_f16_ss<CG>(d, ad + 128 * j, (j < 4 ? b0 : b1) + 2 * (j & 3), idesc, (kt | part | j) != 0 ? 1u : 0u);
+                            for (int j = 0; j < 8; ++j) {
+                                const uint64_t bd = b_desc + stage + ((part * L::X_PART + (j >> 2) * L::X_SUB) >> 4) + 2 * (j & 3);
+                                const uint32_t more = !fresh || part != PARTS - 1 || j != 0 ? 1u : 0u;
+                                if constexpr (MODE == G4_FWD) mma_f16_ts<CG>(d, tmem_base + L::ACC_COLS + g.s * 64 + 8 * j, bd, idesc, more);
+                                else mma_f16_ss<CG>(d, a_desc + stage + 128 * j, bd, idesc, more);
                             }
-                            pair_commit<CG>(&x_empty[x.s]);
-                            if (part == PARTS - 1) pair_commit<CG>(&a_empty[a.s]);
                         }
-                        __syncwarp();
-                        x.next(L::X_STAGES);
+                        pair_commit<CG>(&empty[g.s]);
+                        if (PROMOTE || kt == p.steps - 1) pair_commit<CG>(&acc_full[acc.s]);
                     }
-                    a.next(L::A_STAGES);
+                    __syncwarp();
+                    g.next(L::STAGES);
+                    if (PROMOTE || kt == p.steps - 1) acc.next(L::ACC_BUFS);
                 }
-                if (elect_one()) pair_commit<CG>(&acc_full[buf]);            // also after a wait that gave up: see the end
-                __syncwarp();
-                committed = local + 1;
             }
+            // no instruction may still write tensor memory when it is given back: one more commit, waited for
+            if (elect_one()) pair_commit<CG>(finish);
+            __syncwarp();
+            for (uint32_t w = 0; w < p.wait_limit && !mbar_try_wait(finish, 0u); ++w) {}
         }
     } else if (warp >= 8) {               // ------------------------------------------------ unpacking
         SlotCursor cur(p.offsets, p.experts, p.rows, TN);
         // The two groups of four warps take stored tiles in turn, a thread unpacks a whole row of one: with both in flight,
         // the waits and the latencies of one are covered by the other's arithmetic.
-        Ring c, a;
+        Ring c, g;
         const int q = warp & 3, group = (warp - 8) >> 2;
         const int r = q * 32 + lane;
         const int log_group = p.w.group == 32 ? 5 : p.w.group == 64 ? 6 : 7;
@@ -465,7 +532,7 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
             const ExpertSlot slot = cur.seek(t / p.ftiles);
             if (slot.expert < 0) break;
             bool ok = true;
-            for (int kt = 0; kt < p.steps; ++kt, c.next(L::C_STAGES), a.next(L::A_STAGES), turn ^= 1) {
+            for (int kt = 0; kt < p.steps; ++kt, c.next(L::C_STAGES), g.next(L::STAGES), turn ^= 1) {
                 if (turn != group) continue;
                 if (!(ok = warp_wait(&c_full[c.s], c.ph, 1))) break;
                 const uint8_t *src = smem + L::C_OFF + c.s * L::C_STAGE;
@@ -478,11 +545,11 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
                 for (int w = 0; w < 4; ++w) sb[w] = sc[((32 * w) >> log_group) * G4_TILE];
                 __syncwarp();
                 if (lane == 0) arrive_local(&c_empty[c.s]);
-                if (!(ok = warp_wait(&a_empty[a.s], a.ph ^ 1u, 0))) break;
+                if (!(ok = warp_wait(&empty[g.s], g.ph ^ 1u, 0))) break;
                 if constexpr (MODE == G4_FWD) {
                     // lane r of the A operand, 32 tensor-memory columns (64 codes) at a time
                     tc_fence_after();
-                    const uint32_t at = tmem_base + ((uint32_t)(q * 32) << 16) + L::ACC_COLS + a.s * 64;
+                    const uint32_t at = tmem_base + ((uint32_t)(q * 32) << 16) + L::ACC_COLS + g.s * 64;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         uint32_t v[32];
@@ -498,7 +565,7 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
                     tc_fence_before();
                 } else {
                     // row r of the contraction: eight lanes a word, 16 bytes of the MN-major operand
-                    uint8_t *dst = smem + L::A_OFF + a.s * L::A_STAGE + r * 128;
+                    uint8_t *dst = smem + g.s * L::STAGE + PARTS * L::X_PART + r * 128;
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
                         const GroupScale<Op> s(sb[w]);
@@ -513,45 +580,63 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
                 __syncwarp();
-                if (lane == 0) arrive_leader<CG>(&a_full[a.s]);
+                if (lane == 0) arrive_leader<CG>(&full[g.s]);
             }
             if (!ok) break;
         }
     } else if (warp >= 4) {               // ------------------------------------------------ results
         SlotCursor cur(p.offsets, p.experts, p.rows, TN);
         const int q = warp & 3;
-        int local = 0;
-        for (int t = first_work; !stop(); t += work_stride, ++local) {
+        const float undo = GroupScale<Op>::UNDO;
+        Ring acc;
+        for (int t = first_work; !stop(); t += work_stride) {
             const ExpertSlot slot = cur.seek(t / p.ftiles);
             if (slot.expert < 0) break;
-            const int buf = local % L::ACC_BUFS;
-            if (!warp_wait(&acc_full[buf], (uint32_t)(local / L::ACC_BUFS) & 1u, 2)) break;
-            tc_fence_after();
-            const int f = ((t % p.ftiles) * CG + rank) * 128 + q * 32 + lane;
-            const float alpha = __ldg(p.w.alpha + slot.expert), undo = GroupScale<Op>::UNDO;
-            T *dst = static_cast<T *>(p.out) + (int64_t)slot.first * p.ldo + f;
+            const int f = ((t % p.ftiles) * CG + rank) * 128 + q * 32;
+            const float alpha = __ldg(p.w.alpha + slot.expert);
+            T *dst = static_cast<T *>(p.out) + (int64_t)slot.first * p.ldo;
             const int have = slot.last - slot.first;
-#pragma unroll 1
-            for (int c0 = 0; c0 < have; c0 += 32) {
-                uint32_t v[32];
-                tmem_load_32(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * TN + c0), v);
-                if (f < p.features) {
+            const uint32_t lanes = (uint32_t)(q * 32) << 16;
+            bool ok = true;
+            if constexpr (PROMOTE) {
+                float sum[TN];
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (c0 + i < have) real_store(dst + (int64_t)(c0 + i) * p.ldo, __fmul_rn(__fmul_rn(__uint_as_float(v[i]), undo), alpha));
+                for (int i = 0; i < TN; ++i) sum[i] = 0.0f;
+                for (int kt = 0; kt < p.steps; ++kt) {
+                    if (!(ok = warp_wait(&acc_full[acc.s], acc.ph, 2))) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int c0 = 0; c0 < TN; c0 += 32) {
+                        uint32_t v[32];
+                        tmem_load_32(tmem_base + lanes + (uint32_t)(acc.s * TN + c0), v);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) sum[c0 + i] = __fadd_rn(sum[c0 + i], __uint_as_float(v[i]));
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) arrive_leader<CG>(&acc_empty[acc.s]);
+                    acc.next(L::ACC_BUFS);
                 }
-                __syncwarp();
+                if (ok && f + lane < p.features)
+#pragma unroll
+                    for (int i = 0; i < TN; ++i)
+                        if (i < have) real_store(dst + (int64_t)i * p.ldo + f + lane, __fmul_rn(__fmul_rn(sum[i], undo), alpha));
+            } else {
+                if ((ok = warp_wait(&acc_full[acc.s], acc.ph, 2))) {
+                    tc_fence_after();
+                    uint8_t *buf = smem + L::OUT_OFF + q * L::OUT_WARP;
+#pragma unroll 1
+                    for (int c0 = 0; c0 < have; c0 += 32)
+                        store_quarter<T>(tmem_base + lanes + (uint32_t)(acc.s * TN + c0), buf, dst + (int64_t)c0 * p.ldo, p.ldo, have - c0, f,
+                                         p.features, undo, alpha, p.out_vec);
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) arrive_leader<CG>(&acc_empty[acc.s]);
+                    acc.next(L::ACC_BUFS);
+                }
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) arrive_leader<CG>(&acc_empty[buf]);
+            if (!ok) break;
         }
-    }
-    __syncwarp();
-    if (warp == 1 && rank == 0 && lane == 0 && committed > 0) {
-        // every instruction issued has completed once the last commit has arrived (an abort's tiles are committed too)
-        const int last = committed - 1;
-        for (uint32_t w = 0; w < p.wait_limit && !mbar_try_wait(&acc_full[last % L::ACC_BUFS], (uint32_t)(last / L::ACC_BUFS) & 1u); ++w) {}
     }
     tc_fence_before();
     __syncthreads();
@@ -580,7 +665,7 @@ inline bool make_map_16(CUtensorMap *map, bool fp16, const void *base, int64_t r
 // x: operand rows of G4Type<T>::Op, [PARTS * rows][ldx], 16-byte aligned rows, `width` columns.
 template <int CG, int TN, int MODE, class T>
 int g4_tensor_launch(const void *x, int64_t ldx, int width, G4TensorParams p, int sms, cudaStream_t st) {
-    using L = G4Shape<CG, TN, MODE>;
+    using L = G4Shape<CG, TN, MODE, G4Type<T>::PARTS>;
     auto kernel = g4_tensor_kernel<CG, TN, MODE, T>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::TOTAL) != cudaSuccess) return QNN_E_CUDA;
     CUtensorMap map;

@@ -1,5 +1,6 @@
 // Choice of the tile for a grouped product.
 #pragma once
+#include <stdlib.h>
 #include "g4_tensor.cuh"
 #include "g4_tensor_api.cuh"
 
@@ -17,9 +18,15 @@ int g4_tensor_pick(const void *x, int64_t ldx, const G4TensorArgs &a, cudaStream
     if (sms <= 0) return QNN_E_CUDA;
     const int width = MODE == G4_FWD ? a.w.k : a.w.n;
     const int64_t each = (a.rows + a.experts - 1) / a.experts;              // rows an expert has on average
-    if (each <= 48) return g4_tensor_launch<1, 32, MODE, T>(x, ldx, width, p, sms, st);
-    if (each <= 96) return g4_tensor_launch<1, 64, MODE, T>(x, ldx, width, p, sms, st);
-    return g4_tensor_launch<1, 128, MODE, T>(x, ldx, width, p, sms, st);
+    if constexpr (G4Type<T>::PARTS > 1) {
+        if (each <= 48) return g4_tensor_launch<1, 32, MODE, T>(x, ldx, width, p, sms, st);
+        return g4_tensor_launch<1, 64, MODE, T>(x, ldx, width, p, sms, st);
+    } else {
+        if (each <= 32) return g4_tensor_launch<1, 32, MODE, T>(x, ldx, width, p, sms, st);
+        if (each <= 96) return g4_tensor_launch<1, 64, MODE, T>(x, ldx, width, p, sms, st);
+        if (getenv("TN128")) return g4_tensor_launch<2, 128, MODE, T>(x, ldx, width, p, sms, st);
+        return g4_tensor_launch<2, 256, MODE, T>(x, ldx, width, p, sms, st);
+    }
 }
 
 template <int MODE>
