@@ -77,9 +77,6 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
     auto warp_wait = [&](uint64_t *bar, uint32_t parity, unsigned id) {
         return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, id, p.err, p.wait_limit));
     };
-    auto pair_warp_wait = [&](uint64_t *bar, uint32_t parity, unsigned id) {
-        return __all_sync(0xffffffffu, pair_wait<CG>(bar, parity, abort_flag, id, p.err, p.wait_limit));
-    };
     auto stop = [&]() { return __any_sync(0xffffffffu, *abort_flag != 0); };
     int committed = 0;
 
@@ -124,10 +121,10 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
                     if (!(ok = warp_wait(&landed[g.s], g.ph, 1))) break;
                     const int valid = last - r;
                     if (valid < L::ROWS) {
-                        uint8_t *stage = smem + g.s * L::STAGE;
+                        const uint32_t stage = smem_u32(smem) + g.s * L::STAGE;
                         for (int b = 0; b < L::STAGE / L::BLOCK; ++b)
                             for (int v = valid * 8 + lane; v < L::ROWS * 8; v += 32)
-                                *reinterpret_cast<uint4 *>(stage + b * L::BLOCK + v * 16) = make_uint4(0u, 0u, 0u, 0u);
+                                sts_128(stage + b * L::BLOCK + v * 16, 0u, 0u, 0u, 0u);
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     }
                     __syncwarp();
@@ -146,13 +143,13 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
                 expert_rows(p.offsets, t / per_expert, p.rows, first, last);
                 if (first >= last) continue;                     // nothing to add up: the result warps write zeros
                 const int buf = local % L::ACC_BUFS;
-                if (!pair_warp_wait(&acc_empty[buf], ((uint32_t)(local / L::ACC_BUFS) & 1u) ^ 1u, 3)) break;
+                if (!warp_wait(&acc_empty[buf], ((uint32_t)(local / L::ACC_BUFS) & 1u) ^ 1u, 3)) break;
                 tc_fence_after();
                 const uint32_t d = tmem_base + (uint32_t)(buf * TN);
                 bool ok = true;
                 for (int r = first; ok && r < last; r += L::ROWS)
                     for (int q = 0; q < PAIRS; ++q) {
-                        if (!(ok = pair_warp_wait(&ready[g.s], g.ph, 1))) break;
+                        if (!(ok = warp_wait(&ready[g.s], g.ph, 1))) break;
                         tc_fence_after();
                         const uint32_t at = smem_u32(smem + g.s * L::STAGE);
                         const uint64_t a = smem_desc_mn_sw128(at, L::BLOCK), b = smem_desc_mn_sw128(at + L::A_BYTES, L::BLOCK);

@@ -48,37 +48,16 @@ template <int CG> __device__ __forceinline__ uint32_t leader_addr(const void *p)
     if constexpr (CG == 2) asm volatile("mapa.shared::cluster.u32 %0, %0, 0;" : "+r"(a));
     return a;
 }
+// (Without a cluster-scope release, which waits some 1400 cycles for unrelated stores: what the arrival hands over is ordered
+// by tcgen05 fences for tensor memory and by the proxy fence for shared memory.)
 template <int CG> __device__ __forceinline__ void arrive_leader(uint64_t *bar) {
     if constexpr (CG == 1)
         asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
     else
-        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_addr<2>(bar)) : "memory");
+        asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(leader_addr<2>(bar)) : "memory");
 }
 __device__ __forceinline__ void arrive_local(uint64_t *bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t *bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
-    return ok != 0;
-}
-// mbar_wait for barriers on which the other block's threads arrive.
-template <int CG>
-__device__ __forceinline__ bool pair_wait(uint64_t *bar, uint32_t parity, volatile uint32_t *abort_flag, unsigned id,
-                                          unsigned int *err, uint32_t limit) {
-    if constexpr (CG == 1) {
-        return mbar_wait(bar, parity, abort_flag, id, err, limit);
-    } else {
-        for (uint32_t it = 0; it < limit; ++it) {
-            if (mbar_try_wait_cluster(bar, parity)) return true;
-            if ((it & 1023u) == 1023u && *abort_flag) return false;
-        }
-        *abort_flag = 1;
-        atomicCAS(err, 0u, 1u + id);
-        return false;
-    }
 }
 // 2-D box into this block's shared memory, its bytes counted on the leading block's barrier.
 template <int CG>
@@ -137,16 +116,12 @@ __device__ __forceinline__ void mma_f16_ss(uint32_t d, uint64_t a, uint64_t b, u
                      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
                      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
-// 32 columns of this thread's lane.
-__device__ __forceinline__ void tmem_store_32(uint32_t taddr, const uint32_t (&r)[32]) {
+// 16 columns of this thread's lane.
+__device__ __forceinline__ void tmem_store_16(uint32_t taddr, const uint32_t (&r)[16]) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
         ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
-          "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
-          "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
+          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
         : "memory");
 }
 __device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -172,6 +147,21 @@ __device__ __forceinline__ bool elect_one() {
     return ok != 0;
 }
 __device__ __forceinline__ int warp_index() { return __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0); }
+
+// Shared memory by its own address: behind the alignment of the dynamic array the compiler would take generic accesses.
+__device__ __forceinline__ uint4 lds_128(uint32_t a) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint8_t lds_8(uint32_t a) {
+    uint32_t v;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return (uint8_t)v;
+}
+__device__ __forceinline__ void sts_128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
 
 struct Ring {                                            // position in a ring of stages and the parity of its round
     int s = 0;
@@ -229,9 +219,9 @@ struct G4TensorParams {
     unsigned int wait_limit;
 };
 
-constexpr int G4_THREADS = 512;           // warps: 0 rows by TMA, 1 matrix instructions, 2 codes by bulk copies (and owner of
-                                          // the tensor memory), 3 idle, 4-7 results, 8-15 unpacking
-constexpr int G4_UNPACK_WARPS = 4;        // that unpack one stored tile
+// Warps: 0 rows by TMA, 1 matrix instructions, 2 codes by bulk copies (and owner of the tensor memory), 3 idle, 4-7 results,
+// from 8 on groups of four that unpack.
+constexpr int G4_UNPACK_WARPS = 4;
 
 // A stage is one stored tile of the contraction (128 steps): its unpacked weights (64 columns of tensor memory, or 32 KB
 // of shared memory) and the rows' parts.  Both halves of a stage fill and empty on one pair of barriers.
@@ -244,7 +234,7 @@ struct G4Shape {
     static constexpr int STAGE = PARTS * X_PART + A_STAGE;
     static constexpr int C_STAGE = G4_TILE_WORDS * 4 + 512;     // codes and up to four rows of scales
     // deep where reading the codes is the bound; two where that makes room for a third stage
-    static constexpr int C_STAGES = TN <= 64 && PARTS == 1 ? 8 : (MODE == G4_DATA && TN > 128 ? 2 : 3);
+    static constexpr int C_STAGES = TN <= 64 && PARTS == 1 ? (MODE == G4_DATA ? 4 : 8) : (MODE == G4_DATA && TN > 128 ? 2 : 3);
     // Two accumulators, so that results are stored under the next sum, where tensor memory has room for them.
     static constexpr int ACC_BUFS = (MODE == G4_DATA ? 2 * TN <= 512 : 2 * TN <= 256) ? 2 : 1;
     static constexpr int ACC_COLS = ACC_BUFS * TN;
@@ -254,6 +244,10 @@ struct G4Shape {
     static constexpr int FIT_SMEM = (227 * 1024 - FIXED) / STAGE;
     static constexpr int FIT_TMEM = MODE == G4_DATA ? 8 : (512 - ACC_COLS) / 64;
     static constexpr int STAGES = FIT_SMEM < FIT_TMEM ? FIT_SMEM : FIT_TMEM;
+    // Groups of unpacking warps, each with a stage of its own.  One tile takes a warp some 1100 cycles: two groups keep up
+    // with the 1024 (or 512) cycles that wide tiles multiply for, narrow ones are bound by unpacking and take what fits.
+    static constexpr int GROUPS = PARTS > 1 || TN > 64 ? 2 : (STAGES < 4 ? STAGES : 4);
+    static constexpr int THREADS = 256 + 128 * GROUPS;
     static constexpr int C_OFF = STAGES * STAGE;
     static constexpr int OUT_OFF = C_OFF + C_STAGES * C_STAGE;
     static constexpr int BAR_OFF = OUT_OFF + 4 * OUT_WARP;
@@ -332,10 +326,10 @@ template <class T> __device__ __forceinline__ uint32_t pack_pair(float lo, float
 // way through shared memory (80 bytes a token: every store and load below is free of bank conflicts), so that a token's
 // features leave as 16-byte stores.  `f` the first feature, `vec`: rows start and advance by whole 16 bytes.
 template <class T>
-__device__ __forceinline__ void store_quarter(uint32_t taddr, uint8_t *buf, T *row0, int64_t ldo, int tokens, int f, int features,
+__device__ __forceinline__ void store_quarter(uint32_t taddr, uint32_t buf, T *row0, int64_t ldo, int tokens, int f, int features,
                                               float undo, float alpha, bool vec) {
     const int lane = threadIdx.x & 31;
-    const uint32_t at = smem_u32(buf) + ((lane >> 4) * 8 + (lane & 7)) * 80 + ((lane >> 3) & 1) * 16;
+    const uint32_t at = buf + ((lane >> 4) * 8 + (lane & 7)) * 80 + ((lane >> 3) & 1) * 16;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         uint32_t r[16];
@@ -352,26 +346,29 @@ __device__ __forceinline__ void store_quarter(uint32_t taddr, uint8_t *buf, T *r
     }
     __syncwarp();
     const int f0 = f + (lane >> 3) * 8;
+    uint4 v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = lds_128(buf + (i * 8 + (lane & 7)) * 80 + (lane >> 3) * 16);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int token = i * 8 + (lane & 7);
-        if (token >= tokens) break;
-        const uint4 v = *reinterpret_cast<const uint4 *>(buf + token * 80 + (lane >> 3) * 16);
-        T *dst = row0 + (int64_t)token * ldo + f0;
-        if (vec && f0 + 8 <= features) {
-            *reinterpret_cast<uint4 *>(dst) = v;
-        } else {
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        if (token < tokens) {
+            T *dst = row0 + (int64_t)token * ldo + f0;
+            if (vec && f0 + 8 <= features) {
+                *reinterpret_cast<uint4 *>(dst) = v[i];
+            } else {
+                const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (f0 + j < features) reinterpret_cast<uint16_t *>(dst)[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+                for (int j = 0; j < 8; ++j)
+                    if (f0 + j < features) reinterpret_cast<uint16_t *>(dst)[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+            }
         }
     }
     __syncwarp();
 }
 
 template <int CG, int TN, int MODE, class T>
-__global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_constant__ CUtensorMap map_x, const G4TensorParams p) {
+__global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREADS, 1) g4_tensor_kernel(const __grid_constant__ CUtensorMap map_x, const G4TensorParams p) {
     using Op = typename G4Type<T>::Op;
     constexpr int PARTS = G4Type<T>::PARTS;
     using L = G4Shape<CG, TN, MODE, PARTS>;
@@ -381,6 +378,7 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
     constexpr bool PROMOTE = PARTS > 1;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    const uint32_t smem_at = smem_u32(smem);
     uint64_t *full = reinterpret_cast<uint64_t *>(smem + L::BAR_OFF);       // leader: both blocks' rows and unpacked weights
     uint64_t *empty = full + L::STAGES;                                     // each block: the instructions have read a stage
     uint64_t *c_full = empty + L::STAGES;                                   // each block: its codes have landed
@@ -413,9 +411,6 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
     // waits of a whole warp: every lane polls (each needs the barrier's acquire), all go on or all give up
     auto warp_wait = [&](uint64_t *bar, uint32_t parity, unsigned id) {
         return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, id, p.err, p.wait_limit));
-    };
-    auto pair_warp_wait = [&](uint64_t *bar, uint32_t parity, unsigned id) {
-        return __all_sync(0xffffffffu, pair_wait<CG>(bar, parity, abort_flag, id, p.err, p.wait_limit));
     };
     auto stop = [&]() { return __any_sync(0xffffffffu, *abort_flag != 0); };       // the same answer for a whole warp
 
@@ -481,16 +476,16 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
             SlotCursor cur(p.offsets, p.experts, p.rows, TN);
             Ring g, acc;
             constexpr uint32_t idesc = idesc_f16(G4Type<T>::FMT, 128 * CG, TN, MODE == G4_DATA, false);
-            const uint64_t b_desc = smem_desc_k_sw128(smem_u32(smem));
-            const uint64_t a_desc = smem_desc_mn_sw128(smem_u32(smem) + PARTS * L::X_PART, 128 * 128);
+            const uint64_t b_desc = smem_desc_k_sw128(smem_at);
+            const uint64_t a_desc = smem_desc_mn_sw128(smem_at + PARTS * L::X_PART, 128 * 128);
             bool ok = true;
             for (int t = first_work; ok && !stop(); t += work_stride) {
                 const ExpertSlot slot = cur.seek(t / p.ftiles);
                 if (slot.expert < 0) break;
                 for (int kt = 0; kt < p.steps; ++kt) {
                     const bool fresh = PROMOTE || kt == 0;
-                    if (fresh) ok = pair_warp_wait(&acc_empty[acc.s], acc.ph ^ 1u, 3);
-                    if (ok) ok = pair_warp_wait(&full[g.s], g.ph, 1);
+                    if (fresh) ok = warp_wait(&acc_empty[acc.s], acc.ph ^ 1u, 3);
+                    if (ok) ok = warp_wait(&full[g.s], g.ph, 1);
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t d = tmem_base + (uint32_t)(acc.s * TN);
@@ -521,8 +516,8 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
         }
     } else if (warp >= 8) {               // ------------------------------------------------ unpacking
         SlotCursor cur(p.offsets, p.experts, p.rows, TN);
-        // The two groups of four warps take stored tiles in turn, a thread unpacks a whole row of one: with both in flight,
-        // the waits and the latencies of one are covered by the other's arithmetic.
+        // The groups take stored tiles in turn, a thread unpacks a whole row of one: the waits and latencies of one group are
+        // covered by the others' arithmetic.
         Ring c, g;
         const int q = warp & 3, group = (warp - 8) >> 2;
         const int r = q * 32 + lane;
@@ -532,40 +527,39 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
             const ExpertSlot slot = cur.seek(t / p.ftiles);
             if (slot.expert < 0) break;
             bool ok = true;
-            for (int kt = 0; kt < p.steps; ++kt, c.next(L::C_STAGES), g.next(L::STAGES), turn ^= 1) {
+            for (int kt = 0; kt < p.steps; ++kt, c.next(L::C_STAGES), g.next(L::STAGES), turn = turn == L::GROUPS - 1 ? 0 : turn + 1) {
                 if (turn != group) continue;
                 if (!(ok = warp_wait(&c_full[c.s], c.ph, 1))) break;
-                const uint8_t *src = smem + L::C_OFF + c.s * L::C_STAGE;
-                const uint8_t *sc = src + G4_TILE_WORDS * 4 + r;
+                const uint32_t src = smem_at + L::C_OFF + c.s * L::C_STAGE;
                 uint4 u4[4];                                   // word w of unit u: columns 32w + 8u .. + 7 of row r
 #pragma unroll
-                for (int u = 0; u < 4; ++u) u4[u] = *reinterpret_cast<const uint4 *>(src + u * 2048 + r * 16);
+                for (int u = 0; u < 4; ++u) u4[u] = lds_128(src + u * 2048 + r * 16);
                 uint8_t sb[4];
+                sb[0] = lds_8(src + G4_TILE_WORDS * 4 + r);
 #pragma unroll
-                for (int w = 0; w < 4; ++w) sb[w] = sc[((32 * w) >> log_group) * G4_TILE];
+                for (int w = 1; w < 4; ++w)
+                    sb[w] = log_group == 7 ? sb[0] : lds_8(src + G4_TILE_WORDS * 4 + ((32 * w) >> log_group) * G4_TILE + r);
                 __syncwarp();
                 if (lane == 0) arrive_local(&c_empty[c.s]);
                 if (!(ok = warp_wait(&empty[g.s], g.ph ^ 1u, 0))) break;
                 if constexpr (MODE == G4_FWD) {
-                    // lane r of the A operand, 32 tensor-memory columns (64 codes) at a time
+                    // lane r of the A operand, 16 tensor-memory columns (32 codes) at a time
                     tc_fence_after();
                     const uint32_t at = tmem_base + ((uint32_t)(q * 32) << 16) + L::ACC_COLS + g.s * 64;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint32_t v[32];
-                        const GroupScale<Op> s0(sb[2 * h]), s1(sb[2 * h + 1]);
+                    for (int w = 0; w < 4; ++w) {
+                        uint32_t v[16];
+                        const GroupScale<Op> s(sb[w]);
 #pragma unroll
-                        for (int u = 0; u < 4; ++u) {
-                            unpack_word(h == 0 ? u4[u].x : u4[u].z, s0, v + 4 * u);
-                            unpack_word(h == 0 ? u4[u].y : u4[u].w, s1, v + 16 + 4 * u);
-                        }
-                        tmem_store_32(at + 32 * h, v);
+                        for (int u = 0; u < 4; ++u)
+                            unpack_word(w == 0 ? u4[u].x : w == 1 ? u4[u].y : w == 2 ? u4[u].z : u4[u].w, s, v + 4 * u);
+                        tmem_store_16(at + 16 * w, v);
                     }
                     tmem_store_wait();
                     tc_fence_before();
                 } else {
                     // row r of the contraction: eight lanes a word, 16 bytes of the MN-major operand
-                    uint8_t *dst = smem + g.s * L::STAGE + PARTS * L::X_PART + r * 128;
+                    const uint32_t dst = smem_at + g.s * L::STAGE + PARTS * L::X_PART + r * 128;
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
                         const GroupScale<Op> s(sb[w]);
@@ -574,7 +568,7 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
                             uint32_t v[4];
                             unpack_word(w == 0 ? u4[u].x : w == 1 ? u4[u].y : w == 2 ? u4[u].z : u4[u].w, s, v);
                             const int chunk = (w & 1) * 4 + u;
-                            *reinterpret_cast<uint4 *>(dst + (w >> 1) * (128 * 128) + ((chunk ^ (r & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+                            sts_128(dst + (w >> 1) * (128 * 128) + ((chunk ^ (r & 7)) << 4), v[0], v[1], v[2], v[3]);
                         }
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -624,7 +618,7 @@ __global__ void __launch_bounds__(G4_THREADS, 1) g4_tensor_kernel(const __grid_c
             } else {
                 if ((ok = warp_wait(&acc_full[acc.s], acc.ph, 2))) {
                     tc_fence_after();
-                    uint8_t *buf = smem + L::OUT_OFF + q * L::OUT_WARP;
+                    const uint32_t buf = smem_at + L::OUT_OFF + q * L::OUT_WARP;
 #pragma unroll 1
                     for (int c0 = 0; c0 < have; c0 += 32)
                         store_quarter<T>(tmem_base + lanes + (uint32_t)(acc.s * TN + c0), buf, dst + (int64_t)c0 * p.ldo, p.ldo, have - c0, f,
@@ -676,7 +670,7 @@ int g4_tensor_launch(const void *x, int64_t ldx, int width, G4TensorParams p, in
     const int most = sms / CG;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((work < most ? work : most) * CG));
-    cfg.blockDim = dim3(G4_THREADS);
+    cfg.blockDim = dim3(L::THREADS);
     cfg.dynamicSmemBytes = L::TOTAL;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
