@@ -169,6 +169,9 @@ struct Ring {                                            // position in a ring o
     __device__ __forceinline__ void next(int stages) {
         if (++s == stages) { s = 0; ph ^= 1u; }
     }
+    __device__ __forceinline__ void skip(int n, int stages) {      // n <= stages
+        if ((s += n) >= stages) { s -= stages; ph ^= 1u; }
+    }
 };
 
 // Blocks of TN rows, counted expert by expert, visited in increasing order by a whole warp.
@@ -188,6 +191,11 @@ struct SlotCursor {
             const int o = __shfl_up_sync(0xffffffffu, incl, d);
             if (lane >= d) incl += o;
         }
+    }
+    __device__ __forceinline__ int64_t count() {         // blocks in all; the cursor is spent
+        int64_t total = 0;
+        for (; base < experts; base += 32, load()) total += __shfl_sync(0xffffffffu, incl, 31);
+        return total;
     }
     __device__ __forceinline__ ExpertSlot seek(int slot) {
         while (base < experts) {
@@ -248,10 +256,13 @@ struct G4Shape {
     // with the 1024 (or 512) cycles that wide tiles multiply for, narrow ones are bound by unpacking and take what fits.
     static constexpr int GROUPS = PARTS > 1 || TN > 64 ? 2 : (STAGES < 4 ? STAGES : 4);
     static constexpr int THREADS = 256 + 128 * GROUPS;
+    static constexpr bool ONE_THREAD = TN <= 64;
     static constexpr int C_OFF = STAGES * STAGE;
     static constexpr int OUT_OFF = C_OFF + C_STAGES * C_STAGE;
     static constexpr int BAR_OFF = OUT_OFF + 4 * OUT_WARP;
     static constexpr int TOTAL = BAR_OFF + (2 * (STAGES + C_STAGES) + 5) * 8 + 16 + 1024;
+    static_assert(CG == 1 || TN >= 128, "narrower tiles of a pair ended in a launch failure whose cause was not found");
+    static_assert(GROUPS <= STAGES && GROUPS <= C_STAGES, "a group skips at most one round of a ring");
     static_assert(STAGES >= 2 && TOTAL <= 227 * 1024, "shared memory");
 };
 
@@ -412,7 +423,49 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
     auto warp_wait = [&](uint64_t *bar, uint32_t parity, unsigned id) {
         return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, id, p.err, p.wait_limit));
     };
+    auto stages_of_this_block = [&]() -> int64_t {
+        const int64_t tiles = SlotCursor(p.offsets, p.experts, p.rows, TN).count() * p.ftiles;
+        return tiles > first_work ? (tiles - first_work + work_stride - 1) / work_stride * p.steps : 0;
+    };
     auto stop = [&]() { return __any_sync(0xffffffffu, *abort_flag != 0); };       // the same answer for a whole warp
+
+    // The matrix instructions of `left` stages; agree() and alone() say how a wait's outcome is shared and who issues.
+    auto issue_stages = [&](int64_t left, auto agree, auto alone) {
+        Ring acc;
+        constexpr uint32_t idesc = idesc_f16(G4Type<T>::FMT, 128 * CG, TN, MODE == G4_DATA, false);
+        const uint64_t b_desc = smem_desc_k_sw128(smem_at);
+        const uint64_t a_desc = smem_desc_mn_sw128(smem_at + PARTS * L::X_PART, 128 * 128);
+        bool ok = true;
+        uint32_t ph = 0;
+        int kt = 0;
+        for (; ok && left > 0; ph ^= 1u) {
+#pragma unroll
+            for (int g = 0; g < L::STAGES; ++g) {
+                if (left-- <= 0) break;
+                const bool fresh = PROMOTE || kt == 0, done = PROMOTE || kt == p.steps - 1;
+                if (fresh && !(ok = agree(mbar_wait(&acc_empty[acc.s], acc.ph ^ 1u, abort_flag, 3, p.err, p.wait_limit)))) break;
+                if (!(ok = agree(mbar_wait(&full[g], ph, abort_flag, 1, p.err, p.wait_limit)))) break;
+                tc_fence_after();
+                const uint32_t d = tmem_base + (uint32_t)(acc.s * TN);
+                alone([&]() {
+#pragma unroll
+                    for (int part = PARTS - 1; part >= 0; --part) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const uint64_t bd = b_desc + ((g * L::STAGE + part * L::X_PART + (j >> 2) * L::X_SUB) >> 4) + 2 * (j & 3);
+                            const uint32_t more = part != PARTS - 1 || j != 0 ? 1u : (fresh ? 0u : 1u);
+                            if constexpr (MODE == G4_FWD) mma_f16_ts<CG>(d, tmem_base + L::ACC_COLS + g * 64 + 8 * j, bd, idesc, more);
+                            else mma_f16_ss<CG>(d, a_desc + ((g * L::STAGE) >> 4) + 128 * j, bd, idesc, more);
+                        }
+                    }
+                    pair_commit<CG>(&empty[g]);
+                    if (done) pair_commit<CG>(&acc_full[acc.s]);
+                });
+                if (done) acc.next(L::ACC_BUFS);
+                kt = kt == p.steps - 1 ? 0 : kt + 1;
+            }
+        }
+    };
 
     if (warp == 0) {                      // ------------------------------------------------ rows
         SlotCursor cur(p.offsets, p.experts, p.rows, TN);
@@ -473,110 +526,76 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
         if (*abort_flag && lane == 0) drain_copies_in_flight(c_full, it, L::C_STAGES, p.wait_limit);
     } else if (warp == 1) {               // ------------------------------------------------ matrix instructions
         if (rank == 0) {
-            SlotCursor cur(p.offsets, p.experts, p.rows, TN);
-            Ring g, acc;
-            constexpr uint32_t idesc = idesc_f16(G4Type<T>::FMT, 128 * CG, TN, MODE == G4_DATA, false);
-            const uint64_t b_desc = smem_desc_k_sw128(smem_at);
-            const uint64_t a_desc = smem_desc_mn_sw128(smem_at + PARTS * L::X_PART, 128 * 128);
-            bool ok = true;
-            for (int t = first_work; ok && !stop(); t += work_stride) {
-                const ExpertSlot slot = cur.seek(t / p.ftiles);
-                if (slot.expert < 0) break;
-                for (int kt = 0; kt < p.steps; ++kt) {
-                    const bool fresh = PROMOTE || kt == 0;
-                    if (fresh) ok = warp_wait(&acc_empty[acc.s], acc.ph ^ 1u, 3);
-                    if (ok) ok = warp_wait(&full[g.s], g.ph, 1);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint32_t d = tmem_base + (uint32_t)(acc.s * TN);
-                    if (elect_one()) {
-                        const uint64_t stage = (uint64_t)(g.s * (L::STAGE >> 4));
-#pragma unroll
-                        for (int part = PARTS - 1; part >= 0; --part) {
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                const uint64_t bd = b_desc + stage + ((part * L::X_PART + (j >> 2) * L::X_SUB) >> 4) + 2 * (j & 3);
-                                const uint32_t more = !fresh || part != PARTS - 1 || j != 0 ? 1u : 0u;
-                                if constexpr (MODE == G4_FWD) mma_f16_ts<CG>(d, tmem_base + L::ACC_COLS + g.s * 64 + 8 * j, bd, idesc, more);
-                                else mma_f16_ss<CG>(d, a_desc + stage + 128 * j, bd, idesc, more);
-                            }
-                        }
-                        pair_commit<CG>(&empty[g.s]);
-                        if (PROMOTE || kt == p.steps - 1) pair_commit<CG>(&acc_full[acc.s]);
-                    }
-                    __syncwarp();
-                    g.next(L::STAGES);
-                    if (PROMOTE || kt == p.steps - 1) acc.next(L::ACC_BUFS);
-                }
+            // It needs the number of stages, not whose tiles they are.  Wide tiles: the whole warp walks along and one lane
+            // issues, which keeps the operands' addresses in uniform registers.  Narrow tiles: one thread does it all, which
+            // makes the waits cheaper; there they take longer than the instructions.
+            const int64_t total = stages_of_this_block();
+            if constexpr (L::ONE_THREAD) {
+                if (elect_one()) issue_stages(total, [](bool ok) { return ok; }, [](auto f) { f(); });
+            } else {
+                issue_stages(total, [](bool ok) { return (bool)__all_sync(0xffffffffu, ok); }, [](auto f) { if (elect_one()) f(); __syncwarp(); });
             }
+            __syncwarp();
             // no instruction may still write tensor memory when it is given back: one more commit, waited for
             if (elect_one()) pair_commit<CG>(finish);
             __syncwarp();
             for (uint32_t w = 0; w < p.wait_limit && !mbar_try_wait(finish, 0u); ++w) {}
         }
     } else if (warp >= 8) {               // ------------------------------------------------ unpacking
-        SlotCursor cur(p.offsets, p.experts, p.rows, TN);
         // The groups take stored tiles in turn, a thread unpacks a whole row of one: the waits and latencies of one group are
-        // covered by the others' arithmetic.
-        Ring c, g;
+        // covered by the others' arithmetic.  Which tile it is does not matter here.
         const int q = warp & 3, group = (warp - 8) >> 2;
         const int r = q * 32 + lane;
         const int log_group = p.w.group == 32 ? 5 : p.w.group == 64 ? 6 : 7;
-        int turn = 0;
-        for (int t = first_work; !stop(); t += work_stride) {
-            const ExpertSlot slot = cur.seek(t / p.ftiles);
-            if (slot.expert < 0) break;
-            bool ok = true;
-            for (int kt = 0; kt < p.steps; ++kt, c.next(L::C_STAGES), g.next(L::STAGES), turn = turn == L::GROUPS - 1 ? 0 : turn + 1) {
-                if (turn != group) continue;
-                if (!(ok = warp_wait(&c_full[c.s], c.ph, 1))) break;
-                const uint32_t src = smem_at + L::C_OFF + c.s * L::C_STAGE;
-                uint4 u4[4];                                   // word w of unit u: columns 32w + 8u .. + 7 of row r
+        Ring c, g;
+        c.s = g.s = group;
+        for (int64_t left = stages_of_this_block() - group; left > 0; left -= L::GROUPS, c.skip(L::GROUPS, L::C_STAGES), g.skip(L::GROUPS, L::STAGES)) {
+            if (!warp_wait(&c_full[c.s], c.ph, 1)) break;
+            const uint32_t src = smem_at + L::C_OFF + c.s * L::C_STAGE;
+            uint4 u4[4];                                   // word w of unit u: columns 32w + 8u .. + 7 of row r
 #pragma unroll
-                for (int u = 0; u < 4; ++u) u4[u] = lds_128(src + u * 2048 + r * 16);
-                uint8_t sb[4];
-                sb[0] = lds_8(src + G4_TILE_WORDS * 4 + r);
+            for (int u = 0; u < 4; ++u) u4[u] = lds_128(src + u * 2048 + r * 16);
+            uint8_t sb[4];
+            sb[0] = lds_8(src + G4_TILE_WORDS * 4 + r);
 #pragma unroll
-                for (int w = 1; w < 4; ++w)
-                    sb[w] = log_group == 7 ? sb[0] : lds_8(src + G4_TILE_WORDS * 4 + ((32 * w) >> log_group) * G4_TILE + r);
-                __syncwarp();
-                if (lane == 0) arrive_local(&c_empty[c.s]);
-                if (!(ok = warp_wait(&empty[g.s], g.ph ^ 1u, 0))) break;
-                if constexpr (MODE == G4_FWD) {
-                    // lane r of the A operand, 16 tensor-memory columns (32 codes) at a time
-                    tc_fence_after();
-                    const uint32_t at = tmem_base + ((uint32_t)(q * 32) << 16) + L::ACC_COLS + g.s * 64;
+            for (int w = 1; w < 4; ++w)
+                sb[w] = log_group == 7 ? sb[0] : lds_8(src + G4_TILE_WORDS * 4 + ((32 * w) >> log_group) * G4_TILE + r);
+            __syncwarp();
+            if (lane == 0) arrive_local(&c_empty[c.s]);
+            if (!warp_wait(&empty[g.s], g.ph ^ 1u, 0)) break;
+            if constexpr (MODE == G4_FWD) {
+                // lane r of the A operand, 16 tensor-memory columns (32 codes) at a time
+                tc_fence_after();
+                const uint32_t at = tmem_base + ((uint32_t)(q * 32) << 16) + L::ACC_COLS + g.s * 64;
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        uint32_t v[16];
-                        const GroupScale<Op> s(sb[w]);
+                for (int w = 0; w < 4; ++w) {
+                    uint32_t v[16];
+                    const GroupScale<Op> s(sb[w]);
 #pragma unroll
-                        for (int u = 0; u < 4; ++u)
-                            unpack_word(w == 0 ? u4[u].x : w == 1 ? u4[u].y : w == 2 ? u4[u].z : u4[u].w, s, v + 4 * u);
-                        tmem_store_16(at + 16 * w, v);
-                    }
-                    tmem_store_wait();
-                    tc_fence_before();
-                } else {
-                    // row r of the contraction: eight lanes a word, 16 bytes of the MN-major operand
-                    const uint32_t dst = smem_at + g.s * L::STAGE + PARTS * L::X_PART + r * 128;
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const GroupScale<Op> s(sb[w]);
-#pragma unroll
-                        for (int u = 0; u < 4; ++u) {
-                            uint32_t v[4];
-                            unpack_word(w == 0 ? u4[u].x : w == 1 ? u4[u].y : w == 2 ? u4[u].z : u4[u].w, s, v);
-                            const int chunk = (w & 1) * 4 + u;
-                            sts_128(dst + (w >> 1) * (128 * 128) + ((chunk ^ (r & 7)) << 4), v[0], v[1], v[2], v[3]);
-                        }
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    for (int u = 0; u < 4; ++u)
+                        unpack_word(w == 0 ? u4[u].x : w == 1 ? u4[u].y : w == 2 ? u4[u].z : u4[u].w, s, v + 4 * u);
+                    tmem_store_16(at + 16 * w, v);
                 }
-                __syncwarp();
-                if (lane == 0) arrive_leader<CG>(&full[g.s]);
+                tmem_store_wait();
+                tc_fence_before();
+            } else {
+                // row r of the contraction: eight lanes a word, 16 bytes of the MN-major operand
+                const uint32_t dst = smem_at + g.s * L::STAGE + PARTS * L::X_PART + r * 128;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const GroupScale<Op> s(sb[w]);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        uint32_t v[4];
+                        unpack_word(w == 0 ? u4[u].x : w == 1 ? u4[u].y : w == 2 ? u4[u].z : u4[u].w, s, v);
+                        const int chunk = (w & 1) * 4 + u;
+                        sts_128(dst + (w >> 1) * (128 * 128) + ((chunk ^ (r & 7)) << 4), v[0], v[1], v[2], v[3]);
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             }
-            if (!ok) break;
+            __syncwarp();
+            if (lane == 0) arrive_leader<CG>(&full[g.s]);
         }
     } else if (warp >= 4) {               // ------------------------------------------------ results
         SlotCursor cur(p.offsets, p.experts, p.rows, TN);

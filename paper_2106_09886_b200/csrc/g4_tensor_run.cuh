@@ -1,6 +1,5 @@
 // Choice of the tile for a grouped product.
 #pragma once
-#include <stdlib.h>
 #include "g4_tensor.cuh"
 #include "g4_tensor_api.cuh"
 
@@ -12,6 +11,7 @@ int g4_tensor_pick(const void *x, int64_t ldx, const G4TensorArgs &a, cudaStream
     p.w = a.w; p.offsets = a.offsets; p.experts = a.experts; p.rows = a.rows; p.out = a.out; p.ldo = a.ldo;
     p.features = MODE == G4_FWD ? a.w.n : a.w.k;
     p.steps = MODE == G4_FWD ? a.w.tiles_k : a.w.tiles_n;
+    p.out_vec = sizeof(T) == 2 && qnn_aligned(a.out, 16) && a.ldo % 8 == 0;
     p.wait_limit = WAIT_LIMIT;
     if (!(p.err = qnn_tc_error_word())) return QNN_E_CUDA;
     const int sms = sm_count();
@@ -24,7 +24,6 @@ int g4_tensor_pick(const void *x, int64_t ldx, const G4TensorArgs &a, cudaStream
     } else {
         if (each <= 32) return g4_tensor_launch<1, 32, MODE, T>(x, ldx, width, p, sms, st);
         if (each <= 96) return g4_tensor_launch<1, 64, MODE, T>(x, ldx, width, p, sms, st);
-        if (getenv("TN128")) return g4_tensor_launch<2, 128, MODE, T>(x, ldx, width, p, sms, st);
         return g4_tensor_launch<2, 256, MODE, T>(x, ldx, width, p, sms, st);
     }
 }
