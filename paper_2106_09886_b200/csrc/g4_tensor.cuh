@@ -242,7 +242,7 @@ struct G4Shape {
     static constexpr int STAGE = PARTS * X_PART + A_STAGE;
     static constexpr int C_STAGE = G4_TILE_WORDS * 4 + 512;     // codes and up to four rows of scales
     // deep where reading the codes is the bound; two where that makes room for a third stage
-    static constexpr int C_STAGES = TN <= 64 && PARTS == 1 ? (MODE == G4_DATA ? 4 : 8) : (MODE == G4_DATA && TN > 128 ? 2 : 3);
+    static constexpr int C_STAGES = TN <= 64 && PARTS == 1 && MODE == G4_FWD ? 8 : (MODE == G4_DATA && TN > 128 ? 2 : 4);
     // Two accumulators, so that results are stored under the next sum, where tensor memory has room for them.
     static constexpr int ACC_BUFS = (MODE == G4_DATA ? 2 * TN <= 512 : 2 * TN <= 256) ? 2 : 1;
     static constexpr int ACC_COLS = ACC_BUFS * TN;
@@ -254,15 +254,17 @@ struct G4Shape {
     static constexpr int STAGES = FIT_SMEM < FIT_TMEM ? FIT_SMEM : FIT_TMEM;
     // Groups of unpacking warps, each with a stage of its own.  One tile takes a warp some 1100 cycles: two groups keep up
     // with the 1024 (or 512) cycles that wide tiles multiply for, narrow ones are bound by unpacking and take what fits.
-    static constexpr int GROUPS = PARTS > 1 || TN > 64 ? 2 : (STAGES < 4 ? STAGES : 4);
+    static constexpr int GROUPS = PARTS > 1 || TN > 64 || STAGES < 4 ? 2 : 4;
     static constexpr int THREADS = 256 + 128 * GROUPS;
     static constexpr bool ONE_THREAD = TN <= 64;
     static constexpr int C_OFF = STAGES * STAGE;
     static constexpr int OUT_OFF = C_OFF + C_STAGES * C_STAGE;
     static constexpr int BAR_OFF = OUT_OFF + 4 * OUT_WARP;
     static constexpr int TOTAL = BAR_OFF + (2 * (STAGES + C_STAGES) + 5) * 8 + 16 + 1024;
-    static_assert(CG == 1 || TN >= 128, "narrower tiles of a pair ended in a launch failure whose cause was not found");
-    static_assert(GROUPS <= STAGES && GROUPS <= C_STAGES, "a group skips at most one round of a ring");
+    // A group waits for a phase by its parity, so it must know that the phase before has completed.  Copies of codes may land
+    // out of order: a stage of codes has to come back to the group that waited for it last.  (Unpacked stages are freed in
+    // order, and a group that is G stages on has seen one S + G back freed, which covers the phase before for G <= S.)
+    static_assert(C_STAGES % GROUPS == 0 && GROUPS <= STAGES, "groups and rings");
     static_assert(STAGES >= 2 && TOTAL <= 227 * 1024, "shared memory");
 };
 
