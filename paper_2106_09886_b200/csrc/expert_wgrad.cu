@@ -6,6 +6,11 @@
 // expert's: one warp clears those rows in shared memory before the instructions see them (a zero in one operand alone
 // would not do, as the other may hold NaN or infinity).
 // fp32: both operands are three bf16 parts; the six products of parts down to 2^-16 of the largest are summed.
+//
+// The tensor cores cut a sum towards zero at every addition, so a sum stays in tensor memory for 16 instructions (256 rows;
+// fp32: one block of rows and its six products, smallest first) and the result warps add those to nearest in registers.
+// Bound: writing gw (4 bytes an element) up to some 600 rows an expert, the matrix instructions beyond.  With few tiles
+// the rows are split over the blocks too; the parts are added in a fixed order by a second kernel.
 #include "g4_stage.cuh"
 #include "g4_tensor.cuh"
 
@@ -15,13 +20,15 @@ struct WgradParams {
     const int32_t *offsets;
     int experts, rows, n, k;
     float *gw;
+    int64_t part_stride;                  // elements between the results of two parts of the rows
     int itiles, jtiles;                   // tiles of 128 * CG columns of x, of TN features
+    int parts;                            // parts of an expert's rows
     unsigned int *err;
     unsigned int wait_limit;
 };
 
-constexpr int W_THREADS = 256;            // warps: 0 TMA, 1 matrix instructions, 2 tail rows (and owner of the tensor memory),
-                                          // 3 idle, 4-7 results
+constexpr int W_THREADS = 384;            // warps: 0 TMA, 1 matrix instructions, 2 tail rows (and owner of the tensor memory),
+                                          // 3 idle, 4-11 results: a warp has a quarter of the lanes and half of the columns
 
 template <int CG, int TN>
 struct WShape {
@@ -30,22 +37,44 @@ struct WShape {
     static constexpr int B_COLS = TN / CG;                      // features this block stages
     static constexpr int A_BYTES = 2 * BLOCK;
     static constexpr int STAGE = A_BYTES + B_COLS / 64 * BLOCK;
-    static constexpr int STAGES = 200 * 1024 / STAGE > 8 ? 8 : 200 * 1024 / STAGE;
+    static constexpr int STAGES = 216 * 1024 / STAGE > 8 ? 8 : 216 * 1024 / STAGE;
     static constexpr int BAR_OFF = STAGES * STAGE;
-    static constexpr int TOTAL = BAR_OFF + (3 * STAGES + 4) * 8 + 16 + 1024;
-    static constexpr int ACC_BUFS = 512 / TN >= 2 ? 2 : 1;
-    static_assert(B_COLS % 64 == 0, "features in blocks of 64");
+    static constexpr int TOTAL = BAR_OFF + (3 * STAGES + 5) * 8 + 16 + 1024;
+    static_assert(B_COLS % 64 == 0 && 2 * TN <= 512 && TOTAL <= 227 * 1024, "tile");
 };
 
-// Products of parts, largest first: (x part, dy part).
-__device__ __forceinline__ int pair_x(int q) { return (0x010120 >> (4 * (5 - q))) & 15; }
-__device__ __forceinline__ int pair_dy(int q) { return (0x001102 >> (4 * (5 - q))) & 15; }
+// One tile of one expert: rows [first, last) of its part, first column of x, first feature.
+struct WTile {
+    int expert, part, first, last, i0, j0;
+};
+template <int CG, int TN>
+__device__ __forceinline__ WTile wgrad_tile(const WgradParams &p, int t) {
+    WTile w;
+    w.i0 = (t % p.itiles) * (128 * CG); t /= p.itiles;
+    w.j0 = (t % p.jtiles) * TN; t /= p.jtiles;
+    w.part = t % p.parts;
+    w.expert = t / p.parts;
+    expert_rows(p.offsets, w.expert, p.rows, w.first, w.last);
+    if (p.parts > 1) {                    // whole blocks of rows, as evenly as they go
+        const int blocks = max(0, w.last - w.first + 63) / 64;
+        const int64_t lo = (int64_t)blocks * w.part / p.parts, hi = (int64_t)blocks * (w.part + 1) / p.parts;
+        const int base = w.first;
+        w.last = min(w.last, base + (int)hi * 64);
+        w.first = base + (int)lo * 64;
+    }
+    return w;
+}
+
+// Products of parts, smallest first: (x part, dy part).
+__device__ __forceinline__ int pair_x(int q) { return (0x201010 >> (4 * (5 - q))) & 15; }
+__device__ __forceinline__ int pair_dy(int q) { return (0x021100 >> (4 * (5 - q))) & 15; }
 
 template <int CG, int TN, class T>
 __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid_constant__ CUtensorMap map_x,
                                                                    const __grid_constant__ CUtensorMap map_dy, const WgradParams p) {
     using L = WShape<CG, TN>;
     constexpr int PAIRS = G4Type<T>::PARTS == 1 ? 1 : 6;
+    constexpr int CHUNK = PAIRS == 1 ? 4 : PAIRS;                // stages that are added up in tensor memory
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint64_t *landed = reinterpret_cast<uint64_t *>(smem + L::BAR_OFF);     // each block: its copies of a stage
@@ -53,22 +82,24 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
     uint64_t *empty = ready + L::STAGES;                                    // each block
     uint64_t *acc_full = empty + L::STAGES;                                 // each block
     uint64_t *acc_empty = acc_full + 2;                                     // leader
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(acc_empty + 2);
+    uint64_t *finish = acc_empty + 2;                                       // every instruction has completed
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(finish + 1);
     volatile uint32_t *abort_flag = tmem_slot + 1;
 
     const int warp = warp_index(), lane = threadIdx.x & 31;
     const int rank = (int)pair_rank<CG>();
     const int first_work = blockIdx.x / CG, work_stride = gridDim.x / CG;
-    const int per_expert = p.itiles * p.jtiles, work = p.experts * per_expert;
+    const int work = p.experts * p.parts * p.itiles * p.jtiles;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < L::STAGES; ++s) { mbar_init(&landed[s], 1); mbar_init(&ready[s], CG); mbar_init(&empty[s], 1); }
-        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 4 * CG); }
+        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 8 * CG); }
+        mbar_init(finish, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    if (warp == 2) pair_tmem_alloc<CG>(tmem_slot, L::ACC_BUFS * TN);
+    if (warp == 2) pair_tmem_alloc<CG>(tmem_slot, 2 * TN);
     tc_fence_before();
     __syncthreads();
     pair_sync<CG>();
@@ -78,16 +109,13 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
         return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, id, p.err, p.wait_limit));
     };
     auto stop = [&]() { return __any_sync(0xffffffffu, *abort_flag != 0); };
-    int committed = 0;
 
     if (warp == 0) {
         Ring g;
         long long it = 0;
         for (int t = first_work; t < work && !stop(); t += work_stride) {
-            const int e = t / per_expert, in = t - e * per_expert;
-            int first, last;
-            expert_rows(p.offsets, e, p.rows, first, last);
-            const int i0 = ((in % p.itiles) * CG + rank) * 128, j0 = (in / p.itiles) * TN + rank * L::B_COLS;
+            const WTile w = wgrad_tile<CG, TN>(p, t);
+            const int first = w.first, last = w.last, i0 = w.i0 + rank * 128, j0 = w.j0 + rank * L::B_COLS;
             bool ok = true;
             for (int r = first; ok && r < last; r += L::ROWS)
                 for (int q = 0; q < PAIRS; ++q) {
@@ -112,9 +140,8 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
     } else if (warp == 2) {               // stages whose rows all belong to the expert pass through
         Ring g;
         for (int t = first_work; t < work && !stop(); t += work_stride) {
-            const int e = t / per_expert;
-            int first, last;
-            expert_rows(p.offsets, e, p.rows, first, last);
+            const WTile w = wgrad_tile<CG, TN>(p, t);
+            const int first = w.first, last = w.last;
             bool ok = true;
             for (int r = first; ok && r < last; r += L::ROWS)
                 for (int q = 0; q < PAIRS; ++q) {
@@ -135,84 +162,88 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
         }
     } else if (warp == 1) {
         if (rank == 0) {
-            Ring g;
+            Ring acc;
             constexpr uint32_t idesc = idesc_f16(G4Type<T>::FMT, 128 * CG, TN, true, true);
-            int local = 0;
-            for (int t = first_work; t < work && !stop(); t += work_stride) {
-                int first, last;
-                expert_rows(p.offsets, t / per_expert, p.rows, first, last);
-                if (first >= last) continue;                     // nothing to add up: the result warps write zeros
-                const int buf = local % L::ACC_BUFS;
-                if (!warp_wait(&acc_empty[buf], ((uint32_t)(local / L::ACC_BUFS) & 1u) ^ 1u, 3)) break;
-                tc_fence_after();
-                const uint32_t d = tmem_base + (uint32_t)(buf * TN);
-                bool ok = true;
-                for (int r = first; ok && r < last; r += L::ROWS)
-                    for (int q = 0; q < PAIRS; ++q) {
-                        if (!(ok = warp_wait(&ready[g.s], g.ph, 1))) break;
-                        tc_fence_after();
-                        const uint32_t at = smem_u32(smem + g.s * L::STAGE);
-                        const uint64_t a = smem_desc_mn_sw128(at, L::BLOCK), b = smem_desc_mn_sw128(at + L::A_BYTES, L::BLOCK);
-                        if (elect_one()) {
+            const uint64_t a_desc = smem_desc_mn_sw128(smem_u32(smem), L::BLOCK);
+            const uint64_t b_desc = smem_desc_mn_sw128(smem_u32(smem) + L::A_BYTES, L::BLOCK);
+            int t = first_work, left = 0, chunk = 0;             // stages left of the tile, stages in this sum
+            auto next_tile = [&]() {                             // tiles without rows have no stages
+                for (; left == 0 && t < work; t += work_stride) {
+                    const WTile w = wgrad_tile<CG, TN>(p, t);
+                    left = (max(0, w.last - w.first) + L::ROWS - 1) / L::ROWS * PAIRS;
+                }
+                return left > 0;
+            };
+            bool ok = !stop() && next_tile();
+            for (uint32_t ph = 0; ok; ph ^= 1u) {
 #pragma unroll
-                            for (int j = 0; j < L::ROWS / 16; ++j)
-                                mma_f16_ss<CG>(d, a + 128 * j, b + 128 * j, idesc, ((r - first) | q | j) != 0 ? 1u : 0u);
-                            pair_commit<CG>(&empty[g.s]);
-                        }
-                        __syncwarp();
-                        g.next(L::STAGES);
+                for (int g = 0; g < L::STAGES; ++g) {
+                    if (chunk == 0 && !(ok = warp_wait(&acc_empty[acc.s], acc.ph ^ 1u, 3))) break;
+                    if (!(ok = warp_wait(&ready[g], ph, 1))) break;
+                    tc_fence_after();
+                    const uint32_t d = tmem_base + (uint32_t)(acc.s * TN);
+                    const bool done = chunk == CHUNK - 1 || left == 1;
+                    if (elect_one()) {
+#pragma unroll
+                        for (int j = 0; j < L::ROWS / 16; ++j)
+                            mma_f16_ss<CG>(d, a_desc + ((g * L::STAGE) >> 4) + 128 * j, b_desc + ((g * L::STAGE) >> 4) + 128 * j, idesc,
+                                           j != 0 || chunk != 0 ? 1u : 0u);
+                        pair_commit<CG>(&empty[g]);
+                        if (done) pair_commit<CG>(&acc_full[acc.s]);
                     }
-                if (elect_one()) pair_commit<CG>(&acc_full[buf]);            // also after a wait that gave up: see the end
-                __syncwarp();
-                committed = ++local;
+                    __syncwarp();
+                    chunk = done ? 0 : chunk + 1;
+                    if (done) acc.next(2);
+                    if (--left == 0 && !(ok = next_tile())) break;
+                }
             }
+            // no instruction may still write tensor memory when it is given back: one more commit, waited for
+            if (elect_one()) pair_commit<CG>(finish);
+            __syncwarp();
+            for (uint32_t w = 0; w < p.wait_limit && !mbar_try_wait(finish, 0u); ++w) {}
         }
     } else if (warp >= 4) {
-        const int w = warp & 3;
-        int local = 0;
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        constexpr int COLS = TN / 2;                             // of this warp
+        const uint32_t from = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * COLS);
+        Ring acc;
         for (int t = first_work; t < work && !stop(); t += work_stride) {
-            const int e = t / per_expert, in = t - e * per_expert;
-            int first, last;
-            expert_rows(p.offsets, e, p.rows, first, last);
-            const int i = ((in % p.itiles) * CG + rank) * 128 + w * 32 + lane, j0 = (in / p.itiles) * TN;
-            float *dst = p.gw + ((int64_t)e * p.n + j0) * p.k + i;
-            const int have = min(TN, p.n - j0);
-            if (first >= last) {
-                if (i < p.k)
-                    for (int j = 0; j < have; ++j) dst[(int64_t)j * p.k] = 0.0f;
-                continue;
-            }
-            const int buf = local % L::ACC_BUFS;
-            if (!warp_wait(&acc_full[buf], (uint32_t)(local / L::ACC_BUFS) & 1u, 2)) break;
-            tc_fence_after();
-#pragma unroll 1
-            for (int c0 = 0; c0 < have; c0 += 32) {
-                uint32_t v[32];
-                tmem_load_32(tmem_base + ((uint32_t)(w * 32) << 16) + (uint32_t)(buf * TN + c0), v);
-                if (i < p.k) {
+            const WTile w = wgrad_tile<CG, TN>(p, t);
+            const int i = w.i0 + rank * 128 + quarter * 32 + lane, j0 = w.j0 + half * COLS;
+            float *dst = p.gw + w.part * p.part_stride + ((int64_t)w.expert * p.n + j0) * p.k + i;
+            const int have = i < p.k ? min(COLS, p.n - j0) : 0;
+            const int stages = (max(0, w.last - w.first) + L::ROWS - 1) / L::ROWS * PAIRS;
+            float sum[COLS];
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (c0 + j < have) __stcs(dst + (int64_t)(c0 + j) * p.k, __uint_as_float(v[j]));
+            for (int c = 0; c < COLS; ++c) sum[c] = 0.0f;
+            bool ok = true;
+            for (int s = 0; s < stages; s += CHUNK) {
+                if (!(ok = warp_wait(&acc_full[acc.s], acc.ph, 2))) break;
+                tc_fence_after();
+#pragma unroll
+                for (int c0 = 0; c0 < COLS; c0 += 16) {
+                    uint32_t v[16];
+                    tmem_load_lane_16(from + (uint32_t)(acc.s * TN + c0), v);
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) sum[c0 + c] = __fadd_rn(sum[c0 + c], __uint_as_float(v[c]));
                 }
+                tc_fence_before();
                 __syncwarp();
+                if (lane == 0) arrive_leader<CG>(&acc_empty[acc.s]);
+                acc.next(2);
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) arrive_leader<CG>(&acc_empty[buf]);
-            ++local;
+            if (!ok) break;
+#pragma unroll
+            for (int c = 0; c < COLS; ++c)
+                if (c < have) __stcs(dst + (int64_t)c * p.k, sum[c]);
         }
-    }
-    __syncwarp();
-    if (warp == 1 && rank == 0 && lane == 0 && committed > 0) {
-        const int final_acc = committed - 1;
-        for (uint32_t w = 0; w < p.wait_limit && !mbar_try_wait(&acc_full[final_acc % L::ACC_BUFS], (uint32_t)(final_acc / L::ACC_BUFS) & 1u); ++w) {}
     }
     tc_fence_before();
     __syncthreads();
     pair_sync<CG>();
     if (warp == 2) {
         tc_fence_after();
-        pair_tmem_dealloc<CG>(tmem_base, L::ACC_BUFS * TN);
+        pair_tmem_dealloc<CG>(tmem_base, 2 * TN);
     }
 }
 
@@ -227,7 +258,7 @@ int wgrad_launch(const void *x, int64_t ldx, const void *dy, int64_t lddy, Wgrad
     if (!make_map_16(&map_x, fp16, x, rows, p.k, ldx, L::ROWS) || !make_map_16(&map_dy, fp16, dy, rows, p.n, lddy, L::ROWS)) return QNN_E_CUDA;
     p.itiles = (p.k + 128 * CG - 1) / (128 * CG);
     p.jtiles = (p.n + TN - 1) / TN;
-    const int64_t work = (int64_t)p.experts * p.itiles * p.jtiles;
+    const int64_t work = (int64_t)p.experts * p.parts * p.itiles * p.jtiles;
     if (work > 0x3FFFFFFFll) return QNN_E_RANGE;
     const int most = sms / CG;
     cudaLaunchConfig_t cfg = {};
@@ -248,22 +279,63 @@ int wgrad_launch(const void *x, int64_t ldx, const void *dy, int64_t lddy, Wgrad
     return QNN_OK;
 }
 
+// gw = sum of the parts, in order.
+__global__ void __launch_bounds__(256) wgrad_sum_kernel(const float *__restrict__ part, int parts, int64_t total, float *__restrict__ gw) {
+    for (int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x; v < total; v += (int64_t)gridDim.x * 256) {
+        float s = part[v];
+        for (int q = 1; q < parts; ++q) s = __fadd_rn(s, part[q * total + v]);
+        gw[v] = s;
+    }
+}
+
+// The tile: pairs of blocks on 256 x 256 unless that leaves most of the GPU idle (sized for 148 SMs, so that workspace
+// queries and calls agree).  Parts of the rows: as many as fill the GPU once, each of at least 256 rows on average.
+struct WPlan {
+    bool wide;
+    int parts;
+};
+WPlan wgrad_plan(int64_t rows, int experts, int n, int k) {
+    const int64_t wide = (int64_t)experts * ((k + 255) / 256) * ((n + 255) / 256);
+    const int64_t narrow = (int64_t)experts * ((k + 127) / 128) * ((n + 127) / 128);
+    WPlan w;
+    w.wide = wide >= 74;
+    const int64_t units = w.wide ? 74 : 148, tiles = w.wide ? wide : narrow, each = rows / experts;
+    int64_t parts = units / tiles;
+    if (parts > each / 256) parts = each / 256;
+    w.parts = parts < 1 ? 1 : (int)parts;
+    return w;
+}
+
 template <class T>
-int wgrad(const void *x, int64_t ldx, const void *dy, int64_t lddy, const WgradParams &p, cudaStream_t st) {
+int wgrad(const void *x, int64_t ldx, const void *dy, int64_t lddy, const WgradParams &p, bool wide, cudaStream_t st) {
     const int sms = sm_count();
     if (sms <= 0) return QNN_E_CUDA;
-    return wgrad_launch<1, 128, T>(x, ldx, dy, lddy, p, sms, st);
+    return wide ? wgrad_launch<2, 256, T>(x, ldx, dy, lddy, p, sms, st) : wgrad_launch<1, 128, T>(x, ldx, dy, lddy, p, sms, st);
 }
 
 }  // namespace
 
+size_t qnn_expert_wgrad_parts_bytes(int64_t rows, int experts, int n, int k) {
+    const WPlan plan = wgrad_plan(rows, experts, n, k);
+    return plan.parts > 1 ? ((size_t)plan.parts * experts * n * k * sizeof(float) + 255) / 256 * 256 : 0;
+}
+
 int qnn_expert_wgrad(const void *x, int64_t ldx, const void *dy, int64_t lddy, int type, const int32_t *offsets, int experts, int rows,
-                     int n, int k, float *gw, cudaStream_t st) {
+                     int n, int k, float *gw, float *parts, cudaStream_t st) {
+    const WPlan plan = wgrad_plan(rows, experts, n, k);
     WgradParams p = {};
-    p.offsets = offsets; p.experts = experts; p.rows = rows; p.n = n; p.k = k; p.gw = gw;
+    p.offsets = offsets; p.experts = experts; p.rows = rows; p.n = n; p.k = k;
+    p.parts = plan.parts;
+    p.gw = plan.parts > 1 ? parts : gw;
+    p.part_stride = (int64_t)experts * n * k;
     p.wait_limit = WAIT_LIMIT;
     if (!(p.err = qnn_tc_error_word())) return QNN_E_CUDA;
-    if (type == QNN_F32) return wgrad<float>(x, ldx, dy, lddy, p, st);
-    if (type == QNN_BF16) return wgrad<__nv_bfloat16>(x, ldx, dy, lddy, p, st);
-    return wgrad<__half>(x, ldx, dy, lddy, p, st);
+    int rc;
+    if (type == QNN_F32) rc = wgrad<float>(x, ldx, dy, lddy, p, plan.wide, st);
+    else if (type == QNN_BF16) rc = wgrad<__nv_bfloat16>(x, ldx, dy, lddy, p, plan.wide, st);
+    else rc = wgrad<__half>(x, ldx, dy, lddy, p, plan.wide, st);
+    if (rc != QNN_OK || plan.parts == 1) return rc;
+    const int64_t blocks = (p.part_stride + 255) / 256;
+    wgrad_sum_kernel<<<(unsigned)(blocks < 148 * 8 ? blocks : 148 * 8), 256, 0, st>>>(parts, plan.parts, p.part_stride, gw);
+    return qnn_launch_status();
 }

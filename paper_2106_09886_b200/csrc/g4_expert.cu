@@ -92,7 +92,7 @@ extern "C" int qnn_g4_expert_backward_data(const void *dy, int type, int64_t row
 extern "C" size_t qnn_expert_backward_weights_workspace(const void *dy, const void *x, int type, int64_t rows, int64_t lddy,
                                                         int64_t ldx, int experts, int n, int k) {
     if (!g4_type_ok(type) || !g4_dims_ok(experts, n, k) || rows <= 0 || rows >= G4_MAX_ROWS) return 0;
-    return (g4_rows_in_place(dy, type, lddy) ? 0 : g4_staged_bytes(type, rows, n)) +
+    return qnn_expert_wgrad_parts_bytes(rows, experts, n, k) + (g4_rows_in_place(dy, type, lddy) ? 0 : g4_staged_bytes(type, rows, n)) +
            (g4_rows_in_place(x, type, ldx) ? 0 : g4_staged_bytes(type, rows, k));
 }
 
@@ -111,6 +111,8 @@ extern "C" int qnn_expert_backward_weights(const void *dy, const void *x, int ty
     if (rows == 0)
         return cudaMemsetAsync(gw, 0, (size_t)experts * n * k * sizeof(float), st) == cudaSuccess ? QNN_OK : QNN_E_CUDA;
     uint8_t *ws = static_cast<uint8_t *>(workspace);
+    float *parts = reinterpret_cast<float *>(ws);
+    ws += qnn_expert_wgrad_parts_bytes(rows, experts, n, k);
     if (!g4_rows_in_place(dy, type, lddy)) {
         if ((rc = qnn_stage_rows(dy, type, lddy, (int)rows, n, ws, st)) != QNN_OK) return rc;
         dy = ws;
@@ -122,5 +124,5 @@ extern "C" int qnn_expert_backward_weights(const void *dy, const void *x, int ty
         x = ws;
         ldx = g4_padded_width(k);
     }
-    return qnn_expert_wgrad(x, ldx, dy, lddy, type, offsets, experts, (int)rows, n, k, gw, st);
+    return qnn_expert_wgrad(x, ldx, dy, lddy, type, offsets, experts, (int)rows, n, k, gw, parts, st);
 }

@@ -13,4 +13,5 @@ struct G4TensorArgs {
 int qnn_g4_tensor_fwd(const void *x, int type, int64_t ldx, const G4TensorArgs &a, cudaStream_t st);
 int qnn_g4_tensor_data(const void *dy, int type, int64_t lddy, const G4TensorArgs &a, cudaStream_t st);
 int qnn_expert_wgrad(const void *x, int64_t ldx, const void *dy, int64_t lddy, int type, const int32_t *offsets, int experts, int rows,
-                     int n, int k, float *gw, cudaStream_t st);
+                     int n, int k, float *gw, float *parts, cudaStream_t st);
+size_t qnn_expert_wgrad_parts_bytes(int64_t rows, int experts, int n, int k);      // of `parts` (0: it may be NULL)

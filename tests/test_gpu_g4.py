@@ -211,6 +211,41 @@ def test_expert_backward_weights(t, qnn, dtype, n, k, counts):
 
 
 @pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("n,k,counts", [(70, 90, [2500, 0, 3]), (64, 64, [1111]), (300, 700, [900, 800])], ids=str)
+def test_long_weight_gradients(t, qnn, dtype, n, k, counts):
+    """Many rows on small matrices: sums of many blocks of rows, and rows split over the GPU."""
+    rng = np.random.default_rng(n + k)
+    rows = sum(counts)
+    dy, dy64 = real(t, rng, (rows, n), dtype)
+    x, x64 = real(t, rng, (rows, k), dtype)
+    offsets = offsets_of(t, counts)
+    gw = qnn.expert_gemm_backward_weights(dy, x, offsets)
+    want, mag = np.zeros((len(counts), n, k)), np.zeros((len(counts), n, k))
+
+    def one(e, a, b):
+        want[e], mag[e] = dy64[a:b].T @ x64[a:b], np.abs(dy64[a:b]).T @ np.abs(x64[a:b])
+    grouped(counts, 0, one)
+    check(gw, want, mag, 2 * max(counts) + 64, "fp32")
+    # in the mean the sums are far better than that bound: kept to nearest, they do not drift towards zero
+    assert np.linalg.norm(gw.cpu().double().numpy() - want) <= 1e-6 * np.linalg.norm(want)
+    assert t.equal(gw, qnn.expert_gemm_backward_weights(dy, x, offsets)) and qnn.tensor_path_status() == 0
+
+
+def test_fp32_products_do_not_drift(t, qnn):
+    """fp32 results of a long contraction stay at fp32 accuracy in the mean."""
+    rng = np.random.default_rng(21)
+    n, k, counts = 256, 4096, [200, 100]
+    codes, scales, alpha, dense = ref.random_weights(rng, 2, n, k, 128)
+    w = handle(qnn, t, codes, scales, alpha, n, k, 128)
+    x, x64 = real(t, rng, (300, k), "fp32")
+    y = qnn.g4_expert_gemm(x, w, offsets_of(t, counts)).cpu().double().numpy()
+    want = np.concatenate([x64[:200] @ dense[0].T, x64[200:] @ dense[1].T])
+    assert np.linalg.norm(y - want) <= 1e-6 * np.linalg.norm(want)
+    few = qnn.g4_matvec(x[:3], qnn.G4Weights(w.codes[:1], w.scales[:1], w.alpha[:1], n, k, 128)).cpu().double().numpy()
+    assert np.linalg.norm(few - want[:3]) <= 1e-6 * np.linalg.norm(want[:3])
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES)
 def test_rows_of_no_expert_are_left_alone(t, qnn, dtype):
     """Rows in front of the first and behind the last expert hold NaN and take no part; their results are not written."""
     rng = np.random.default_rng(11)
