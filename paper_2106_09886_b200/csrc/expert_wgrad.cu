@@ -47,22 +47,23 @@ struct WShape {
 struct WTile {
     int expert, part, first, last, i0, j0;
 };
-template <int CG, int TN>
-__device__ __forceinline__ WTile wgrad_tile(const WgradParams &p, int t) {
+__device__ __noinline__ WTile wgrad_tile_of(const int32_t *offsets, int rows, int itiles, int jtiles, int parts, int i_step, int j_step, int t) {
     WTile w;
-    w.i0 = (t % p.itiles) * (128 * CG); t /= p.itiles;
-    w.j0 = (t % p.jtiles) * TN; t /= p.jtiles;
-    w.part = t % p.parts;
-    w.expert = t / p.parts;
-    expert_rows(p.offsets, w.expert, p.rows, w.first, w.last);
-    if (p.parts > 1) {                    // whole blocks of rows, as evenly as they go
+    w.i0 = t % itiles * i_step; t /= itiles;
+    w.j0 = t % jtiles * j_step; t /= jtiles;
+    w.part = t % parts;
+    w.expert = t / parts;
+    expert_rows(offsets, w.expert, rows, w.first, w.last);
+    if (parts > 1) {                      // whole blocks of rows, as evenly as they go (at most 148 parts: no overflow)
         const int blocks = max(0, w.last - w.first + 63) / 64;
-        const int64_t lo = (int64_t)blocks * w.part / p.parts, hi = (int64_t)blocks * (w.part + 1) / p.parts;
-        const int base = w.first;
-        w.last = min(w.last, base + (int)hi * 64);
-        w.first = base + (int)lo * 64;
+        const int lo = blocks * w.part / parts, hi = blocks * (w.part + 1) / parts, base = w.first;
+        w.last = min(w.last, base + hi * 64);
+        w.first = base + lo * 64;
     }
     return w;
+}
+template <int CG, int TN> __device__ __forceinline__ WTile wgrad_tile(const WgradParams &p, int t) {
+    return wgrad_tile_of(p.offsets, p.rows, p.itiles, p.jtiles, p.parts, 128 * CG, TN, t);
 }
 
 // Products of parts, smallest first: (x part, dy part).
@@ -92,6 +93,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
     const int work = p.experts * p.parts * p.itiles * p.jtiles;
 
     if (threadIdx.x == 0) {
+#pragma unroll 1
         for (int s = 0; s < L::STAGES; ++s) { mbar_init(&landed[s], 1); mbar_init(&ready[s], CG); mbar_init(&empty[s], 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 8 * CG); }
         mbar_init(finish, 1);
@@ -106,18 +108,21 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
     auto warp_wait = [&](uint64_t *bar, uint32_t parity, unsigned id) {
-        return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, id, p.err, p.wait_limit));
+        return __all_sync(0xffffffffu, short_wait(bar, parity, abort_flag, id, p.err, p.wait_limit));
     };
     auto stop = [&]() { return __any_sync(0xffffffffu, *abort_flag != 0); };
 
     if (warp == 0) {
         Ring g;
         long long it = 0;
+#pragma unroll 1
         for (int t = first_work; t < work && !stop(); t += work_stride) {
             const WTile w = wgrad_tile<CG, TN>(p, t);
             const int first = w.first, last = w.last, i0 = w.i0 + rank * 128, j0 = w.j0 + rank * L::B_COLS;
             bool ok = true;
+#pragma unroll 1
             for (int r = first; ok && r < last; r += L::ROWS)
+#pragma unroll 1
                 for (int q = 0; q < PAIRS; ++q) {
                     if (!(ok = warp_wait(&empty[g.s], g.ph ^ 1u, 0))) break;
                     if (elect_one()) {
@@ -139,17 +144,22 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
         if (*abort_flag && lane == 0) drain_copies_in_flight(landed, it, L::STAGES, p.wait_limit);
     } else if (warp == 2) {               // stages whose rows all belong to the expert pass through
         Ring g;
+#pragma unroll 1
         for (int t = first_work; t < work && !stop(); t += work_stride) {
             const WTile w = wgrad_tile<CG, TN>(p, t);
             const int first = w.first, last = w.last;
             bool ok = true;
+#pragma unroll 1
             for (int r = first; ok && r < last; r += L::ROWS)
+#pragma unroll 1
                 for (int q = 0; q < PAIRS; ++q) {
                     if (!(ok = warp_wait(&landed[g.s], g.ph, 1))) break;
                     const int valid = last - r;
                     if (valid < L::ROWS) {
                         const uint32_t stage = smem_u32(smem) + g.s * L::STAGE;
+#pragma unroll 1
                         for (int b = 0; b < L::STAGE / L::BLOCK; ++b)
+#pragma unroll 1
                             for (int v = valid * 8 + lane; v < L::ROWS * 8; v += 32)
                                 sts_128(stage + b * L::BLOCK + v * 16, 0u, 0u, 0u, 0u);
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -168,6 +178,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
             const uint64_t b_desc = smem_desc_mn_sw128(smem_u32(smem) + L::A_BYTES, L::BLOCK);
             int t = first_work, left = 0, chunk = 0;             // stages left of the tile, stages in this sum
             auto next_tile = [&]() {                             // tiles without rows have no stages
+#pragma unroll 1
                 for (; left == 0 && t < work; t += work_stride) {
                     const WTile w = wgrad_tile<CG, TN>(p, t);
                     left = (max(0, w.last - w.first) + L::ROWS - 1) / L::ROWS * PAIRS;
@@ -175,6 +186,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
                 return left > 0;
             };
             bool ok = !stop() && next_tile();
+#pragma unroll 1
             for (uint32_t ph = 0; ok; ph ^= 1u) {
 #pragma unroll
                 for (int g = 0; g < L::STAGES; ++g) {
@@ -200,6 +212,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
             // no instruction may still write tensor memory when it is given back: one more commit, waited for
             if (elect_one()) pair_commit<CG>(finish);
             __syncwarp();
+#pragma unroll 1
             for (uint32_t w = 0; w < p.wait_limit && !mbar_try_wait(finish, 0u); ++w) {}
         }
     } else if (warp >= 4) {
@@ -207,6 +220,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
         constexpr int COLS = TN / 2;                             // of this warp
         const uint32_t from = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * COLS);
         Ring acc;
+#pragma unroll 1
         for (int t = first_work; t < work && !stop(); t += work_stride) {
             const WTile w = wgrad_tile<CG, TN>(p, t);
             const int i = w.i0 + rank * 128 + quarter * 32 + lane, j0 = w.j0 + half * COLS;
@@ -217,6 +231,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
 #pragma unroll
             for (int c = 0; c < COLS; ++c) sum[c] = 0.0f;
             bool ok = true;
+#pragma unroll 1
             for (int s = 0; s < stages; s += CHUNK) {
                 if (!(ok = warp_wait(&acc_full[acc.s], acc.ph, 2))) break;
                 tc_fence_after();
@@ -234,8 +249,8 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
             }
             if (!ok) break;
 #pragma unroll
-            for (int c = 0; c < COLS; ++c)
-                if (c < have) __stcs(dst + (int64_t)c * p.k, sum[c]);
+            for (int c = 0; c < COLS; ++c, dst += p.k)
+                if (c < have) __stcs(dst, sum[c]);
         }
     }
     tc_fence_before();

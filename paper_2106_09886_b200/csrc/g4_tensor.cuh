@@ -59,6 +59,23 @@ template <int CG> __device__ __forceinline__ void arrive_leader(uint64_t *bar) {
 __device__ __forceinline__ void arrive_local(uint64_t *bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
+// mbar_wait with its polling loop in one place: these kernels hold many roles, and code that does not fit the instruction
+// cache costs them more than any instruction does.
+__device__ __noinline__ bool mbar_poll(uint64_t *bar, uint32_t parity, volatile uint32_t *abort_flag, unsigned id, unsigned int *err,
+                                       uint32_t limit) {
+#pragma unroll 1
+    for (uint32_t it = 0; it < limit; ++it) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((it & 1023u) == 1023u && *abort_flag) return false;
+    }
+    *abort_flag = 1;
+    atomicCAS(err, 0u, 1u + id);
+    return false;
+}
+__device__ __forceinline__ bool short_wait(uint64_t *bar, uint32_t parity, volatile uint32_t *abort_flag, unsigned id,
+                                           unsigned int *err, uint32_t limit) {
+    return mbar_try_wait(bar, parity) || mbar_poll(bar, parity, abort_flag, id, err, limit);
+}
 // 2-D box into this block's shared memory, its bytes counted on the leading block's barrier.
 template <int CG>
 __device__ __forceinline__ void pair_load_2d(void *dst, const CUtensorMap *map, uint64_t *bar, int x, int y) {
@@ -201,12 +218,8 @@ struct SlotCursor {
             if (lane >= d) incl += o;
         }
     }
-    __device__ __forceinline__ int64_t count() {         // blocks in all; the cursor is spent
-        int64_t total = 0;
-        for (; base < experts; base += 32, load()) total += __shfl_sync(0xffffffffu, incl, 31);
-        return total;
-    }
     __device__ __forceinline__ ExpertSlot seek(int slot) {
+#pragma unroll 1
         while (base < experts) {
             const unsigned hit = __ballot_sync(0xffffffffu, slot < before + incl);
             if (hit) {
@@ -221,6 +234,19 @@ struct SlotCursor {
         return {-1, 0, 0};
     }
 };
+
+// Blocks of `tile` rows in all; by a whole warp.
+__device__ __noinline__ int64_t count_slots(const int32_t *offsets, int experts, int rows, int tile) {
+    int64_t total = 0;
+    for (int e = threadIdx.x & 31; e < experts; e += 32) {
+        int a, b;
+        expert_rows(offsets, e, rows, a, b);
+        total += b > a ? (b - a + tile - 1) / tile : 0;
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+    return total;
+}
 
 struct G4TensorParams {
     G4Weights w;
@@ -416,7 +442,9 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
     const int first_work = blockIdx.x / CG, work_stride = gridDim.x / CG;
 
     if (threadIdx.x == 0) {
+#pragma unroll 1
         for (int s = 0; s < L::STAGES; ++s) { mbar_init(&full[s], G4_UNPACK_WARPS * CG + 1); mbar_init(&empty[s], 1); }
+#pragma unroll 1
         for (int s = 0; s < L::C_STAGES; ++s) { mbar_init(&c_full[s], 1); mbar_init(&c_empty[s], G4_UNPACK_WARPS); }
         for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 4 * CG); }
         mbar_init(finish, 1);
@@ -432,10 +460,10 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
     const uint32_t tmem_base = *tmem_slot;
     // waits of a whole warp: every lane polls (each needs the barrier's acquire), all go on or all give up
     auto warp_wait = [&](uint64_t *bar, uint32_t parity, unsigned id) {
-        return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, id, p.err, p.wait_limit));
+        return __all_sync(0xffffffffu, short_wait(bar, parity, abort_flag, id, p.err, p.wait_limit));
     };
     auto stages_of_this_block = [&]() -> int64_t {
-        const int64_t tiles = SlotCursor(p.offsets, p.experts, p.rows, TN).count() * p.ftiles;
+        const int64_t tiles = count_slots(p.offsets, p.experts, p.rows, TN) * p.ftiles;
         return tiles > first_work ? (tiles - first_work + work_stride - 1) / work_stride * p.steps : 0;
     };
     auto stop = [&]() { return __any_sync(0xffffffffu, *abort_flag != 0); };       // the same answer for a whole warp
@@ -449,13 +477,14 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
         bool ok = true;
         uint32_t ph = 0;
         int kt = 0;
+#pragma unroll 1
         for (; ok && left > 0; ph ^= 1u) {
 #pragma unroll
             for (int g = 0; g < L::STAGES; ++g) {
                 if (left-- <= 0) break;
                 const bool fresh = PROMOTE || kt == 0, done = PROMOTE || kt == p.steps - 1;
-                if (fresh && !(ok = agree(mbar_wait(&acc_empty[acc.s], acc.ph ^ 1u, abort_flag, 3, p.err, p.wait_limit)))) break;
-                if (!(ok = agree(mbar_wait(&full[g], ph, abort_flag, 1, p.err, p.wait_limit)))) break;
+                if (fresh && !(ok = agree(short_wait(&acc_empty[acc.s], acc.ph ^ 1u, abort_flag, 3, p.err, p.wait_limit)))) break;
+                if (!(ok = agree(short_wait(&full[g], ph, abort_flag, 1, p.err, p.wait_limit)))) break;
                 tc_fence_after();
                 const uint32_t d = tmem_base + (uint32_t)(acc.s * TN);
                 alone([&]() {
@@ -482,11 +511,13 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
         SlotCursor cur(p.offsets, p.experts, p.rows, TN);
         Ring g;
         long long it = 0;
+#pragma unroll 1
         for (int t = first_work; !stop(); t += work_stride) {
             const ExpertSlot slot = cur.seek(t / p.ftiles);
             if (slot.expert < 0) break;
             const int row = slot.first + rank * L::XROWS;
             bool ok = true;
+#pragma unroll 1
             for (int kt = 0; kt < p.steps; ++kt) {
                 if (!(ok = warp_wait(&empty[g.s], g.ph ^ 1u, 0))) break;
                 if (elect_one()) {
@@ -506,6 +537,7 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
         }
         // after an abort the copies in flight may still land (their barriers may never complete, with unpacking stopped)
         if (*abort_flag && it > 0)
+#pragma unroll 1
             for (int i = 0; i < 1000; ++i) __nanosleep(1000);
     } else if (warp == 2) {               // ------------------------------------------------ codes and scales
         SlotCursor cur(p.offsets, p.experts, p.rows, TN);
@@ -513,6 +545,7 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
         long long it = 0;
         const int groups = G4_TILE / p.w.group;
         const int64_t stride = MODE == G4_FWD ? 1 : p.w.tiles_k;            // stored tiles between steps of the contraction
+#pragma unroll 1
         for (int t = first_work; !stop(); t += work_stride) {
             const ExpertSlot slot = cur.seek(t / p.ftiles);
             if (slot.expert < 0) break;
@@ -520,6 +553,7 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
             const int f = min((t % p.ftiles) * CG + rank, (MODE == G4_FWD ? p.w.tiles_n : p.w.tiles_k) - 1);
             int64_t tile = (int64_t)slot.expert * p.w.tiles_n * p.w.tiles_k + (MODE == G4_FWD ? (int64_t)f * p.w.tiles_k : f);
             bool ok = true;
+#pragma unroll 1
             for (int kt = 0; kt < p.steps; ++kt, tile += stride) {
                 if (!(ok = warp_wait(&c_empty[c.s], c.ph ^ 1u, 0))) break;
                 if (elect_one()) {
@@ -550,6 +584,7 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
             // no instruction may still write tensor memory when it is given back: one more commit, waited for
             if (elect_one()) pair_commit<CG>(finish);
             __syncwarp();
+#pragma unroll 1
             for (uint32_t w = 0; w < p.wait_limit && !mbar_try_wait(finish, 0u); ++w) {}
         }
     } else if (warp >= 8) {               // ------------------------------------------------ unpacking
@@ -560,6 +595,7 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
         const int log_group = p.w.group == 32 ? 5 : p.w.group == 64 ? 6 : 7;
         Ring c, g;
         c.s = g.s = group;
+#pragma unroll 1
         for (int64_t left = stages_of_this_block() - group; left > 0; left -= L::GROUPS, c.skip(L::GROUPS, L::C_STAGES), g.skip(L::GROUPS, L::STAGES)) {
             if (!warp_wait(&c_full[c.s], c.ph, 1)) break;
             const uint32_t src = smem_at + L::C_OFF + c.s * L::C_STAGE;
@@ -613,6 +649,7 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
         const int q = warp & 3;
         const float undo = GroupScale<Op>::UNDO;
         Ring acc;
+#pragma unroll 1
         for (int t = first_work; !stop(); t += work_stride) {
             const ExpertSlot slot = cur.seek(t / p.ftiles);
             if (slot.expert < 0) break;
@@ -626,6 +663,7 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
                 float sum[TN];
 #pragma unroll
                 for (int i = 0; i < TN; ++i) sum[i] = 0.0f;
+#pragma unroll 1
                 for (int kt = 0; kt < p.steps; ++kt) {
                     if (!(ok = warp_wait(&acc_full[acc.s], acc.ph, 2))) break;
                     tc_fence_after();
