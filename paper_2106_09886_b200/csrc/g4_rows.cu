@@ -8,13 +8,22 @@
 // Group scales multiply the fp32 sums of a group, not the weights.  (The tensor memory path needs 128 features and a
 // pipeline per thread block; with a few rows its fixed cost is the larger part.)
 //
+// A block takes a stored row of tiles (128 features): one warp streams its tiles of 8 KB through a ring in shared memory by
+// bulk copies, which keeps some 50 KB a block in flight at no cost in registers; eight warps multiply, 16 features each, all
+// with the same columns of x, which lie in shared memory, converted once.  The contraction is split over a cluster of up to
+// eight blocks, whose sums are added in a fixed order through distributed shared memory.
 // fp32 rows are split exactly into three bf16 parts (8 + 8 + 8 bits) that occupy three of the instruction's columns.
 #include "g4_rows.cuh"
+#include "tc_ptx.cuh"
 
 namespace {
 
-constexpr int WARPS = 8;
+constexpr int WARPS = 8;                                  // that multiply; one more copies
 constexpr int STRIP = 16;                                 // features of one matrix instruction
+constexpr int THREADS = (WARPS + 1) * 32;
+constexpr int C_STAGE = G4_TILE_WORDS * 4 + 512;          // codes and up to four rows of scales
+constexpr int C_STAGES = 6;
+constexpr int X_PITCH = 320;                              // bytes of a column's 128 elements: 16-byte reads without bank conflicts
 
 template <class T> struct RowType;
 template <> struct RowType<__nv_bfloat16> { static constexpr int PARTS = 1; };
@@ -55,157 +64,231 @@ __device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Eight consecutive elements x[i .. i+7] of a row as four packed pairs: this lane's column of the B operand.  `part`
-// selects the part of a split fp32 row.  VEC: rows start and advance by whole 16 bytes.  Elements from k on are zero.
-template <class T, bool VEC>
-__device__ __forceinline__ uint4 load_octet(const T *__restrict__ row, int i, int k, int part) {
-    if (row == nullptr || i >= k) return make_uint4(0u, 0u, 0u, 0u);
-    if constexpr (sizeof(T) == 2) {
-        if (VEC && i + 8 <= k) return __ldg(reinterpret_cast<const uint4 *>(row + i));
-        uint16_t v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = i + j < k ? __ldg(reinterpret_cast<const unsigned short *>(row) + i + j) : (uint16_t)0;
-        return make_uint4(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16, v[4] | (uint32_t)v[5] << 16, v[6] | (uint32_t)v[7] << 16);
-    } else {
-        float v[8];
-        if (VEC && i + 8 <= k) {
-            const float4 lo = __ldg(reinterpret_cast<const float4 *>(row + i)), hi = __ldg(reinterpret_cast<const float4 *>(row + i) + 1);
-            v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w; v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = i + j < k ? __ldg(row + i + j) : 0.0f;
-        }
-        uint32_t b[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) b[j] = split_part_bits(v[j], part);
-        return make_uint4(__byte_perm(b[0], b[1], 0x7632), __byte_perm(b[2], b[3], 0x7632), __byte_perm(b[4], b[5], 0x7632), __byte_perm(b[6], b[7], 0x7632));
-    }
-}
-
-// A thread block computes 16 * (8 / kparts) features for one block of rows (NT * 8 / PARTS of them); its warps are
-// arranged as 8 / kparts feature strips x kparts parts of the contraction, whose sums are added in a fixed order.
-template <class T, int NT, int GROUP, bool VEC>
-__global__ void __launch_bounds__(WARPS * 32) g4_rows_kernel(const T *__restrict__ x, int64_t ldx, int rows,
-                                                            const int32_t *__restrict__ offsets, int experts, G4Weights w,
-                                                            T *__restrict__ y, int64_t ldy, int log_kparts) {
-    constexpr int PARTS = RowType<T>::PARTS, CAP = NT * 8 / PARTS, GROUPS = G4_TILE / GROUP, U = 2;
-    __shared__ float sums[WARPS][STRIP][NT * 8 + 1];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-    const ExpertSlot slot = expert_slot(offsets, experts, rows, CAP, blockIdx.y);
-    if (slot.expert < 0) return;
-
-    const int kparts = 1 << log_kparts, strips = WARPS >> log_kparts;
-    const int part = warp & (kparts - 1), strip = warp >> log_kparts;
-    const int j0 = (blockIdx.x * strips + strip) * STRIP;               // first feature of this warp
-    float acc[NT][4] = {};
-    if (j0 < w.n) {
-        // column lane/4 of the B operand: row and part of x
-        const T *xrow[NT];
-        int xpart[NT];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const int col = t * 8 + g, r = slot.first + col / PARTS;
-            xrow[t] = col / PARTS < CAP && r < slot.last ? x + (int64_t)r * ldx : nullptr;
-            xpart[t] = col % PARTS;
-        }
-        const int64_t tile0 = ((int64_t)slot.expert * w.tiles_n + j0 / G4_TILE) * w.tiles_k;
-        const int rr = j0 % G4_TILE + g;
-        const uint4 *codes = reinterpret_cast<const uint4 *>(w.codes + tile0 * G4_TILE_WORDS) + c * G4_TILE + rr;
-        const uint8_t *scales = w.scales + tile0 * (GROUPS * G4_TILE) + (GROUPS > 1 ? (c & (GROUPS - 1)) * G4_TILE : 0) + rr;
+// Elements [i0, i0 + 128 * tiles) of `have` rows of x as columns in shared memory: tile t, column c at (t * cols + c) *
+// X_PITCH; zeros from element k on.  fp32 rows become PARTS columns each.  `vec`: 16 bytes at a time.
+template <class T>
+__device__ __noinline__ void stage_columns(const T *x, int64_t ldx, int have, int i0, int tiles, int k, int cols, uint32_t xs, bool vec) {
+    constexpr int PARTS = RowType<T>::PARTS;
+    // warps of a row: all eight for one row, one when there are many
+    const int log_warps = have == 1 ? 3 : have == 2 ? 2 : have <= 4 ? 1 : 0;
+    const int row0 = threadIdx.x >> (5 + log_warps), rows_at_once = WARPS >> log_warps;
+    const int lane0 = threadIdx.x & ((32 << log_warps) - 1), lanes = 32 << log_warps;
+    if (vec) {
+        if constexpr (PARTS == 1) {
+            const int octets = tiles * 16;
 #pragma unroll 1
-        for (int kt = part; kt < w.tiles_k; kt += U * kparts) {
-            uint4 lo[U], hi[U];                                         // features g and g + 8: unit c of their 128 codes
-            float slo[U], shi[U];                                       // their scales of group c
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int at = kt + u * kparts;
-                if (at < w.tiles_k) {
-                    lo[u] = __ldcs(codes + (int64_t)at * (G4_TILE_WORDS / 4));
-                    hi[u] = __ldcs(codes + (int64_t)at * (G4_TILE_WORDS / 4) + 8);
-                    slo[u] = __fmul_rn(g4_scale_f32(__ldg(scales + (int64_t)at * (GROUPS * G4_TILE))), CodeScale<T>::UNDO);
-                    shi[u] = __fmul_rn(g4_scale_f32(__ldg(scales + (int64_t)at * (GROUPS * G4_TILE) + 8)), CodeScale<T>::UNDO);
-                } else {
-                    lo[u] = hi[u] = make_uint4(0u, 0u, 0u, 0u);
-                    slo[u] = shi[u] = 0.0f;
+            for (int r = row0; r < have; r += rows_at_once) {
+                const T *src = x + (int64_t)r * ldx + i0;
+#pragma unroll 4
+                for (int o = lane0; o < octets; o += lanes) {
+                    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                    if (i0 + o * 8 < k) v = __ldg(reinterpret_cast<const uint4 *>(src) + o);
+                    sts_128(xs + ((o >> 4) * cols + r) * X_PITCH + (o & 15) * 16, v.x, v.y, v.z, v.w);
                 }
             }
+        }
+    } else {
+#pragma unroll 1
+        for (int r = row0; r < have; r += rows_at_once) {
+            const T *src = x + (int64_t)r * ldx + i0;
+#pragma unroll 4
+            for (int o = lane0; o < tiles * 128; o += lanes) {
+                const uint32_t at = xs + ((o >> 7) * cols + r * PARTS) * X_PITCH + (o & 127) * 2;
+                if constexpr (PARTS == 1) {
+                    const unsigned short v = i0 + o < k ? __ldg(reinterpret_cast<const unsigned short *>(src) + o) : (unsigned short)0;
+                    asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"(v) : "memory");
+                } else {
+                    const float v = i0 + o < k ? __ldg(src + o) : 0.0f;
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int at = kt + u * kparts;
-                if (at >= w.tiles_k) break;
+                    for (int p = 0; p < PARTS; ++p)
+                        asm volatile("st.shared.u16 [%0], %1;" ::"r"(at + p * X_PITCH), "h"((unsigned short)(split_part_bits(v, p) >> 16)) : "memory");
+                }
+            }
+        }
+    }
+}
+__device__ __forceinline__ void multiplying_warps_sync() { asm volatile("bar.sync 1, %0;" ::"n"(WARPS * 32) : "memory"); }
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// Block (row of stored tiles, rank in the cluster) x block of rows of one expert.  The cluster's ranks share the contraction.
+template <class T, int NT, int GROUP>
+__global__ void __launch_bounds__(THREADS, 2) g4_rows_kernel(const T *__restrict__ x, int64_t ldx, int rows, const int32_t *__restrict__ offsets,
+                                                         int experts, G4Weights w, T *__restrict__ y, int64_t ldy, int log_ranks, bool vec,
+                                                         unsigned int *err, unsigned int wait_limit) {
+    constexpr int PARTS = RowType<T>::PARTS, COLS = NT * 8, CAP = COLS / PARTS, GROUPS = G4_TILE / GROUP;
+    constexpr int X_TILES = 16 / NT;                                    // tiles of x held at a time
+    extern __shared__ __align__(128) uint8_t smem[];
+    uint8_t *xbuf = smem + C_STAGES * C_STAGE;
+    uint64_t *full = reinterpret_cast<uint64_t *>(xbuf + X_TILES * COLS * X_PITCH);
+    uint64_t *empty = full + C_STAGES;
+    volatile uint32_t *abort_flag = reinterpret_cast<uint32_t *>(empty + C_STAGES);
+    const uint32_t cs = smem_u32(smem), xs = smem_u32(xbuf);
+    const int warp = warp_index(), lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    const int ranks = 1 << log_ranks, rank = blockIdx.x & (ranks - 1), jt = blockIdx.x >> log_ranks;
+
+    const ExpertSlot slot = expert_slot(offsets, experts, rows, CAP, blockIdx.y);
+    if (slot.expert < 0) return;                                        // (for every block of the cluster)
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C_STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], WARPS); }
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    __syncthreads();
+    const int first = w.tiles_k * rank >> log_ranks, last = w.tiles_k * (rank + 1) >> log_ranks;
+    const int have = slot.last - slot.first;
+    float acc[NT][4] = {};
+
+    if (warp == WARPS) {
+        Ring s;
+        int64_t tile = ((int64_t)slot.expert * w.tiles_n + jt) * w.tiles_k + first;
+        int it = 0;
+#pragma unroll 1
+        for (; it < last - first; ++it, ++tile) {
+            if (!__all_sync(0xffffffffu, short_wait(&empty[s.s], s.ph ^ 1u, abort_flag, 0, err, wait_limit))) break;
+            if (elect_one()) {
+                uint8_t *dst = smem + s.s * C_STAGE;
+                mbar_expect_tx(&full[s.s], G4_TILE_WORDS * 4 + GROUPS * G4_TILE);
+                bulk_load(dst, w.codes + tile * G4_TILE_WORDS, G4_TILE_WORDS * 4, &full[s.s]);
+                bulk_load(dst + G4_TILE_WORDS * 4, w.scales + tile * (GROUPS * G4_TILE), GROUPS * G4_TILE, &full[s.s]);
+            }
+            __syncwarp();
+            s.next(C_STAGES);
+        }
+        if (*abort_flag && lane == 0) drain_copies_in_flight(full, it, C_STAGES, wait_limit);
+        __syncwarp();
+    } else {
+        Ring s;
+        bool ok = true;
+#pragma unroll 1
+        for (int t0 = first; ok && t0 < last; t0 += X_TILES) {
+            const int here = min(X_TILES, last - t0);
+            if (t0 > first) multiplying_warps_sync();                   // the columns are still being read
+            stage_columns<T>(x + (int64_t)slot.first * ldx, ldx, have, t0 * G4_TILE, here, w.k, COLS, xs, vec);
+            multiplying_warps_sync();
+            const uint32_t at_row = cs + (c * G4_TILE + warp * STRIP + g) * 16;
+            uint32_t at_col = xs + g * X_PITCH + c * 16;
+#pragma unroll 1
+            for (int t = 0; t < here; ++t, at_col += COLS * X_PITCH) {
+                if (!(ok = __all_sync(0xffffffffu, short_wait(&full[s.s], s.ph, abort_flag, 1, err, wait_limit)))) break;
+                const uint32_t src = at_row + s.s * C_STAGE;
+                const uint4 lo = lds_128(src), hi = lds_128(src + 128);     // unit c of features g and g + 8 of the strip
+                const uint32_t sc = cs + s.s * C_STAGE + G4_TILE_WORDS * 4 + (GROUPS > 1 ? (c & (GROUPS - 1)) * G4_TILE : 0) + warp * STRIP + g;
+                const uint8_t blo = lds_8(sc), bhi = lds_8(sc + 8);         // their scales of group c
+                __syncwarp();
+                if (lane == 0) arrive_local(&empty[s.s]);
+                s.next(C_STAGES);
+                const float slo = __fmul_rn(g4_scale_f32(blo), CodeScale<T>::UNDO), shi = __fmul_rn(g4_scale_f32(bhi), CodeScale<T>::UNDO);
                 float sum[NT][4];
 #pragma unroll
                 for (int ww = 0; ww < 4; ++ww) {
-                    uint4 b[NT];
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) b[t] = load_octet<T, VEC>(xrow[t], at * G4_TILE + ww * 32 + c * 8, w.k, xpart[t]);
                     if ((ww * 32) % GROUP == 0) {
 #pragma unroll
-                        for (int t = 0; t < NT; ++t) sum[t][0] = sum[t][1] = sum[t][2] = sum[t][3] = 0.0f;
+                        for (int n = 0; n < NT; ++n) sum[n][0] = sum[n][1] = sum[n][2] = sum[n][3] = 0.0f;
                     }
-                    const uint32_t wl = ww == 0 ? lo[u].x : ww == 1 ? lo[u].y : ww == 2 ? lo[u].z : lo[u].w;
-                    const uint32_t wh = ww == 0 ? hi[u].x : ww == 1 ? hi[u].y : ww == 2 ? hi[u].z : hi[u].w;
+                    const uint32_t wl = ww == 0 ? lo.x : ww == 1 ? lo.y : ww == 2 ? lo.z : lo.w;
+                    const uint32_t wh = ww == 0 ? hi.x : ww == 1 ? hi.y : ww == 2 ? hi.z : hi.w;
                     const uint32_t l0 = code_pair<T>(wl, 0), l1 = code_pair<T>(wl, 1), l2 = code_pair<T>(wl, 2), l3 = code_pair<T>(wl, 3);
                     const uint32_t h0 = code_pair<T>(wh, 0), h1 = code_pair<T>(wh, 1), h2 = code_pair<T>(wh, 2), h3 = code_pair<T>(wh, 3);
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        mma_16x8x16<T>(sum[t], l0, h0, l1, h1, b[t].x, b[t].y);
-                        mma_16x8x16<T>(sum[t], l2, h2, l3, h3, b[t].z, b[t].w);
+                    for (int n = 0; n < NT; ++n) {
+                        const uint4 b = lds_128(at_col + n * 8 * X_PITCH + ww * 64);
+                        mma_16x8x16<T>(sum[n], l0, h0, l1, h1, b.x, b.y);
+                        mma_16x8x16<T>(sum[n], l2, h2, l3, h3, b.z, b.w);
                     }
                     if ((ww * 32 + 32) % GROUP == 0) {
                         const int grp = ww * 32 / GROUP;                // quad lane `grp` holds that group's scales
-                        const float s0 = GROUPS == 1 ? slo[u] : __shfl_sync(0xffffffffu, slo[u], grp, 4);
-                        const float s1 = GROUPS == 1 ? shi[u] : __shfl_sync(0xffffffffu, shi[u], grp, 4);
+                        const float s0 = GROUPS == 1 ? slo : __shfl_sync(0xffffffffu, slo, grp, 4);
+                        const float s1 = GROUPS == 1 ? shi : __shfl_sync(0xffffffffu, shi, grp, 4);
 #pragma unroll
-                        for (int t = 0; t < NT; ++t) {
-                            acc[t][0] = __fmaf_rn(s0, sum[t][0], acc[t][0]);
-                            acc[t][1] = __fmaf_rn(s0, sum[t][1], acc[t][1]);
-                            acc[t][2] = __fmaf_rn(s1, sum[t][2], acc[t][2]);
-                            acc[t][3] = __fmaf_rn(s1, sum[t][3], acc[t][3]);
+                        for (int n = 0; n < NT; ++n) {
+                            acc[n][0] = __fmaf_rn(s0, sum[n][0], acc[n][0]);
+                            acc[n][1] = __fmaf_rn(s0, sum[n][1], acc[n][1]);
+                            acc[n][2] = __fmaf_rn(s1, sum[n][2], acc[n][2]);
+                            acc[n][3] = __fmaf_rn(s1, sum[n][3], acc[n][3]);
                         }
                     }
                 }
             }
         }
-    }
+        multiplying_warps_sync();                                       // the columns of x make room for the sums
+        float *sums = reinterpret_cast<float *>(xbuf);                  // [128 features][COLS + 1]
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        sums[warp][g][t * 8 + 2 * c] = acc[t][0];
-        sums[warp][g][t * 8 + 2 * c + 1] = acc[t][1];
-        sums[warp][g + 8][t * 8 + 2 * c] = acc[t][2];
-        sums[warp][g + 8][t * 8 + 2 * c + 1] = acc[t][3];
+        for (int n = 0; n < NT; ++n) {
+            float *at = sums + (warp * STRIP + g) * (COLS + 1) + n * 8 + 2 * c;
+            at[0] = acc[n][0];
+            at[1] = acc[n][1];
+            at[8 * (COLS + 1)] = acc[n][2];
+            at[8 * (COLS + 1) + 1] = acc[n][3];
+        }
     }
-    __syncthreads();
+    if (log_ranks) cluster_sync();
+    else __syncthreads();
+    // each rank adds up its share of the features over all ranks, in their order
     const float alpha = __ldg(w.alpha + slot.expert);
-    const int feats = strips * STRIP, jbase = blockIdx.x * feats, have = slot.last - slot.first;
-    for (int v = threadIdx.x; v < feats * have; v += WARPS * 32) {
-        const int f = v % feats, r = v / feats, j = jbase + f;
+    const int log_feats = 7 - log_ranks;
+#pragma unroll 1
+    for (int v = threadIdx.x; v < have << log_feats; v += THREADS) {
+        const int f = (rank << log_feats) + (v & ((1 << log_feats) - 1)), r = v >> log_feats, j = jt * G4_TILE + f;
         if (j >= w.n) continue;
+        const uint32_t at = xs + (f * (COLS + 1) + r * PARTS) * 4;
         float total = 0.0f;
-        for (int p = 0; p < kparts; ++p) {
-            const float *s = sums[(f / STRIP) * kparts + p][f % STRIP] + r * PARTS;
-            float one = s[PARTS - 1];                                   // smallest part first
+#pragma unroll 1
+        for (int q = 0; q < ranks; ++q) {
+            uint32_t there;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(q));
+            float one = 0.0f;
 #pragma unroll
-            for (int q = PARTS - 2; q >= 0; --q) one = __fadd_rn(one, s[q]);
+            for (int p = PARTS - 1; p >= 0; --p) {                      // smallest part first
+                float s;
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(s) : "r"(there + p * 4) : "memory");
+                one = __fadd_rn(one, s);
+            }
             total = __fadd_rn(total, one);
         }
         real_store(y + (int64_t)(slot.first + r) * ldy + j, __fmul_rn(total, alpha));
     }
+    if (log_ranks) cluster_sync();                                      // nobody leaves while its sums are read
 }
 
 template <class T, int NT, int GROUP>
 int launch(const T *x, int64_t ldx, int rows, const int32_t *offsets, int experts, const G4Weights &w, T *y, int64_t ldy, cudaStream_t st) {
     constexpr int CAP = NT * 8 / RowType<T>::PARTS;
-    int log_kparts = 0;
-    while (log_kparts < 3 && (2 << log_kparts) <= w.tiles_k) ++log_kparts;
+    constexpr int SMEM = C_STAGES * C_STAGE + 16 / NT * NT * 8 * X_PITCH + 2 * C_STAGES * 8 + 16;
+    auto kernel = g4_rows_kernel<T, NT, GROUP>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess) return QNN_E_CUDA;
     const int64_t slots = offsets ? expert_slots_most(rows, experts, CAP) : (rows + CAP - 1) / CAP;
     if (slots > 65535) return QNN_E_RANGE;
-    const int feats = STRIP * (WARPS >> log_kparts);
-    const dim3 grid((unsigned)((w.n + feats - 1) / feats), (unsigned)slots);
-    const bool vec = qnn_aligned(x, 16) && (ldx * (int64_t)sizeof(T)) % 16 == 0;
-    if (vec) g4_rows_kernel<T, NT, GROUP, true><<<grid, WARPS * 32, 0, st>>>(x, ldx, rows, offsets, experts, w, y, ldy, log_kparts);
-    else g4_rows_kernel<T, NT, GROUP, false><<<grid, WARPS * 32, 0, st>>>(x, ldx, rows, offsets, experts, w, y, ldy, log_kparts);
-    return qnn_launch_status();
+    // Ranks of a cluster: what ends first when two blocks fit an SM, a block costs three tiles' time besides its tiles
+    int log_ranks = 0;
+    int64_t best = INT64_MAX;
+    for (int l = 0; l < 4 && (1 << l) <= w.tiles_k; ++l) {
+        const int64_t blocks = slots * w.tiles_n << l, rounds = (blocks + 2 * 148 - 1) / (2 * 148);
+        const int64_t cost = rounds * ((w.tiles_k + (1 << l) - 1) / (1 << l) + 3);
+        if (cost < best) { best = cost; log_ranks = l; }
+    }
+    unsigned int *err = qnn_tc_error_word();
+    if (!err) return QNN_E_CUDA;
+    const bool vec = sizeof(T) == 2 && qnn_aligned(x, 16) && ldx % 8 == 0 && w.k % 8 == 0;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(w.tiles_n << log_ranks), (unsigned)slots);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = SMEM;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 1u << log_ranks;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = log_ranks ? 1 : 0;
+    if (cudaLaunchKernelEx(&cfg, kernel, x, ldx, rows, offsets, experts, w, y, ldy, log_ranks, vec, err, WAIT_LIMIT) != cudaSuccess) {
+        cudaGetLastError();
+        return QNN_E_CUDA;
+    }
+    return QNN_OK;
 }
 
 template <class T, int NT>

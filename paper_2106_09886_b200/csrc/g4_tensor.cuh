@@ -56,26 +56,6 @@ template <int CG> __device__ __forceinline__ void arrive_leader(uint64_t *bar) {
     else
         asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(leader_addr<2>(bar)) : "memory");
 }
-__device__ __forceinline__ void arrive_local(uint64_t *bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-// mbar_wait with its polling loop in one place: these kernels hold many roles, and code that does not fit the instruction
-// cache costs them more than any instruction does.
-__device__ __noinline__ bool mbar_poll(uint64_t *bar, uint32_t parity, volatile uint32_t *abort_flag, unsigned id, unsigned int *err,
-                                       uint32_t limit) {
-#pragma unroll 1
-    for (uint32_t it = 0; it < limit; ++it) {
-        if (mbar_try_wait(bar, parity)) return true;
-        if ((it & 1023u) == 1023u && *abort_flag) return false;
-    }
-    *abort_flag = 1;
-    atomicCAS(err, 0u, 1u + id);
-    return false;
-}
-__device__ __forceinline__ bool short_wait(uint64_t *bar, uint32_t parity, volatile uint32_t *abort_flag, unsigned id,
-                                           unsigned int *err, uint32_t limit) {
-    return mbar_try_wait(bar, parity) || mbar_poll(bar, parity, abort_flag, id, err, limit);
-}
 // 2-D box into this block's shared memory, its bytes counted on the leading block's barrier.
 template <int CG>
 __device__ __forceinline__ void pair_load_2d(void *dst, const CUtensorMap *map, uint64_t *bar, int x, int y) {
@@ -85,10 +65,6 @@ __device__ __forceinline__ void pair_load_2d(void *dst, const CUtensorMap *map, 
         asm volatile(
             "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
             ::"r"(smem_u32(dst)), "l"(map), "r"(leader_addr<2>(bar)), "r"(x), "r"(y) : "memory");
-}
-__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
 }
 template <int CG> __device__ __forceinline__ void pair_tmem_alloc(uint32_t *slot, uint32_t ncols) {   // one whole warp per block
     if constexpr (CG == 1) {
@@ -164,41 +140,6 @@ __host__ __device__ constexpr uint32_t idesc_f16(uint32_t fmt, int m, int n, boo
     return (1u << 4) | (fmt << 7) | (fmt << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
            ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
-
-// One lane of a converged warp, chosen so that the compiler knows the branch for a single-thread region of uniform values
-// (instructions that take uniform registers are then issued straight; behind lane == 0 each operand is moved over first).
-__device__ __forceinline__ bool elect_one() {
-    uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
-    return ok != 0;
-}
-__device__ __forceinline__ int warp_index() { return __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0); }
-
-// Shared memory by its own address: behind the alignment of the dynamic array the compiler would take generic accesses.
-__device__ __forceinline__ uint4 lds_128(uint32_t a) {
-    uint4 v;
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint8_t lds_8(uint32_t a) {
-    uint32_t v;
-    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-    return (uint8_t)v;
-}
-__device__ __forceinline__ void sts_128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
-    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
-}
-
-struct Ring {                                            // position in a ring of stages and the parity of its round
-    int s = 0;
-    uint32_t ph = 0;
-    __device__ __forceinline__ void next(int stages) {
-        if (++s == stages) { s = 0; ph ^= 1u; }
-    }
-    __device__ __forceinline__ void skip(int n, int stages) {      // n <= stages
-        if ((s += n) >= stages) { s -= stages; ph ^= 1u; }
-    }
-};
 
 // Blocks of TN rows, counted expert by expert, visited in increasing order by a whole warp.
 struct SlotCursor {
