@@ -2,7 +2,9 @@
 
 Argument marshalling only -- every step runs inside the library's CUDA kernels.  The
 library must have been built (``python -m paper_2106_09886_b200.build``); importing this
-module without it raises ImportError, and there is no CPU fallback.
+module without it raises ImportError, and there is no CPU fallback.  The calls on 4-bit
+weights, which a decoding step makes by the hundred, are marshalled by a compiled module
+(csrc/binding.cpp) instead of ctypes.
 """
 from __future__ import annotations
 
@@ -115,6 +117,7 @@ def _load() -> C.CDLL:
 
 
 lib = _load()
+from . import _binding  # noqa: E402  (needs torch and libqnn.so)
 
 
 def status_string(status: int) -> str:
@@ -373,85 +376,18 @@ class G4Weights(NamedTuple):
     group: int               # weights of a row that share a scale: 32, 64 or 128
 
 
-def _real_rows(t: torch.Tensor, width: int, name: str) -> tuple[int, int, int]:
-    """Checks a [rows, width] operand whose rows may be strided: (type code, rows, row stride)."""
-    code = REAL_TYPES.get(t.dtype)
-    if code is None:
-        raise ValueError(f"{name} must be float32, bfloat16 or float16")
-    if t.dim() != 2:
-        raise ValueError(f"{name} must be [rows, {width}]")
-    (rows, cols), (ld, step) = t.shape, t.stride()
-    if cols != width:
-        raise ValueError(f"{name} must be [rows, {width}]")
-    if t.get_device() != _current_device():                     # (-1 for a CPU tensor)
-        raise ValueError(f"{name} must be on the current CUDA device")
-    if rows <= 1:
-        ld = max(ld, width)
-    if step != 1 and width > 1 and rows > 0 or ld < width:
-        raise ValueError(f"{name} must have contiguous rows that do not overlap")
-    return code, rows, ld
-
-
-def _current_device() -> int:
-    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
-
-
-def _g4_check(w: G4Weights, device: int) -> int:
-    """Checks the three arrays of a handle against its sizes (device: index of the rows' device); returns the number of matrices."""
-    codes, scales, alpha, n, k, group = w
-    if group != 128 and group != 64 and group != 32:
-        raise ValueError("group must be 32, 64 or 128")
-    if (codes.dtype is not torch.int32 or scales.dtype is not torch.uint8 or alpha.dtype is not torch.float32
-            or not codes.is_contiguous() or not scales.is_contiguous() or not alpha.is_contiguous()):
-        raise ValueError("codes, scales and alpha must be contiguous int32, uint8 and float32")
-    experts, tn, tk = codes.shape[0], (n + 127) // 128, (k + 127) // 128
-    if n < 1 or k < 1 or codes.shape != (experts, tn, tk, 4, 128, 4):
-        raise ValueError("codes do not have the shape of an n x k matrix")
-    if scales.shape != (experts, tn, tk, 128 // group, 128) or alpha.shape != (experts,):
-        raise ValueError("scales or alpha do not have the shape that goes with the codes")
-    if codes.get_device() != device or scales.get_device() != device or alpha.get_device() != device:
-        raise ValueError("the weights must be on the device of the rows")
-    return experts
-
-
-def _expert_offsets(offsets: torch.Tensor, device: int) -> int:
-    if offsets.dtype is not torch.int32 or offsets.dim() != 1 or not offsets.is_contiguous() or offsets.get_device() != device:
-        raise ValueError("offsets must be contiguous int32 [experts + 1] on the device of the rows")
-    experts = offsets.numel() - 1
-    if experts < 1:
-        raise ValueError("offsets must have experts + 1 entries")
-    return experts
-
-
-def _out_rows(out, rows: int, width: int, like: torch.Tensor, name: str, stream) -> tuple[torch.Tensor, int]:
-    """The result and its row stride: a given one is checked, a missing one allocated for the stream that will write it."""
-    if out is None:
-        return _on_stream(stream, lambda: like.new_empty((rows, width))), width
-    code, have, ld = _real_rows(out, width, name)
-    if out.dtype is not like.dtype or have != rows:
-        raise ValueError(f"{name} must be [{rows}, {width}] {like.dtype}")
-    return out, ld
-
-
-def _on_stream(stream, make):
-    """Runs an allocation so that its memory belongs to `stream` (a block freed early is then reused in that stream's order)."""
+def _on_stream(stream, call):
+    """Runs a call, and what it allocates, on `stream` (a block freed early is then reused in that stream's order)."""
     if stream is None:
-        return make()
+        return call()
     with torch.cuda.stream(stream):
-        return make()
+        return call()
 
 
-def _raw_stream(stream, device: int) -> int:
-    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
-
-
-def _scratch(nbytes: int, like: torch.Tensor, workspace, stream) -> tuple[torch.Tensor | None, int, int]:
-    """(what keeps the workspace alive, its address, its bytes)"""
-    if workspace is None:
-        if nbytes == 0:
-            return None, 0, 0
-        workspace = _on_stream(stream, lambda: like.new_empty(nbytes, dtype=torch.uint8))
-    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+def _result(r, call: str) -> torch.Tensor:
+    if r.__class__ is int:
+        raise QnnError(r, call)
+    return r
 
 
 def g4_pack_weights(w: torch.Tensor, group: int = 128, stream=None) -> G4Weights:
@@ -474,66 +410,29 @@ def g4_pack_weights(w: torch.Tensor, group: int = 128, stream=None) -> G4Weights
 
 def g4_matvec(x: torch.Tensor, w: G4Weights, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """x [rows, k] (few rows; their stride is free) times one 4-bit matrix -> [rows, n] of x's type."""
-    n, k = w.n, w.k
-    code, rows, ldx = _real_rows(x, k, "x")
-    device = x.get_device()
-    if _g4_check(w, device) != 1:
-        raise ValueError("g4_matvec takes one matrix")
-    out, ldo = _out_rows(out, rows, n, x, "out", stream)
-    _check(lib.qnn_g4_matvec(x.data_ptr(), code, rows, ldx, w.codes.data_ptr(), w.scales.data_ptr(), w.alpha.data_ptr(), n, k,
-                             w.group, out.data_ptr(), ldo, _raw_stream(stream, device)), "qnn_g4_matvec")
-    return out
-
-
-def _expert_product(query, call, name: str, a: torch.Tensor, w: G4Weights, width: int, width_out: int, offsets: torch.Tensor,
-                    out, workspace, stream) -> torch.Tensor:
-    code, rows, lda = _real_rows(a, width, "x" if width == w.k else "dy")
-    device = a.get_device()
-    experts = _g4_check(w, device)
-    if _expert_offsets(offsets, device) != experts:
-        raise ValueError("offsets must have experts + 1 entries")
-    out, ldo = _out_rows(out, rows, width_out, a, "out", stream)
-    pa = a.data_ptr()
-    keep, ws, ws_bytes = _scratch(query(pa, code, rows, lda, experts, w.n, w.k), a, workspace, stream)
-    _check(call(pa, code, rows, lda, offsets.data_ptr(), experts, w.codes.data_ptr(), w.scales.data_ptr(), w.alpha.data_ptr(), w.n,
-                w.k, w.group, out.data_ptr(), ldo, ws, ws_bytes, _raw_stream(stream, device)), name)
-    return out
+    if stream is None:
+        return _result(_binding.g4_matvec(x, *w, out), "qnn_g4_matvec")
+    return _result(_on_stream(stream, lambda: _binding.g4_matvec(x, *w, out)), "qnn_g4_matvec")
 
 
 def g4_expert_gemm(x: torch.Tensor, w: G4Weights, offsets: torch.Tensor, out: torch.Tensor | None = None,
                    workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """x [rows, k], rows sorted by expert (expert e owns rows offsets[e] .. offsets[e+1]) -> [rows, n] of x's type."""
-    return _expert_product(lib.qnn_g4_expert_gemm_workspace, lib.qnn_g4_expert_gemm, "qnn_g4_expert_gemm", x, w, w.k, w.n, offsets,
-                           out, workspace, stream)
+    return _result(_on_stream(stream, lambda: _binding.g4_expert_gemm(x, *w, offsets, out, workspace)), "qnn_g4_expert_gemm")
 
 
 def g4_expert_gemm_backward_data(dy: torch.Tensor, w: G4Weights, offsets: torch.Tensor, out: torch.Tensor | None = None,
                                  workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Gradient of g4_expert_gemm with respect to x: dy [rows, n] -> [rows, k] of dy's type."""
-    return _expert_product(lib.qnn_g4_expert_backward_data_workspace, lib.qnn_g4_expert_backward_data,
-                           "qnn_g4_expert_backward_data", dy, w, w.n, w.k, offsets, out, workspace, stream)
+    return _result(_on_stream(stream, lambda: _binding.g4_expert_gemm_backward_data(dy, *w, offsets, out, workspace)),
+                   "qnn_g4_expert_backward_data")
 
 
 def expert_gemm_backward_weights(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Tensor, gw: torch.Tensor | None = None,
                                  workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Gradient of g4_expert_gemm with respect to the decoded weights: dy [rows, n], x [rows, k] -> fp32 [experts, n, k]."""
-    n, k = dy.shape[-1], x.shape[-1]
-    code, rows, lddy = _real_rows(dy, n, "dy")
-    xcode, xrows, ldx = _real_rows(x, k, "x")
-    if xcode != code or xrows != rows:
-        raise ValueError("dy and x must have the same type and number of rows")
-    device = x.get_device()
-    experts = _expert_offsets(offsets, device)
-    if gw is None:
-        gw = _on_stream(stream, lambda: dy.new_empty((experts, n, k), dtype=torch.float32))
-    elif _dev(gw, torch.float32, "gw").shape != (experts, n, k) or gw.get_device() != device:
-        raise ValueError("gw must be [experts, n, k] on the device of the rows")
-    pd, px = dy.data_ptr(), x.data_ptr()
-    keep, ws, ws_bytes = _scratch(lib.qnn_expert_backward_weights_workspace(pd, px, code, rows, lddy, ldx, experts, n, k), dy,
-                                  workspace, stream)
-    _check(lib.qnn_expert_backward_weights(pd, px, code, rows, lddy, ldx, offsets.data_ptr(), experts, n, k, gw.data_ptr(), ws,
-                                           ws_bytes, _raw_stream(stream, device)), "qnn_expert_backward_weights")
-    return gw
+    return _result(_on_stream(stream, lambda: _binding.expert_gemm_backward_weights(dy, x, offsets, gw, workspace)),
+                   "qnn_expert_backward_weights")
 
 
 def unpack_codes_f32(planes: torch.Tensor, rows: int, k: int, bits: int, transpose: bool = False, stream=None) -> torch.Tensor:

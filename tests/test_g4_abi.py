@@ -146,12 +146,21 @@ def test_binding_refusals(qnn):
                  lambda: qnn.g4_pack_weights(torch.zeros((8, 64)))):
         with pytest.raises(ValueError):
             call()
-    assert qnn._g4_check(w, -1) == 1
-    for bad in (w._replace(group=16), w._replace(n=129), w._replace(k=129), w._replace(codes=w.codes.float()),
-                w._replace(scales=w.scales[..., :64]), w._replace(alpha=torch.ones(2)),
-                w._replace(codes=w.codes.expand(2, -1, -1, -1, -1, -1))):
+    # shapes and types are looked at before devices
+    for bad, why in ((w._replace(group=16), "group"), (w._replace(n=129), "codes"), (w._replace(k=129), "codes"), (w._replace(n=0), "codes"),
+                     (w._replace(codes=w.codes.float()), "codes"), (w._replace(scales=w.scales[..., :64].contiguous()), "scales"),
+                     (w._replace(alpha=torch.ones(2)), "alpha"), (w._replace(codes=w.codes.expand(2, -1, -1, -1, -1, -1)), "codes"),
+                     (w._replace(codes=None), "codes")):
+        with pytest.raises(ValueError, match=why):
+            qnn.g4_matvec(cpu, bad)
+    for bad, why in ((torch.tensor([0, 2]), "offsets"), (torch.tensor([0], dtype=torch.int32), "offsets"),
+                     (torch.zeros((2, 2), dtype=torch.int32), "offsets"), (torch.tensor([0, 1, 2], dtype=torch.int32), "experts"), (None, "offsets")):
+        with pytest.raises(ValueError, match=why):
+            qnn.g4_expert_gemm(cpu, w, bad)
+    for bad in (cpu.double(), cpu[:, :63], cpu[0], cpu.expand(2, 2, 64), torch.zeros(64, 2).t(), cpu[:1].expand(4, 64), None):
         with pytest.raises(ValueError):
-            qnn._g4_check(bad, -1)
-    for bad in (torch.tensor([0, 2]), torch.tensor([0], dtype=torch.int32), torch.zeros((2, 2), dtype=torch.int32)):
-        with pytest.raises(ValueError):
-            qnn._expert_offsets(bad, -1)
+            qnn.g4_matvec(bad, w)
+    with pytest.raises(ValueError, match="type"):
+        qnn.expert_gemm_backward_weights(torch.zeros((2, 8)), cpu.bfloat16(), offsets)
+    with pytest.raises(ValueError, match="current CUDA device"):
+        qnn.g4_matvec(cpu, w)
