@@ -21,8 +21,10 @@ namespace {
 constexpr int WARPS = 8;                                  // that multiply; one more copies
 constexpr int STRIP = 16;                                 // features of one matrix instruction
 constexpr int THREADS = (WARPS + 1) * 32;
-constexpr int C_STAGE = G4_TILE_WORDS * 4 + 512;          // codes and up to four rows of scales
-constexpr int C_STAGES = 6;
+constexpr int C_TILE = G4_TILE_WORDS * 4 + 512;           // codes and up to four rows of scales
+constexpr int U = 2;                                      // tiles of a stage: one wait, and their reads overlap
+constexpr int C_STAGE = U * C_TILE;
+constexpr int C_STAGES = 3;
 constexpr int X_PITCH = 320;                              // bytes of a column's 128 elements: 16-byte reads without bank conflicts
 
 template <class T> struct RowType;
@@ -119,7 +121,7 @@ __global__ void __launch_bounds__(THREADS, 2) g4_rows_kernel(const T *__restrict
                                                          int experts, G4Weights w, T *__restrict__ y, int64_t ldy, int log_ranks, bool vec,
                                                          unsigned int *err, unsigned int wait_limit) {
     constexpr int PARTS = RowType<T>::PARTS, COLS = NT * 8, CAP = COLS / PARTS, GROUPS = G4_TILE / GROUP;
-    constexpr int X_TILES = 16 / NT;                                    // tiles of x held at a time
+    constexpr int X_TILES = 16 / NT / U * U;                            // tiles of x held at a time
     extern __shared__ __align__(128) uint8_t smem[];
     uint8_t *xbuf = smem + C_STAGES * C_STAGE;
     uint64_t *full = reinterpret_cast<uint64_t *>(xbuf + X_TILES * COLS * X_PITCH);
@@ -138,7 +140,7 @@ __global__ void __launch_bounds__(THREADS, 2) g4_rows_kernel(const T *__restrict
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     __syncthreads();
-    const int first = w.tiles_k * rank >> log_ranks, last = w.tiles_k * (rank + 1) >> log_ranks;
+    const int first = (int)((int64_t)w.tiles_k * rank >> log_ranks), last = (int)((int64_t)w.tiles_k * (rank + 1) >> log_ranks);
     const int have = slot.last - slot.first;
     float acc[NT][4] = {};
 
@@ -147,13 +149,18 @@ __global__ void __launch_bounds__(THREADS, 2) g4_rows_kernel(const T *__restrict
         int64_t tile = ((int64_t)slot.expert * w.tiles_n + jt) * w.tiles_k + first;
         int it = 0;
 #pragma unroll 1
-        for (; it < last - first; ++it, ++tile) {
+        for (int t = first; t < last; t += U, tile += U, ++it) {
             if (!__all_sync(0xffffffffu, short_wait(&empty[s.s], s.ph ^ 1u, abort_flag, 0, err, wait_limit))) break;
             if (elect_one()) {
-                uint8_t *dst = smem + s.s * C_STAGE;
-                mbar_expect_tx(&full[s.s], G4_TILE_WORDS * 4 + GROUPS * G4_TILE);
-                bulk_load(dst, w.codes + tile * G4_TILE_WORDS, G4_TILE_WORDS * 4, &full[s.s]);
-                bulk_load(dst + G4_TILE_WORDS * 4, w.scales + tile * (GROUPS * G4_TILE), GROUPS * G4_TILE, &full[s.s]);
+                const int here = min(U, last - t);
+                mbar_expect_tx(&full[s.s], here * (G4_TILE_WORDS * 4 + GROUPS * G4_TILE));
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (u >= here) break;
+                    uint8_t *dst = smem + s.s * C_STAGE + u * C_TILE;
+                    bulk_load(dst, w.codes + (tile + u) * G4_TILE_WORDS, G4_TILE_WORDS * 4, &full[s.s]);
+                    bulk_load(dst + G4_TILE_WORDS * 4, w.scales + (tile + u) * (GROUPS * G4_TILE), GROUPS * G4_TILE, &full[s.s]);
+                }
             }
             __syncwarp();
             s.next(C_STAGES);
@@ -172,46 +179,58 @@ __global__ void __launch_bounds__(THREADS, 2) g4_rows_kernel(const T *__restrict
             const uint32_t at_row = cs + (c * G4_TILE + warp * STRIP + g) * 16;
             uint32_t at_col = xs + g * X_PITCH + c * 16;
 #pragma unroll 1
-            for (int t = 0; t < here; ++t, at_col += COLS * X_PITCH) {
+            for (int t = 0; t < here; t += U, at_col += U * COLS * X_PITCH) {
                 if (!(ok = __all_sync(0xffffffffu, short_wait(&full[s.s], s.ph, abort_flag, 1, err, wait_limit)))) break;
-                const uint32_t src = at_row + s.s * C_STAGE;
-                const uint4 lo = lds_128(src), hi = lds_128(src + 128);     // unit c of features g and g + 8 of the strip
-                const uint32_t sc = cs + s.s * C_STAGE + G4_TILE_WORDS * 4 + (GROUPS > 1 ? (c & (GROUPS - 1)) * G4_TILE : 0) + warp * STRIP + g;
-                const uint8_t blo = lds_8(sc), bhi = lds_8(sc + 8);         // their scales of group c
-                __syncwarp();
-                if (lane == 0) arrive_local(&empty[s.s]);
-                s.next(C_STAGES);
-                const float slo = __fmul_rn(g4_scale_f32(blo), CodeScale<T>::UNDO), shi = __fmul_rn(g4_scale_f32(bhi), CodeScale<T>::UNDO);
-                float sum[NT][4];
+                uint4 lo[U], hi[U];                                         // unit c of features g and g + 8 of the strip
+                uint8_t blo[U], bhi[U];                                     // their scales of group c
 #pragma unroll
-                for (int ww = 0; ww < 4; ++ww) {
-                    if ((ww * 32) % GROUP == 0) {
+                for (int u = 0; u < U; ++u) {                               // (behind an odd end: what an earlier stage left, not used)
+                    const uint32_t src = at_row + s.s * C_STAGE + u * C_TILE;
+                    lo[u] = lds_128(src);
+                    hi[u] = lds_128(src + 128);
+                    const uint32_t sc = cs + s.s * C_STAGE + u * C_TILE + G4_TILE_WORDS * 4 + (GROUPS > 1 ? (c & (GROUPS - 1)) * G4_TILE : 0) + warp * STRIP + g;
+                    blo[u] = lds_8(sc);
+                    bhi[u] = lds_8(sc + 8);
+                }
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) sum[n][0] = sum[n][1] = sum[n][2] = sum[n][3] = 0.0f;
-                    }
-                    const uint32_t wl = ww == 0 ? lo.x : ww == 1 ? lo.y : ww == 2 ? lo.z : lo.w;
-                    const uint32_t wh = ww == 0 ? hi.x : ww == 1 ? hi.y : ww == 2 ? hi.z : hi.w;
-                    const uint32_t l0 = code_pair<T>(wl, 0), l1 = code_pair<T>(wl, 1), l2 = code_pair<T>(wl, 2), l3 = code_pair<T>(wl, 3);
-                    const uint32_t h0 = code_pair<T>(wh, 0), h1 = code_pair<T>(wh, 1), h2 = code_pair<T>(wh, 2), h3 = code_pair<T>(wh, 3);
+                for (int u = 0; u < U; ++u) {
+                    if (t + u >= here) break;
+                    const float slo = __fmul_rn(g4_scale_f32(blo[u]), CodeScale<T>::UNDO), shi = __fmul_rn(g4_scale_f32(bhi[u]), CodeScale<T>::UNDO);
+                    float sum[NT][4];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        const uint4 b = lds_128(at_col + n * 8 * X_PITCH + ww * 64);
-                        mma_16x8x16<T>(sum[n], l0, h0, l1, h1, b.x, b.y);
-                        mma_16x8x16<T>(sum[n], l2, h2, l3, h3, b.z, b.w);
-                    }
-                    if ((ww * 32 + 32) % GROUP == 0) {
-                        const int grp = ww * 32 / GROUP;                // quad lane `grp` holds that group's scales
-                        const float s0 = GROUPS == 1 ? slo : __shfl_sync(0xffffffffu, slo, grp, 4);
-                        const float s1 = GROUPS == 1 ? shi : __shfl_sync(0xffffffffu, shi, grp, 4);
+                    for (int ww = 0; ww < 4; ++ww) {
+                        if ((ww * 32) % GROUP == 0) {
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) sum[n][0] = sum[n][1] = sum[n][2] = sum[n][3] = 0.0f;
+                        }
+                        const uint32_t wl = ww == 0 ? lo[u].x : ww == 1 ? lo[u].y : ww == 2 ? lo[u].z : lo[u].w;
+                        const uint32_t wh = ww == 0 ? hi[u].x : ww == 1 ? hi[u].y : ww == 2 ? hi[u].z : hi[u].w;
+                        const uint32_t l0 = code_pair<T>(wl, 0), l1 = code_pair<T>(wl, 1), l2 = code_pair<T>(wl, 2), l3 = code_pair<T>(wl, 3);
+                        const uint32_t h0 = code_pair<T>(wh, 0), h1 = code_pair<T>(wh, 1), h2 = code_pair<T>(wh, 2), h3 = code_pair<T>(wh, 3);
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            acc[n][0] = __fmaf_rn(s0, sum[n][0], acc[n][0]);
-                            acc[n][1] = __fmaf_rn(s0, sum[n][1], acc[n][1]);
-                            acc[n][2] = __fmaf_rn(s1, sum[n][2], acc[n][2]);
-                            acc[n][3] = __fmaf_rn(s1, sum[n][3], acc[n][3]);
+                            const uint4 b = lds_128(at_col + (u * COLS + n * 8) * X_PITCH + ww * 64);
+                            mma_16x8x16<T>(sum[n], l0, h0, l1, h1, b.x, b.y);
+                            mma_16x8x16<T>(sum[n], l2, h2, l3, h3, b.z, b.w);
+                        }
+                        if ((ww * 32 + 32) % GROUP == 0) {
+                            const int grp = ww * 32 / GROUP;                // quad lane `grp` holds that group's scales
+                            const float s0 = GROUPS == 1 ? slo : __shfl_sync(0xffffffffu, slo, grp, 4);
+                            const float s1 = GROUPS == 1 ? shi : __shfl_sync(0xffffffffu, shi, grp, 4);
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) {
+                                acc[n][0] = __fmaf_rn(s0, sum[n][0], acc[n][0]);
+                                acc[n][1] = __fmaf_rn(s0, sum[n][1], acc[n][1]);
+                                acc[n][2] = __fmaf_rn(s1, sum[n][2], acc[n][2]);
+                                acc[n][3] = __fmaf_rn(s1, sum[n][3], acc[n][3]);
+                            }
                         }
                     }
                 }
+                // only now: an arrival does not wait for loads whose values nobody has used yet
+                __syncwarp();
+                if (lane == 0) arrive_local(&empty[s.s]);
+                s.next(C_STAGES);
             }
         }
         multiplying_warps_sync();                                       // the columns of x make room for the sums
@@ -235,19 +254,21 @@ __global__ void __launch_bounds__(THREADS, 2) g4_rows_kernel(const T *__restrict
         const int f = (rank << log_feats) + (v & ((1 << log_feats) - 1)), r = v >> log_feats, j = jt * G4_TILE + f;
         if (j >= w.n) continue;
         const uint32_t at = xs + (f * (COLS + 1) + r * PARTS) * 4;
-        float total = 0.0f;
-#pragma unroll 1
-        for (int q = 0; q < ranks; ++q) {
+        float one[8][PARTS], total = 0.0f;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {                                   // all loads first: each takes a round trip
+            if (q >= ranks) break;
             uint32_t there;
             asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(q));
-            float one = 0.0f;
 #pragma unroll
-            for (int p = PARTS - 1; p >= 0; --p) {                      // smallest part first
-                float s;
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(s) : "r"(there + p * 4) : "memory");
-                one = __fadd_rn(one, s);
-            }
-            total = __fadd_rn(total, one);
+            for (int p = 0; p < PARTS; ++p) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(one[q][p]) : "r"(there + p * 4) : "memory");
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            if (q >= ranks) break;
+#pragma unroll
+            for (int p = PARTS - 2; p >= 0; --p) one[q][PARTS - 1] = __fadd_rn(one[q][PARTS - 1], one[q][p]);     // smallest first
+            total = __fadd_rn(total, one[q][PARTS - 1]);
         }
         real_store(y + (int64_t)(slot.first + r) * ldy + j, __fmul_rn(total, alpha));
     }
@@ -257,7 +278,7 @@ __global__ void __launch_bounds__(THREADS, 2) g4_rows_kernel(const T *__restrict
 template <class T, int NT, int GROUP>
 int launch(const T *x, int64_t ldx, int rows, const int32_t *offsets, int experts, const G4Weights &w, T *y, int64_t ldy, cudaStream_t st) {
     constexpr int CAP = NT * 8 / RowType<T>::PARTS;
-    constexpr int SMEM = C_STAGES * C_STAGE + 16 / NT * NT * 8 * X_PITCH + 2 * C_STAGES * 8 + 16;
+    constexpr int SMEM = C_STAGES * C_STAGE + 16 / NT / U * U * NT * 8 * X_PITCH + 2 * C_STAGES * 8 + 16;
     auto kernel = g4_rows_kernel<T, NT, GROUP>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess) return QNN_E_CUDA;
     const int64_t slots = offsets ? expert_slots_most(rows, experts, CAP) : (rows + CAP - 1) / CAP;

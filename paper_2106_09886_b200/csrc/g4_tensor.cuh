@@ -548,8 +548,6 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
 #pragma unroll
             for (int w = 1; w < 4; ++w)
                 sb[w] = log_group == 7 ? sb[0] : lds_8(src + G4_TILE_WORDS * 4 + ((32 * w) >> log_group) * G4_TILE + r);
-            __syncwarp();
-            if (lane == 0) arrive_local(&c_empty[c.s]);
             if (!warp_wait(&empty[g.s], g.ph ^ 1u, 0)) break;
             if constexpr (MODE == G4_FWD) {
                 // lane r of the A operand, 16 tensor-memory columns (32 codes) at a time
@@ -583,7 +581,10 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             }
             __syncwarp();
-            if (lane == 0) arrive_leader<CG>(&full[g.s]);
+            if (lane == 0) {
+                arrive_local(&c_empty[c.s]);              // only now: an arrival does not wait for loads nobody has used yet
+                arrive_leader<CG>(&full[g.s]);
+            }
         }
     } else if (warp >= 4) {               // ------------------------------------------------ results
         SlotCursor cur(p.offsets, p.experts, p.rows, TN);

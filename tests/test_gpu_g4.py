@@ -92,7 +92,7 @@ def test_pack_special_values(t, qnn):
 @pytest.mark.parametrize("dtype", ref.TYPES)
 @pytest.mark.parametrize("group", [32, 64, 128])
 @pytest.mark.parametrize("rows,n,k", [(1, 1, 1), (1, 7, 3), (2, 128, 128), (3, 129, 255), (1, 257, 1000), (8, 64, 2049),
-                                      (5, 16, 1032), (11, 200, 136), (17, 130, 640), (33, 48, 264), (1, 1040, 4096), (2, 16, 8200)])
+                                      (5, 16, 1032), (11, 200, 136), (17, 130, 640), (33, 48, 264), (1, 1040, 4096), (2, 16, 8200), (4, 300, 16384)])
 def test_matvec(t, qnn, dtype, group, rows, n, k):
     rng = np.random.default_rng(rows * 1000003 + n * 1009 + k + group)
     codes, scales, alpha, dense = ref.random_weights(rng, 1, n, k, group)
@@ -229,6 +229,26 @@ def test_long_weight_gradients(t, qnn, dtype, n, k, counts):
     # in the mean the sums are far better than that bound: kept to nearest, they do not drift towards zero
     assert np.linalg.norm(gw.cpu().double().numpy() - want) <= 1e-6 * np.linalg.norm(want)
     assert t.equal(gw, qnn.expert_gemm_backward_weights(dy, x, offsets)) and qnn.tensor_path_status() == 0
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("n,k,counts", [(256, 4000, [40, 30]), (2050, 256, [40, 30]), (1408, 1920, [300, 0, 200, 17])], ids=str)
+def test_long_contractions_and_many_tiles(t, qnn, dtype, n, k, counts):
+    """Rings that go round many times, blocks that take many tiles, in both directions."""
+    rng = np.random.default_rng(n * 3 + k)
+    codes, scales, alpha, dense = ref.random_weights(rng, len(counts), n, k, 64)
+    w = handle(qnn, t, codes, scales, alpha, n, k, 64)
+    rows = sum(counts)
+    x, x64 = real(t, rng, (rows, k), dtype)
+    dy, dy64 = real(t, rng, (rows, n), dtype)
+    offsets = offsets_of(t, counts)
+    y, dx = qnn.g4_expert_gemm(x, w, offsets), qnn.g4_expert_gemm_backward_data(dy, w, offsets)
+
+    def one(e, a, b):
+        check(y[a:b], x64[a:b] @ dense[e].T, np.abs(x64[a:b]) @ np.abs(dense[e]).T, k, dtype)
+        check(dx[a:b], dy64[a:b] @ dense[e], np.abs(dy64[a:b]) @ np.abs(dense[e]), n, dtype)
+    grouped(counts, 0, one)
+    assert qnn.tensor_path_status() == 0
 
 
 def test_fp32_products_do_not_drift(t, qnn):
