@@ -10,8 +10,9 @@
 //
 // A block takes a stored row of tiles (128 features): one warp streams its tiles of 8 KB through a ring in shared memory by
 // bulk copies, which keeps some 50 KB a block in flight at no cost in registers; eight warps multiply, 16 features each, all
-// with the same columns of x, which lie in shared memory, converted once.  The contraction is split over a cluster of up to
-// eight blocks, whose sums are added in a fixed order through distributed shared memory.
+// with the same columns of x.  Aligned 16-bit rows of x travel with the codes; others are converted into shared memory,
+// once for the block, some tiles at a time.  The contraction is split over a cluster of up to eight blocks, whose sums are
+// added in a fixed order through distributed shared memory.
 // fp32 rows are split exactly into three bf16 parts (8 + 8 + 8 bits) that occupy three of the instruction's columns.
 #include "g4_rows.cuh"
 #include "tc_ptx.cuh"
@@ -67,43 +68,40 @@ __device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t
 }
 
 // Elements [i0, i0 + 128 * tiles) of `have` rows of x as columns in shared memory: tile t, column c at (t * cols + c) *
-// X_PITCH; zeros from element k on.  fp32 rows become PARTS columns each.  `vec`: 16 bytes at a time.
+// X_PITCH; zeros from element k on.  fp32 rows become PARTS columns each.  Element by element (consecutive threads,
+// consecutive elements), many loads in flight.
 template <class T>
-__device__ __noinline__ void stage_columns(const T *x, int64_t ldx, int have, int i0, int tiles, int k, int cols, uint32_t xs, bool vec) {
-    constexpr int PARTS = RowType<T>::PARTS;
+__device__ __noinline__ void stage_columns(const T *x, int64_t ldx, int have, int i0, int tiles, int k, int cols, uint32_t xs) {
+    constexpr int PARTS = RowType<T>::PARTS, BATCH = 16;
     // warps of a row: all eight for one row, one when there are many
     const int log_warps = have == 1 ? 3 : have == 2 ? 2 : have <= 4 ? 1 : 0;
-    const int row0 = threadIdx.x >> (5 + log_warps), rows_at_once = WARPS >> log_warps;
-    const int lane0 = threadIdx.x & ((32 << log_warps) - 1), lanes = 32 << log_warps;
-    if (vec) {
-        if constexpr (PARTS == 1) {
-            const int octets = tiles * 16;
+    const int lanes = 32 << log_warps, lane0 = threadIdx.x & (lanes - 1);
 #pragma unroll 1
-            for (int r = row0; r < have; r += rows_at_once) {
-                const T *src = x + (int64_t)r * ldx + i0;
-#pragma unroll 4
-                for (int o = lane0; o < octets; o += lanes) {
-                    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                    if (i0 + o * 8 < k) v = __ldg(reinterpret_cast<const uint4 *>(src) + o);
-                    sts_128(xs + ((o >> 4) * cols + r) * X_PITCH + (o & 15) * 16, v.x, v.y, v.z, v.w);
+    for (int r = threadIdx.x >> (5 + log_warps); r < have; r += WARPS >> log_warps) {
+        const T *src = x + (int64_t)r * ldx + i0;
+#pragma unroll 1
+        for (int o0 = lane0; o0 < tiles * 128; o0 += BATCH * lanes) {
+            uint32_t v[BATCH];
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j) {
+                const int o = o0 + j * lanes;
+                v[j] = 0u;
+                if (o < tiles * 128 && i0 + o < k) {
+                    if constexpr (PARTS == 1) v[j] = __ldg(reinterpret_cast<const unsigned short *>(src) + o);
+                    else v[j] = __float_as_uint(__ldg(src + o));
                 }
             }
-        }
-    } else {
-#pragma unroll 1
-        for (int r = row0; r < have; r += rows_at_once) {
-            const T *src = x + (int64_t)r * ldx + i0;
-#pragma unroll 4
-            for (int o = lane0; o < tiles * 128; o += lanes) {
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j) {
+                const int o = o0 + j * lanes;
+                if (o >= tiles * 128) break;
                 const uint32_t at = xs + ((o >> 7) * cols + r * PARTS) * X_PITCH + (o & 127) * 2;
                 if constexpr (PARTS == 1) {
-                    const unsigned short v = i0 + o < k ? __ldg(reinterpret_cast<const unsigned short *>(src) + o) : (unsigned short)0;
-                    asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"(v) : "memory");
+                    asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"((unsigned short)v[j]) : "memory");
                 } else {
-                    const float v = i0 + o < k ? __ldg(src + o) : 0.0f;
 #pragma unroll
                     for (int p = 0; p < PARTS; ++p)
-                        asm volatile("st.shared.u16 [%0], %1;" ::"r"(at + p * X_PITCH), "h"((unsigned short)(split_part_bits(v, p) >> 16)) : "memory");
+                        asm volatile("st.shared.u16 [%0], %1;" ::"r"(at + p * X_PITCH), "h"((unsigned short)(split_part_bits(__uint_as_float(v[j]), p) >> 16)) : "memory");
                 }
             }
         }
@@ -116,18 +114,26 @@ __device__ __forceinline__ void cluster_sync() {
 }
 
 // Block (row of stored tiles, rank in the cluster) x block of rows of one expert.  The cluster's ranks share the contraction.
-template <class T, int NT, int GROUP>
+// STREAM: the rows of x start and advance by whole 16 bytes and travel with the codes.
+template <class T, int NT, bool STREAM> struct RowsShape {
+    static constexpr int X_TILE = NT * 8 * X_PITCH;
+    static constexpr int STAGE = C_STAGE + (STREAM ? U * X_TILE : 0);
+    static constexpr int X_TILES = 16 / NT / U * U;                     // tiles of converted x held at a time
+    static constexpr int X_OFF = C_STAGES * STAGE;
+    static constexpr int BAR_OFF = X_OFF + (STREAM ? 0 : X_TILES * X_TILE);
+    static constexpr int TOTAL = BAR_OFF + 2 * C_STAGES * 8 + 16;
+};
+template <class T, int NT, int GROUP, bool STREAM>
 __global__ void __launch_bounds__(THREADS, 2) g4_rows_kernel(const T *__restrict__ x, int64_t ldx, int rows, const int32_t *__restrict__ offsets,
-                                                         int experts, G4Weights w, T *__restrict__ y, int64_t ldy, int log_ranks, bool vec,
+                                                         int experts, G4Weights w, T *__restrict__ y, int64_t ldy, int log_ranks,
                                                          unsigned int *err, unsigned int wait_limit) {
     constexpr int PARTS = RowType<T>::PARTS, COLS = NT * 8, CAP = COLS / PARTS, GROUPS = G4_TILE / GROUP;
-    constexpr int X_TILES = 16 / NT / U * U;                            // tiles of x held at a time
+    using L = RowsShape<T, NT, STREAM>;
     extern __shared__ __align__(128) uint8_t smem[];
-    uint8_t *xbuf = smem + C_STAGES * C_STAGE;
-    uint64_t *full = reinterpret_cast<uint64_t *>(xbuf + X_TILES * COLS * X_PITCH);
+    uint64_t *full = reinterpret_cast<uint64_t *>(smem + L::BAR_OFF);
     uint64_t *empty = full + C_STAGES;
     volatile uint32_t *abort_flag = reinterpret_cast<uint32_t *>(empty + C_STAGES);
-    const uint32_t cs = smem_u32(smem), xs = smem_u32(xbuf);
+    const uint32_t cs = smem_u32(smem), xs = cs + L::X_OFF;
     const int warp = warp_index(), lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     const int ranks = 1 << log_ranks, rank = blockIdx.x & (ranks - 1), jt = blockIdx.x >> log_ranks;
 
@@ -151,16 +157,35 @@ __global__ void __launch_bounds__(THREADS, 2) g4_rows_kernel(const T *__restrict
 #pragma unroll 1
         for (int t = first; t < last; t += U, tile += U, ++it) {
             if (!__all_sync(0xffffffffu, short_wait(&empty[s.s], s.ph ^ 1u, abort_flag, 0, err, wait_limit))) break;
+            const int here = min(U, last - t);
+            uint8_t *stage = smem + s.s * L::STAGE;
+            const int end = min(w.k - t * G4_TILE, here * G4_TILE);         // elements of x in this stage
+            if constexpr (STREAM) {
+                if (end < here * G4_TILE && lane < have) {                  // the contraction ends inside: zeros behind it
+                    const uint32_t row = cs + s.s * L::STAGE + C_STAGE + (here - 1) * L::X_TILE + lane * X_PITCH;
+#pragma unroll 1
+                    for (int o = end - (here - 1) * G4_TILE; o < G4_TILE; o += 8) sts_128(row + o * 2, 0u, 0u, 0u, 0u);
+                }
+                __syncwarp();
+            }
             if (elect_one()) {
-                const int here = min(U, last - t);
-                mbar_expect_tx(&full[s.s], here * (G4_TILE_WORDS * 4 + GROUPS * G4_TILE));
+                mbar_expect_tx(&full[s.s], here * (G4_TILE_WORDS * 4 + GROUPS * G4_TILE) + (STREAM ? have * end * 2 : 0));
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     if (u >= here) break;
-                    uint8_t *dst = smem + s.s * C_STAGE + u * C_TILE;
-                    bulk_load(dst, w.codes + (tile + u) * G4_TILE_WORDS, G4_TILE_WORDS * 4, &full[s.s]);
-                    bulk_load(dst + G4_TILE_WORDS * 4, w.scales + (tile + u) * (GROUPS * G4_TILE), GROUPS * G4_TILE, &full[s.s]);
+                    bulk_load(stage + u * C_TILE, w.codes + (tile + u) * G4_TILE_WORDS, G4_TILE_WORDS * 4, &full[s.s]);
+                    bulk_load(stage + u * C_TILE + G4_TILE_WORDS * 4, w.scales + (tile + u) * (GROUPS * G4_TILE), GROUPS * G4_TILE, &full[s.s]);
                 }
+            }
+            if constexpr (STREAM) {
+                __syncwarp();
+                if (lane < have)
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        if (u >= here) break;
+                        bulk_load(stage + C_STAGE + u * L::X_TILE + lane * X_PITCH, x + (int64_t)(slot.first + lane) * ldx + (t + u) * G4_TILE,
+                                  min(G4_TILE, end - u * G4_TILE) * 2, &full[s.s]);
+                    }
             }
             __syncwarp();
             s.next(C_STAGES);
@@ -171,24 +196,26 @@ __global__ void __launch_bounds__(THREADS, 2) g4_rows_kernel(const T *__restrict
         Ring s;
         bool ok = true;
 #pragma unroll 1
-        for (int t0 = first; ok && t0 < last; t0 += X_TILES) {
-            const int here = min(X_TILES, last - t0);
-            if (t0 > first) multiplying_warps_sync();                   // the columns are still being read
-            stage_columns<T>(x + (int64_t)slot.first * ldx, ldx, have, t0 * G4_TILE, here, w.k, COLS, xs, vec);
-            multiplying_warps_sync();
+        for (int t0 = first; ok && t0 < last; t0 += STREAM ? last : L::X_TILES) {
+            const int here = STREAM ? last - first : min(L::X_TILES, last - t0);
+            if constexpr (!STREAM) {
+                if (t0 > first) multiplying_warps_sync();               // the columns are still being read
+                stage_columns<T>(x + (int64_t)slot.first * ldx, ldx, have, t0 * G4_TILE, here, w.k, COLS, xs);
+                multiplying_warps_sync();
+            }
             const uint32_t at_row = cs + (c * G4_TILE + warp * STRIP + g) * 16;
-            uint32_t at_col = xs + g * X_PITCH + c * 16;
+            uint32_t at_col = (STREAM ? cs + C_STAGE : xs) + g * X_PITCH + c * 16;
 #pragma unroll 1
-            for (int t = 0; t < here; t += U, at_col += U * COLS * X_PITCH) {
+            for (int t = 0; t < here; t += U) {
                 if (!(ok = __all_sync(0xffffffffu, short_wait(&full[s.s], s.ph, abort_flag, 1, err, wait_limit)))) break;
                 uint4 lo[U], hi[U];                                         // unit c of features g and g + 8 of the strip
                 uint8_t blo[U], bhi[U];                                     // their scales of group c
 #pragma unroll
                 for (int u = 0; u < U; ++u) {                               // (behind an odd end: what an earlier stage left, not used)
-                    const uint32_t src = at_row + s.s * C_STAGE + u * C_TILE;
+                    const uint32_t src = at_row + s.s * L::STAGE + u * C_TILE;
                     lo[u] = lds_128(src);
                     hi[u] = lds_128(src + 128);
-                    const uint32_t sc = cs + s.s * C_STAGE + u * C_TILE + G4_TILE_WORDS * 4 + (GROUPS > 1 ? (c & (GROUPS - 1)) * G4_TILE : 0) + warp * STRIP + g;
+                    const uint32_t sc = cs + s.s * L::STAGE + u * C_TILE + G4_TILE_WORDS * 4 + (GROUPS > 1 ? (c & (GROUPS - 1)) * G4_TILE : 0) + warp * STRIP + g;
                     blo[u] = lds_8(sc);
                     bhi[u] = lds_8(sc + 8);
                 }
@@ -209,7 +236,7 @@ __global__ void __launch_bounds__(THREADS, 2) g4_rows_kernel(const T *__restrict
                         const uint32_t h0 = code_pair<T>(wh, 0), h1 = code_pair<T>(wh, 1), h2 = code_pair<T>(wh, 2), h3 = code_pair<T>(wh, 3);
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            const uint4 b = lds_128(at_col + (u * COLS + n * 8) * X_PITCH + ww * 64);
+                            const uint4 b = lds_128(at_col + (STREAM ? s.s * L::STAGE : t * L::X_TILE) + u * L::X_TILE + n * 8 * X_PITCH + ww * 64);
                             mma_16x8x16<T>(sum[n], l0, h0, l1, h1, b.x, b.y);
                             mma_16x8x16<T>(sum[n], l2, h2, l3, h3, b.z, b.w);
                         }
@@ -233,8 +260,8 @@ __global__ void __launch_bounds__(THREADS, 2) g4_rows_kernel(const T *__restrict
                 s.next(C_STAGES);
             }
         }
-        multiplying_warps_sync();                                       // the columns of x make room for the sums
-        float *sums = reinterpret_cast<float *>(xbuf);                  // [128 features][COLS + 1]
+        multiplying_warps_sync();                                       // all tiles have been used: room for the sums
+        float *sums = reinterpret_cast<float *>(smem);                  // [128 features][COLS + 1]
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             float *at = sums + (warp * STRIP + g) * (COLS + 1) + n * 8 + 2 * c;
@@ -253,7 +280,7 @@ __global__ void __launch_bounds__(THREADS, 2) g4_rows_kernel(const T *__restrict
     for (int v = threadIdx.x; v < have << log_feats; v += THREADS) {
         const int f = (rank << log_feats) + (v & ((1 << log_feats) - 1)), r = v >> log_feats, j = jt * G4_TILE + f;
         if (j >= w.n) continue;
-        const uint32_t at = xs + (f * (COLS + 1) + r * PARTS) * 4;
+        const uint32_t at = cs + (f * (COLS + 1) + r * PARTS) * 4;
         float one[8][PARTS], total = 0.0f;
 #pragma unroll
         for (int q = 0; q < 8; ++q) {                                   // all loads first: each takes a round trip
@@ -275,25 +302,24 @@ __global__ void __launch_bounds__(THREADS, 2) g4_rows_kernel(const T *__restrict
     if (log_ranks) cluster_sync();                                      // nobody leaves while its sums are read
 }
 
-template <class T, int NT, int GROUP>
+template <class T, int NT, int GROUP, bool STREAM>
 int launch(const T *x, int64_t ldx, int rows, const int32_t *offsets, int experts, const G4Weights &w, T *y, int64_t ldy, cudaStream_t st) {
-    constexpr int CAP = NT * 8 / RowType<T>::PARTS;
-    constexpr int SMEM = C_STAGES * C_STAGE + 16 / NT / U * U * NT * 8 * X_PITCH + 2 * C_STAGES * 8 + 16;
-    auto kernel = g4_rows_kernel<T, NT, GROUP>;
+    constexpr int CAP = NT * 8 / RowType<T>::PARTS, SMEM = RowsShape<T, NT, STREAM>::TOTAL;
+    auto kernel = g4_rows_kernel<T, NT, GROUP, STREAM>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess) return QNN_E_CUDA;
     const int64_t slots = offsets ? expert_slots_most(rows, experts, CAP) : (rows + CAP - 1) / CAP;
     if (slots > 65535) return QNN_E_RANGE;
-    // Ranks of a cluster: what ends first when two blocks fit an SM, a block costs three tiles' time besides its tiles
+    // Ranks of a cluster: what ends first when two blocks fit an SM and a block costs three tiles' time besides its own, one
+    // more for each doubling of the cluster (3 x 4097 x 1000 fp32: 5.6 us with four ranks, 7.6 with eight, 7.2 with one)
     int log_ranks = 0;
     int64_t best = INT64_MAX;
     for (int l = 0; l < 4 && (1 << l) <= w.tiles_k; ++l) {
         const int64_t blocks = slots * w.tiles_n << l, rounds = (blocks + 2 * 148 - 1) / (2 * 148);
-        const int64_t cost = rounds * ((w.tiles_k + (1 << l) - 1) / (1 << l) + 3);
+        const int64_t cost = rounds * ((w.tiles_k + (1 << l) - 1) / (1 << l) + 3 + l);
         if (cost < best) { best = cost; log_ranks = l; }
     }
     unsigned int *err = qnn_tc_error_word();
     if (!err) return QNN_E_CUDA;
-    const bool vec = sizeof(T) == 2 && qnn_aligned(x, 16) && ldx % 8 == 0 && w.k % 8 == 0;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(w.tiles_n << log_ranks), (unsigned)slots);
     cfg.blockDim = dim3(THREADS);
@@ -305,18 +331,24 @@ int launch(const T *x, int64_t ldx, int rows, const int32_t *offsets, int expert
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = log_ranks ? 1 : 0;
-    if (cudaLaunchKernelEx(&cfg, kernel, x, ldx, rows, offsets, experts, w, y, ldy, log_ranks, vec, err, WAIT_LIMIT) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, kernel, x, ldx, rows, offsets, experts, w, y, ldy, log_ranks, err, WAIT_LIMIT) != cudaSuccess) {
         cudaGetLastError();
         return QNN_E_CUDA;
     }
     return QNN_OK;
 }
 
-template <class T, int NT>
+template <class T, int NT, bool STREAM>
 int by_group(const T *x, int64_t ldx, int rows, const int32_t *offsets, int experts, const G4Weights &w, T *y, int64_t ldy, cudaStream_t st) {
-    if (w.group == 32) return launch<T, NT, 32>(x, ldx, rows, offsets, experts, w, y, ldy, st);
-    if (w.group == 64) return launch<T, NT, 64>(x, ldx, rows, offsets, experts, w, y, ldy, st);
-    return launch<T, NT, 128>(x, ldx, rows, offsets, experts, w, y, ldy, st);
+    if (w.group == 32) return launch<T, NT, 32, STREAM>(x, ldx, rows, offsets, experts, w, y, ldy, st);
+    if (w.group == 64) return launch<T, NT, 64, STREAM>(x, ldx, rows, offsets, experts, w, y, ldy, st);
+    return launch<T, NT, 128, STREAM>(x, ldx, rows, offsets, experts, w, y, ldy, st);
+}
+template <class T, int NT>
+int by_rows(const T *x, int64_t ldx, int rows, const int32_t *offsets, int experts, const G4Weights &w, T *y, int64_t ldy, cudaStream_t st) {
+    if constexpr (sizeof(T) == 2)
+        if (qnn_aligned(x, 16) && ldx % 8 == 0 && w.k % 8 == 0) return by_group<T, NT, true>(x, ldx, rows, offsets, experts, w, y, ldy, st);
+    return by_group<T, NT, false>(x, ldx, rows, offsets, experts, w, y, ldy, st);
 }
 
 // Columns per block: the fewest instructions' worth that hold the rows, at most 4 (32 columns).
@@ -326,10 +358,10 @@ int by_columns(const void *xv, int64_t ldx, int rows, const int32_t *offsets, in
     const T *x = static_cast<const T *>(xv);
     T *y = static_cast<T *>(yv);
     const int cols = rows_together * RowType<T>::PARTS;
-    if (cols <= 8) return by_group<T, 1>(x, ldx, rows, offsets, experts, w, y, ldy, st);
-    if (cols <= 16) return by_group<T, 2>(x, ldx, rows, offsets, experts, w, y, ldy, st);
-    if (cols <= 24) return by_group<T, 3>(x, ldx, rows, offsets, experts, w, y, ldy, st);
-    return by_group<T, 4>(x, ldx, rows, offsets, experts, w, y, ldy, st);
+    if (cols <= 8) return by_rows<T, 1>(x, ldx, rows, offsets, experts, w, y, ldy, st);
+    if (cols <= 16) return by_rows<T, 2>(x, ldx, rows, offsets, experts, w, y, ldy, st);
+    if (cols <= 24) return by_rows<T, 3>(x, ldx, rows, offsets, experts, w, y, ldy, st);
+    return by_rows<T, 4>(x, ldx, rows, offsets, experts, w, y, ldy, st);
 }
 
 }  // namespace
