@@ -22,7 +22,10 @@ namespace {
 constexpr int WARPS = 8;                                  // that multiply; one more copies
 constexpr int STRIP = 16;                                 // features of one matrix instruction
 constexpr int THREADS = (WARPS + 1) * 32;
-constexpr int C_TILE = G4_TILE_WORDS * 4 + 512;           // codes and up to four rows of scales
+constexpr int UNIT = 128 * 16;                            // a quarter of a tile's codes: 16 bytes of each row
+constexpr int UNIT_PITCH = UNIT + 32;                     // (the four lanes of a quad read the same row of the four units)
+constexpr int SCALES_AT = 4 * UNIT_PITCH;
+constexpr int C_TILE = SCALES_AT + 512;                   // codes and up to four rows of scales
 constexpr int U = 2;                                      // tiles of a stage: one wait, and their reads overlap
 constexpr int C_STAGE = U * C_TILE;
 constexpr int C_STAGES = 3;
@@ -60,10 +63,10 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t word, int p) {
 template <class T>
 __device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     if constexpr (std::is_same<T, __half>::value)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
     else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
@@ -122,9 +125,10 @@ template <class T, int NT, bool STREAM> struct RowsShape {
     static constexpr int X_OFF = C_STAGES * STAGE;
     static constexpr int BAR_OFF = X_OFF + (STREAM ? 0 : X_TILES * X_TILE);
     static constexpr int TOTAL = BAR_OFF + 2 * C_STAGES * 8 + 16;
+    static constexpr int BLOCKS = STREAM && NT == 1 ? 3 : 2;            // that fit an SM
 };
 template <class T, int NT, int GROUP, bool STREAM>
-__global__ void __launch_bounds__(THREADS, 2) g4_rows_kernel(const T *__restrict__ x, int64_t ldx, int rows, const int32_t *__restrict__ offsets,
+__global__ void __launch_bounds__(THREADS, RowsShape<T, NT, STREAM>::BLOCKS) g4_rows_kernel(const T *__restrict__ x, int64_t ldx, int rows, const int32_t *__restrict__ offsets,
                                                          int experts, G4Weights w, T *__restrict__ y, int64_t ldy, int log_ranks,
                                                          unsigned int *err, unsigned int wait_limit) {
     constexpr int PARTS = RowType<T>::PARTS, COLS = NT * 8, CAP = COLS / PARTS, GROUPS = G4_TILE / GROUP;
@@ -173,8 +177,10 @@ __global__ void __launch_bounds__(THREADS, 2) g4_rows_kernel(const T *__restrict
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     if (u >= here) break;
-                    bulk_load(stage + u * C_TILE, w.codes + (tile + u) * G4_TILE_WORDS, G4_TILE_WORDS * 4, &full[s.s]);
-                    bulk_load(stage + u * C_TILE + G4_TILE_WORDS * 4, w.scales + (tile + u) * (GROUPS * G4_TILE), GROUPS * G4_TILE, &full[s.s]);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        bulk_load(stage + u * C_TILE + q * UNIT_PITCH, w.codes + (tile + u) * G4_TILE_WORDS + q * (UNIT / 4), UNIT, &full[s.s]);
+                    bulk_load(stage + u * C_TILE + SCALES_AT, w.scales + (tile + u) * (GROUPS * G4_TILE), GROUPS * G4_TILE, &full[s.s]);
                 }
             }
             if constexpr (STREAM) {
@@ -203,8 +209,8 @@ __global__ void __launch_bounds__(THREADS, 2) g4_rows_kernel(const T *__restrict
                 stage_columns<T>(x + (int64_t)slot.first * ldx, ldx, have, t0 * G4_TILE, here, w.k, COLS, xs);
                 multiplying_warps_sync();
             }
-            const uint32_t at_row = cs + (c * G4_TILE + warp * STRIP + g) * 16;
-            uint32_t at_col = (STREAM ? cs + C_STAGE : xs) + g * X_PITCH + c * 16;
+            const uint32_t at_row = cs + c * UNIT_PITCH + (warp * STRIP + g) * 16;
+            const uint32_t at_col = (STREAM ? C_STAGE : L::X_OFF) + g * X_PITCH + c * 16;
 #pragma unroll 1
             for (int t = 0; t < here; t += U) {
                 if (!(ok = __all_sync(0xffffffffu, short_wait(&full[s.s], s.ph, abort_flag, 1, err, wait_limit)))) break;
@@ -215,7 +221,7 @@ __global__ void __launch_bounds__(THREADS, 2) g4_rows_kernel(const T *__restrict
                     const uint32_t src = at_row + s.s * L::STAGE + u * C_TILE;
                     lo[u] = lds_128(src);
                     hi[u] = lds_128(src + 128);
-                    const uint32_t sc = cs + s.s * L::STAGE + u * C_TILE + G4_TILE_WORDS * 4 + (GROUPS > 1 ? (c & (GROUPS - 1)) * G4_TILE : 0) + warp * STRIP + g;
+                    const uint32_t sc = cs + s.s * L::STAGE + u * C_TILE + SCALES_AT + (GROUPS > 1 ? (c & (GROUPS - 1)) * G4_TILE : 0) + warp * STRIP + g;
                     blo[u] = lds_8(sc);
                     bhi[u] = lds_8(sc + 8);
                 }
@@ -223,12 +229,14 @@ __global__ void __launch_bounds__(THREADS, 2) g4_rows_kernel(const T *__restrict
                 for (int u = 0; u < U; ++u) {
                     if (t + u >= here) break;
                     const float slo = __fmul_rn(g4_scale_f32(blo[u]), CodeScale<T>::UNDO), shi = __fmul_rn(g4_scale_f32(bhi[u]), CodeScale<T>::UNDO);
-                    float sum[NT][4];
+                    float sum[NT][2][4];                                    // two chains: an instruction takes long to answer
 #pragma unroll
                     for (int ww = 0; ww < 4; ++ww) {
                         if ((ww * 32) % GROUP == 0) {
 #pragma unroll
-                            for (int n = 0; n < NT; ++n) sum[n][0] = sum[n][1] = sum[n][2] = sum[n][3] = 0.0f;
+                            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) sum[n][i >> 2][i & 3] = 0.0f;
                         }
                         const uint32_t wl = ww == 0 ? lo[u].x : ww == 1 ? lo[u].y : ww == 2 ? lo[u].z : lo[u].w;
                         const uint32_t wh = ww == 0 ? hi[u].x : ww == 1 ? hi[u].y : ww == 2 ? hi[u].z : hi[u].w;
@@ -236,9 +244,9 @@ __global__ void __launch_bounds__(THREADS, 2) g4_rows_kernel(const T *__restrict
                         const uint32_t h0 = code_pair<T>(wh, 0), h1 = code_pair<T>(wh, 1), h2 = code_pair<T>(wh, 2), h3 = code_pair<T>(wh, 3);
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            const uint4 b = lds_128(at_col + (STREAM ? s.s * L::STAGE : t * L::X_TILE) + u * L::X_TILE + n * 8 * X_PITCH + ww * 64);
-                            mma_16x8x16<T>(sum[n], l0, h0, l1, h1, b.x, b.y);
-                            mma_16x8x16<T>(sum[n], l2, h2, l3, h3, b.z, b.w);
+                            const uint4 b = *reinterpret_cast<const uint4 *>(smem + at_col + (STREAM ? s.s * L::STAGE : t * L::X_TILE) + u * L::X_TILE + n * 8 * X_PITCH + ww * 64);
+                            mma_16x8x16<T>(sum[n][0], l0, h0, l1, h1, b.x, b.y);
+                            mma_16x8x16<T>(sum[n][1], l2, h2, l3, h3, b.z, b.w);
                         }
                         if ((ww * 32 + 32) % GROUP == 0) {
                             const int grp = ww * 32 / GROUP;                // quad lane `grp` holds that group's scales
@@ -246,10 +254,10 @@ __global__ void __launch_bounds__(THREADS, 2) g4_rows_kernel(const T *__restrict
                             const float s1 = GROUPS == 1 ? shi : __shfl_sync(0xffffffffu, shi, grp, 4);
 #pragma unroll
                             for (int n = 0; n < NT; ++n) {
-                                acc[n][0] = __fmaf_rn(s0, sum[n][0], acc[n][0]);
-                                acc[n][1] = __fmaf_rn(s0, sum[n][1], acc[n][1]);
-                                acc[n][2] = __fmaf_rn(s1, sum[n][2], acc[n][2]);
-                                acc[n][3] = __fmaf_rn(s1, sum[n][3], acc[n][3]);
+                                acc[n][0] = __fmaf_rn(s0, __fadd_rn(sum[n][0][0], sum[n][1][0]), acc[n][0]);
+                                acc[n][1] = __fmaf_rn(s0, __fadd_rn(sum[n][0][1], sum[n][1][1]), acc[n][1]);
+                                acc[n][2] = __fmaf_rn(s1, __fadd_rn(sum[n][0][2], sum[n][1][2]), acc[n][2]);
+                                acc[n][3] = __fmaf_rn(s1, __fadd_rn(sum[n][0][3], sum[n][1][3]), acc[n][3]);
                             }
                         }
                     }
@@ -309,12 +317,13 @@ int launch(const T *x, int64_t ldx, int rows, const int32_t *offsets, int expert
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess) return QNN_E_CUDA;
     const int64_t slots = offsets ? expert_slots_most(rows, experts, CAP) : (rows + CAP - 1) / CAP;
     if (slots > 65535) return QNN_E_RANGE;
-    // Ranks of a cluster: what ends first when two blocks fit an SM and a block costs three tiles' time besides its own, one
+    // Ranks of a cluster: what ends first when a block costs three tiles' time besides its own, one
     // more for each doubling of the cluster (3 x 4097 x 1000 fp32: 5.6 us with four ranks, 7.6 with eight, 7.2 with one)
     int log_ranks = 0;
     int64_t best = INT64_MAX;
     for (int l = 0; l < 4 && (1 << l) <= w.tiles_k; ++l) {
-        const int64_t blocks = slots * w.tiles_n << l, rounds = (blocks + 2 * 148 - 1) / (2 * 148);
+        const int64_t blocks = slots * w.tiles_n << l, at_once = RowsShape<T, NT, STREAM>::BLOCKS * 148;
+        const int64_t rounds = (blocks + at_once - 1) / at_once;
         const int64_t cost = rounds * ((w.tiles_k + (1 << l) - 1) / (1 << l) + 3 + l);
         if (cost < best) { best = cost; log_ranks = l; }
     }
