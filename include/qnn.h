@@ -310,12 +310,15 @@ int qnn_g4_pack_weights(const void *w, int type, int experts, int n, int k, int6
                         uint8_t *scales, float *alpha, void *stream);
 
 /*
- * Few rows times one matrix: y[r][j] = sum_i x[r][i] * W[j][i].  The single-token form of a layer: it reads the codes
- * once and is meant for up to about 32 rows; more rows give the right result but belong to qnn_g4_expert_gemm.
+ * Rows times one matrix: y[r][j] = sum_i x[r][i] * W[j][i].  The single-token form of a layer, fastest for a handful of rows
+ * (it then reads the codes once and needs no workspace); any number is right.
  *   x  [rows][ldx] (ldx >= k), y [rows][ldy] (ldy >= n), both of `type`; rows = 0 is allowed and does nothing.
+ *   workspace  as for the grouped products below, qnn_g4_matvec_workspace(...) bytes.
  */
+size_t qnn_g4_matvec_workspace(const void *x, int type, int64_t rows, int64_t ldx, int n, int k);
 int qnn_g4_matvec(const void *x, int type, int64_t rows, int64_t ldx, const uint32_t *codes, const uint8_t *scales,
-                  const float *alpha, int n, int k, int group, void *y, int64_t ldy, void *stream);
+                  const float *alpha, int n, int k, int group, void *y, int64_t ldy, void *workspace, size_t workspace_bytes,
+                  void *stream);
 
 /*
  * Products grouped by expert.  Rows are sorted by expert: expert e owns rows offsets[e] .. offsets[e + 1] - 1
@@ -330,8 +333,9 @@ int qnn_g4_matvec(const void *x, int type, int64_t rows, int64_t ldx, const uint
  * rows = 0 is allowed (backward_weights then writes zeros).  rows < 2^31 / 256.
  *   workspace  device scratch owned by the caller, 256-byte aligned, of at least qnn_g4_expert_*_workspace(...) bytes
  *              (which may be 0; workspace may then be NULL).  It holds real operands that the tensor cores cannot read
- *              where they lie: the three parts of fp32 rows, and rows whose address or stride is not a multiple of 16
- *              bytes.  The query looks at the addresses for their alignment only.
+ *              where they lie (the three parts of fp32 rows, and rows whose address or stride is not a multiple of 16
+ *              bytes), and the parts of sums that were split to fill the GPU; those are added in a fixed order, so
+ *              results repeat bit for bit.  The query looks at the addresses for their alignment only.
  * Waits inside the kernels are bounded and reported by qnn_tensor_path_status.
  */
 size_t qnn_g4_expert_gemm_workspace(const void *x, int type, int64_t rows, int64_t ldx, int experts, int n, int k);

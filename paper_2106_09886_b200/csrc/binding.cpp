@@ -115,7 +115,7 @@ at::Tensor workspace_for(PyObject *workspace, size_t need, const at::Tensor &lik
 
 PyObject *answer(int status, at::Tensor &&result) { return status == QNN_OK ? THPVariable_Wrap(std::move(result)) : PyLong_FromLong(status); }
 
-// g4_matvec(x, codes, scales, alpha, n, k, group, out)
+// g4_matvec(x, codes, scales, alpha, n, k, group, out, workspace)
 PyObject *g4_matvec(PyObject *const *a) {
     const at::Tensor &x = tensor_of(a[0], "x must be a tensor");
     const Weights w = weights_of(a + 1);
@@ -124,8 +124,10 @@ PyObject *g4_matvec(PyObject *const *a) {
     void *stream = stream_for(x, {&w.codes, &w.scales, &w.alpha});
     int64_t ldo;
     at::Tensor out = result_for(a[7], x, r.rows, w.n, &ldo);
+    const at::Tensor ws = workspace_for(a[8], qnn_g4_matvec_workspace(x.data_ptr(), r.type, r.rows, r.ld, (int)w.n, (int)w.k), x);
     const int status = qnn_g4_matvec(x.data_ptr(), r.type, r.rows, r.ld, (const uint32_t *)w.codes.data_ptr(), (const uint8_t *)w.scales.data_ptr(),
-                                     (const float *)w.alpha.data_ptr(), (int)w.n, (int)w.k, (int)w.group, out.data_ptr(), ldo, stream);
+                                     (const float *)w.alpha.data_ptr(), (int)w.n, (int)w.k, (int)w.group, out.data_ptr(), ldo,
+                                     ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? ws.nbytes() : 0, stream);
     return answer(status, std::move(out));
 }
 
@@ -194,7 +196,7 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t count) {
 }
 
 PyMethodDef methods[] = {
-    {"g4_matvec", (PyCFunction)(void (*)(void))entry<g4_matvec, 8>, METH_FASTCALL, nullptr},
+    {"g4_matvec", (PyCFunction)(void (*)(void))entry<g4_matvec, 9>, METH_FASTCALL, nullptr},
     {"g4_expert_gemm", (PyCFunction)(void (*)(void))entry<g4_expert<false>, 10>, METH_FASTCALL, nullptr},
     {"g4_expert_gemm_backward_data", (PyCFunction)(void (*)(void))entry<g4_expert<true>, 10>, METH_FASTCALL, nullptr},
     {"expert_gemm_backward_weights", (PyCFunction)(void (*)(void))entry<expert_weights, 5>, METH_FASTCALL, nullptr},

@@ -24,24 +24,89 @@ int check_workspace(const void *ws, size_t have, size_t need) {
     return qnn_aligned(ws, 256) ? QNN_OK : QNN_E_ALIGN;
 }
 
+// Few rows for each expert: the form that needs no full tile (g4_rows.cu).
+bool few_rows(int type, int64_t rows, int experts) { return rows <= (type == QNN_F32 ? 2 : 4) * (int64_t)experts; }
+// And for one matrix.  16 x 16384 x 8192 in fp16: 35 us there, NN us as a split product; 3 x 4097 x 1000 in fp32: 6 and NN us.
+bool few_rows_one(int type, int64_t rows) { return rows <= (type == QNN_F32 ? 4 : 8); }
+
+size_t product_workspace(bool data, const void *x, int type, int64_t rows, int64_t ldx, int experts, int width, int features) {
+    const G4Plan plan = g4_tensor_plan(data, type == QNN_F32, rows, experts, features, g4_tiles(width));
+    return (g4_rows_in_place(x, type, ldx) ? 0 : g4_staged_bytes(type, rows, width)) + g4_sums_bytes(plan, rows, features);
+}
+
+int product(bool data, const void *x, int type, int64_t rows, int64_t ldx, const int32_t *offsets, int experts, const G4Weights &w, void *out,
+            int64_t ldo, void *workspace, cudaStream_t st) {
+    const int width = data ? w.n : w.k;
+    uint8_t *ws = static_cast<uint8_t *>(workspace);
+    G4TensorArgs a{w, offsets, experts, (int)rows, out, ldo, nullptr};
+    if (!g4_rows_in_place(x, type, ldx)) {
+        const int rc = qnn_stage_rows(x, type, ldx, (int)rows, width, ws, st);
+        if (rc != QNN_OK) return rc;
+        x = ws;
+        ldx = g4_padded_width(width);
+        ws += g4_staged_bytes(type, rows, width);
+    }
+    a.sums = ws;
+    return data ? qnn_g4_tensor_data(x, type, ldx, a, st) : qnn_g4_tensor_fwd(x, type, ldx, a, st);
+}
+
 }  // namespace
 
+G4Plan g4_tensor_plan(bool data, bool fp32, int64_t rows, int experts, int features, int steps) {
+    struct Tile {
+        int tokens, blocks, cycles_fwd, cycles_data;
+    };
+    static const Tile narrow[] = {{32, 1, 560, 760}, {64, 1, 620, 980}, {128, 2, 820, 1020}, {256, 2, 1050, 1280}};
+    static const Tile split3[] = {{32, 1, 900, 1100}, {64, 1, 1500, 1700}};
+    G4Plan best = {64, 1, steps};
+    int64_t least = INT64_MAX;
+    for (int i = 0; i < (fp32 ? 2 : 4); ++i) {
+        const Tile &t = fp32 ? split3[i] : narrow[i];
+        // blocks of rows: experts with rows get half to one and a half times the mean
+        const int64_t active = rows < experts ? rows : experts;
+        int64_t slots = 0;
+        if (experts == 1) slots = (rows + t.tokens - 1) / t.tokens;
+        else
+            for (int u = 0; u < 8; ++u) {
+                const int64_t r = rows * (9 + 2 * u) / (16 * active);
+                slots += active * ((r > 0 ? r : 1) + t.tokens - 1) / t.tokens;
+            }
+        if (experts > 1) slots = (slots + 7) / 8;
+        const int64_t tiles = slots * ((g4_tiles(features) + t.blocks - 1) / t.blocks), units = 148 / t.blocks;
+        for (int parts = 1; parts <= 8; ++parts) {
+            const int each = (steps + parts - 1) / parts;
+            if (parts > 1 && (each < 2 || (steps + each - 1) / each != parts)) continue;
+            const int64_t rounds = (tiles * parts + units - 1) / units;
+            const int64_t cost = rounds * ((int64_t)each * (data ? t.cycles_data : t.cycles_fwd) + 3000) +
+                                 (parts > 1 ? 4000 + (int64_t)parts * rows * features / 400 : 0);
+            if (cost < least) { least = cost; best = {t.tokens, parts, each}; }
+        }
+    }
+    return best;
+}
+
+extern "C" size_t qnn_g4_matvec_workspace(const void *x, int type, int64_t rows, int64_t ldx, int n, int k) {
+    if (!g4_type_ok(type) || !g4_dims_ok(1, n, k) || rows <= 0 || rows >= G4_MAX_ROWS || few_rows_one(type, rows)) return 0;
+    return product_workspace(false, x, type, rows, ldx, 1, k, n);
+}
+
 extern "C" int qnn_g4_matvec(const void *x, int type, int64_t rows, int64_t ldx, const uint32_t *codes, const uint8_t *scales,
-                             const float *alpha, int n, int k, int group, void *y, int64_t ldy, void *stream) {
+                             const float *alpha, int n, int k, int group, void *y, int64_t ldy, void *workspace,
+                             size_t workspace_bytes, void *stream) {
     int rc = check_weights(1, codes, scales, alpha, n, k, group);
     if (rc == QNN_OK) rc = check_rows(x, type, rows, ldx, k);
     if (rc == QNN_OK) rc = check_rows(y, type, rows, ldy, n);
+    if (rc == QNN_OK) rc = check_workspace(workspace, workspace_bytes, qnn_g4_matvec_workspace(x, type, rows, ldx, n, k));
     if (rc != QNN_OK || rows == 0) return rc;
     const G4Weights w{codes, scales, alpha, n, k, group, g4_tiles(n), g4_tiles(k)};
-    return qnn_g4_rows(x, type, ldx, (int)rows, nullptr, 1, w, y, ldy, rows < 32 ? (int)rows : 32, static_cast<cudaStream_t>(stream));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (few_rows_one(type, rows)) return qnn_g4_rows(x, type, ldx, (int)rows, nullptr, 1, w, y, ldy, (int)rows, st);
+    return product(false, x, type, rows, ldx, nullptr, 1, w, y, ldy, workspace, st);
 }
 
-// Few rows for each expert: the form that reads the codes once for a handful of rows and splits the contraction.
-static bool g4_few_rows(int64_t rows, int experts) { return rows <= 8 * (int64_t)experts; }
-
 extern "C" size_t qnn_g4_expert_gemm_workspace(const void *x, int type, int64_t rows, int64_t ldx, int experts, int n, int k) {
-    if (!g4_type_ok(type) || !g4_dims_ok(experts, n, k) || rows <= 0 || rows >= G4_MAX_ROWS) return 0;
-    return g4_few_rows(rows, experts) || g4_rows_in_place(x, type, ldx) ? 0 : g4_staged_bytes(type, rows, k);
+    if (!g4_type_ok(type) || !g4_dims_ok(experts, n, k) || rows <= 0 || rows >= G4_MAX_ROWS || few_rows(type, rows, experts)) return 0;
+    return product_workspace(false, x, type, rows, ldx, experts, k, n);
 }
 
 extern "C" int qnn_g4_expert_gemm(const void *x, int type, int64_t rows, int64_t ldx, const int32_t *offsets, int experts,
@@ -56,17 +121,15 @@ extern "C" int qnn_g4_expert_gemm(const void *x, int type, int64_t rows, int64_t
     if (rc != QNN_OK || rows == 0) return rc;
     const G4Weights w{codes, scales, alpha, n, k, group, g4_tiles(n), g4_tiles(k)};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (g4_few_rows(rows, experts)) return qnn_g4_rows(x, type, ldx, (int)rows, offsets, experts, w, y, ldy, 8, st);
-    const G4TensorArgs a{w, offsets, experts, (int)rows, y, ldy};
-    if (g4_rows_in_place(x, type, ldx)) return qnn_g4_tensor_fwd(x, type, ldx, a, st);
-    rc = qnn_stage_rows(x, type, ldx, (int)rows, k, workspace, st);
-    return rc != QNN_OK ? rc : qnn_g4_tensor_fwd(workspace, type, g4_padded_width(k), a, st);
+    if (few_rows(type, rows, experts))
+        return qnn_g4_rows(x, type, ldx, (int)rows, offsets, experts, w, y, ldy, type == QNN_F32 ? 2 : 8, st);
+    return product(false, x, type, rows, ldx, offsets, experts, w, y, ldy, workspace, st);
 }
 
 extern "C" size_t qnn_g4_expert_backward_data_workspace(const void *dy, int type, int64_t rows, int64_t lddy, int experts, int n,
                                                         int k) {
     if (!g4_type_ok(type) || !g4_dims_ok(experts, n, k) || rows <= 0 || rows >= G4_MAX_ROWS) return 0;
-    return g4_rows_in_place(dy, type, lddy) ? 0 : g4_staged_bytes(type, rows, n);
+    return product_workspace(true, dy, type, rows, lddy, experts, n, k);
 }
 
 extern "C" int qnn_g4_expert_backward_data(const void *dy, int type, int64_t rows, int64_t lddy, const int32_t *offsets,
@@ -82,11 +145,7 @@ extern "C" int qnn_g4_expert_backward_data(const void *dy, int type, int64_t row
         rc = check_workspace(workspace, workspace_bytes, qnn_g4_expert_backward_data_workspace(dy, type, rows, lddy, experts, n, k));
     if (rc != QNN_OK || rows == 0) return rc;
     const G4Weights w{codes, scales, alpha, n, k, group, g4_tiles(n), g4_tiles(k)};
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const G4TensorArgs a{w, offsets, experts, (int)rows, dx, lddx};
-    if (g4_rows_in_place(dy, type, lddy)) return qnn_g4_tensor_data(dy, type, lddy, a, st);
-    rc = qnn_stage_rows(dy, type, lddy, (int)rows, n, workspace, st);
-    return rc != QNN_OK ? rc : qnn_g4_tensor_data(workspace, type, g4_padded_width(n), a, st);
+    return product(true, dy, type, rows, lddy, offsets, experts, w, dx, lddx, workspace, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" size_t qnn_expert_backward_weights_workspace(const void *dy, const void *x, int type, int64_t rows, int64_t lddy,

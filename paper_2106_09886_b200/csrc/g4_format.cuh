@@ -36,8 +36,14 @@ __device__ __forceinline__ float g4_scale_f32(uint8_t b) {
     return (float)v;
 }
 
-// Rows [first, last) of expert e; empty where offsets decrease, clamped to the rows that exist.
+// Rows [first, last) of expert e; empty where offsets decrease, clamped to the rows that exist.  offsets NULL = one matrix
+// that owns every row.
 __device__ __forceinline__ void expert_rows(const int32_t *offsets, int e, int rows, int &first, int &last) {
+    if (!offsets) {
+        first = 0;
+        last = rows;
+        return;
+    }
     first = min(max(__ldg(offsets + e), 0), rows);
     last = min(max(__ldg(offsets + e + 1), 0), rows);
 }

@@ -189,6 +189,23 @@ __device__ __noinline__ int64_t count_slots(const int32_t *offsets, int experts,
     return total;
 }
 
+// Work item t: a part of the contraction of a tile of features x a block of rows.
+struct G4Item {
+    int slot, f, part, lo, steps;
+};
+__device__ __noinline__ G4Item g4_item(int t, int parts, int ftiles, int steps, int steps_each) {
+    const int tile = t / parts, part = t - tile * parts, slot = tile / ftiles;
+    return {slot, tile - slot * ftiles, part, part * steps_each, min(steps_each, steps - part * steps_each)};
+}
+// Steps of the items first, first + stride, ...
+__device__ __noinline__ int64_t g4_stages(int64_t items, int first, int stride, int parts, int steps, int steps_each) {
+    int64_t total = 0;
+    if (parts == 1) return items > first ? (items - first + stride - 1) / stride * steps : 0;
+#pragma unroll 1
+    for (int64_t t = first; t < items; t += stride) total += min(steps_each, steps - (int)(t % parts) * steps_each);
+    return total;
+}
+
 struct G4TensorParams {
     G4Weights w;
     const int32_t *offsets;
@@ -198,6 +215,10 @@ struct G4TensorParams {
     int features;                         // width of the result
     int ftiles;                           // tiles of 128 * CG features
     int steps;                            // stored tiles along the contraction
+    // With few tiles the contraction is split: `parts` items of steps_each (the last one maybe fewer) steps per tile, whose
+    // fp32 results go to sums [part][rows][features], to be added in order by g4_sum_parts_kernel.
+    int parts, steps_each;
+    float *sums;
     bool out_vec;                         // the result's rows start and advance by whole 16 bytes
     unsigned int *err;
     unsigned int wait_limit;
@@ -403,9 +424,10 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
     auto warp_wait = [&](uint64_t *bar, uint32_t parity, unsigned id) {
         return __all_sync(0xffffffffu, short_wait(bar, parity, abort_flag, id, p.err, p.wait_limit));
     };
-    auto stages_of_this_block = [&]() -> int64_t {
-        const int64_t tiles = count_slots(p.offsets, p.experts, p.rows, TN) * p.ftiles;
-        return tiles > first_work ? (tiles - first_work + work_stride - 1) / work_stride * p.steps : 0;
+    auto item = [&](int t) { return g4_item(t, p.parts, p.ftiles, p.steps, p.steps_each); };
+    auto stages_of_this_block = [&]() {
+        const int64_t items = count_slots(p.offsets, p.experts, p.rows, TN) * p.ftiles * p.parts;
+        return g4_stages(items, first_work, work_stride, p.parts, p.steps, p.steps_each);
     };
     auto stop = [&]() { return __any_sync(0xffffffffu, *abort_flag != 0); };       // the same answer for a whole warp
 
@@ -417,13 +439,13 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
         const uint64_t a_desc = smem_desc_mn_sw128(smem_at + PARTS * L::X_PART, 128 * 128);
         bool ok = true;
         uint32_t ph = 0;
-        int kt = 0;
+        int kt = 0, t = first_work, steps = item(t).steps;
 #pragma unroll 1
         for (; ok && left > 0; ph ^= 1u) {
 #pragma unroll
             for (int g = 0; g < L::STAGES; ++g) {
                 if (left-- <= 0) break;
-                const bool fresh = PROMOTE || kt == 0, done = PROMOTE || kt == p.steps - 1;
+                const bool fresh = PROMOTE || kt == 0, done = PROMOTE || kt == steps - 1;
                 if (fresh && !(ok = agree(short_wait(&acc_empty[acc.s], acc.ph ^ 1u, abort_flag, 3, p.err, p.wait_limit)))) break;
                 if (!(ok = agree(short_wait(&full[g], ph, abort_flag, 1, p.err, p.wait_limit)))) break;
                 tc_fence_after();
@@ -443,7 +465,11 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
                     if (done) pair_commit<CG>(&acc_full[acc.s]);
                 });
                 if (done) acc.next(L::ACC_BUFS);
-                kt = kt == p.steps - 1 ? 0 : kt + 1;
+                if (++kt == steps) {
+                    kt = 0;
+                    t += work_stride;
+                    steps = item(t).steps;
+                }
             }
         }
     };
@@ -454,12 +480,13 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
         long long it = 0;
 #pragma unroll 1
         for (int t = first_work; !stop(); t += work_stride) {
-            const ExpertSlot slot = cur.seek(t / p.ftiles);
+            const G4Item work = item(t);
+            const ExpertSlot slot = cur.seek(work.slot);
             if (slot.expert < 0) break;
-            const int row = slot.first + rank * L::XROWS;
+            const int row = slot.first + rank * L::XROWS, lo = work.lo, hi = lo + work.steps;
             bool ok = true;
 #pragma unroll 1
-            for (int kt = 0; kt < p.steps; ++kt) {
+            for (int kt = lo; kt < hi; ++kt) {
                 if (!(ok = warp_wait(&empty[g.s], g.ph ^ 1u, 0))) break;
                 if (elect_one()) {
                     if (rank == 0) mbar_expect_tx(&full[g.s], CG * PARTS * L::X_PART);
@@ -488,14 +515,15 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
         const int64_t stride = MODE == G4_FWD ? 1 : p.w.tiles_k;            // stored tiles between steps of the contraction
 #pragma unroll 1
         for (int t = first_work; !stop(); t += work_stride) {
-            const ExpertSlot slot = cur.seek(t / p.ftiles);
+            const G4Item work = item(t);
+            const ExpertSlot slot = cur.seek(work.slot);
             if (slot.expert < 0) break;
             // a block whose features lie past the end repeats the last tile; its results are not stored
-            const int f = min((t % p.ftiles) * CG + rank, (MODE == G4_FWD ? p.w.tiles_n : p.w.tiles_k) - 1);
-            int64_t tile = (int64_t)slot.expert * p.w.tiles_n * p.w.tiles_k + (MODE == G4_FWD ? (int64_t)f * p.w.tiles_k : f);
+            const int f = min(work.f * CG + rank, (MODE == G4_FWD ? p.w.tiles_n : p.w.tiles_k) - 1);
+            int64_t tile = (int64_t)slot.expert * p.w.tiles_n * p.w.tiles_k + (MODE == G4_FWD ? (int64_t)f * p.w.tiles_k : f) + work.lo * stride;
             bool ok = true;
 #pragma unroll 1
-            for (int kt = 0; kt < p.steps; ++kt, tile += stride) {
+            for (int kt = 0; kt < work.steps; ++kt, tile += stride) {
                 if (!(ok = warp_wait(&c_empty[c.s], c.ph ^ 1u, 0))) break;
                 if (elect_one()) {
                     mbar_expect_tx(&c_full[c.s], G4_TILE_WORDS * 4 + groups * G4_TILE);
@@ -593,20 +621,22 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
         Ring acc;
 #pragma unroll 1
         for (int t = first_work; !stop(); t += work_stride) {
-            const ExpertSlot slot = cur.seek(t / p.ftiles);
+            const G4Item work = item(t);
+            const ExpertSlot slot = cur.seek(work.slot);
             if (slot.expert < 0) break;
-            const int f = ((t % p.ftiles) * CG + rank) * 128 + q * 32;
+            const int f = (work.f * CG + rank) * 128 + q * 32;
             const float alpha = __ldg(p.w.alpha + slot.expert);
             T *dst = static_cast<T *>(p.out) + (int64_t)slot.first * p.ldo;
             const int have = slot.last - slot.first;
             const uint32_t lanes = (uint32_t)(q * 32) << 16;
+            float *sums = p.sums + ((int64_t)work.part * p.rows + slot.first) * p.features + f + lane;      // (only with parts)
             bool ok = true;
             if constexpr (PROMOTE) {
                 float sum[TN];
 #pragma unroll
                 for (int i = 0; i < TN; ++i) sum[i] = 0.0f;
-#pragma unroll 1
-                for (int kt = 0; kt < p.steps; ++kt) {
+                #pragma unroll 1
+                for (int kt = 0; kt < work.steps; ++kt) {
                     if (!(ok = warp_wait(&acc_full[acc.s], acc.ph, 2))) break;
                     tc_fence_after();
 #pragma unroll
@@ -624,15 +654,33 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
                 if (ok && f + lane < p.features)
 #pragma unroll
                     for (int i = 0; i < TN; ++i)
-                        if (i < have) real_store(dst + (int64_t)i * p.ldo + f + lane, __fmul_rn(__fmul_rn(sum[i], undo), alpha));
+                        if (i < have) {
+                            const float v = __fmul_rn(__fmul_rn(sum[i], undo), alpha);
+                            if (p.parts == 1) real_store(dst + (int64_t)i * p.ldo + f + lane, v);
+                            else sums[(int64_t)i * p.features] = v;
+                        }
             } else {
                 if ((ok = warp_wait(&acc_full[acc.s], acc.ph, 2))) {
                     tc_fence_after();
                     const uint32_t buf = smem_at + L::OUT_OFF + q * L::OUT_WARP;
+                    if (p.parts > 1) {
+#pragma unroll 1
+                        for (int c0 = 0; c0 < have; c0 += 16) {
+                            uint32_t v[16];
+                            tmem_load_lane_16(tmem_base + lanes + (uint32_t)(acc.s * TN + c0), v);
+                            if (f + lane < p.features) {
+#pragma unroll
+                                for (int i = 0; i < 16; ++i)
+                                    if (c0 + i < have) sums[(int64_t)(c0 + i) * p.features] = __fmul_rn(__fmul_rn(__uint_as_float(v[i]), undo), alpha);
+                            }
+                            __syncwarp();
+                        }
+                    } else {
 #pragma unroll 1
                     for (int c0 = 0; c0 < have; c0 += 32)
                         store_quarter<T>(tmem_base + lanes + (uint32_t)(acc.s * TN + c0), buf, dst + (int64_t)c0 * p.ldo, p.ldo, have - c0, f,
                                          p.features, undo, alpha, p.out_vec);
+                    }
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) arrive_leader<CG>(&acc_empty[acc.s]);
@@ -666,6 +714,28 @@ inline bool make_map_16(CUtensorMap *map, bool fp16, const void *base, int64_t r
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// out[r][f] = sum over the parts, in order, of the rows that belong to an expert.
+template <class T>
+__global__ void __launch_bounds__(256) g4_sum_parts_kernel(const float *__restrict__ sums, int parts, int rows, int features,
+                                                          const int32_t *__restrict__ offsets, int experts, T *out, int64_t ldo) {
+    int first = 0, last = rows;
+    if (offsets) {
+        first = min(max(__ldg(offsets), 0), rows);
+        last = min(max(__ldg(offsets + experts), 0), rows);
+    }
+    const int f = blockIdx.x * 256 + threadIdx.x;
+    if (f >= features) return;
+    for (int r = first + blockIdx.y; r < last; r += gridDim.y) {
+        const float *src = sums + (int64_t)r * features + f;
+        float v[8], total = 0.0f;
+#pragma unroll
+        for (int p = 0; p < 8; ++p) v[p] = p < parts ? __ldcs(src + (int64_t)p * rows * features) : 0.0f;
+#pragma unroll
+        for (int p = 0; p < 8; ++p) total = __fadd_rn(total, v[p]);
+        real_store(out + (int64_t)r * ldo + f, total);
+    }
+}
+
 // x: operand rows of G4Type<T>::Op, [PARTS * rows][ldx], 16-byte aligned rows, `width` columns.
 template <int CG, int TN, int MODE, class T>
 int g4_tensor_launch(const void *x, int64_t ldx, int width, G4TensorParams p, int sms, cudaStream_t st) {
@@ -675,7 +745,7 @@ int g4_tensor_launch(const void *x, int64_t ldx, int width, G4TensorParams p, in
     CUtensorMap map;
     if (!make_map_16(&map, std::is_same<T, __half>::value, x, (int64_t)p.rows * G4Type<T>::PARTS, width, ldx, L::XROWS)) return QNN_E_CUDA;
     p.ftiles = (g4_tiles(p.features) + CG - 1) / CG;
-    const int64_t work = expert_slots_most(p.rows, p.experts, TN) * p.ftiles;
+    const int64_t work = expert_slots_most(p.rows, p.experts, TN) * p.ftiles * p.parts;
     if (work > 0x3FFFFFFFll) return QNN_E_RANGE;
     const int most = sms / CG;
     cudaLaunchConfig_t cfg = {};
@@ -692,6 +762,11 @@ int g4_tensor_launch(const void *x, int64_t ldx, int width, G4TensorParams p, in
     if (cudaLaunchKernelEx(&cfg, kernel, map, p) != cudaSuccess) {
         cudaGetLastError();
         return QNN_E_CUDA;
+    }
+    if (p.parts > 1) {
+        const dim3 grid((unsigned)((p.features + 255) / 256), (unsigned)(p.rows < 1024 ? p.rows : 1024));
+        g4_sum_parts_kernel<T><<<grid, 256, 0, st>>>(p.sums, p.parts, p.rows, p.features, p.offsets, p.experts, static_cast<T *>(p.out), p.ldo);
+        return qnn_launch_status();
     }
     return QNN_OK;
 }

@@ -17,15 +17,16 @@ int g4_tensor_pick(const void *x, int64_t ldx, const G4TensorArgs &a, cudaStream
     const int sms = sm_count();
     if (sms <= 0) return QNN_E_CUDA;
     const int width = MODE == G4_FWD ? a.w.k : a.w.n;
-    const int64_t each = (a.rows + a.experts - 1) / a.experts;              // rows an expert has on average
-    if constexpr (G4Type<T>::PARTS > 1) {
-        if (each <= 48) return g4_tensor_launch<1, 32, MODE, T>(x, ldx, width, p, sms, st);
-        return g4_tensor_launch<1, 64, MODE, T>(x, ldx, width, p, sms, st);
-    } else {
-        if (each <= 32) return g4_tensor_launch<1, 32, MODE, T>(x, ldx, width, p, sms, st);
-        if (each <= 96) return g4_tensor_launch<1, 64, MODE, T>(x, ldx, width, p, sms, st);
-        return g4_tensor_launch<2, 256, MODE, T>(x, ldx, width, p, sms, st);
+    const G4Plan plan = g4_tensor_plan(MODE == G4_DATA, sizeof(T) == 4, a.rows, a.experts, p.features, p.steps);
+    p.steps_each = plan.steps_each;
+    p.parts = plan.parts;
+    p.sums = static_cast<float *>(a.sums);
+    if (plan.tokens == 32) return g4_tensor_launch<1, 32, MODE, T>(x, ldx, width, p, sms, st);
+    if constexpr (G4Type<T>::PARTS == 1) {
+        if (plan.tokens == 128) return g4_tensor_launch<2, 128, MODE, T>(x, ldx, width, p, sms, st);
+        if (plan.tokens == 256) return g4_tensor_launch<2, 256, MODE, T>(x, ldx, width, p, sms, st);
     }
+    return g4_tensor_launch<1, 64, MODE, T>(x, ldx, width, p, sms, st);
 }
 
 template <int MODE>

@@ -27,7 +27,7 @@ EXPORTS = [
     "qnn_mbit_encoder_backward", "qnn_bgemm_backward_data_workspace", "qnn_bgemm_backward_data",
     "qnn_bgemm_backward_weights_workspace", "qnn_bgemm_backward_weights", "qnn_bconv2d_backward_data_workspace",
     "qnn_bconv2d_backward_data", "qnn_bconv2d_backward_weights_workspace", "qnn_bconv2d_backward_weights", "qnn_unpack_codes_f32",
-    "qnn_g4_codes_bytes", "qnn_g4_scales_bytes", "qnn_g4_pack_weights", "qnn_g4_matvec", "qnn_g4_expert_gemm_workspace",
+    "qnn_g4_codes_bytes", "qnn_g4_scales_bytes", "qnn_g4_pack_weights", "qnn_g4_matvec_workspace", "qnn_g4_matvec", "qnn_g4_expert_gemm_workspace",
     "qnn_g4_expert_gemm", "qnn_g4_expert_backward_data_workspace", "qnn_g4_expert_backward_data",
     "qnn_expert_backward_weights_workspace", "qnn_expert_backward_weights",
     "qnn_tensor_path_status", "qnn_last_device_status", "qnn_selftest_bounded_wait", "qnn_bgemm_int8_tensor_workspace", "qnn_bgemm_int8_tensor",
@@ -88,7 +88,9 @@ def _load() -> C.CDLL:
     lib.qnn_g4_scales_bytes.restype = sz
     lib.qnn_g4_scales_bytes.argtypes = [i] * 4
     lib.qnn_g4_pack_weights.argtypes = [p, i, i, i, i, i64, i, p, p, p, p]
-    lib.qnn_g4_matvec.argtypes = [p, i, i64, i64, p, p, p, i, i, i, p, i64, p]
+    lib.qnn_g4_matvec_workspace.restype = sz
+    lib.qnn_g4_matvec_workspace.argtypes = [p, i, i64, i64, i, i]
+    lib.qnn_g4_matvec.argtypes = [p, i, i64, i64, p, p, p, i, i, i, p, i64, p, sz, p]
     lib.qnn_g4_expert_gemm_workspace.restype = sz
     lib.qnn_g4_expert_gemm_workspace.argtypes = [p, i, i64, i64, i, i, i]
     lib.qnn_g4_expert_gemm.argtypes = [p, i, i64, i64, p, i, p, p, p, i, i, i, p, i64, p, sz, p]
@@ -408,11 +410,12 @@ def g4_pack_weights(w: torch.Tensor, group: int = 128, stream=None) -> G4Weights
     return G4Weights(codes, scales, alpha, n, k, group)
 
 
-def g4_matvec(x: torch.Tensor, w: G4Weights, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
-    """x [rows, k] (few rows; their stride is free) times one 4-bit matrix -> [rows, n] of x's type."""
+def g4_matvec(x: torch.Tensor, w: G4Weights, out: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+              stream=None) -> torch.Tensor:
+    """x [rows, k] (meant for few rows; their stride is free) times one 4-bit matrix -> [rows, n] of x's type."""
     if stream is None:
-        return _result(_binding.g4_matvec(x, *w, out), "qnn_g4_matvec")
-    return _result(_on_stream(stream, lambda: _binding.g4_matvec(x, *w, out)), "qnn_g4_matvec")
+        return _result(_binding.g4_matvec(x, *w, out, workspace), "qnn_g4_matvec")
+    return _result(_on_stream(stream, lambda: _binding.g4_matvec(x, *w, out, workspace)), "qnn_g4_matvec")
 
 
 def g4_expert_gemm(x: torch.Tensor, w: G4Weights, offsets: torch.Tensor, out: torch.Tensor | None = None,

@@ -67,10 +67,10 @@ def test_pack_refusals(qnn, p):
 def test_matvec_refusals(qnn, p):
     f = qnn.lib.qnn_g4_matvec
     mis = ctypes.c_void_p(p.value + 4)
-    ok = (p, 1, 2, 64, p, p, p, 8, 64, 32, p, 8, None)
+    ok = (p, 1, 2, 64, p, p, p, 8, 64, 32, p, 8, None, 0, None)
 
     def call(**kw):
-        names = ("x", "type", "rows", "ldx", "codes", "scales", "alpha", "n", "k", "group", "y", "ldy", "stream")
+        names = ("x", "type", "rows", "ldx", "codes", "scales", "alpha", "n", "k", "group", "y", "ldy", "ws", "ws_bytes", "stream")
         return f(*[kw.get(name, v) for name, v in zip(names, ok)])
 
     for bad in ({"x": None}, {"y": None}, {"codes": None}, {"scales": None}, {"alpha": None}, {"type": 7}, {"rows": -1},
@@ -81,6 +81,9 @@ def test_matvec_refusals(qnn, p):
     assert call(rows=1 << 31) == qnn.E_RANGE
     assert call(rows=0) == qnn.OK and call(rows=0, x=None, y=None) == qnn.OK       # nothing to do, nothing launched
     assert call(rows=0, group=48) == qnn.E_ARG
+    need = qnn.lib.qnn_g4_matvec_workspace(p, 0, 200, 64, 8, 64)
+    assert need > 0 and call(type=0, rows=200) == qnn.E_ARG and call(type=0, rows=200, ws=p, ws_bytes=need - 1) == qnn.E_ARG
+    assert call(type=0, rows=200, ws=mis, ws_bytes=need) == qnn.E_ALIGN
 
 
 @pytest.mark.parametrize("name", ["qnn_g4_expert_gemm", "qnn_g4_expert_backward_data"])
