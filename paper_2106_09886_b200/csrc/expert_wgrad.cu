@@ -303,8 +303,9 @@ __global__ void __launch_bounds__(256) wgrad_sum_kernel(const float *__restrict_
     }
 }
 
-// The tile: pairs of blocks on 256 x 256 unless that leaves most of the GPU idle (sized for 148 SMs, so that workspace
-// queries and calls agree).  Parts of the rows: as many as fill the GPU once, each of at least 256 rows on average.
+// The tile: pairs of blocks on 256 x 256, or single blocks on 128 x 128 where those need fewer rounds of the GPU (a round of
+// wide tiles takes about a quarter longer; sized for 148 SMs, so that workspace queries and calls agree).  Parts of the
+// rows: as many as fill the GPU once, each of at least 256 rows on average.
 struct WPlan {
     bool wide;
     int parts;
@@ -313,7 +314,7 @@ WPlan wgrad_plan(int64_t rows, int experts, int n, int k) {
     const int64_t wide = (int64_t)experts * ((k + 255) / 256) * ((n + 255) / 256);
     const int64_t narrow = (int64_t)experts * ((k + 127) / 128) * ((n + 127) / 128);
     WPlan w;
-    w.wide = wide >= 74;
+    w.wide = (wide + 73) / 74 * 5 <= (narrow + 147) / 148 * 4;
     const int64_t units = w.wide ? 74 : 148, tiles = w.wide ? wide : narrow, each = rows / experts;
     int64_t parts = units / tiles;
     if (parts > each / 256) parts = each / 256;

@@ -26,7 +26,7 @@ int check_workspace(const void *ws, size_t have, size_t need) {
 
 // Few rows for each expert: the form that needs no full tile (g4_rows.cu).
 bool few_rows(int type, int64_t rows, int experts) { return rows <= (type == QNN_F32 ? 2 : 4) * (int64_t)experts; }
-// And for one matrix.  16 x 16384 x 8192 in fp16: 35 us there, NN us as a split product; 3 x 4097 x 1000 in fp32: 6 and NN us.
+// And for one matrix.  16 x 16384 x 8192 in fp16: 35 us there, 23.5 us as a split product.
 bool few_rows_one(int type, int64_t rows) { return rows <= (type == QNN_F32 ? 4 : 8); }
 
 size_t product_workspace(bool data, const void *x, int type, int64_t rows, int64_t ldx, int experts, int width, int features) {
@@ -172,16 +172,13 @@ extern "C" int qnn_expert_backward_weights(const void *dy, const void *x, int ty
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     float *parts = reinterpret_cast<float *>(ws);
     ws += qnn_expert_wgrad_parts_bytes(rows, experts, n, k);
-    if (!g4_rows_in_place(dy, type, lddy)) {
-        if ((rc = qnn_stage_rows(dy, type, lddy, (int)rows, n, ws, st)) != QNN_OK) return rc;
-        dy = ws;
-        lddy = g4_padded_width(n);
-        ws += g4_staged_bytes(type, rows, n);
-    }
-    if (!g4_rows_in_place(x, type, ldx)) {
-        if ((rc = qnn_stage_rows(x, type, ldx, (int)rows, k, ws, st)) != QNN_OK) return rc;
-        x = ws;
-        ldx = g4_padded_width(k);
-    }
+    const bool stage_dy = !g4_rows_in_place(dy, type, lddy), stage_x = !g4_rows_in_place(x, type, ldx);
+    void *to_dy = ws, *to_x = ws + (stage_dy ? g4_staged_bytes(type, rows, n) : 0);
+    if (stage_dy && stage_x) rc = qnn_stage_rows_two(dy, lddy, n, to_dy, x, ldx, k, to_x, type, (int)rows, st);
+    else if (stage_dy) rc = qnn_stage_rows(dy, type, lddy, (int)rows, n, to_dy, st);
+    else if (stage_x) rc = qnn_stage_rows(x, type, ldx, (int)rows, k, to_x, st);
+    if (rc != QNN_OK) return rc;
+    if (stage_dy) { dy = to_dy; lddy = g4_padded_width(n); }
+    if (stage_x) { x = to_x; ldx = g4_padded_width(k); }
     return qnn_expert_wgrad(x, ldx, dy, lddy, type, offsets, experts, (int)rows, n, k, gw, parts, st);
 }

@@ -15,3 +15,6 @@ static inline size_t g4_staged_bytes(int type, int64_t rows, int width) {
 }
 // dst [parts][rows][padded width].
 int qnn_stage_rows(const void *src, int type, int64_t ld, int rows, int width, void *dst, cudaStream_t st);
+// Two operands with the same rows in one launch.
+int qnn_stage_rows_two(const void *src_a, int64_t ld_a, int width_a, void *dst_a, const void *src_b, int64_t ld_b, int width_b, void *dst_b,
+                       int type, int rows, cudaStream_t st);
