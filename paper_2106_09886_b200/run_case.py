@@ -5,6 +5,7 @@
     python -m paper_2106_09886_b200.run_case encode --rows 4096 --k 4096 --bits 2
     python -m paper_2106_09886_b200.run_case backward_conv --N 32 --H 14 --W 14 --C 256 --Cout 256
     python -m paper_2106_09886_b200.run_case stack  --net vgg16 [--batch 64] [--layers 0,1] [--table]
+    python -m paper_2106_09886_b200.run_case experts --tokens 512 --experts 8 --top 2 --hidden 1024 --inner 2048
 
 Inputs are drawn on the device (half-normal activations, normal weights); this is a timing and
 profiling driver, correctness is the business of the test-suite.  Times are CUDA-event times of
@@ -228,6 +229,77 @@ def time_backward_conv(N, H, W, C, Cout, R, S, stride, pad, ab, wb, reps=5, warm
             "workspace_mb": [wsd.numel() / 1e6, wsw.numel() / 1e6]}
 
 
+class ExpertsLayer:
+    """A feed-forward layer of experts on 4-bit weights: every token goes through `top` of them, out = sum of gate * W2_e
+    silu(W1_e x).  The real weights are kept for training: a step takes the gradient of the decoded weights for theirs
+    (straight-through) and packs them again.  A 4-bit matrix reads the layer's output, as the last layer of a decoder would."""
+
+    def __init__(self, hidden, inner, experts, top, classes, group=128, dtype=torch.bfloat16, seed=0, dev="cuda:0"):
+        g = torch.Generator(device=dev).manual_seed(seed)
+        self.top, self.group, self.dtype = top, group, dtype
+        self.w1 = torch.randn((experts, inner, hidden), device=dev, generator=g) * hidden ** -0.5
+        self.w2 = torch.randn((experts, hidden, inner), device=dev, generator=g) * inner ** -0.5
+        self.router = torch.randn((experts, hidden), device=dev, generator=g) * hidden ** -0.5
+        self.head = qnn.g4_pack_weights(torch.randn((classes, hidden), device=dev, generator=g) * hidden ** -0.5, group)
+        self.pack()
+
+    def pack(self):
+        self.q1, self.q2 = qnn.g4_pack_weights(self.w1, self.group), qnn.g4_pack_weights(self.w2, self.group)
+
+    def plan(self, x):
+        """Rows sorted by expert: (token of each row, its gate, offsets); the split never leaves the device."""
+        gate, expert = torch.softmax(x.float() @ self.router.t(), 1).topk(self.top, 1)
+        flat = expert.reshape(-1)
+        order = torch.sort(flat, stable=True).indices
+        counts = (flat.view(-1, 1) == torch.arange(self.router.shape[0], device=x.device)).sum(0)
+        offsets = torch.zeros(counts.numel() + 1, dtype=torch.int32, device=x.device)
+        offsets[1:] = counts.cumsum(0)
+        return order // self.top, (gate / gate.sum(1, keepdim=True)).reshape(-1)[order].to(x.dtype), offsets
+
+    def forward(self, x):
+        token, gate, offsets = self.plan(x)
+        rows = x[token]
+        h = qnn.g4_expert_gemm(rows, self.q1, offsets)
+        y = qnn.g4_expert_gemm(torch.nn.functional.silu(h), self.q2, offsets)
+        out = torch.zeros_like(x, dtype=torch.float32).index_add_(0, token, (y * gate.view(-1, 1)).float())
+        return out.to(x.dtype), (token, gate, offsets, rows, h)
+
+    def logits(self, x):
+        return qnn.g4_matvec(self.forward(x)[0], self.head)
+
+    def train_step(self, x, target, rate):
+        """One step of gradient descent on 0.5 * mean squared error; the gates are held fixed.  Returns the loss."""
+        out, (token, gate, offsets, rows, h) = self.forward(x)
+        diff = out.float() - target
+        dy = (diff[token] * gate.float().view(-1, 1)).to(x.dtype)
+        a = torch.nn.functional.silu(h)
+        dw2 = qnn.expert_gemm_backward_weights(dy, a, offsets)
+        da = qnn.g4_expert_gemm_backward_data(dy, self.q2, offsets)
+        s = torch.sigmoid(h.float())
+        dh = (da.float() * s * (1 + h.float() * (1 - s))).to(x.dtype)
+        dw1 = qnn.expert_gemm_backward_weights(dh, rows, offsets)
+        dx = qnn.g4_expert_gemm_backward_data(dh, self.q1, offsets)          # what a layer below would be given
+        self.w1 -= rate / x.shape[0] * dw1
+        self.w2 -= rate / x.shape[0] * dw2
+        self.pack()
+        return float(0.5 * diff.square().sum(1).mean()), dx
+
+
+def time_experts(tokens, experts, top, hidden, inner, group=128, dtype="bf16", reps=5, warmup=3, dev="cuda:0"):
+    kind = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}[dtype]
+    layer = ExpertsLayer(hidden, inner, experts, top, 4 * hidden, group, kind, dev=dev)
+    g = torch.Generator(device=dev).manual_seed(1)
+    x = torch.randn((tokens, hidden), device=dev, generator=g).to(kind)
+    target = torch.randn((tokens, hidden), device=dev, generator=g)
+    prompt = statistics.median(_time_calls(lambda i: layer.forward(x), reps, warmup))
+    token = statistics.median(_time_calls(lambda i: layer.logits(x[:1]), reps, warmup))
+    losses = []
+    step = statistics.median(_time_calls(lambda i: losses.append(layer.train_step(x, target, 0.05)[0]), reps, warmup))
+    return {"call": "experts", "tokens": tokens, "experts": experts, "top": top, "hidden": hidden, "inner": inner, "group": group,
+            "dtype": dtype, "forward_ms": prompt, "one_token_ms": token, "train_step_ms": step, "first_loss": losses[0],
+            "last_loss": losses[-1], "status": qnn.tensor_path_status()}
+
+
 def _report(call, Mg, Ng, Kg, ab, wb, times):
     ms = statistics.median(times)
     macs = float(Mg) * Ng * Kg
@@ -267,7 +339,11 @@ def main():
     k.add_argument("--batch", type=int, default=0)
     k.add_argument("--layers", type=str, default="")
     k.add_argument("--table", action="store_true")
-    for s in (g, c, e, k, mb, bw, bc):
+    x = sub.add_parser("experts")
+    for name, default in (("tokens", 512), ("experts", 8), ("top", 2), ("hidden", 1024), ("inner", 2048), ("group", 128)):
+        x.add_argument(f"--{name}", type=int, default=default)
+    x.add_argument("--dtype", choices=["bf16", "fp16", "fp32"], default="bf16")
+    for s in (g, c, e, k, mb, bw, bc, x):
         s.add_argument("--reps", type=int, default=5)
         s.add_argument("--warmup", type=int, default=3)
         s.add_argument("--sets", type=int, default=3)
@@ -280,6 +356,8 @@ def main():
         r = time_backward(a.m, a.n, a.k, a.ab, a.wb, a.reps, a.warmup)
     elif a.case == "backward_conv":
         r = time_backward_conv(a.N, a.H, a.W, a.C, a.Cout, a.R, a.S, a.stride, a.pad, a.ab, a.wb, a.reps, a.warmup)
+    elif a.case == "experts":
+        r = time_experts(a.tokens, a.experts, a.top, a.hidden, a.inner, a.group, a.dtype, a.reps, a.warmup)
     elif a.case == "mbit":
         r = time_mbit(a.n, a.bits, a.reps, a.warmup)
     elif a.case == "stack":

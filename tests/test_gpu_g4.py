@@ -473,3 +473,30 @@ def test_many_experts(t, qnn):
     some = qnn.g4_expert_gemm(x[:3], w, offsets_of(t, np.minimum(counts, [1] + 30 * [0] + [2] + 68 * [0])))
     grouped(counts, 0, lambda e, a, b: check(y[a:b], x64[a:b] @ dense[e].T, np.abs(x64[a:b]) @ np.abs(dense[e]).T, k, "fp16"))
     check(some[1:3], x64[1:3] @ dense[31].T, np.abs(x64[1:3]) @ np.abs(dense[31]).T, k, "fp16")
+
+
+def test_experts_layer_runs_and_learns(t, qnn):
+    """The layer of run_case: forward equals the same layer on decoded weights, training brings the loss down."""
+    from paper_2106_09886_b200.run_case import ExpertsLayer
+    layer = ExpertsLayer(192, 320, 6, 2, 200, group=64, dtype=t.float32, seed=3)
+    g = t.Generator(device=DEV).manual_seed(4)
+    x = t.randn((75, 192), device=DEV, generator=g)
+
+    def dense(q):
+        c, s = q.codes.cpu().numpy(), q.scales.cpu().numpy()
+        return np.stack([ref.decode(c[e], s[e], q.alpha[e].item(), q.n, q.k, q.group) for e in range(c.shape[0])])
+    token, gate, offsets = layer.plan(x)
+    assert sorted(token.tolist()) == sorted(2 * list(range(75))) and offsets[-1].item() == 150
+    w1, w2, x64 = dense(layer.q1), dense(layer.q2), x.cpu().double().numpy()
+    want, bounds = np.zeros((75, 192)), offsets.tolist()
+    for e in range(6):
+        for r in range(bounds[e], bounds[e + 1]):
+            h = w1[e] @ x64[token[r].item()]
+            want[token[r].item()] += gate[r].item() * (w2[e] @ (h / (1 + np.exp(-h))))
+    got = layer.forward(x)[0].cpu().double().numpy()
+    assert np.linalg.norm(got - want) <= 1e-5 * np.linalg.norm(want)
+    logits = layer.logits(x[:1])
+    assert logits.shape == (1, 200) and bool(logits.isfinite().all())
+    target = t.randn((75, 192), device=DEV, generator=g)
+    losses = [layer.train_step(x, target, 0.5)[0] for _ in range(12)]
+    assert losses[-1] < 0.9 * losses[0] and qnn.tensor_path_status() == 0
