@@ -307,7 +307,10 @@ __global__ void __launch_bounds__(THREADS, RowsShape<T, NT, STREAM>::BLOCKS) g4_
         }
         real_store(y + (int64_t)(slot.first + r) * ldy + j, __fmul_rn(total, alpha));
     }
-    if (log_ranks) cluster_sync();                                      // nobody leaves while its sums are read
+    if (log_ranks) {                                                    // nobody leaves while its sums are read; they have
+        asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");      // been, so nothing is waited for but that
+        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    }
 }
 
 template <class T, int NT, int GROUP, bool STREAM>
