@@ -107,6 +107,8 @@ __global__ void __launch_bounds__(W_THREADS, 1) expert_wgrad_kernel(const __grid
     pair_sync<CG>();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+    start_next();
+    wait_for_previous();
     auto warp_wait = [&](uint64_t *bar, uint32_t parity, unsigned id) {
         return __all_sync(0xffffffffu, short_wait(bar, parity, abort_flag, id, p.err, p.wait_limit));
     };
@@ -281,12 +283,9 @@ int wgrad_launch(const void *x, int64_t ldx, const void *dy, int64_t lddy, Wgrad
     cfg.blockDim = dim3(W_THREADS);
     cfg.dynamicSmemBytes = L::TOTAL;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = CG;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = CG > 1 ? 1 : 0;
+    LaunchAttrs attrs(CG);
+    cfg.attrs = attrs.a;
+    cfg.numAttrs = CG > 1 ? 2 : 1;
     if (cudaLaunchKernelEx(&cfg, kernel, map_x, map_dy, p) != cudaSuccess) {
         cudaGetLastError();
         return QNN_E_CUDA;

@@ -141,8 +141,6 @@ __global__ void __launch_bounds__(THREADS, RowsShape<T, NT, STREAM>::BLOCKS) g4_
     const int warp = warp_index(), lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     const int ranks = 1 << log_ranks, rank = blockIdx.x & (ranks - 1), jt = blockIdx.x >> log_ranks;
 
-    const ExpertSlot slot = expert_slot(offsets, experts, rows, CAP, blockIdx.y);
-    if (slot.expert < 0) return;                                        // (for every block of the cluster)
     if (threadIdx.x == 0) {
         for (int s = 0; s < C_STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], WARPS); }
         *abort_flag = 0;
@@ -150,6 +148,10 @@ __global__ void __launch_bounds__(THREADS, RowsShape<T, NT, STREAM>::BLOCKS) g4_
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     __syncthreads();
+    start_next();
+    wait_for_previous();
+    const ExpertSlot slot = expert_slot(offsets, experts, rows, CAP, blockIdx.y);
+    if (slot.expert < 0) return;                                        // (for every block of the cluster)
     const int first = (int)((int64_t)w.tiles_k * rank >> log_ranks), last = (int)((int64_t)w.tiles_k * (rank + 1) >> log_ranks);
     const int have = slot.last - slot.first;
     float acc[NT][4] = {};
@@ -337,12 +339,9 @@ int launch(const T *x, int64_t ldx, int rows, const int32_t *offsets, int expert
     cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = SMEM;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 1u << log_ranks;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = log_ranks ? 1 : 0;
+    LaunchAttrs attrs((1u << log_ranks));
+    cfg.attrs = attrs.a;
+    cfg.numAttrs = (1u << log_ranks) > 1 ? 2 : 1;
     if (cudaLaunchKernelEx(&cfg, kernel, x, ldx, rows, offsets, experts, w, y, ldy, log_ranks, err, WAIT_LIMIT) != cudaSuccess) {
         cudaGetLastError();
         return QNN_E_CUDA;

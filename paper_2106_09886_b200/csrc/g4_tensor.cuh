@@ -420,6 +420,8 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
     pair_sync<CG>();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+    start_next();
+    wait_for_previous();
     // waits of a whole warp: every lane polls (each needs the barrier's acquire), all go on or all give up
     auto warp_wait = [&](uint64_t *bar, uint32_t parity, unsigned id) {
         return __all_sync(0xffffffffu, short_wait(bar, parity, abort_flag, id, p.err, p.wait_limit));
@@ -753,12 +755,9 @@ int g4_tensor_launch(const void *x, int64_t ldx, int width, G4TensorParams p, in
     cfg.blockDim = dim3(L::THREADS);
     cfg.dynamicSmemBytes = L::TOTAL;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = CG;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = CG > 1 ? 1 : 0;
+    LaunchAttrs attrs(CG);
+    cfg.attrs = attrs.a;
+    cfg.numAttrs = CG > 1 ? 2 : 1;
     if (cudaLaunchKernelEx(&cfg, kernel, map, p) != cudaSuccess) {
         cudaGetLastError();
         return QNN_E_CUDA;

@@ -167,6 +167,12 @@ __device__ __forceinline__ void arrive_local(uint64_t *bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 
+// A kernel launched with programmatic stream serialization may start while the kernel before it in the stream still runs:
+// start_next lets the one behind it do the same, wait_for_previous (by every thread, ahead of its first access to memory that
+// any kernel writes) is where the stream's order is kept.
+__device__ __forceinline__ void start_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // ------------------------------------------------------------------------------------------------ host side
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
@@ -192,5 +198,17 @@ int sm_count() {
         return 0;
     return sms;
 }
+
+// Attributes of a launch with clusters of `cluster` blocks along x that may start early.
+struct LaunchAttrs {
+    cudaLaunchAttribute a[2];
+    explicit LaunchAttrs(unsigned cluster) {
+        a[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        a[0].val.programmaticStreamSerializationAllowed = 1;
+        a[1].id = cudaLaunchAttributeClusterDimension;
+        a[1].val.clusterDim.x = cluster;
+        a[1].val.clusterDim.y = a[1].val.clusterDim.z = 1;
+    }
+};
 
 }  // namespace
