@@ -295,6 +295,8 @@ int wgrad_launch(const void *x, int64_t ldx, const void *dy, int64_t lddy, Wgrad
 
 // gw = sum of the parts, in order.
 __global__ void __launch_bounds__(256) wgrad_sum_kernel(const float *__restrict__ part, int parts, int64_t total, float *__restrict__ gw) {
+    start_next();
+    wait_for_previous();
     for (int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x; v < total; v += (int64_t)gridDim.x * 256) {
         float s = part[v];
         for (int q = 1; q < parts; ++q) s = __fadd_rn(s, part[q * total + v]);
@@ -351,6 +353,5 @@ int qnn_expert_wgrad(const void *x, int64_t ldx, const void *dy, int64_t lddy, i
     else rc = wgrad<__half>(x, ldx, dy, lddy, p, plan.wide, st);
     if (rc != QNN_OK || plan.parts == 1) return rc;
     const int64_t blocks = (p.part_stride + 255) / 256;
-    wgrad_sum_kernel<<<(unsigned)(blocks < 148 * 8 ? blocks : 148 * 8), 256, 0, st>>>(parts, plan.parts, p.part_stride, gw);
-    return qnn_launch_status();
+    return launch_early(wgrad_sum_kernel, (unsigned)(blocks < 148 * 8 ? blocks : 148 * 8), 256, st, parts, plan.parts, p.part_stride, gw);
 }

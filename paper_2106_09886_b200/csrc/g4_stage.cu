@@ -2,6 +2,7 @@
 // Streaming; bound: HBM (reads the rows once, writes 2 bytes per element and part).  Needed for fp32 rows, which become
 // three bf16 parts, and for rows that are not aligned.
 #include "g4_stage.cuh"
+#include "tc_ptx.cuh"
 
 namespace {
 
@@ -16,6 +17,8 @@ struct StageJob {
 // A thread rewrites eight columns of a row; z picks one of two operands with the same rows.
 template <class T>
 __global__ void __launch_bounds__(256) stage_rows_kernel(StageJob first, StageJob second, int rows) {
+    start_next();
+    wait_for_previous();
     const StageJob &job = blockIdx.z ? second : first;
     const int o = blockIdx.x * 32 + threadIdx.x, i = o * 8;
     if (o >= job.octets) return;
@@ -56,9 +59,8 @@ StageJob job_of(const void *src, int64_t ld, int width, void *dst) {
 int stage(const StageJob &a, const StageJob &b, int jobs, int type, int rows, cudaStream_t st) {
     const int octets = jobs > 1 && b.octets > a.octets ? b.octets : a.octets, ys = (rows + 7) / 8;
     const dim3 grid((octets + 31) / 32, ys < 32768 ? ys : 32768, jobs), block(32, 8);
-    if (type == QNN_F32) stage_rows_kernel<float><<<grid, block, 0, st>>>(a, b, rows);
-    else stage_rows_kernel<uint16_t><<<grid, block, 0, st>>>(a, b, rows);      // the two 2-byte types are copied as they are
-    return qnn_launch_status();
+    if (type == QNN_F32) return launch_early(stage_rows_kernel<float>, grid, block, st, a, b, rows);
+    return launch_early(stage_rows_kernel<uint16_t>, grid, block, st, a, b, rows);      // the two 2-byte types are copied as they are
 }
 
 }  // namespace

@@ -720,6 +720,8 @@ inline bool make_map_16(CUtensorMap *map, bool fp16, const void *base, int64_t r
 template <class T>
 __global__ void __launch_bounds__(256) g4_sum_parts_kernel(const float *__restrict__ sums, int parts, int rows, int features,
                                                           const int32_t *__restrict__ offsets, int experts, T *out, int64_t ldo) {
+    start_next();
+    wait_for_previous();
     int first = 0, last = rows;
     if (offsets) {
         first = min(max(__ldg(offsets), 0), rows);
@@ -764,8 +766,8 @@ int g4_tensor_launch(const void *x, int64_t ldx, int width, G4TensorParams p, in
     }
     if (p.parts > 1) {
         const dim3 grid((unsigned)((p.features + 255) / 256), (unsigned)(p.rows < 1024 ? p.rows : 1024));
-        g4_sum_parts_kernel<T><<<grid, 256, 0, st>>>(p.sums, p.parts, p.rows, p.features, p.offsets, p.experts, static_cast<T *>(p.out), p.ldo);
-        return qnn_launch_status();
+        return launch_early(g4_sum_parts_kernel<T>, grid, 256, st, p.sums, p.parts, p.rows, p.features, p.offsets, p.experts,
+                            static_cast<T *>(p.out), p.ldo);
     }
     return QNN_OK;
 }

@@ -211,4 +211,19 @@ struct LaunchAttrs {
     }
 };
 
+// A launch without clusters that may start early.
+template <class... P, class... A>
+int launch_early(void (*kernel)(P...), dim3 grid, dim3 block, cudaStream_t st, A... args) {
+    LaunchAttrs attrs(1);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.stream = st;
+    cfg.attrs = attrs.a;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, P(args)...) == cudaSuccess) return QNN_OK;
+    cudaGetLastError();
+    return QNN_E_CUDA;
+}
+
 }  // namespace
