@@ -42,7 +42,7 @@ struct WShape {
     static constexpr int STAGES = 216 * 1024 / STAGE > 8 ? 8 : 216 * 1024 / STAGE;
     static constexpr int BAR_OFF = STAGES * STAGE;
     static constexpr int TOTAL = BAR_OFF + (3 * STAGES + 5) * 8 + 16 + 1024;
-    static_assert(B_COLS % 64 == 0 && 2 * TN <= 512 && TOTAL <= 227 * 1024, "tile");
+    static_assert(B_COLS % 64 == 0 && 2 * TN <= 512 && TOTAL <= 227 * 1024 && TOTAL > 114 * 1024, "tile");   // (one block an SM)
 };
 
 // One tile of one expert: rows [first, last) of its part, first column of x, first feature.

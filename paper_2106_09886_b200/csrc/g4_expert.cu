@@ -69,7 +69,7 @@ G4Plan g4_tensor_plan(bool data, bool fp32, int64_t rows, int experts, int featu
         else
             for (int u = 0; u < 8; ++u) {
                 const int64_t r = rows * (9 + 2 * u) / (16 * active);
-                slots += active * ((r > 0 ? r : 1) + t.tokens - 1) / t.tokens;
+                slots += active * (((r > 0 ? r : 1) + t.tokens - 1) / t.tokens);
             }
         if (experts > 1) slots = (slots + 7) / 8;
         const int64_t tiles = slots * ((g4_tiles(features) + t.blocks - 1) / t.blocks), units = 148 / t.blocks;

@@ -261,7 +261,10 @@ struct G4Shape {
     static constexpr int C_OFF = STAGES * STAGE;
     static constexpr int OUT_OFF = C_OFF + C_STAGES * C_STAGE;
     static constexpr int BAR_OFF = OUT_OFF + 4 * OUT_WARP;
-    static constexpr int TOTAL = BAR_OFF + (2 * (STAGES + C_STAGES) + 5) * 8 + 16 + 1024;
+    static constexpr int USED = BAR_OFF + (2 * (STAGES + C_STAGES) + 5) * 8 + 16 + 1024;
+    // At least half of an SM's shared memory, so that a block of the next kernel, started early, never waits for tensor memory
+    // that this one holds.
+    static constexpr int TOTAL = USED > 115 * 1024 ? USED : 115 * 1024;
     // A group waits for a phase by its parity, so it must know that the phase before has completed.  Copies of codes may land
     // out of order: a stage of codes has to come back to the group that waited for it last.  (Unpacked stages are freed in
     // order, and a group that is G stages on has seen one S + G back freed, which covers the phase before for G <= S.)
