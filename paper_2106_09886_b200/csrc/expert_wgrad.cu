@@ -296,7 +296,7 @@ int wgrad_launch(const void *x, int64_t ldx, const void *dy, int64_t lddy, Wgrad
 }
 
 // gw = sum of the parts, in order.
-__global__ void __launch_bounds__(256) wgrad_sum_kernel(const float *__restrict__ part, int parts, int64_t total, float *__restrict__ gw) {
+__global__ void __launch_bounds__(256) wgrad_sum_kernel(const float *part, int parts, int64_t total, float *gw) {
     start_next();
     wait_for_previous();
     for (int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x; v < total; v += (int64_t)gridDim.x * 256) {

@@ -44,8 +44,8 @@ __device__ __forceinline__ void expert_rows(const int32_t *offsets, int e, int r
         last = rows;
         return;
     }
-    first = min(max(__ldg(offsets + e), 0), rows);
-    last = min(max(__ldg(offsets + e + 1), 0), rows);
+    first = min(max(offsets[e], 0), rows);
+    last = min(max(offsets[e + 1], 0), rows);
 }
 
 // The slot-th block of `tile` rows, blocks counted expert by expert: its expert and rows, or expert -1 past the last.
@@ -91,10 +91,9 @@ static inline int64_t expert_slots_most(int64_t rows, int experts, int tile) {
 }
 
 // Element loads and stores of the real operands.
-template <class T> __device__ __forceinline__ float real_load(const T *p);
-template <> __device__ __forceinline__ float real_load<float>(const float *p) { return __ldg(p); }
-template <> __device__ __forceinline__ float real_load<__nv_bfloat16>(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
-template <> __device__ __forceinline__ float real_load<__half>(const __half *p) { return __half2float(*p); }
+__device__ __forceinline__ float real_load(const float *p) { return *p; }
+__device__ __forceinline__ float real_load(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
+__device__ __forceinline__ float real_load(const __half *p) { return __half2float(*p); }
 __device__ __forceinline__ void real_store(float *p, float v) { *p = v; }
 __device__ __forceinline__ void real_store(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void real_store(__half *p, float v) { *p = __float2half_rn(v); }

@@ -92,8 +92,8 @@ __device__ __noinline__ void stage_columns(const T *x, int64_t ldx, int have, in
                 const int o = o0 + j * lanes;
                 v[j] = 0u;
                 if (o < tiles * 128 && i0 + o < k) {
-                    if constexpr (PARTS == 1) v[j] = __ldg(reinterpret_cast<const unsigned short *>(src) + o);
-                    else v[j] = __float_as_uint(__ldg(src + o));
+                    if constexpr (PARTS == 1) v[j] = reinterpret_cast<const unsigned short *>(src)[o];
+                    else v[j] = __float_as_uint(src[o]);
                 }
             }
 #pragma unroll
@@ -130,8 +130,8 @@ template <class T, int NT, bool STREAM> struct RowsShape {
     static constexpr int BLOCKS = STREAM && NT == 1 ? 3 : 2;            // that fit an SM
 };
 template <class T, int NT, int GROUP, bool STREAM>
-__global__ void __launch_bounds__(THREADS, RowsShape<T, NT, STREAM>::BLOCKS) g4_rows_kernel(const T *__restrict__ x, int64_t ldx, int rows, const int32_t *__restrict__ offsets,
-                                                         int experts, G4Weights w, T *__restrict__ y, int64_t ldy, int log_ranks,
+__global__ void __launch_bounds__(THREADS, RowsShape<T, NT, STREAM>::BLOCKS) g4_rows_kernel(const T *x, int64_t ldx, int rows, const int32_t *offsets,
+                                                         int experts, G4Weights w, T *y, int64_t ldy, int log_ranks,
                                                          unsigned int *err, unsigned int wait_limit) {
     constexpr int PARTS = RowType<T>::PARTS, COLS = NT * 8, CAP = COLS / PARTS, GROUPS = G4_TILE / GROUP;
     using L = RowsShape<T, NT, STREAM>;
@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(THREADS, RowsShape<T, NT, STREAM>::BLOCKS) g4_
     if (log_ranks) cluster_sync();
     else __syncthreads();
     // each rank adds up its share of the features over all ranks, in their order
-    const float alpha = __ldg(w.alpha + slot.expert);
+    const float alpha = w.alpha[slot.expert];
     const int log_feats = 7 - log_ranks;
 #pragma unroll 1
     for (int v = threadIdx.x; v < have << log_feats; v += THREADS) {

@@ -29,16 +29,16 @@ __global__ void __launch_bounds__(256) stage_rows_kernel(StageJob first, StageJo
         if constexpr (sizeof(T) == 2) {
             uint16_t e[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = i + j < job.width ? __ldg(reinterpret_cast<const unsigned short *>(s) + j) : (uint16_t)0;
+            for (int j = 0; j < 8; ++j) e[j] = i + j < job.width ? reinterpret_cast<const unsigned short *>(s)[j] : (uint16_t)0;
             *dst = make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
         } else {
             float f[8];
             if (job.vec && i + 8 <= job.width) {
-                const float4 a = __ldg(reinterpret_cast<const float4 *>(s)), b = __ldg(reinterpret_cast<const float4 *>(s) + 1);
+                const float4 a = reinterpret_cast<const float4 *>(s)[0], b = reinterpret_cast<const float4 *>(s)[1];
                 f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
             } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) f[j] = i + j < job.width ? __ldg(s + j) : 0.0f;
+                for (int j = 0; j < 8; ++j) f[j] = i + j < job.width ? s[j] : 0.0f;
             }
 #pragma unroll
             for (int p = 0; p < 3; ++p) {

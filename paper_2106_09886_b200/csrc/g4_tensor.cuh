@@ -634,7 +634,7 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
             const ExpertSlot slot = cur.seek(work.slot);
             if (slot.expert < 0) break;
             const int f = (work.f * CG + rank) * 128 + q * 32;
-            const float alpha = __ldg(p.w.alpha + slot.expert);
+            const float alpha = p.w.alpha[slot.expert];
             T *dst = static_cast<T *>(p.out) + (int64_t)slot.first * p.ldo;
             const int have = slot.last - slot.first;
             const uint32_t lanes = (uint32_t)(q * 32) << 16;
@@ -725,14 +725,14 @@ inline bool make_map_16(CUtensorMap *map, bool fp16, const void *base, int64_t r
 
 // out[r][f] = sum over the parts, in order, of the rows that belong to an expert.
 template <class T>
-__global__ void __launch_bounds__(256) g4_sum_parts_kernel(const float *__restrict__ sums, int parts, int rows, int features,
-                                                          const int32_t *__restrict__ offsets, int experts, T *out, int64_t ldo) {
+__global__ void __launch_bounds__(256) g4_sum_parts_kernel(const float *sums, int parts, int rows, int features,
+                                                          const int32_t *offsets, int experts, T *out, int64_t ldo) {
     start_next();
     wait_for_previous();
     int first = 0, last = rows;
     if (offsets) {
-        first = min(max(__ldg(offsets), 0), rows);
-        last = min(max(__ldg(offsets + experts), 0), rows);
+        first = min(max(offsets[0], 0), rows);
+        last = min(max(offsets[experts], 0), rows);
     }
     const int f = blockIdx.x * 256 + threadIdx.x;
     if (f >= features) return;

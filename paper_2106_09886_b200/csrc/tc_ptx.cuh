@@ -169,7 +169,9 @@ __device__ __forceinline__ void arrive_local(uint64_t *bar) {
 
 // A kernel launched with programmatic stream serialization may start while the kernel before it in the stream still runs:
 // start_next lets the one behind it do the same, wait_for_previous (by every thread, ahead of its first access to memory that
-// any kernel writes) is where the stream's order is kept.
+// any kernel writes) is where the stream's order is kept.  What an earlier kernel may have written is not read-only for the
+// whole life of such a kernel, so it is read by coherent loads alone: no __ldg and no const __restrict__ parameters, which
+// the compiler may turn into non-coherent loads and move ahead of the wait.
 __device__ __forceinline__ void start_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 

@@ -1,0 +1,48 @@
+"""What the source of the kernels on 4-bit weights has to keep, where no run of them would show that it does not."""
+import re
+from pathlib import Path
+
+CSRC = Path(__file__).resolve().parent.parent / "paper_2106_09886_b200" / "csrc"
+
+
+def code(name):
+    """A source file without its comments."""
+    text = (CSRC / name).read_text()
+    return re.sub(r"//[^\n]*", "", re.sub(r"/\*.*?\*/", "", text, flags=re.S))
+
+
+def with_headers(name, seen=None):
+    """A source file and the files of its own folder that it includes."""
+    seen = set() if seen is None else seen
+    if name not in seen and (CSRC / name).exists():
+        seen.add(name)
+        for other in re.findall(r'#include "([^"]+)"', code(name)):
+            with_headers(other, seen)
+    return seen
+
+
+def early_units():
+    return sorted(p.name for p in CSRC.glob("*.cu") if any("wait_for_previous();" in code(f) for f in with_headers(p.name) if f != "tc_ptx.cuh"))
+
+
+def test_kernels_that_start_early_read_memory_coherently():
+    """A kernel under programmatic stream serialization starts while the kernel ahead of it may still write what it will read.
+    That memory is not read-only for the kernel's whole life, so no load may take the read-only path, neither by __ldg nor by
+    a const __restrict__ parameter from which the compiler may infer it."""
+    units = early_units()
+    assert {"g4_rows.cu", "g4_stage.cu", "g4_tensor_fwd.cu", "g4_tensor_data.cu", "expert_wgrad.cu"} <= set(units)
+    for unit in units:
+        for name in with_headers(unit):
+            for word in ("__ldg", "__restrict__", ".nc"):
+                assert word not in code(name), f"{name} (in {unit}): {word}"
+
+
+def test_every_kernel_that_starts_early_waits():
+    """And each of them waits for the stream's order, all its threads, before its first role begins."""
+    for name in ("g4_rows.cu", "g4_stage.cu", "g4_tensor.cuh", "expert_wgrad.cu"):
+        kernels = re.split(r"__global__", code(name))[1:]
+        assert kernels
+        for body in kernels:
+            assert body.count("wait_for_previous();") == 1, name
+            ahead = body[:body.index("wait_for_previous();")]
+            assert "offsets[" not in ahead and "expert_slot" not in ahead and "SlotCursor" not in ahead and "load(" not in ahead, name
