@@ -62,13 +62,14 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t word, int p) {
     return r;
 }
 
+// Volatile, as is every load of its operands: what a stage's release has to come after may not be moved behind it.
 template <class T>
 __device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     if constexpr (std::is_same<T, __half>::value)
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
     else
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
@@ -247,7 +248,7 @@ __global__ void __launch_bounds__(THREADS, RowsShape<T, NT, STREAM>::BLOCKS) g4_
                         const uint32_t h0 = code_pair<T>(wh, 0), h1 = code_pair<T>(wh, 1), h2 = code_pair<T>(wh, 2), h3 = code_pair<T>(wh, 3);
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            const uint4 b = *reinterpret_cast<const uint4 *>(smem + at_col + (STREAM ? s.s * L::STAGE : t * L::X_TILE) + u * L::X_TILE + n * 8 * X_PITCH + ww * 64);
+                            const uint4 b = lds_128(cs + at_col + (STREAM ? s.s * L::STAGE : t * L::X_TILE) + u * L::X_TILE + n * 8 * X_PITCH + ww * 64);
                             mma_16x8x16<T>(sum[n][0], l0, h0, l1, h1, b.x, b.y);
                             mma_16x8x16<T>(sum[n][1], l2, h2, l3, h3, b.z, b.w);
                         }
@@ -265,7 +266,8 @@ __global__ void __launch_bounds__(THREADS, RowsShape<T, NT, STREAM>::BLOCKS) g4_
                         }
                     }
                 }
-                // only now: an arrival does not wait for loads whose values nobody has used yet
+                // only now: an arrival does not wait for loads whose values nobody has used yet (the instructions that use them
+                // are volatile, so they stay ahead of it)
                 __syncwarp();
                 if (lane == 0) arrive_local(&empty[s.s]);
                 s.next(C_STAGES);

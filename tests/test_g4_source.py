@@ -46,3 +46,16 @@ def test_every_kernel_that_starts_early_waits():
             assert body.count("wait_for_previous();") == 1, name
             ahead = body[:body.index("wait_for_previous();")]
             assert "offsets[" not in ahead and "expert_slot" not in ahead and "SlotCursor" not in ahead and "load(" not in ahead, name
+
+
+def test_few_row_ring_is_released_behind_its_last_use():
+    """An arrival on a stage's barrier does not wait for shared-memory loads in flight, so it must come after the instructions
+    that use their values.  The compiler keeps that order only among volatile statements: the matrix instruction and every load
+    of its operands are, and the arrival follows them."""
+    text = code("g4_rows.cu")
+    mma = re.search(r"void mma_16x8x16\(.*?\n\}", text, flags=re.S).group(0)
+    assert mma.count("mma.sync") == 2 and len(re.findall(r"\basm\s+volatile\s*\(\s*\"mma\.sync", mma)) == 2
+    kernel = text[text.index("g4_rows_kernel("):]
+    assert "reinterpret_cast<const uint4 *>(smem" not in kernel
+    assert kernel.index("lds_128(") < kernel.index("mma_16x8x16<T>(") < kernel.index("arrive_local(&empty")
+    assert re.search(r"asm volatile\(\"ld\.shared\.v4", code("tc_ptx.cuh"))
