@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(THREADS, RowsShape<T, NT, STREAM>::BLOCKS) g4_
         Ring s;
         bool ok = true;
 #pragma unroll 1
-        for (int t0 = first; ok && t0 < last; t0 += STREAM ? last : L::X_TILES) {
+        for (int t0 = first; t0 < last; t0 += STREAM ? last : L::X_TILES) {      // (a warp that gave up still comes to the barriers)
             const int here = STREAM ? last - first : min(L::X_TILES, last - t0);
             if constexpr (!STREAM) {
                 if (t0 > first) multiplying_warps_sync();               // the columns are still being read
@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(THREADS, RowsShape<T, NT, STREAM>::BLOCKS) g4_
             const uint32_t at_row = cs + c * UNIT_PITCH + (warp * STRIP + g) * 16;
             const uint32_t at_col = (STREAM ? C_STAGE : L::X_OFF) + g * X_PITCH + c * 16;
 #pragma unroll 1
-            for (int t = 0; t < here; t += U) {
+            for (int t = 0; ok && t < here; t += U) {
                 if (!(ok = __all_sync(0xffffffffu, short_wait(&full[s.s], s.ph, abort_flag, 1, err, wait_limit)))) break;
                 uint4 lo[U], hi[U];                                         // unit c of features g and g + 8 of the strip
                 uint8_t blo[U], bhi[U];                                     // their scales of group c

@@ -59,3 +59,17 @@ def test_few_row_ring_is_released_behind_its_last_use():
     assert "reinterpret_cast<const uint4 *>(smem" not in kernel
     assert kernel.index("lds_128(") < kernel.index("mma_16x8x16<T>(") < kernel.index("arrive_local(&empty")
     assert re.search(r"asm volatile\(\"ld\.shared\.v4", code("tc_ptx.cuh"))
+
+
+def test_few_rows_barriers_are_reached_by_warps_that_gave_up():
+    """The multiplying warps meet at barriers around each set of converted columns.  A warp whose bounded wait ran out must still
+    come to every one of them, or the others would wait there without a limit: the loop that holds the barriers goes by the
+    sizes alone, only the one inside it stops early."""
+    text = code("g4_rows.cu")
+    outer = re.search(r"for \(int t0 = first;([^;]*);", text)
+    assert outer and outer.group(1).strip() == "t0 < last"
+    body = text[outer.end():text.index("float *sums", outer.end())]
+    inner = body.index("for (int t = 0; ok && t < here;")
+    ahead, behind = body[:inner], body[body.index("s.next(C_STAGES);", inner):]
+    assert ahead.count("multiplying_warps_sync();") == 2 and behind.count("multiplying_warps_sync();") == 1
+    assert "break" not in ahead and "break" not in behind and "return" not in body
