@@ -40,7 +40,7 @@ def both_ways(t, step, outputs):
         step(i, lambda: None)
     t.cuda.synchronize()
     for i, (a, b) in enumerate(zip(outputs, want)):
-        assert bool(b.isfinite().all()) and t.equal(a, b), f"output {i}"
+        assert t.equal(a, b), f"output {i}"                      # (a NaN is not equal to itself: everything has been written)
 
 
 @pytest.mark.parametrize("dtype", ref.TYPES)
