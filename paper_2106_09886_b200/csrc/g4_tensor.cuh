@@ -219,6 +219,9 @@ struct G4TensorParams {
     int features;                         // width of the result
     int ftiles;                           // tiles of 128 * CG features
     int steps;                            // stored tiles along the contraction
+    // Most items that offsets in order can make, below 2^30.  Offsets that decrease can name the same rows again and again and
+    // make more items than 31 bits count; every role stops here.
+    int items;
     // With few tiles the contraction is split: `parts` items of steps_each (the last one maybe fewer) steps per tile, whose
     // fp32 results go to sums [part][rows][features], to be added in order by g4_sum_parts_kernel.
     int parts, steps_each;
@@ -436,7 +439,7 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
     auto item = [&](int t) { return g4_item(t, p.parts, p.ftiles, p.steps, p.steps_each); };
     auto stages_of_this_block = [&]() {
         const int64_t items = count_slots(p.offsets, p.experts, p.rows, TN) * p.ftiles * p.parts;
-        return g4_stages(items, first_work, work_stride, p.parts, p.steps, p.steps_each);
+        return g4_stages(items < p.items ? items : p.items, first_work, work_stride, p.parts, p.steps, p.steps_each);
     };
     auto stop = [&]() { return __any_sync(0xffffffffu, *abort_flag != 0); };       // the same answer for a whole warp
 
@@ -488,7 +491,7 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
         Ring g;
         long long it = 0;
 #pragma unroll 1
-        for (int t = first_work; !stop(); t += work_stride) {
+        for (int t = first_work; t < p.items && !stop(); t += work_stride) {
             const G4Item work = item(t);
             const ExpertSlot slot = cur.seek(work.slot);
             if (slot.expert < 0) break;
@@ -523,7 +526,7 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
         const int groups = G4_TILE / p.w.group;
         const int64_t stride = MODE == G4_FWD ? 1 : p.w.tiles_k;            // stored tiles between steps of the contraction
 #pragma unroll 1
-        for (int t = first_work; !stop(); t += work_stride) {
+        for (int t = first_work; t < p.items && !stop(); t += work_stride) {
             const G4Item work = item(t);
             const ExpertSlot slot = cur.seek(work.slot);
             if (slot.expert < 0) break;
@@ -629,7 +632,7 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
         const float undo = GroupScale<Op>::UNDO;
         Ring acc;
 #pragma unroll 1
-        for (int t = first_work; !stop(); t += work_stride) {
+        for (int t = first_work; t < p.items && !stop(); t += work_stride) {
             const G4Item work = item(t);
             const ExpertSlot slot = cur.seek(work.slot);
             if (slot.expert < 0) break;
@@ -758,6 +761,7 @@ int g4_tensor_launch(const void *x, int64_t ldx, int width, G4TensorParams p, in
     p.ftiles = (g4_tiles(p.features) + CG - 1) / CG;
     const int64_t work = expert_slots_most(p.rows, p.experts, TN) * p.ftiles * p.parts;
     if (work > 0x3FFFFFFFll) return QNN_E_RANGE;
+    p.items = (int)work;
     const int most = sms / CG;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((work < most ? work : most) * CG));

@@ -73,3 +73,16 @@ def test_few_rows_barriers_are_reached_by_warps_that_gave_up():
     ahead, behind = body[:inner], body[body.index("s.next(C_STAGES);", inner):]
     assert ahead.count("multiplying_warps_sync();") == 2 and behind.count("multiplying_warps_sync();") == 1
     assert "break" not in ahead and "break" not in behind and "return" not in body
+
+
+def test_items_of_a_grouped_product_are_bounded_whatever_the_offsets_hold():
+    """Offsets are read on the device and may decrease, against the contract; 4096 experts that all claim every one of 2^23 - 1 rows
+    make 2^30 blocks of 32 rows, times the tiles of features more than an int counts.  Every role's loop over items ends at a
+    bound that the host has checked, so no item number wraps and no row is computed from one that did."""
+    experts, rows, tile = 4096, 2 ** 31 // 256 - 1, 32
+    assert experts // 2 * -(-rows // tile) * (4096 // 128) > 2 ** 31            # every second expert, 4096 features
+    text = code("g4_tensor.cuh")
+    loops = re.findall(r"for \(int t = first_work;([^;]*);", text)
+    assert len(loops) == 3 and all(c.strip() == "t < p.items && !stop()" for c in loops)
+    assert re.search(r"g4_stages\(items < p\.items \? items : p\.items,", text)
+    assert text.index("work > 0x3FFFFFFFll") < text.index("p.items = (int)work;")

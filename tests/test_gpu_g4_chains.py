@@ -107,3 +107,23 @@ def test_weight_gradients_back_to_back(t, qnn, dtype, n, k, rows):
         sync()
     both_ways(t, step, gws)
     assert qnn.tensor_path_status() == 0
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES)
+def test_experts_that_claim_the_same_rows_end_in_bounds(t, qnn, dtype):
+    """Offsets that go back and forth between 0 and the number of rows, against the contract: the calls end, report nothing, and
+    write inside their results only."""
+    rng = np.random.default_rng(31)
+    experts, n, k, rows = 40, 136, 72, 200
+    w = handle(qnn, t, rng, experts, n, k, 64)
+    kind = ref.torch_type(dtype)
+    x = t.from_numpy(rng.standard_normal((rows, k)).astype(np.float32)).to(DEV).to(kind)
+    dy = t.from_numpy(rng.standard_normal((rows, n)).astype(np.float32)).to(DEV).to(kind)
+    offsets = t.tensor([0, rows] * 20 + [0], dtype=t.int32, device=DEV)
+    y, dx = t.full((rows + 2, n), 5.0, dtype=kind, device=DEV), t.full((rows + 2, k), 5.0, dtype=kind, device=DEV)
+    for many in (rows, 60):                                   # tiles for the tensor memory, and the form for few rows
+        qnn.g4_expert_gemm(x[:many], w, offsets, out=y[1:many + 1])
+        qnn.g4_expert_gemm_backward_data(dy[:many], w, offsets, out=dx[1:many + 1])
+        t.cuda.synchronize()
+        assert bool((y[[0, -1]] == 5.0).all()) and bool((dx[[0, -1]] == 5.0).all())
+    assert qnn.tensor_path_status() == 0
