@@ -90,6 +90,16 @@ static inline int64_t expert_slots_most(int64_t rows, int experts, int tile) {
     return (rows + some * (tile - 1)) / tile;
 }
 
+// Sums are kept in units of alpha * undo, undo a power of two that keeps one product of a row's element and a weight below
+// the element itself (|scale * q| <= 6720): a sum overflows only where the result, or one of its parts, is within a factor
+// alpha * undo of doing so, or past it.  The two factors below give sum * undo * alpha with one rounding and without leaving
+// fp32 on the way: undo goes with a small alpha first, and last behind a large one.
+struct SumScale {
+    float first, second;
+    __device__ __forceinline__ SumScale(float alpha, float undo) : first(alpha < 1.0f ? alpha * undo : alpha), second(alpha < 1.0f ? 1.0f : undo) {}
+    __device__ __forceinline__ float of(float sum) const { return sum * first * second; }
+};
+
 // Element loads and stores of the real operands.
 __device__ __forceinline__ float real_load(const float *p) { return *p; }
 __device__ __forceinline__ float real_load(const __nv_bfloat16 *p) { return __bfloat162float(*p); }

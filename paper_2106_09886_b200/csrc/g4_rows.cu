@@ -41,8 +41,9 @@ template <> struct RowType<float> { static constexpr int PARTS = 3; };
 // Pair p of a code word as numbers of the operand's type, exact:
 //   bf16  the bare nibble is the subnormal t * 2^-133; times 2^127 minus 15 * 2^-7 it is q / 128;
 //   fp16  the nibble under the exponent of 1024 is 1024 + 16t; an eighth of it minus 143 is q.
-template <class T> struct CodeScale { static constexpr float UNDO = 128.0f; };
-template <> struct CodeScale<__half> { static constexpr float UNDO = 1.0f; };
+// The group's scale takes that factor out, and for the types with fp32's range leaves 2^-13, for the last multiplication to undo.
+template <class T> struct CodeScale { static constexpr float GROUP = 128.0f / 8192.0f, UNDO = 8192.0f; };
+template <> struct CodeScale<__half> { static constexpr float GROUP = 1.0f, UNDO = 1.0f; };
 template <class T>
 __device__ __forceinline__ uint32_t code_pair(uint32_t word, int p) {
     uint32_t r;
@@ -232,7 +233,7 @@ __global__ void __launch_bounds__(THREADS, RowsShape<T, NT, STREAM>::BLOCKS) g4_
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     if (t + u >= here) break;
-                    const float slo = __fmul_rn(g4_scale_f32(blo[u]), CodeScale<T>::UNDO), shi = __fmul_rn(g4_scale_f32(bhi[u]), CodeScale<T>::UNDO);
+                    const float slo = __fmul_rn(g4_scale_f32(blo[u]), CodeScale<T>::GROUP), shi = __fmul_rn(g4_scale_f32(bhi[u]), CodeScale<T>::GROUP);
                     float sum[NT][2][4];                                    // two chains: an instruction takes long to answer
 #pragma unroll
                     for (int ww = 0; ww < 4; ++ww) {
@@ -289,7 +290,7 @@ __global__ void __launch_bounds__(THREADS, RowsShape<T, NT, STREAM>::BLOCKS) g4_
     if (log_ranks) cluster_sync();
     else __syncthreads();
     // each rank adds up its share of the features over all ranks, in their order
-    const float alpha = w.alpha[slot.expert];
+    const SumScale scale(w.alpha[slot.expert], CodeScale<T>::UNDO);
     const int log_feats = 7 - log_ranks;
 #pragma unroll 1
     for (int v = threadIdx.x; v < have << log_feats; v += THREADS) {
@@ -312,7 +313,7 @@ __global__ void __launch_bounds__(THREADS, RowsShape<T, NT, STREAM>::BLOCKS) g4_
             for (int p = PARTS - 2; p >= 0; --p) one[q][PARTS - 1] = __fadd_rn(one[q][PARTS - 1], one[q][p]);     // smallest first
             total = __fadd_rn(total, one[q][PARTS - 1]);
         }
-        real_store(y + (int64_t)(slot.first + r) * ldy + j, __fmul_rn(total, alpha));
+        real_store(y + (int64_t)(slot.first + r) * ldy + j, scale.of(total));
     }
     if (log_ranks) {                                                    // nobody leaves while its sums are read; they have
         asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");      // been, so nothing is waited for but that

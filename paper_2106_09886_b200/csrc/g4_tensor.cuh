@@ -347,7 +347,7 @@ template <class T> __device__ __forceinline__ uint32_t pack_pair(float lo, float
 // features leave as 16-byte stores.  `f` the first feature, `vec`: rows start and advance by whole 16 bytes.
 template <class T>
 __device__ __forceinline__ void store_quarter(uint32_t taddr, uint32_t buf, T *row0, int64_t ldo, int tokens, int f, int features,
-                                              float undo, float alpha, bool vec) {
+                                              SumScale scale, bool vec) {
     const int lane = threadIdx.x & 31;
     const uint32_t at = buf + ((lane >> 4) * 8 + (lane & 7)) * 80 + ((lane >> 3) & 1) * 16;
 #pragma unroll
@@ -358,7 +358,7 @@ __device__ __forceinline__ void store_quarter(uint32_t taddr, uint32_t buf, T *r
         uint32_t v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            v[i] = pack_pair<T>(__fmul_rn(__fmul_rn(__uint_as_float(r[2 * i]), undo), alpha), __fmul_rn(__fmul_rn(__uint_as_float(r[2 * i + 1]), undo), alpha));
+            v[i] = pack_pair<T>(scale.of(__uint_as_float(r[2 * i])), scale.of(__uint_as_float(r[2 * i + 1])));
 #pragma unroll
         for (int i = 0; i < 2; ++i)                       // tokens 16i .. 16i + 15, features 16h .. 16h + 15
             asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};"
@@ -629,7 +629,6 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
     } else if (warp >= 4) {               // ------------------------------------------------ results
         SlotCursor cur(p.offsets, p.experts, p.rows, TN);
         const int q = warp & 3;
-        const float undo = GroupScale<Op>::UNDO;
         Ring acc;
 #pragma unroll 1
         for (int t = first_work; t < p.items && !stop(); t += work_stride) {
@@ -637,7 +636,7 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
             const ExpertSlot slot = cur.seek(work.slot);
             if (slot.expert < 0) break;
             const int f = (work.f * CG + rank) * 128 + q * 32;
-            const float alpha = p.w.alpha[slot.expert];
+            const SumScale scale(p.w.alpha[slot.expert], GroupScale<Op>::UNDO);
             T *dst = static_cast<T *>(p.out) + (int64_t)slot.first * p.ldo;
             const int have = slot.last - slot.first;
             const uint32_t lanes = (uint32_t)(q * 32) << 16;
@@ -667,7 +666,7 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
 #pragma unroll
                     for (int i = 0; i < TN; ++i)
                         if (i < have) {
-                            const float v = __fmul_rn(__fmul_rn(sum[i], undo), alpha);
+                            const float v = scale.of(sum[i]);
                             if (p.parts == 1) real_store(dst + (int64_t)i * p.ldo + f + lane, v);
                             else sums[(int64_t)i * p.features] = v;
                         }
@@ -683,7 +682,7 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
                             if (f + lane < p.features) {
 #pragma unroll
                                 for (int i = 0; i < 16; ++i)
-                                    if (c0 + i < have) sums[(int64_t)(c0 + i) * p.features] = __fmul_rn(__fmul_rn(__uint_as_float(v[i]), undo), alpha);
+                                    if (c0 + i < have) sums[(int64_t)(c0 + i) * p.features] = scale.of(__uint_as_float(v[i]));
                             }
                             __syncwarp();
                         }
@@ -691,7 +690,7 @@ __global__ void __launch_bounds__(G4Shape<CG, TN, MODE, G4Type<T>::PARTS>::THREA
 #pragma unroll 1
                     for (int c0 = 0; c0 < have; c0 += 32)
                         store_quarter<T>(tmem_base + lanes + (uint32_t)(acc.s * TN + c0), buf, dst + (int64_t)c0 * p.ldo, p.ldo, have - c0, f,
-                                         p.features, undo, alpha, p.out_vec);
+                                         p.features, scale, p.out_vec);
                     }
                     tc_fence_before();
                     __syncwarp();
