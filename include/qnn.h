@@ -286,9 +286,15 @@ int qnn_bconv2d_backward_weights(const float *g, const uint32_t *a_planes, int a
  *   alpha   fp32 [experts]
  * group is 32, 64 or 128; n and k are at most 65535*16, experts at most 4096.
  *
- * Element types of real operands: QNN_F32, QNN_BF16, QNN_F16.  Every product is accumulated in fp32 and rounded once to
- * the result's type.  bf16 and fp16 operands enter exactly; an fp32 operand enters as the exact sum of three bf16 numbers
- * (24 significant bits = 8 + 8 + 8), one tensor-core product each.
+ * Element types of real operands: QNN_F32, QNN_BF16, QNN_F16.  Sums are kept in fp32 and results rounded once to their type.
+ * bf16 and fp16 operands enter exactly.  An fp32 operand enters as the sum of three bf16 numbers (24 significant bits =
+ * 8 + 8 + 8), which is exact for magnitudes of 2^-79 and up; below, a product with a weight is off by at most
+ * 2^-109 * alpha, as its smaller parts leave the range of bf16 and fp32.  Three tensor-core products, one for each part.  Where
+ * both operands are fp32 (backward_weights), six of the nine products of parts are taken; the three that are left out
+ * (second times third part both ways, and third times third) are below 2^-21 of a product, and always of its sign.
+ * Infinities and NaN give what the formula gives, with one exception: in backward_weights an infinity times an fp32 number
+ * below 2^-133 may be NaN.  Sums of bf16 and fp32 rows are kept divided by alpha * 2^13 (few rows) or alpha * 2^15:
+ * partial sums beyond 3.4e38 times that overflow.
  */
 #define QNN_F32 0
 #define QNN_BF16 1

@@ -5,7 +5,8 @@
 // that a warp stores 32 neighbouring elements of a row of gw.  An expert's last block of rows reaches into the next
 // expert's: one warp clears those rows in shared memory before the instructions see them (a zero in one operand alone
 // would not do, as the other may hold NaN or infinity).
-// fp32: both operands are three bf16 parts; the six products of parts down to 2^-16 of the largest are summed.
+// fp32: both operands are three bf16 parts, below 1, 2^-7 and 2^-15 of the leading bit; the six products of parts whose bound is
+// 2^-15 or more are summed, the three others together are below 2^-21 of the product.
 //
 // The tensor cores cut a sum towards zero at every addition, so a sum stays in tensor memory for 16 instructions (256 rows;
 // fp32: one block of rows and its six products, smallest first) and the result warps add those to nearest in registers.

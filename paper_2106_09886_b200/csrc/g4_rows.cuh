@@ -8,7 +8,7 @@ int qnn_g4_rows(const void *x, int type, int64_t ldx, int rows, const int32_t *o
                 int64_t ldy, int rows_together, cudaStream_t st);
 
 // fp32 = part 0 + part 1 + part 2, each with at most 8 significant bits (a bf16 in the upper half of the returned word):
-// cutting towards zero leaves 16, then 8 bits.  An infinity is (one of its sign, 0, the infinity): where both operands are
+// cutting towards zero leaves 16, then 8 bits.  (Below 2^-110 the last bits fall under bf16's smallest step and are cut.)  An infinity is (one of its sign, 0, the infinity): where both operands are
 // split, the largest part of one meets every part of the other, and lower parts of finite values may be 0, which an infinity
 // there would turn into NaN.  So part 2 meets part 0 alone, which is not 0 unless the value is (or lies below 2^-133, the
 // smallest bf16).  A NaN is part 0 alone.
