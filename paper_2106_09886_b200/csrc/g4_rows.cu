@@ -368,17 +368,16 @@ int by_rows(const T *x, int64_t ldx, int rows, const int32_t *offsets, int exper
     return by_group<T, NT, false>(x, ldx, rows, offsets, experts, w, y, ldy, st);
 }
 
-// Columns per block: the fewest instructions' worth that hold the rows, at most 4 (32 columns).
+// Columns per block: eight, one instruction's worth, which hold eight rows of 2-byte elements or two of fp32; sixteen for more
+// fp32 rows together (the callers give at most 8 and 4).
 template <class T>
 int by_columns(const void *xv, int64_t ldx, int rows, const int32_t *offsets, int experts, const G4Weights &w, void *yv, int64_t ldy,
                int rows_together, cudaStream_t st) {
     const T *x = static_cast<const T *>(xv);
     T *y = static_cast<T *>(yv);
-    const int cols = rows_together * RowType<T>::PARTS;
-    if (cols <= 8) return by_rows<T, 1>(x, ldx, rows, offsets, experts, w, y, ldy, st);
-    if (cols <= 16) return by_rows<T, 2>(x, ldx, rows, offsets, experts, w, y, ldy, st);
-    if (cols <= 24) return by_rows<T, 3>(x, ldx, rows, offsets, experts, w, y, ldy, st);
-    return by_rows<T, 4>(x, ldx, rows, offsets, experts, w, y, ldy, st);
+    if constexpr (RowType<T>::PARTS > 1)
+        if (rows_together * RowType<T>::PARTS > 8) return by_rows<T, 2>(x, ldx, rows, offsets, experts, w, y, ldy, st);
+    return by_rows<T, 1>(x, ldx, rows, offsets, experts, w, y, ldy, st);
 }
 
 }  // namespace

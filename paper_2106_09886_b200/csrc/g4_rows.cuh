@@ -3,7 +3,7 @@
 #include <type_traits>
 #include "g4_format.cuh"
 
-// Rows of x in blocks of `rows_together` (expert by expert when offsets is given) times their matrix.
+// Rows of x in blocks of `rows_together` (at most 8, fp32 at most 4; expert by expert when offsets is given) times their matrix.
 int qnn_g4_rows(const void *x, int type, int64_t ldx, int rows, const int32_t *offsets, int experts, const G4Weights &w, void *y,
                 int64_t ldy, int rows_together, cudaStream_t st);
 
