@@ -359,6 +359,14 @@ int qnn_expert_backward_weights(const void *dy, const void *x, int type, int64_t
                                 size_t workspace_bytes, void *stream);
 
 /*
+ * Which kernel serves such a call; sizes alone decide it.  product: 0 forward (experts = 1 and one = 1: qnn_g4_matvec), 1
+ * backward_data, 2 backward_weights.  *tile: 0 the form for few rows; else rows of a tile for products 0 and 1 (32 or 64 by one
+ * block, 128 or 256 by a pair), features of a tile for product 2 (128 by one block, 256 by a pair).  *parts: parts of the
+ * contraction.  Nothing is launched.
+ */
+int qnn_g4_plan(int product, int one, int type, int64_t rows, int experts, int n, int k, int *tile, int *parts);
+
+/*
  * Planes [rows][bits][qnn_row_words(k)] -> the odd codes q = sum_i 2^(i-1) * plane_i (Eq. 8) as fp32:
  * out[row*ld + col] (transpose = 0, ld >= k) or out[col*ld + row] (transpose != 0, ld >= rows).
  */

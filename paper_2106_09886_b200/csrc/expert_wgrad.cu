@@ -335,6 +335,12 @@ int wgrad(const void *x, int64_t ldx, const void *dy, int64_t lddy, const WgradP
 
 }  // namespace
 
+void qnn_expert_wgrad_plan(int64_t rows, int experts, int n, int k, int *tile, int *parts) {
+    const WPlan plan = wgrad_plan(rows, experts, n, k);
+    *tile = plan.wide ? 256 : 128;
+    *parts = plan.parts;
+}
+
 size_t qnn_expert_wgrad_parts_bytes(int64_t rows, int experts, int n, int k) {
     const WPlan plan = wgrad_plan(rows, experts, n, k);
     return plan.parts > 1 ? ((size_t)plan.parts * experts * n * k * sizeof(float) + 255) / 256 * 256 : 0;

@@ -182,3 +182,20 @@ extern "C" int qnn_expert_backward_weights(const void *dy, const void *x, int ty
     if (stage_x) { x = to_x; ldx = g4_padded_width(k); }
     return qnn_expert_wgrad(x, ldx, dy, lddy, type, offsets, experts, (int)rows, n, k, gw, parts, st);
 }
+
+extern "C" int qnn_g4_plan(int product, int one, int type, int64_t rows, int experts, int n, int k, int *tile, int *parts) {
+    if (product < 0 || product > 2 || !tile || !parts || !g4_type_ok(type) || !g4_dims_ok(experts, n, k) || rows <= 0 ||
+        (one && (product != 0 || experts != 1)))
+        return QNN_E_ARG;
+    if (rows >= G4_MAX_ROWS) return QNN_E_RANGE;
+    if (product == 2) {
+        qnn_expert_wgrad_plan(rows, experts, n, k, tile, parts);
+        return QNN_OK;
+    }
+    const bool data = product == 1;
+    const G4Plan plan = g4_tensor_plan(data, type == QNN_F32, rows, experts, data ? k : n, g4_tiles(data ? n : k));
+    const bool few = !data && (one ? few_rows_one(type, rows) : few_rows(type, rows, experts));
+    *tile = few ? 0 : plan.tokens;
+    *parts = few ? 1 : plan.parts;
+    return QNN_OK;
+}

@@ -27,4 +27,5 @@ int qnn_g4_tensor_fwd(const void *x, int type, int64_t ldx, const G4TensorArgs &
 int qnn_g4_tensor_data(const void *dy, int type, int64_t lddy, const G4TensorArgs &a, cudaStream_t st);
 int qnn_expert_wgrad(const void *x, int64_t ldx, const void *dy, int64_t lddy, int type, const int32_t *offsets, int experts, int rows,
                      int n, int k, float *gw, float *parts, cudaStream_t st);
+void qnn_expert_wgrad_plan(int64_t rows, int experts, int n, int k, int *tile, int *parts);
 size_t qnn_expert_wgrad_parts_bytes(int64_t rows, int experts, int n, int k);      // of `parts` (0: it may be NULL)

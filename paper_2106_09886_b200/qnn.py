@@ -29,7 +29,7 @@ EXPORTS = [
     "qnn_bconv2d_backward_data", "qnn_bconv2d_backward_weights_workspace", "qnn_bconv2d_backward_weights", "qnn_unpack_codes_f32",
     "qnn_g4_codes_bytes", "qnn_g4_scales_bytes", "qnn_g4_pack_weights", "qnn_g4_matvec_workspace", "qnn_g4_matvec", "qnn_g4_expert_gemm_workspace",
     "qnn_g4_expert_gemm", "qnn_g4_expert_backward_data_workspace", "qnn_g4_expert_backward_data",
-    "qnn_expert_backward_weights_workspace", "qnn_expert_backward_weights",
+    "qnn_expert_backward_weights_workspace", "qnn_expert_backward_weights", "qnn_g4_plan",
     "qnn_tensor_path_status", "qnn_last_device_status", "qnn_selftest_bounded_wait", "qnn_bgemm_int8_tensor_workspace", "qnn_bgemm_int8_tensor",
     "qnn_absmax_f32", "qnn_fc_forward_host", "qnn_fc_forward_host_pipelined", "qnn_fc_forward_noalloc", "qnn_probe_bitops", "qnn_probe_naive_sgemm", "qnn_probe_copy", "qnn_popcounts_per_output",
 ]
@@ -100,6 +100,7 @@ def _load() -> C.CDLL:
     lib.qnn_expert_backward_weights_workspace.restype = sz
     lib.qnn_expert_backward_weights_workspace.argtypes = [p, p, i, i64, i64, i64, i, i, i]
     lib.qnn_expert_backward_weights.argtypes = [p, p, i, i64, i64, i64, p, i, i, i, p, p, sz, p]
+    lib.qnn_g4_plan.argtypes = [i, i, i, i64, i, i, i, C.POINTER(i), C.POINTER(i)]
     lib.qnn_tensor_path_status.argtypes = [C.POINTER(C.c_uint)]
     lib.qnn_last_device_status.argtypes = [C.POINTER(C.c_uint)]
     lib.qnn_selftest_bounded_wait.argtypes = [u, p]
@@ -436,6 +437,15 @@ def expert_gemm_backward_weights(dy: torch.Tensor, x: torch.Tensor, offsets: tor
     """Gradient of g4_expert_gemm with respect to the decoded weights: dy [rows, n], x [rows, k] -> fp32 [experts, n, k]."""
     return _result(_on_stream(stream, lambda: _binding.expert_gemm_backward_weights(dy, x, offsets, gw, workspace)),
                    "qnn_expert_backward_weights")
+
+
+def g4_plan(product: str, dtype: torch.dtype, rows: int, experts: int, n: int, k: int) -> tuple[int, int]:
+    """(tile, parts) of the kernel that serves such a call: product "matvec", "experts", "data" or "weights"; tile 0 is the form
+    for few rows (include/qnn.h, qnn_g4_plan)."""
+    tile, parts = C.c_int(), C.c_int()
+    which = {"matvec": 0, "experts": 0, "data": 1, "weights": 2}[product]
+    _check(lib.qnn_g4_plan(which, int(product == "matvec"), REAL_TYPES[dtype], rows, experts, n, k, C.byref(tile), C.byref(parts)), "qnn_g4_plan")
+    return tile.value, parts.value
 
 
 def unpack_codes_f32(planes: torch.Tensor, rows: int, k: int, bits: int, transpose: bool = False, stream=None) -> torch.Tensor:
