@@ -1,11 +1,13 @@
 """Build libqnn.so from csrc/*.cu with nvcc for sm_100a (no torch involved), and the tensor-argument module of the binding,
-_binding.so, from csrc/binding.cpp with the host compiler against the installed torch.
+_binding.<ABI tag>.so, from csrc/binding.cpp with the host compiler against the installed torch.  The module holds for one
+Python and one torch; its digest covers both, so that another one of either rebuilds it.
 
     python -m paper_2106_09886_b200.build [--force]
 """
 from __future__ import annotations
 
 import hashlib
+import importlib.metadata
 import importlib.util
 import os
 import subprocess
@@ -18,7 +20,8 @@ PKG = Path(__file__).resolve().parent
 CSRC = PKG / "csrc"
 INCLUDE = PKG.parent / "include"
 LIB = PKG / "libqnn.so"
-BINDING = PKG / "_binding.so"
+BINDING = PKG / f"_binding{sysconfig.get_config_var('EXT_SUFFIX')}"
+BINDING_STAMP = PKG / "_binding.so.digest"
 STAMP = PKG / "libqnn.so.digest"
 
 COMPILE_FLAGS = [
@@ -37,14 +40,23 @@ def _digest() -> str:
     """Content digest of everything the library is built from (file times do not survive copies of the tree)."""
     h = hashlib.sha256()
     h.update(" ".join(COMPILE_FLAGS + LINK_FLAGS).encode())
-    for path in sources() + sorted(CSRC.glob("*.cuh")) + sorted(CSRC.glob("*.cpp")) + sorted(INCLUDE.glob("*.h")):
+    for path in sources() + sorted(CSRC.glob("*.cuh")) + sorted(INCLUDE.glob("*.h")):
         h.update(path.name.encode())
         h.update(path.read_bytes())
     return h.hexdigest()
 
 
+def _stale(built: Path, stamp: Path, digest: str) -> bool:
+    return not built.exists() or not stamp.exists() or stamp.read_text().strip() != digest
+
+
 def needs_build() -> bool:
-    return not LIB.exists() or not BINDING.exists() or not STAMP.exists() or STAMP.read_text().strip() != _digest()
+    return _stale(LIB, STAMP, _digest()) or _binding_stale()
+
+
+def _binding_stale() -> bool:
+    """(Without torch there is nothing that the module could serve, and the library is built alone.)"""
+    return importlib.util.find_spec("torch") is not None and _stale(BINDING, BINDING_STAMP, _binding_digest())
 
 
 def _compile(nvcc: str, src: Path, obj: Path, verbose: bool) -> str:
@@ -57,23 +69,37 @@ def _compile(nvcc: str, src: Path, obj: Path, verbose: bool) -> str:
     return r.stderr
 
 
-def _build_binding() -> None:
+def _binding_command(out: Path) -> list[str]:
     torch = Path(importlib.util.find_spec("torch").origin).parent
-    tmp = BINDING.with_suffix(f".tmp{os.getpid()}.so")
-    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++20", "-fPIC", "-shared", f"-I{INCLUDE}", f"-I{sysconfig.get_path('include')}",
-           f"-I{torch / 'include'}", f"-I{torch / 'include/torch/csrc/api/include'}", "-I/usr/local/cuda/include", "-o", str(tmp),
-           str(CSRC / "binding.cpp"), f"-L{torch / 'lib'}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", f"-L{PKG}", "-l:libqnn.so",
-           "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{torch / 'lib'}"]
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++20", "-fPIC", "-shared", f"-I{INCLUDE}", f"-I{sysconfig.get_path('include')}",
+            f"-I{torch / 'include'}", f"-I{torch / 'include/torch/csrc/api/include'}", "-I/usr/local/cuda/include", "-o", str(out),
+            str(CSRC / "binding.cpp"), f"-L{torch / 'lib'}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", f"-L{PKG}", "-l:libqnn.so",
+            "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{torch / 'lib'}"]
+
+
+def _binding_digest() -> str:
+    """Everything the module depends on: its source, the library's header, the command, and the versions of Python and torch."""
+    h = hashlib.sha256()
+    h.update(" ".join(_binding_command(Path("out"))).replace(str(PKG.parent), "").encode())      # (the tree may be copied elsewhere)
+    h.update(f"{sys.version} torch {importlib.metadata.version('torch')}".encode())
+    for path in [CSRC / "binding.cpp"] + sorted(INCLUDE.glob("*.h")):
+        h.update(path.name.encode())
+        h.update(path.read_bytes())
+    return h.hexdigest()
+
+
+def _build_binding() -> None:
+    tmp = PKG / f"_binding.tmp{os.getpid()}.so"
+    cmd = _binding_command(tmp)
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"{cmd[0]} failed on binding.cpp:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, BINDING)
+    (PKG / "_binding.so").unlink(missing_ok=True)            # the name without a tag, of earlier builds
+    BINDING_STAMP.write_text(_binding_digest() + "\n")
 
 
-def build(force: bool = False, verbose: bool = False) -> Path:
-    """Compile every csrc/*.cu to an object file (in parallel), link them into libqnn.so, and build the binding's module."""
-    if not force and not needs_build():
-        return LIB
+def _build_library(verbose: bool) -> None:
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     objdir = PKG / "_build"
     objdir.mkdir(exist_ok=True)
@@ -87,8 +113,15 @@ def build(force: bool = False, verbose: bool = False) -> Path:
     tmp = LIB.with_suffix(f".tmp{os.getpid()}.so")
     subprocess.check_call([nvcc, *LINK_FLAGS, "-o", str(tmp), *map(str, objs)])
     os.replace(tmp, LIB)
-    _build_binding()
     STAMP.write_text(_digest() + "\n")
+
+
+def build(force: bool = False, verbose: bool = False) -> Path:
+    """Compile every csrc/*.cu to an object file (in parallel) and link them into libqnn.so; build the binding's module."""
+    if force or _stale(LIB, STAMP, _digest()):
+        _build_library(verbose)
+    if force or _binding_stale():
+        _build_binding()
     return LIB
 
 

@@ -120,7 +120,21 @@ def _load() -> C.CDLL:
 
 
 lib = _load()
-from . import _binding  # noqa: E402  (needs torch and libqnn.so)
+_binding = None
+
+
+def _load_binding():
+    """The compiled module of the 4-bit-weight calls, at the first of them: it holds for the Python and the torch that it was
+    built with, which nothing else here depends on."""
+    global _binding
+    if _binding is None:
+        try:
+            from . import _binding as module
+        except ImportError as exc:
+            raise ImportError(f"the calls on 4-bit weights need their compiled module ({exc}); build it with "
+                              "python -m paper_2106_09886_b200.build") from exc
+        _binding = module
+    return _binding
 
 
 def status_string(status: int) -> str:
@@ -415,27 +429,27 @@ def g4_matvec(x: torch.Tensor, w: G4Weights, out: torch.Tensor | None = None, wo
               stream=None) -> torch.Tensor:
     """x [rows, k] (meant for few rows; their stride is free) times one 4-bit matrix -> [rows, n] of x's type."""
     if stream is None:
-        return _result(_binding.g4_matvec(x, *w, out, workspace), "qnn_g4_matvec")
-    return _result(_on_stream(stream, lambda: _binding.g4_matvec(x, *w, out, workspace)), "qnn_g4_matvec")
+        return _result((_binding or _load_binding()).g4_matvec(x, *w, out, workspace), "qnn_g4_matvec")
+    return _result(_on_stream(stream, lambda: _load_binding().g4_matvec(x, *w, out, workspace)), "qnn_g4_matvec")
 
 
 def g4_expert_gemm(x: torch.Tensor, w: G4Weights, offsets: torch.Tensor, out: torch.Tensor | None = None,
                    workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """x [rows, k], rows sorted by expert (expert e owns rows offsets[e] .. offsets[e+1]) -> [rows, n] of x's type."""
-    return _result(_on_stream(stream, lambda: _binding.g4_expert_gemm(x, *w, offsets, out, workspace)), "qnn_g4_expert_gemm")
+    return _result(_on_stream(stream, lambda: (_binding or _load_binding()).g4_expert_gemm(x, *w, offsets, out, workspace)), "qnn_g4_expert_gemm")
 
 
 def g4_expert_gemm_backward_data(dy: torch.Tensor, w: G4Weights, offsets: torch.Tensor, out: torch.Tensor | None = None,
                                  workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Gradient of g4_expert_gemm with respect to x: dy [rows, n] -> [rows, k] of dy's type."""
-    return _result(_on_stream(stream, lambda: _binding.g4_expert_gemm_backward_data(dy, *w, offsets, out, workspace)),
+    return _result(_on_stream(stream, lambda: (_binding or _load_binding()).g4_expert_gemm_backward_data(dy, *w, offsets, out, workspace)),
                    "qnn_g4_expert_backward_data")
 
 
 def expert_gemm_backward_weights(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Tensor, gw: torch.Tensor | None = None,
                                  workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Gradient of g4_expert_gemm with respect to the decoded weights: dy [rows, n], x [rows, k] -> fp32 [experts, n, k]."""
-    return _result(_on_stream(stream, lambda: _binding.expert_gemm_backward_weights(dy, x, offsets, gw, workspace)),
+    return _result(_on_stream(stream, lambda: (_binding or _load_binding()).expert_gemm_backward_weights(dy, x, offsets, gw, workspace)),
                    "qnn_expert_backward_weights")
 
 
