@@ -416,10 +416,14 @@ def g4_pack_weights(w: torch.Tensor, group: int = 128, stream=None) -> G4Weights
     if group not in (32, 64, 128) or experts < 1 or n < 1 or k < 1:
         raise QnnError(E_ARG, "qnn_g4_pack_weights")
     shape = (experts, (n + 127) // 128, (k + 127) // 128)
-    codes, scales, alpha = _on_stream(stream, lambda: (
-        torch.empty(shape + (4, 128, 4), dtype=torch.int32, device=w.device),
-        torch.empty(shape + (128 // group, 128), dtype=torch.uint8, device=w.device),
-        torch.empty(experts, dtype=torch.float32, device=w.device)))
+
+    def arrays():
+        if w.get_device() != torch.cuda.current_device():
+            raise ValueError("w must be on the current CUDA device")
+        return (torch.empty(shape + (4, 128, 4), dtype=torch.int32, device=w.device),
+                torch.empty(shape + (128 // group, 128), dtype=torch.uint8, device=w.device),
+                torch.empty(experts, dtype=torch.float32, device=w.device))
+    codes, scales, alpha = _on_stream(stream, arrays)
     _check(lib.qnn_g4_pack_weights(_ptr(w), REAL_TYPES[w.dtype], experts, n, k, k, group, _ptr(codes), _ptr(scales), _ptr(alpha),
                                    _stream(stream)), "qnn_g4_pack_weights")
     return G4Weights(codes, scales, alpha, n, k, group)
