@@ -7,6 +7,7 @@
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
+#include <c10/core/GradMode.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -35,6 +36,12 @@ int type_of(const at::Tensor &t) {
     }
 }
 
+// These calls record no gradients: an operand that requires one, while they are recorded, would lose it without a word.
+void check_no_graph(const at::Tensor &t) {
+    if (t.requires_grad() && c10::GradMode::is_enabled())
+        throw Refused("these calls record no gradients: detach tensors that require grad, or call under torch.no_grad()");
+}
+
 struct Rows {
     int type;
     int64_t rows, ld;
@@ -42,6 +49,7 @@ struct Rows {
 // [rows, width] whose rows may lie apart but not overlap; width < 0: any.
 Rows rows_of(const at::Tensor &t, int64_t width) {
     Rows r;
+    check_no_graph(t);
     r.type = type_of(t);
     if (t.dim() != 2 || (width >= 0 && t.size(1) != width)) throw Refused("rows must be [rows, width] with the width of the weights");
     r.rows = t.size(0);
@@ -64,6 +72,7 @@ Weights weights_of(PyObject *const *a) {
     if (w.codes.scalar_type() != at::kInt || w.scales.scalar_type() != at::kByte || w.alpha.scalar_type() != at::kFloat ||
         !w.codes.is_contiguous() || !w.scales.is_contiguous() || !w.alpha.is_contiguous())
         throw Refused("codes, scales and alpha must be contiguous int32, uint8 and float32");
+    check_no_graph(w.alpha);
     const int64_t tn = (w.n + 127) / 128, tk = (w.k + 127) / 128;
     const auto c = w.codes.sizes(), s = w.scales.sizes();
     if (w.n < 1 || w.k < 1 || c.size() != 6 || c[1] != tn || c[2] != tk || c[3] != 4 || c[4] != 128 || c[5] != 4)
@@ -163,6 +172,7 @@ PyObject *expert_weights(PyObject *const *a) {
     at::Tensor gw;
     if (given(a[3])) {
         gw = tensor_of(a[3], "gw must be a tensor");
+        check_no_graph(gw);
         if (gw.scalar_type() != at::kFloat || !gw.is_contiguous() || !gw.is_cuda() || gw.get_device() != x.get_device() || gw.dim() != 3 ||
             gw.size(0) != experts || gw.size(1) != n || gw.size(2) != k)
             throw Refused("gw must be contiguous float32 [experts, n, k] on the device of the rows");

@@ -384,7 +384,12 @@ def bconv2d_backward_weights(g: torch.Tensor, a_planes: torch.Tensor, ab: int, H
 
 
 class G4Weights(NamedTuple):
-    """Group-scaled 4-bit weights of one matrix or of several experts' (the storage of include/qnn.h)."""
+    """Group-scaled 4-bit weights of one matrix or of several experts' (the storage of include/qnn.h).
+
+    The calls on them are not joined to torch's autograd: their backward products are calls of their own.  Rows (and alpha, and
+    results) that require grad are refused while gradients are recorded; inside an autograd.Function or torch.no_grad() they
+    are not.  Packing takes weights that require grad: codes have no gradient, and the straight-through one goes to the
+    weights that were packed."""
     codes: torch.Tensor      # int32 [experts, ceil(n/128), ceil(k/128), 4, 128, 4]
     scales: torch.Tensor     # uint8 [experts, ceil(n/128), ceil(k/128), 128 // group, 128], 1-4-3 floats
     alpha: torch.Tensor      # fp32 [experts]

@@ -167,3 +167,24 @@ def test_binding_refusals(qnn):
         qnn.expert_gemm_backward_weights(torch.zeros((2, 8)), cpu.bfloat16(), offsets)
     with pytest.raises(ValueError, match="current CUDA device"):
         qnn.g4_matvec(cpu, w)
+
+
+def test_operands_that_require_grad_are_refused_while_gradients_are_recorded(qnn):
+    """The calls record no gradients; a result without a graph must not come back as if nothing were missing."""
+    import torch
+    w = qnn.G4Weights(torch.zeros((1, 1, 1, 4, 128, 4), dtype=torch.int32), torch.zeros((1, 1, 1, 4, 128), dtype=torch.uint8),
+                      torch.ones(1), 8, 64, 32)
+    offsets = torch.tensor([0, 2], dtype=torch.int32)
+    x, dy = torch.zeros((2, 64)), torch.zeros((2, 8))
+    xg, dyg = torch.zeros((2, 64), requires_grad=True), torch.zeros((2, 8), requires_grad=True)
+    calls = (lambda: qnn.g4_matvec(xg, w), lambda: qnn.g4_expert_gemm(xg, w, offsets), lambda: qnn.g4_expert_gemm(xg * 2, w, offsets),
+             lambda: qnn.g4_expert_gemm_backward_data(dyg, w, offsets), lambda: qnn.expert_gemm_backward_weights(dyg, x, offsets),
+             lambda: qnn.expert_gemm_backward_weights(dy, xg, offsets),
+             lambda: qnn.g4_matvec(x, w._replace(alpha=torch.ones(1, requires_grad=True))))
+    for call in calls:
+        with pytest.raises(ValueError, match="record no gradients"):
+            call()
+        with torch.no_grad(), pytest.raises(ValueError, match="device"):       # past that check, on to the next
+            call()
+    with pytest.raises(ValueError, match="device"):
+        qnn.g4_matvec(xg.detach(), w)

@@ -30,3 +30,27 @@ def test_packing_looks_at_the_device(t, qnn, monkeypatch):
     assert not launched
     monkeypatch.undo()
     assert qnn.g4_pack_weights(w).alpha.item() > 0
+
+
+def test_results_that_require_grad_are_refused_and_functions_are_not(t, qnn):
+    """Results given by the caller; and the way that stays open: the calls inside an autograd.Function."""
+    offsets = t.tensor([0, 5], dtype=t.int32, device=DEV)
+    w = qnn.g4_pack_weights(t.randn((24, 40), device=DEV).requires_grad_())
+    x = t.randn((5, 40), device=DEV)
+    dy = t.randn((5, 24), device=DEV)
+    with pytest.raises(ValueError, match="record no gradients"):
+        qnn.g4_expert_gemm(x, w, offsets, out=t.zeros((5, 24), device=DEV, requires_grad=True))
+    with pytest.raises(ValueError, match="record no gradients"):
+        qnn.expert_gemm_backward_weights(dy, x, offsets, gw=t.zeros((1, 24, 40), device=DEV, requires_grad=True))
+
+    class Product(t.autograd.Function):
+        @staticmethod
+        def forward(ctx, x):
+            return qnn.g4_expert_gemm(x, w, offsets)
+
+        @staticmethod
+        def backward(ctx, dy):
+            return qnn.g4_expert_gemm_backward_data(dy.contiguous(), w, offsets)
+    xg = x.clone().requires_grad_()
+    (Product.apply(xg) * dy).sum().backward()
+    assert t.equal(xg.grad, qnn.g4_expert_gemm_backward_data(dy, w, offsets))
