@@ -248,20 +248,26 @@ class ExpertsLayer:
 
     def plan(self, x):
         """Rows sorted by expert: (token of each row, its gate, offsets); the split never leaves the device."""
+        return self.route(x)[1:]
+
+    def route(self, x):
+        """The places that the sorted rows come from (token * top + choice), and plan's answer."""
         gate, expert = torch.softmax(x.float() @ self.router.t(), 1).topk(self.top, 1)
         flat = expert.reshape(-1)
         order = torch.sort(flat, stable=True).indices
         counts = (flat.view(-1, 1) == torch.arange(self.router.shape[0], device=x.device)).sum(0)
         offsets = torch.zeros(counts.numel() + 1, dtype=torch.int32, device=x.device)
         offsets[1:] = counts.cumsum(0)
-        return order // self.top, (gate / gate.sum(1, keepdim=True)).reshape(-1)[order].to(x.dtype), offsets
+        return order, order // self.top, (gate / gate.sum(1, keepdim=True)).reshape(-1)[order].to(x.dtype), offsets
 
     def forward(self, x):
-        token, gate, offsets = self.plan(x)
+        order, token, gate, offsets = self.route(x)
         rows = x[token]
         h = qnn.g4_expert_gemm(rows, self.q1, offsets)
         y = qnn.g4_expert_gemm(torch.nn.functional.silu(h), self.q2, offsets)
-        out = torch.zeros_like(x, dtype=torch.float32).index_add_(0, token, (y * gate.view(-1, 1)).float())
+        slots = torch.empty_like(y)
+        slots[order] = y * gate.view(-1, 1)                         # a token's rows together again, added in a fixed order
+        out = slots.view(x.shape[0], self.top, -1).float().sum(1)
         return out.to(x.dtype), (token, gate, offsets, rows, h)
 
     def logits(self, x):

@@ -54,3 +54,13 @@ def test_results_that_require_grad_are_refused_and_functions_are_not(t, qnn):
     xg = x.clone().requires_grad_()
     (Product.apply(xg) * dy).sum().backward()
     assert t.equal(xg.grad, qnn.g4_expert_gemm_backward_data(dy, w, offsets))
+
+
+def test_experts_layer_repeats_its_bits(t, qnn):
+    """Four experts a token: their results are added in a fixed order, so the layer of run_case gives the same bits every time."""
+    from paper_2106_09886_b200.run_case import ExpertsLayer
+    layer = ExpertsLayer(256, 384, 8, 4, 64, group=64, dtype=t.float32, seed=5)
+    x = t.randn((700, 256), device=DEV, generator=t.Generator(device=DEV).manual_seed(6))
+    first = layer.forward(x)[0]
+    for _ in range(20):
+        assert t.equal(layer.forward(x)[0], first)
