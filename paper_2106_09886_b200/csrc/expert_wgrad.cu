@@ -12,8 +12,8 @@
 // fp32: one block of rows and its six products, smallest first) and the result warps add those to nearest in registers.
 // Bound: writing gw (4 bytes an element) up to some 600 rows an expert, the matrix instructions beyond.  With few tiles
 // the rows are split over the blocks too; the parts are added in a fixed order by a second kernel.
-// Measured: 4096 rows, eight experts 2048 x 4096, bf16: 87 us (268 MB of gw at 3.1 TB/s); 8192 rows, one expert 4096 x 4096:
-// 200 us, 1.37 PFLOP/s.
+// Measured in a replayed graph, and as calls back to back: 4096 rows, eight experts 2048 x 4096, bf16: 90 and 101 us (268 MB of
+// gw at 3.0 and 2.7 TB/s); 8192 rows, one expert 4096 x 4096: 207 and 244 us, 1.33 and 1.13 PFLOP/s.
 #include "g4_stage.cuh"
 #include "g4_tensor.cuh"
 

@@ -26,7 +26,8 @@ int check_workspace(const void *ws, size_t have, size_t need) {
 
 // Few rows for each expert: the form that needs no full tile (g4_rows.cu).
 bool few_rows(int type, int64_t rows, int experts) { return rows <= (type == QNN_F32 ? 2 : 4) * (int64_t)experts; }
-// And for one matrix.  16 x 16384 x 8192 in fp16: 35 us there, 23.5 us as a split product.
+// And for one matrix.  Drawn at one size: 16 x 16384 x 8192 in fp16 takes 35 us there and 22.5 us in 32-row tiles of the tensor-memory
+// form.  (A small matrix has few such tiles: 16 x 1024 x 1024 makes eight.)
 bool few_rows_one(int type, int64_t rows) { return rows <= (type == QNN_F32 ? 4 : 8); }
 
 size_t product_workspace(bool data, const void *x, int type, int64_t rows, int64_t ldx, int experts, int width, int features) {

@@ -14,8 +14,8 @@
 // once for the block, some tiles at a time.  The contraction is split over a cluster of up to eight blocks, whose sums are
 // added in a fixed order through distributed shared memory.
 // fp32 rows are split exactly into three bf16 parts (8 + 8 + 8 bits) that occupy three of the instruction's columns.
-// Measured: 1 x 8192 x 8192 11.6 us (3.0 TB/s of codes and scales), 1 x 4096 x 4096 5.4, 1 x 1024 x 1024 3.1; issue-bound
-// (162 instructions per warp and tile) with some 3 us of start and joining around it.
+// Measured in a replayed graph: 1 x 8192 x 8192 13.6 to 14.1 us (2.5 TB/s of codes and scales), 1 x 4096 x 4096 6.1, 1 x 1024 x 1024
+// 3.1; issue-bound (164 instructions per warp and tile in all) with some 3 us of start and joining around it.
 #include "g4_rows.cuh"
 #include "tc_ptx.cuh"
 

@@ -1,7 +1,7 @@
 // Products grouped by expert on the fifth-generation tensor cores: result = weights x rows, accumulated in tensor memory
 // with the weight features as the 128 lanes of an accumulator and the rows (tokens) as its columns, so that a stored
-// 128 x 128 tile of codes is unpacked once and multiplied with up to 256 tokens, and a ragged number of tokens only
-// narrows the columns.
+// 128 x 128 tile of codes is unpacked once and multiplied with up to 256 tokens.  An expert's last tile multiplies all its
+// columns too, whatever rows follow in memory; only the stores stop at the expert's last row.
 //
 //   G4_FWD   y[r][j]  = alpha sum_i W[j][i] x[r][i]:  lanes j, contraction over i.  A thread owns a lane and unpacks the
 //            64 codes of its row straight into the A operand in tensor memory: no shared-memory round trip, one group
@@ -15,9 +15,11 @@
 // CG = 2: a pair of thread blocks (cluster) works on 256 lanes x TN tokens with cta_group::2 instructions, each block
 // holding its 128 lanes of weights and half of the tokens, which halves what is read per product.
 //
-// Bound: the tensor pipe for many tokens (16384 rows, eight experts 4096 x 4096, bf16: 386 us, 1.42 PFLOP/s); unpacking for
-// few (1024 rows, 32 experts 2048 x 4096, fp16: 45 us, some 600 cycles a stored tile); shared-memory bandwidth for the data
-// gradient, whose unpacked weights pass through it (4096 rows, eight experts 4096 x 4096: 118-131 us, 1.05-1.16 PFLOP/s).
+// Bound, with times in a replayed graph and of calls from Python back to back: the tensor pipe for many tokens (16384 rows,
+// eight experts 4096 x 4096, bf16: 390 and 454 us, 1.41 and 1.21 PFLOP/s, the latter under the power cap); unpacking for few
+// (1024 rows, 32 experts 2048 x 4096, fp16: 45 and 54 us, some 600 cycles a stored tile); the tensor pipe for the data
+// gradient too, where it is busy (86 % of the cycles in which an SM has a block), but 4096 rows on eight 4096 x 4096 experts
+// make 20 tiles, a quarter of whose columns are padding, and 320 items for 74 pairs, 4.3 rounds that take 5 (123 and 142 us).
 #pragma once
 #include "tc_ptx.cuh"
 #include "g4_rows.cuh"
