@@ -367,6 +367,95 @@ int qnn_expert_backward_weights(const void *dy, const void *x, int type, int64_t
 int qnn_g4_plan(int product, int one, int type, int64_t rows, int experts, int n, int k, int *tile, int *parts);
 
 /*
+ * Rows in 8 bits: int8 codes [rows][ldc] with one fp32 scale for each row; element i of row r stands for scale[r] * code[r][i].  The
+ * operands of qnn_i8_gemm (rows are tokens, or output features of a weight matrix).  Codes are -127 .. 127 in two's complement, not
+ * odd: 8-bit odd codes need 9 bits.  Rows start on 16 bytes: the array is 16-byte aligned and ldc a multiple of 16; entries
+ * from `width` on are never read nor written.
+ *   scale = max(max|x| / 127, 2^-126)      code = x / scale, the fp32 quotient rounded to nearest, half to even
+ * A row that holds an infinity or NaN gets scale NaN and codes 0: all of it, and every product with it, is NaN.
+ * width is at most 16384, rows below 2^31.  rows = 0 is allowed and does nothing.
+ *   x, out     [rows][ld] of `type`, ld >= width, any alignment of the element size (rows on 16 bytes are faster)
+ */
+int qnn_i8_quantize(const void *x, int type, int64_t rows, int width, int64_t ldx, int8_t *codes, int64_t ldc, float *scales, void *stream);
+int qnn_i8_decode(const int8_t *codes, const float *scales, int64_t rows, int width, int64_t ldc, int type, void *out, int64_t ldo,
+                  void *stream);
+
+/*
+ * Product of rows in 8 bits: y[r][j] = x_scales[r] * w_scales[j] * sum_i x[r][i] * w[j][i] (+ bias[j]), on the int8 tensor cores.  The sum is
+ * a whole number, exact in int32; it is rounded to fp32, multiplied by the token's scale, by the feature's, the bias added (each
+ * rounded once, in that order), and the result rounded to `type`.
+ *   x  int8 [rows][ldx], w int8 [n][ldw], rows of the format above (any codes, -128 too)
+ *   bias  fp32 [n] or NULL;  y  [rows][ldy] of `type`, ldy >= n, any alignment of its element size
+ * k at most 131071 (128 * 128 * k fits int32), n at most 65535*16, rows < 2^31 / 256; QNN_E_RANGE beyond.  rows = 0 is allowed and does
+ * nothing.  No workspace.  Waits inside the kernels are bounded and reported by qnn_tensor_path_status.
+ * qnn_i8_plan: which kernel serves such a call; sizes alone decide it.  *tile: tokens of a tile; *ranks: blocks that share the
+ * contraction of a tile of 128 features (added as whole numbers, so results repeat bit for bit), or 0 for a pair of blocks and 256
+ * features.  Nothing is launched.
+ */
+int qnn_i8_gemm(const int8_t *x, const float *x_scales, int64_t rows, int64_t ldx, const int8_t *w, const float *w_scales, int n, int k,
+                int64_t ldw, const float *bias, int type, void *y, int64_t ldy, void *stream);
+int qnn_i8_plan(int64_t rows, int n, int k, int *tile, int *ranks);
+
+/*
+ * Root-mean-square norm of rows, with the addition of a residual ahead of it, and its result as real numbers, in 8 bits, or both:
+ *   h = x + residual, rounded to `type`;   rstd = 1 / sqrt(mean over the row of h^2 + eps);   y = (h * gain) * rstd
+ * in fp32 (squares are summed in fp32: rows beyond 1.8e19 have rstd 0), rounded once where y is written.
+ *   residual   [rows][ldr] of `type`, or NULL: h is x, and h, ldh are ignored
+ *   gain       [width] of gain_type, which is `type` or QNN_F32
+ *   h          out, given when residual is; it may be x or residual itself (each element is read before it is written)
+ *   y          out, optional; it may be x where there is no residual
+ *   codes, scales   out, optional: the rows y, before any rounding to `type`, in 8 bits as above.  One of y and codes is given.
+ *   rstd       out, optional fp32 [rows], for the backward products
+ * eps >= 0; sizes, alignment and rows = 0 as above.
+ *
+ * Backward, given dy = dC/dy (through codes: straight through) and, optional, dh = what reaches h by another way:
+ *   dx = rstd * (dy * gain - u * mean(dy * gain * u)) + dh with u = h * rstd     (also the residual's gradient)
+ *   dgain = sum over the rows of dy * u, fp32 [width], added in a fixed order; zeros for rows = 0
+ * dx may be dy or dh.  workspace: device scratch owned by the caller, 256-byte aligned, qnn_rms_norm_backward_workspace(...) bytes.
+ */
+int qnn_rms_norm(const void *x, int type, int64_t rows, int width, int64_t ldx, const void *residual, int64_t ldr, const void *gain,
+                 int gain_type, float eps, void *h, int64_t ldh, void *y, int64_t ldy, int8_t *codes, int64_t ldc, float *scales,
+                 float *rstd, void *stream);
+size_t qnn_rms_norm_backward_workspace(int64_t rows, int width);
+int qnn_rms_norm_backward(const void *dy, int type, int64_t rows, int width, int64_t lddy, const void *h, int64_t ldh, const void *gain,
+                          int gain_type, const float *rstd, const void *dh, int64_t lddh, void *dx, int64_t lddx, float *dgain,
+                          void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Routing of tokens to experts, ahead of the products grouped by expert.  With logits l of a token:
+ *   scores   s = softmax(l), or 1 / (1 + exp(-l)) with QNN_ROUTE_SIGMOID
+ *   keys     s + bias where a bias is given (it decides the choice alone and has no gradient), else l itself (s grows with it)
+ *   groups   experts lie in `groups` equal groups; the top_groups groups of the largest key (QNN_ROUTE_GROUPS_BY_TWO: of the largest
+ *            sum of two keys; without a bias, of two scores) stay, ties to the lowest group
+ *   choice   the `top` largest keys, in that order, ties to the lowest expert.  Decisions are those of scores in 64 bits.
+ *   weights  factor * s of the chosen, QNN_ROUTE_RENORMALISE: factor * s / (sum of the chosen s); in fp32
+ * An expert whose logit or bias is -infinity (or whose bias is NaN) is not chosen; where fewer than `top` are left, the rest of
+ * the places get expert -1 and weight 0.  mask (optional, one byte a token): a token with 0 is padding and gets no expert.  A
+ * token whose logits hold NaN (or +infinity, with softmax) gets no expert and weights NaN.
+ * The plan of the grouped products, optional (order, place and offsets are given together or not at all):
+ *   offsets  int32 [experts + 1], rows of expert e are offsets[e] .. offsets[e + 1] - 1
+ *   order    int32 [tokens * top]: the slot (token * top + choice) of each row; an expert's slots keep their order; -1 from
+ *            offsets[experts] on
+ *   place    int32 [tokens][top]: the row of each slot, -1 where it has no expert
+ *   logits   [tokens][ld] of `type`, ld >= experts;  chosen int32, weights fp32 [tokens][top]
+ * experts at most 1024, top at most 32, groups at most 32 and a divisor of experts, top <= top_groups * experts / groups,
+ * tokens * top < 2^31.  tokens = 0 is allowed (offsets become 0).  workspace: device scratch owned by the caller, 256-byte aligned,
+ * qnn_route_workspace(...) bytes (0: it may be NULL), needed with a plan only.
+ *
+ * Backward: dlogits [tokens][ldd] of `type`, fully written, from dweights fp32 [tokens][top], the logits and the choice (experts
+ * outside 0 .. experts - 1 count as none).  flags and factor as in the call; the bias has no part in it.
+ */
+#define QNN_ROUTE_SIGMOID 1u
+#define QNN_ROUTE_RENORMALISE 2u
+#define QNN_ROUTE_GROUPS_BY_TWO 4u
+size_t qnn_route_workspace(int64_t tokens, int experts, int top);
+int qnn_route(const void *logits, int type, int64_t tokens, int experts, int64_t ld, int top, unsigned flags, const float *bias, int groups,
+              int top_groups, float factor, const uint8_t *mask, int32_t *chosen, float *weights, int32_t *order, int32_t *place,
+              int32_t *offsets, void *workspace, size_t workspace_bytes, void *stream);
+int qnn_route_backward(const float *dweights, const void *logits, int type, int64_t tokens, int experts, int64_t ld, int top, unsigned flags,
+                       const int32_t *chosen, float factor, void *dlogits, int64_t ldd, void *stream);
+
+/*
  * Planes [rows][bits][qnn_row_words(k)] -> the odd codes q = sum_i 2^(i-1) * plane_i (Eq. 8) as fp32:
  * out[row*ld + col] (transpose = 0, ld >= k) or out[col*ld + row] (transpose != 0, ld >= rows).
  */

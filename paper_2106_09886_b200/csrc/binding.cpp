@@ -1,4 +1,4 @@
-// Tensor arguments of the 4-bit-weight calls -> the C ABI (include/qnn.h): checks, the result's allocation on the current
+// Tensor arguments of the calls of a decoding step (4-bit weights, rows in 8 bits, norms, routing) -> the C ABI (include/qnn.h): checks, the result's allocation on the current
 // stream, and the call, in one step from Python.  A step of decoding makes these calls for every layer with microseconds of
 // work each; through ctypes the marshalling alone took longer than the small ones run (a call with a new result 10.7 us, of which
 // 2.9 the launch, and 4.5 here; with a result given 8.9 and 3.4).
@@ -6,9 +6,11 @@
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
+#include <ATen/ops/empty_strided.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <c10/core/GradMode.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -190,6 +192,253 @@ PyObject *expert_weights(PyObject *const *a) {
     return answer(status, std::move(gw));
 }
 
+// ------------------------------------------------------------------------------------------------ rows in 8 bits, norms, routing
+
+int64_t whole_units(int64_t k) { return (k + 15) / 16 * 16; }
+void check_int(int64_t v) {
+    if (v > INT32_MAX) throw Refused("a size does not fit 32 bits");
+}
+int64_t int_of(PyObject *o) {
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) throw python_error();
+    return v;
+}
+float float_of(PyObject *o) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw python_error();
+    return (float)v;
+}
+void *pointer(const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
+
+// A tuple of results, or the status.
+PyObject *answers(int status, std::initializer_list<at::Tensor *> results) {
+    if (status != QNN_OK) return PyLong_FromLong(status);
+    PyObject *tuple = PyTuple_New((Py_ssize_t)results.size());
+    if (!tuple) throw python_error();
+    Py_ssize_t i = 0;
+    for (at::Tensor *t : results) PyTuple_SET_ITEM(tuple, i++, THPVariable_Wrap(std::move(*t)));
+    return tuple;
+}
+
+// An optional tensor of `size` contiguous elements of a type.
+at::Tensor vector_of(PyObject *o, at::ScalarType type, int64_t size, const char *what) {
+    if (!given(o)) return at::Tensor();
+    const at::Tensor &t = tensor_of(o, what);
+    check_no_graph(t);
+    if (t.scalar_type() != type || t.numel() != size || !t.is_contiguous()) throw Refused(what);
+    return t;
+}
+
+struct Codes {
+    const at::Tensor &codes, &scales;
+    int64_t rows, k, ld;
+};
+// args: codes int8 [rows, k], scales fp32 [rows]
+Codes codes_of(PyObject *const *a) {
+    Codes c{tensor_of(a[0], "codes must be a tensor"), tensor_of(a[1], "scales must be a tensor"), 0, 0, 0};
+    check_no_graph(c.scales);
+    if (c.codes.scalar_type() != at::kChar || c.codes.dim() != 2 || c.scales.scalar_type() != at::kFloat || c.scales.dim() != 1 || !c.scales.is_contiguous())
+        throw Refused("rows in 8 bits are codes int8 [rows, k] and contiguous scales float32 [rows]");
+    c.rows = c.codes.size(0);
+    c.k = c.codes.size(1);
+    c.ld = c.rows > 1 ? c.codes.stride(0) : std::max(c.codes.stride(0), whole_units(c.k));
+    if (c.rows <= 1 && c.ld % 16 != 0) c.ld = whole_units(c.ld);
+    if (c.scales.size(0) != c.rows) throw Refused("codes and scales must have the same number of rows");
+    if ((c.k > 1 && c.rows > 0 && c.codes.stride(1) != 1) || c.ld < c.k) throw Refused("rows of codes must be contiguous and must not overlap");
+    check_int(c.k);
+    return c;
+}
+// Room for rows in 8 bits, each starting on 16 bytes.
+at::Tensor new_codes(const at::Tensor &like, int64_t rows, int64_t k) {
+    return at::empty_strided({rows, k}, {whole_units(k), 1}, like.options().dtype(at::kChar));
+}
+void check_like(const at::Tensor &t, const Rows &r, const at::Tensor &like, const Rows &l) {
+    if (r.type != l.type || r.rows != l.rows || t.size(1) != like.size(1)) throw Refused("all rows must have the same type and shape");
+}
+
+// i8_quantize(x)
+PyObject *i8_quantize(PyObject *const *a) {
+    const at::Tensor &x = tensor_of(a[0], "x must be a tensor");
+    const Rows r = rows_of(x, -1);
+    const int64_t k = x.size(1);
+    check_int(k);
+    void *stream = stream_for(x, {});
+    at::Tensor codes = new_codes(x, r.rows, k), scales = at::empty({r.rows}, x.options().dtype(at::kFloat));
+    const int status = qnn_i8_quantize(x.data_ptr(), r.type, r.rows, (int)k, r.ld, (int8_t *)codes.data_ptr(), whole_units(k), (float *)scales.data_ptr(), stream);
+    return answers(status, {&codes, &scales});
+}
+
+at::ScalarType real_type_of(PyObject *o) {
+    if (!THPDtype_Check(o)) throw Refused("dtype must be a torch.dtype");
+    const at::ScalarType t = reinterpret_cast<THPDtype *>(o)->scalar_type;
+    if (t != at::kFloat && t != at::kBFloat16 && t != at::kHalf) throw Refused("dtype must be float32, bfloat16 or float16");
+    return t;
+}
+int code_of(at::ScalarType t) { return t == at::kFloat ? QNN_F32 : t == at::kBFloat16 ? QNN_BF16 : QNN_F16; }
+// Rows of a result: as given, checked, or new.
+at::Tensor rows_for(PyObject *out, const at::Tensor &like, at::ScalarType type, int64_t rows, int64_t width, int64_t *ld) {
+    if (!given(out)) {
+        *ld = width;
+        return at::empty({rows, width}, like.options().dtype(type));
+    }
+    const at::Tensor &t = tensor_of(out, "out must be a tensor");
+    const Rows r = rows_of(t, width);
+    if (t.scalar_type() != type || r.rows != rows || !t.is_cuda() || t.get_device() != like.get_device())
+        throw Refused("out must be [rows, width] of the result's type and on the device of the rows");
+    *ld = r.ld;
+    return t;
+}
+
+// i8_decode(codes, scales, dtype, out)
+PyObject *i8_decode(PyObject *const *a) {
+    const Codes c = codes_of(a);
+    const at::ScalarType type = real_type_of(a[2]);
+    void *stream = stream_for(c.codes, {&c.scales});
+    int64_t ld;
+    at::Tensor out = rows_for(a[3], c.codes, type, c.rows, c.k, &ld);
+    const int status = qnn_i8_decode((const int8_t *)c.codes.data_ptr(), (const float *)c.scales.data_ptr(), c.rows, (int)c.k, c.ld, code_of(type),
+                                     out.data_ptr(), ld, stream);
+    return answer(status, std::move(out));
+}
+
+// i8_gemm(x codes, x scales, w codes, w scales, dtype, bias, out)
+PyObject *i8_gemm(PyObject *const *a) {
+    const Codes x = codes_of(a), w = codes_of(a + 2);
+    if (x.k != w.k) throw Refused("rows and weights must have the same length");
+    check_int(w.rows);
+    const at::ScalarType type = real_type_of(a[4]);
+    const at::Tensor bias = vector_of(a[5], at::kFloat, w.rows, "bias must be contiguous float32 [features]");
+    void *stream = bias.defined() ? stream_for(x.codes, {&x.scales, &w.codes, &w.scales, &bias}) : stream_for(x.codes, {&x.scales, &w.codes, &w.scales});
+    int64_t ld;
+    at::Tensor out = rows_for(a[6], x.codes, type, x.rows, w.rows, &ld);
+    const int status = qnn_i8_gemm((const int8_t *)x.codes.data_ptr(), (const float *)x.scales.data_ptr(), x.rows, x.ld, (const int8_t *)w.codes.data_ptr(),
+                                   (const float *)w.scales.data_ptr(), (int)w.rows, (int)w.k, w.ld, (const float *)pointer(bias), code_of(type),
+                                   out.data_ptr(), ld, stream);
+    return answer(status, std::move(out));
+}
+
+// The gain of a norm: [width] of the rows' type or float32.
+const at::Tensor &gain_of(PyObject *o, const Rows &r, int64_t width, int *type) {
+    const at::Tensor &g = tensor_of(o, "gain must be a tensor");
+    check_no_graph(g);
+    *type = type_of(g);
+    if (g.dim() != 1 || g.size(0) != width || !g.is_contiguous() || (*type != r.type && *type != QNN_F32))
+        throw Refused("gain must be contiguous [width] of the rows' type or float32");
+    return g;
+}
+
+// rms_norm(x, gain, eps, residual, real, eight): (y, codes, scales, h, rstd), None for what is not asked for; h is x without a residual
+PyObject *rms_norm(PyObject *const *a) {
+    const at::Tensor &x = tensor_of(a[0], "x must be a tensor");
+    const Rows r = rows_of(x, -1);
+    const int64_t k = x.size(1);
+    check_int(k);
+    int gain_type;
+    const at::Tensor &gain = gain_of(a[1], r, k, &gain_type);
+    const float eps = float_of(a[2]);
+    const bool real = PyObject_IsTrue(a[4]) == 1, eight = PyObject_IsTrue(a[5]) == 1;
+    at::Tensor residual, h, y, codes, scales;
+    int64_t ldr = 0;
+    void *stream;
+    if (given(a[3])) {
+        residual = tensor_of(a[3], "residual must be a tensor");
+        const Rows q = rows_of(residual, k);
+        check_like(residual, q, x, r);
+        ldr = q.ld;
+        stream = stream_for(x, {&gain, &residual});
+        h = at::empty({r.rows, k}, x.options());
+    } else {
+        stream = stream_for(x, {&gain});
+    }
+    if (real) y = at::empty({r.rows, k}, x.options());
+    if (eight) {
+        codes = new_codes(x, r.rows, k);
+        scales = at::empty({r.rows}, x.options().dtype(at::kFloat));
+    }
+    at::Tensor rstd = at::empty({r.rows}, x.options().dtype(at::kFloat));
+    const int status = qnn_rms_norm(x.data_ptr(), r.type, r.rows, (int)k, r.ld, pointer(residual), ldr, gain.data_ptr(), gain_type, eps, pointer(h), k,
+                                    pointer(y), k, (int8_t *)pointer(codes), whole_units(k), (float *)pointer(scales), (float *)rstd.data_ptr(), stream);
+    if (!h.defined()) h = x;
+    return answers(status, {&y, &codes, &scales, &h, &rstd});
+}
+
+// rms_norm_backward(dy, h, gain, rstd, dh, workspace): (dx, dgain)
+PyObject *rms_norm_backward(PyObject *const *a) {
+    const at::Tensor &dy = tensor_of(a[0], "dy must be a tensor"), &h = tensor_of(a[1], "h must be a tensor");
+    const Rows r = rows_of(dy, -1), q = rows_of(h, -1);
+    check_like(h, q, dy, r);
+    const int64_t k = dy.size(1);
+    check_int(k);
+    int gain_type;
+    const at::Tensor &gain = gain_of(a[2], r, k, &gain_type);
+    if (!given(a[3])) throw Refused("rstd must be contiguous float32 [rows]");
+    const at::Tensor rstd = vector_of(a[3], at::kFloat, r.rows, "rstd must be contiguous float32 [rows]");
+    at::Tensor dh;
+    int64_t lddh = 0;
+    void *stream;
+    if (given(a[4])) {
+        dh = tensor_of(a[4], "dh must be a tensor");
+        const Rows d = rows_of(dh, k);
+        check_like(dh, d, dy, r);
+        lddh = d.ld;
+        stream = stream_for(dy, {&h, &gain, &rstd, &dh});
+    } else {
+        stream = stream_for(dy, {&h, &gain, &rstd});
+    }
+    at::Tensor dx = at::empty({r.rows, k}, dy.options()), dgain = at::empty({k}, dy.options().dtype(at::kFloat));
+    const at::Tensor ws = workspace_for(a[5], qnn_rms_norm_backward_workspace(r.rows, (int)k), dy);
+    const int status = qnn_rms_norm_backward(dy.data_ptr(), r.type, r.rows, (int)k, r.ld, h.data_ptr(), q.ld, gain.data_ptr(), gain_type,
+                                             (const float *)rstd.data_ptr(), pointer(dh), lddh, dx.data_ptr(), k, (float *)dgain.data_ptr(), pointer(ws),
+                                             ws.defined() ? ws.nbytes() : 0, stream);
+    return answers(status, {&dx, &dgain});
+}
+
+// route(logits, top, flags, bias, groups, top_groups, factor, mask, workspace): (experts, weights, order, place, offsets)
+PyObject *route(PyObject *const *a) {
+    const at::Tensor &logits = tensor_of(a[0], "logits must be a tensor");
+    const Rows r = rows_of(logits, -1);
+    const int64_t experts = logits.size(1), top = int_of(a[1]), groups = int_of(a[4]), top_groups = int_of(a[5]);
+    if (experts > 1024 || top < 1 || top > 32 || groups < 1 || groups > 32 || top_groups < 1 || top_groups > 32) return PyLong_FromLong(QNN_E_ARG);
+    const at::Tensor bias = vector_of(a[3], at::kFloat, experts, "bias must be contiguous float32 [experts]");
+    at::Tensor mask;
+    if (given(a[7])) {
+        mask = tensor_of(a[7], "mask must be a tensor");
+        if ((mask.scalar_type() != at::kBool && mask.scalar_type() != at::kByte) || mask.numel() != r.rows || !mask.is_contiguous())
+            throw Refused("mask must be contiguous bool or uint8 [tokens]");
+    }
+    void *stream = stream_for(logits, {});
+    for (const at::Tensor *t : std::initializer_list<const at::Tensor *>{&bias, &mask})
+        if (t->defined()) stream_for(*t, {&logits});
+    const auto whole = logits.options().dtype(at::kInt);
+    at::Tensor chosen = at::empty({r.rows, top}, whole), weights = at::empty({r.rows, top}, logits.options().dtype(at::kFloat));
+    at::Tensor order = at::empty({r.rows * top}, whole), place = at::empty({r.rows, top}, whole), offsets = at::empty({experts + 1}, whole);
+    const at::Tensor ws = workspace_for(a[8], qnn_route_workspace(r.rows, (int)experts, (int)top), logits);
+    const int status = qnn_route(logits.data_ptr(), r.type, r.rows, (int)experts, r.ld, (int)top, (unsigned)int_of(a[2]), (const float *)pointer(bias),
+                                 (int)groups, (int)top_groups, float_of(a[6]), (const uint8_t *)pointer(mask), (int32_t *)chosen.data_ptr(),
+                                 (float *)weights.data_ptr(), (int32_t *)order.data_ptr(), (int32_t *)place.data_ptr(), (int32_t *)offsets.data_ptr(),
+                                 pointer(ws), ws.defined() ? ws.nbytes() : 0, stream);
+    return answers(status, {&chosen, &weights, &order, &place, &offsets});
+}
+
+// route_backward(dweights, logits, experts, flags, factor, out)
+PyObject *route_backward(PyObject *const *a) {
+    const at::Tensor &dweights = tensor_of(a[0], "dweights must be a tensor"), &logits = tensor_of(a[1], "logits must be a tensor"),
+                     &chosen = tensor_of(a[2], "experts must be a tensor");
+    const Rows r = rows_of(logits, -1);
+    check_no_graph(dweights);
+    if (dweights.scalar_type() != at::kFloat || chosen.scalar_type() != at::kInt || dweights.dim() != 2 || chosen.dim() != 2 ||
+        dweights.sizes() != chosen.sizes() || dweights.size(0) != r.rows || !dweights.is_contiguous() || !chosen.is_contiguous())
+        throw Refused("dweights and experts must be contiguous float32 and int32 [tokens, top]");
+    const int64_t experts = logits.size(1), top = chosen.size(1);
+    if (experts > 1024 || top > 32) return PyLong_FromLong(QNN_E_ARG);
+    void *stream = stream_for(logits, {&dweights, &chosen});
+    int64_t ld;
+    at::Tensor out = result_for(a[5], logits, r.rows, experts, &ld);
+    const int status = qnn_route_backward((const float *)dweights.data_ptr(), logits.data_ptr(), r.type, r.rows, (int)experts, r.ld, (int)top,
+                                          (unsigned)int_of(a[3]), (const int32_t *)chosen.data_ptr(), float_of(a[4]), out.data_ptr(), ld, stream);
+    return answer(status, std::move(out));
+}
+
 template <PyObject *(*F)(PyObject *const *), int ARGS>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t count) {
     HANDLE_TH_ERRORS
@@ -211,6 +460,13 @@ PyMethodDef methods[] = {
     {"g4_expert_gemm", (PyCFunction)(void (*)(void))entry<g4_expert<false>, 10>, METH_FASTCALL, nullptr},
     {"g4_expert_gemm_backward_data", (PyCFunction)(void (*)(void))entry<g4_expert<true>, 10>, METH_FASTCALL, nullptr},
     {"expert_gemm_backward_weights", (PyCFunction)(void (*)(void))entry<expert_weights, 5>, METH_FASTCALL, nullptr},
+    {"i8_quantize", (PyCFunction)(void (*)(void))entry<i8_quantize, 1>, METH_FASTCALL, nullptr},
+    {"i8_decode", (PyCFunction)(void (*)(void))entry<i8_decode, 4>, METH_FASTCALL, nullptr},
+    {"i8_gemm", (PyCFunction)(void (*)(void))entry<i8_gemm, 7>, METH_FASTCALL, nullptr},
+    {"rms_norm", (PyCFunction)(void (*)(void))entry<rms_norm, 6>, METH_FASTCALL, nullptr},
+    {"rms_norm_backward", (PyCFunction)(void (*)(void))entry<rms_norm_backward, 6>, METH_FASTCALL, nullptr},
+    {"route", (PyCFunction)(void (*)(void))entry<route, 9>, METH_FASTCALL, nullptr},
+    {"route_backward", (PyCFunction)(void (*)(void))entry<route_backward, 6>, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "tensor arguments of the 4-bit-weight calls", -1, methods, nullptr, nullptr, nullptr, nullptr};
 

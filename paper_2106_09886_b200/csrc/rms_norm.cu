@@ -1,0 +1,540 @@
+// Rows of real numbers: the residual's addition and the root-mean-square norm, with the result as real numbers, in 8 bits with a
+// scale for each row, or both; rows into 8 bits without a norm, and back; the norm's backward products.
+//
+//   h = round(x + residual)     rstd = 1 / sqrt(mean(h^2) + eps)     y = (h * gain) * rstd
+//   scale = max|y| / 127        code = rint(y / scale)
+//
+// Bound: HBM.  A row is read once and stays in registers, in its own type (h is rounded to it, so nothing is lost).  The order
+// (h * gain) * rstd makes max|y| = max|h * gain| * rstd exactly, rounding being monotone: the sum of squares and the largest
+// magnitude come out of one pass and one reduction, and the codes follow from the registers.
+#include "real_rows.cuh"
+#include "tc_ptx.cuh"
+
+namespace {
+
+constexpr int NORM_MAX_WIDTH = 16384;
+
+struct NormParams {
+    const void *x, *residual, *gain;          // residual NULL: h is x.  gain NULL: no norm (y = x)
+    int64_t ldx, ldr, ldh, ldy, ldc;
+    int64_t rows;
+    int width;
+    float eps;
+    void *h, *y;
+    int8_t *codes;
+    float *scales, *rstd;
+};
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) v = __fadd_rn(v, __shfl_xor_sync(0xffffffffu, v, d));
+    return v;
+}
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) v = max_or_nan(v, __shfl_xor_sync(0xffffffffu, v, d));
+    return v;
+}
+
+// Over the threads of a row: blockDim.x of them, whole warps.
+template <bool SUM> __device__ __forceinline__ void block_sum_and_max(float &sum, float &most, float (*parts)[32]) {
+    if constexpr (SUM) sum = warp_sum(sum);
+    most = warp_max(most);
+    if (blockDim.x > 32) {
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+        if (lane == 0) { parts[0][warp] = sum; parts[1][warp] = most; }
+        __syncthreads();
+        if constexpr (SUM) sum = warp_sum(lane < warps ? parts[0][lane] : 0.0f);
+        most = warp_max(lane < warps ? parts[1][lane] : 0.0f);
+    }
+}
+__device__ __forceinline__ float norm_factor(float sum, const NormParams &p) {
+    return __frcp_rn(__fsqrt_rn(__fadd_rn(__fdiv_rn(sum, (float)p.width), p.eps)));
+}
+
+// A row by `blockDim.x` threads (y: rows of a block, more than one for rows of a single warp).  Each thread holds NV packs of 16
+// bytes.  NORM = false: codes of the rows themselves.
+template <class T, class G, int NV, bool NORM>
+__global__ void __launch_bounds__(NV == 1 ? 1024 : 512) norm_rows_kernel(const NormParams p) {
+    __shared__ float parts[2][32];
+    start_next();
+    wait_for_previous();
+    const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    if (row >= p.rows) return;                                      // (whole warps: blocks of several rows have one warp a row)
+    constexpr int V = 16 / sizeof(T);
+    const int packs = p.width / V, step = blockDim.x;
+    typedef Pack<T, V> PT;
+    typedef Pack<G, V> PG;
+    PT v[NV], r[NV];
+    PG g[NV];
+    const T *x = static_cast<const T *>(p.x) + row * p.ldx;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int i = threadIdx.x + j * step;
+        if (i < packs) v[j] = reinterpret_cast<const PT *>(x)[i];
+    }
+    if constexpr (NORM) {
+        if (p.residual) {
+            const T *res = static_cast<const T *>(p.residual) + row * p.ldr;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const int i = threadIdx.x + j * step;
+                if (i < packs) r[j] = reinterpret_cast<const PT *>(res)[i];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int i = threadIdx.x + j * step;
+            if (i < packs) g[j] = static_cast<const PG *>(p.gain)[i];
+        }
+        if (p.residual) {
+            T *h = static_cast<T *>(p.h) + row * p.ldh;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const int i = threadIdx.x + j * step;
+                if (i < packs) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) v[j].e[e] = from_f32<T>(__fadd_rn(to_f32(v[j].e[e]), to_f32(r[j].e[e])));
+                    reinterpret_cast<PT *>(h)[i] = v[j];
+                }
+            }
+        }
+    }
+    float sum = 0.0f, most = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        if (threadIdx.x + j * step < packs)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                float a = to_f32(v[j].e[e]);
+                if constexpr (NORM) {
+                    sum = __fmaf_rn(a, a, sum);
+                    a = __fmul_rn(a, to_f32(g[j].e[e]));
+                }
+                most = max_or_nan(most, fabsf(a));
+            }
+    }
+    block_sum_and_max<NORM>(sum, most, parts);
+    float rstd = 1.0f;
+    if constexpr (NORM) {
+        rstd = norm_factor(sum, p);
+        if (p.rstd && threadIdx.x == 0) p.rstd[row] = rstd;
+        most = __fmul_rn(most, rstd);
+        if (p.y) {
+            T *y = static_cast<T *>(p.y) + row * p.ldy;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const int i = threadIdx.x + j * step;
+                if (i < packs) {
+                    PT o;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) o.e[e] = from_f32<T>(__fmul_rn(__fmul_rn(to_f32(v[j].e[e]), to_f32(g[j].e[e])), rstd));
+                    reinterpret_cast<PT *>(y)[i] = o;
+                }
+            }
+        }
+    }
+    if (!NORM || p.codes) {
+        const RowScale s(most);
+        if (threadIdx.x == 0) p.scales[row] = s.scale;
+        int8_t *codes = p.codes + row * p.ldc;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int i = threadIdx.x + j * step;
+            if (i < packs) {
+                Pack<int8_t, V> o;
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    float a = to_f32(v[j].e[e]);
+                    if constexpr (NORM) a = __fmul_rn(__fmul_rn(a, to_f32(g[j].e[e])), rstd);
+                    o.e[e] = (int8_t)s.code(a);
+                }
+                reinterpret_cast<Pack<int8_t, V> *>(codes)[i] = o;
+            }
+        }
+    }
+}
+
+// Rows whose start, stride or width is not a multiple of 16 bytes: element by element, read again (from the caches) where the
+// packs above stay in registers.
+template <class T, class G, bool NORM>
+__global__ void __launch_bounds__(512) norm_any_kernel(const NormParams p) {
+    __shared__ float parts[2][32];
+    start_next();
+    wait_for_previous();
+    const int64_t row = blockIdx.x;
+    const T *x = static_cast<const T *>(p.x) + row * p.ldx;
+    const G *gain = static_cast<const G *>(p.gain);
+    float sum = 0.0f, most = 0.0f;
+    if (NORM && p.residual) {
+        const T *res = static_cast<const T *>(p.residual) + row * p.ldr;
+        T *h = static_cast<T *>(p.h) + row * p.ldh;
+#pragma unroll 8
+        for (int i = threadIdx.x; i < p.width; i += blockDim.x) {
+            const T v = from_f32<T>(__fadd_rn(to_f32(x[i]), to_f32(res[i])));
+            const float a = to_f32(v);
+            h[i] = v;
+            sum = __fmaf_rn(a, a, sum);
+            most = max_or_nan(most, fabsf(__fmul_rn(a, to_f32(gain[i]))));
+        }
+        x = h;                                                      // (each thread reads what it has written itself)
+    } else {
+#pragma unroll 8
+        for (int i = threadIdx.x; i < p.width; i += blockDim.x) {
+            float a = to_f32(x[i]);
+            if constexpr (NORM) {
+                sum = __fmaf_rn(a, a, sum);
+                a = __fmul_rn(a, to_f32(gain[i]));
+            }
+            most = max_or_nan(most, fabsf(a));
+        }
+    }
+    block_sum_and_max<NORM>(sum, most, parts);
+    float rstd = 1.0f;
+    if constexpr (NORM) {
+        rstd = norm_factor(sum, p);
+        if (p.rstd && threadIdx.x == 0) p.rstd[row] = rstd;
+        most = __fmul_rn(most, rstd);
+    }
+    const bool coded = !NORM || p.codes;
+    const RowScale s(most);
+    if (coded && threadIdx.x == 0) p.scales[row] = s.scale;
+    int8_t *codes = p.codes + row * p.ldc;
+    T *y = static_cast<T *>(p.y) + row * p.ldy;
+#pragma unroll 8
+    for (int i = threadIdx.x; i < p.width; i += blockDim.x) {
+        float a = to_f32(x[i]);
+        if constexpr (NORM) a = __fmul_rn(__fmul_rn(a, to_f32(gain[i])), rstd);
+        if (NORM && p.y) y[i] = from_f32<T>(a);
+        if (coded) codes[i] = (int8_t)s.code(a);
+    }
+}
+
+static inline int whole_warps(int threads) { return (threads + 31) / 32 * 32; }
+template <class T, class G, int NV, bool NORM>
+int norm_launch(const NormParams &p, int packs, cudaStream_t st) {
+    const int threads = whole_warps((packs + NV - 1) / NV), together = threads == 32 ? 4 : 1;
+    const int64_t blocks = (p.rows + together - 1) / together;
+    return launch_early(norm_rows_kernel<T, G, NV, NORM>, dim3((unsigned)blocks), dim3(threads, together), st, p);
+}
+template <class T, class G, bool NORM>
+int norm_typed(const NormParams &p, bool vec, cudaStream_t st) {
+    if (!vec) return launch_early(norm_any_kernel<T, G, NORM>, dim3((unsigned)p.rows), dim3(p.width <= 256 ? whole_warps(p.width) : p.width <= 4096 ? 256 : 512), st, p);
+    const int packs = p.width / (16 / (int)sizeof(T));
+    if (packs <= 1024 && (p.rows <= 296 || packs <= 32)) return norm_launch<T, G, 1, NORM>(p, packs, st);
+    if (packs <= 1024) return norm_launch<T, G, 2, NORM>(p, packs, st);
+    if (packs <= 2048) return norm_launch<T, G, 4, NORM>(p, packs, st);
+    return norm_launch<T, G, 8, NORM>(p, packs, st);
+}
+
+int check_real(const void *p, int type, int64_t ld, int width) {
+    if (!p || ld < width) return QNN_E_ARG;
+    return qnn_aligned(p, g4_type_bytes(type)) ? QNN_OK : QNN_E_ALIGN;
+}
+int check_codes(const int8_t *codes, const float *scales, int64_t ldc, int width) {
+    if (!codes || !scales || ldc < width) return QNN_E_ARG;
+    return qnn_aligned(codes, 16) && ldc % 16 == 0 && qnn_aligned(scales, 4) ? QNN_OK : QNN_E_ALIGN;
+}
+// Can rows be accessed 16 bytes at a time?
+bool in_packs(const void *p, int type, int64_t ld) { return qnn_aligned(p, 16) && ld * g4_type_bytes(type) % 16 == 0; }
+
+// ------------------------------------------------------------------------------------------------ codes back to numbers
+
+template <class T, int V>
+__global__ void __launch_bounds__(256) decode_kernel(const int8_t *codes, const float *scales, int64_t rows, int width, int64_t ldc, T *out, int64_t ldo) {
+    start_next();
+    wait_for_previous();
+    const int packs = width / V, i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= packs) return;
+    for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
+        const Pack<int8_t, V> c = reinterpret_cast<const Pack<int8_t, V> *>(codes + row * ldc)[i];
+        const float s = scales[row];
+        Pack<T, V> o;
+#pragma unroll
+        for (int e = 0; e < V; ++e) o.e[e] = from_f32<T>(__fmul_rn((float)c.e[e], s));
+        reinterpret_cast<Pack<T, V> *>(out + row * ldo)[i] = o;
+    }
+}
+template <class T>
+int decode(const int8_t *codes, const float *scales, int64_t rows, int width, int64_t ldc, void *out, int64_t ldo, bool vec, cudaStream_t st) {
+    constexpr int V = 16 / sizeof(T);
+    T *o = static_cast<T *>(out);
+    const unsigned ys = (unsigned)(rows < 65535 ? rows : 65535);
+    if (vec) return launch_early(decode_kernel<T, V>, dim3((width / V + 255) / 256, ys), dim3(256), st, codes, scales, rows, width, ldc, o, ldo);
+    return launch_early(decode_kernel<T, 1>, dim3((width + 255) / 256, ys), dim3(256), st, codes, scales, rows, width, ldc, o, ldo);
+}
+
+// ------------------------------------------------------------------------------------------------ backward products
+
+// dx = rstd * a - h * rstd^3 * mean(a * h) + dh with a = dy * gain; dgain = sum over the rows of dy * h * rstd.
+// A block takes every gridDim.x-th row and keeps dgain of its columns in registers; the blocks' sums are added in a fixed order
+// by a second kernel, so results repeat bit for bit.
+struct NormBackParams {
+    const void *dy, *h, *gain, *dh;           // dh NULL: no gradient reaches h by another way
+    const float *rstd;
+    int64_t lddy, ldh, lddh, lddx, rows;
+    int width;
+    void *dx;
+    float *sums;                              // [gridDim.x][width]
+};
+
+template <class T, class G, int NV>
+__global__ void __launch_bounds__(NV == 1 ? 256 : 512) norm_back_kernel(const NormBackParams p) {
+    __shared__ float parts[2][32];
+    start_next();
+    wait_for_previous();
+    constexpr int V = 16 / sizeof(T);
+    typedef Pack<T, V> PT;
+    typedef Pack<G, V> PG;
+    const int packs = p.width / V, step = blockDim.x;
+    float sum[NV][V];
+    PG g[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int i = threadIdx.x + j * step;
+        if (i < packs) g[j] = static_cast<const PG *>(p.gain)[i];
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum[j][e] = 0.0f;
+    }
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    int side = 0;
+    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, side ^= 1) {
+        PT dy[NV], h[NV], dh[NV];
+        const T *dys = static_cast<const T *>(p.dy) + row * p.lddy, *hs = static_cast<const T *>(p.h) + row * p.ldh;
+        float dot = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int i = threadIdx.x + j * step;
+            if (i < packs) {
+                dy[j] = reinterpret_cast<const PT *>(dys)[i];
+                h[j] = reinterpret_cast<const PT *>(hs)[i];
+            }
+        }
+        if (p.dh) {
+            const T *dhs = static_cast<const T *>(p.dh) + row * p.lddh;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const int i = threadIdx.x + j * step;
+                if (i < packs) dh[j] = reinterpret_cast<const PT *>(dhs)[i];
+            }
+        }
+        const float r = p.rstd[row];
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (threadIdx.x + j * step < packs)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float d = to_f32(dy[j].e[e]), u = __fmul_rn(to_f32(h[j].e[e]), r);
+                    dot = __fmaf_rn(__fmul_rn(d, to_f32(g[j].e[e])), u, dot);
+                    sum[j][e] = __fmaf_rn(d, u, sum[j][e]);
+                }
+        dot = warp_sum(dot);
+        if (warps > 1) {
+            if (lane == 0) parts[side][warp] = dot;               // (two sides: the next row's sums do not wait for this one's readers)
+            __syncthreads();
+            dot = warp_sum(lane < warps ? parts[side][lane] : 0.0f);
+        }
+        const float mean = __fdiv_rn(dot, (float)p.width);
+        T *dxs = static_cast<T *>(p.dx) + row * p.lddx;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int i = threadIdx.x + j * step;
+            if (i < packs) {
+                PT o;
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float u = __fmul_rn(to_f32(h[j].e[e]), r);
+                    float d = __fmul_rn(__fmaf_rn(-u, mean, __fmul_rn(to_f32(dy[j].e[e]), to_f32(g[j].e[e]))), r);
+                    if (p.dh) d = __fadd_rn(d, to_f32(dh[j].e[e]));
+                    o.e[e] = from_f32<T>(d);
+                }
+                reinterpret_cast<PT *>(dxs)[i] = o;
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int i = threadIdx.x + j * step;
+        if (i < packs)
+#pragma unroll
+            for (int e = 0; e < V; ++e) p.sums[(int64_t)blockIdx.x * p.width + i * V + e] = sum[j][e];
+    }
+}
+
+// The same element by element, for rows that cannot be accessed in packs; a thread's sums are in shared memory.
+template <class T, class G>
+__global__ void __launch_bounds__(512) norm_back_any_kernel(const NormBackParams p) {
+    extern __shared__ float sums[];
+    __shared__ float parts[2][32];
+    start_next();
+    wait_for_previous();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    const G *gain = static_cast<const G *>(p.gain);
+    for (int i = threadIdx.x; i < p.width; i += blockDim.x) sums[i] = 0.0f;
+    int side = 0;
+    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, side ^= 1) {
+        const T *dy = static_cast<const T *>(p.dy) + row * p.lddy, *h = static_cast<const T *>(p.h) + row * p.ldh;
+        const T *dh = static_cast<const T *>(p.dh) + row * p.lddh;
+        T *dx = static_cast<T *>(p.dx) + row * p.lddx;
+        const float r = p.rstd[row];
+        float dot = 0.0f;
+#pragma unroll 4
+        for (int i = threadIdx.x; i < p.width; i += blockDim.x) {
+            const float d = to_f32(dy[i]), u = __fmul_rn(to_f32(h[i]), r);
+            dot = __fmaf_rn(__fmul_rn(d, to_f32(gain[i])), u, dot);
+            sums[i] = __fmaf_rn(d, u, sums[i]);
+        }
+        dot = warp_sum(dot);
+        if (lane == 0) parts[side][warp] = dot;
+        __syncthreads();
+        const float mean = __fdiv_rn(warp_sum(lane < warps ? parts[side][lane] : 0.0f), (float)p.width);
+#pragma unroll 4
+        for (int i = threadIdx.x; i < p.width; i += blockDim.x) {
+            const float u = __fmul_rn(to_f32(h[i]), r);
+            float d = __fmul_rn(__fmaf_rn(-u, mean, __fmul_rn(to_f32(dy[i]), to_f32(gain[i]))), r);
+            if (p.dh) d = __fadd_rn(d, to_f32(dh[i]));
+            dx[i] = from_f32<T>(d);
+        }
+    }
+    for (int i = threadIdx.x; i < p.width; i += blockDim.x) p.sums[(int64_t)blockIdx.x * p.width + i] = sums[i];
+}
+
+// dgain[c] = sum over `parts` rows of sums.  Eight threads a column, whose sums are added in order.
+__global__ void __launch_bounds__(256) norm_gain_kernel(const float *sums, int parts, int width, float *dgain) {
+    __shared__ float part[8][32];
+    start_next();
+    wait_for_previous();
+    const int c = blockIdx.x * 32 + threadIdx.x;
+    float sum = 0.0f;
+    if (c < width)
+#pragma unroll 8
+        for (int q = threadIdx.y; q < parts; q += 8) sum = __fadd_rn(sum, sums[(int64_t)q * width + c]);
+    part[threadIdx.y][threadIdx.x] = sum;
+    __syncthreads();
+    if (threadIdx.y == 0 && c < width) {
+        for (int q = 1; q < 8; ++q) sum = __fadd_rn(sum, part[q][threadIdx.x]);
+        dgain[c] = sum;
+    }
+}
+
+// Blocks of the backward kernel; sized for 148 SMs, so that workspace queries and calls agree.
+int back_blocks(int64_t rows) { return (int)(rows < 296 ? rows : 296); }
+
+template <class T, class G, int NV>
+int back_launch(const NormBackParams &p, int packs, cudaStream_t st) {
+    return launch_early(norm_back_kernel<T, G, NV>, dim3(back_blocks(p.rows)), dim3(whole_warps((packs + NV - 1) / NV)), st, p);
+}
+template <class T, class G>
+int back_any_launch(const NormBackParams &p, cudaStream_t st) {
+    auto kernel = norm_back_any_kernel<T, G>;
+    const int smem = p.width * (int)sizeof(float);
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NORM_MAX_WIDTH * (int)sizeof(float)) != cudaSuccess) return QNN_E_CUDA;
+    LaunchAttrs attrs(1);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(back_blocks(p.rows));
+    cfg.blockDim = dim3(p.width <= 512 ? whole_warps(p.width) : 512);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attrs.a;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess) return QNN_OK;
+    cudaGetLastError();
+    return QNN_E_CUDA;
+}
+template <class T, class G>
+int back_typed(const NormBackParams &p, bool vec, float *dgain, cudaStream_t st) {
+    const int packs = p.width / (16 / (int)sizeof(T));
+    int rc;
+    if (!vec || packs > 2048) rc = back_any_launch<T, G>(p, st);
+    else if (packs <= 256) rc = back_launch<T, G, 1>(p, packs, st);
+    else if (packs <= 1024) rc = back_launch<T, G, 2>(p, packs, st);
+    else rc = back_launch<T, G, 4>(p, packs, st);
+    if (rc != QNN_OK) return rc;
+    return launch_early(norm_gain_kernel, dim3((p.width + 31) / 32), dim3(32, 8), st, p.sums, back_blocks(p.rows), p.width, dgain);
+}
+
+// f(T, G) for the element type and the gain's (that type or fp32)
+template <class F> int by_types(int type, int gain_type, F f) {
+    if (type == QNN_F32) return f(float(), float());
+    if (type == QNN_BF16) return gain_type == QNN_F32 ? f(__nv_bfloat16(), float()) : f(__nv_bfloat16(), __nv_bfloat16());
+    return gain_type == QNN_F32 ? f(__half(), float()) : f(__half(), __half());
+}
+int check_gain(const void *gain, int gain_type, int type) {
+    if (!gain || !(gain_type == type || gain_type == QNN_F32)) return QNN_E_ARG;
+    return qnn_aligned(gain, g4_type_bytes(gain_type)) ? QNN_OK : QNN_E_ALIGN;
+}
+
+}  // namespace
+
+extern "C" int qnn_rms_norm(const void *x, int type, int64_t rows, int width, int64_t ldx, const void *residual, int64_t ldr, const void *gain,
+                            int gain_type, float eps, void *h, int64_t ldh, void *y, int64_t ldy, int8_t *codes, int64_t ldc, float *scales,
+                            float *rstd, void *stream) {
+    if (!g4_type_ok(type) || rows < 0 || width < 1 || !(eps >= 0.0f && eps <= 3.0e38f)) return QNN_E_ARG;
+    if (width > NORM_MAX_WIDTH || rows > ROWS_MAX) return QNN_E_RANGE;
+    int rc = check_gain(gain, gain_type, type);
+    if (rc != QNN_OK || rows == 0) return rc;
+    if (!y && !codes) return QNN_E_ARG;
+    if ((rc = check_real(x, type, ldx, width)) != QNN_OK) return rc;
+    if (residual && (rc = check_real(residual, type, ldr, width)) != QNN_OK) return rc;
+    if (residual && (rc = check_real(h, type, ldh, width)) != QNN_OK) return rc;
+    if (y && (rc = check_real(y, type, ldy, width)) != QNN_OK) return rc;
+    if (codes && (rc = check_codes(codes, scales, ldc, width)) != QNN_OK) return rc;
+    if (rstd && !qnn_aligned(rstd, 4)) return QNN_E_ALIGN;
+    const bool vec = width * g4_type_bytes(type) % 16 == 0 && in_packs(x, type, ldx) && qnn_aligned(gain, 16) &&
+                     (!residual || (in_packs(residual, type, ldr) && in_packs(h, type, ldh))) && (!y || in_packs(y, type, ldy));
+    const NormParams p{x, residual, gain, ldx, ldr, ldh, ldy, ldc, rows, width, eps, h, y, codes, scales, rstd};
+    return by_types(type, gain_type, [&](auto t, auto g) { return norm_typed<decltype(t), decltype(g), true>(p, vec, static_cast<cudaStream_t>(stream)); });
+}
+
+extern "C" int qnn_i8_quantize(const void *x, int type, int64_t rows, int width, int64_t ldx, int8_t *codes, int64_t ldc, float *scales,
+                               void *stream) {
+    if (!g4_type_ok(type) || rows < 0 || width < 1) return QNN_E_ARG;
+    if (width > NORM_MAX_WIDTH || rows > ROWS_MAX) return QNN_E_RANGE;
+    if (rows == 0) return QNN_OK;
+    int rc = check_real(x, type, ldx, width);
+    if (rc == QNN_OK) rc = check_codes(codes, scales, ldc, width);
+    if (rc != QNN_OK) return rc;
+    const bool vec = width * g4_type_bytes(type) % 16 == 0 && in_packs(x, type, ldx);
+    NormParams p{};
+    p.x = x; p.ldx = ldx; p.rows = rows; p.width = width; p.codes = codes; p.ldc = ldc; p.scales = scales;
+    return by_types(type, type, [&](auto t, auto) { return norm_typed<decltype(t), decltype(t), false>(p, vec, static_cast<cudaStream_t>(stream)); });
+}
+
+extern "C" int qnn_i8_decode(const int8_t *codes, const float *scales, int64_t rows, int width, int64_t ldc, int type, void *out, int64_t ldo,
+                             void *stream) {
+    if (!g4_type_ok(type) || rows < 0 || width < 1) return QNN_E_ARG;
+    if (rows > ROWS_MAX) return QNN_E_RANGE;
+    if (rows == 0) return QNN_OK;
+    int rc = check_codes(codes, scales, ldc, width);
+    if (rc == QNN_OK) rc = check_real(out, type, ldo, width);
+    if (rc != QNN_OK) return rc;
+    const bool vec = width * g4_type_bytes(type) % 16 == 0 && in_packs(out, type, ldo);
+    return by_types(type, type, [&](auto t, auto) { return decode<decltype(t)>(codes, scales, rows, width, ldc, out, ldo, vec, static_cast<cudaStream_t>(stream)); });
+}
+
+extern "C" size_t qnn_rms_norm_backward_workspace(int64_t rows, int width) {
+    if (rows < 1 || rows > ROWS_MAX || width < 1 || width > NORM_MAX_WIDTH) return 0;
+    return ((size_t)back_blocks(rows) * (size_t)width * sizeof(float) + 255) / 256 * 256;
+}
+
+extern "C" int qnn_rms_norm_backward(const void *dy, int type, int64_t rows, int width, int64_t lddy, const void *h, int64_t ldh,
+                                     const void *gain, int gain_type, const float *rstd, const void *dh, int64_t lddh, void *dx, int64_t lddx,
+                                     float *dgain, void *workspace, size_t workspace_bytes, void *stream) {
+    if (!g4_type_ok(type) || rows < 0 || width < 1 || !dgain) return QNN_E_ARG;
+    if (width > NORM_MAX_WIDTH || rows > ROWS_MAX) return QNN_E_RANGE;
+    if (!qnn_aligned(dgain, 4)) return QNN_E_ALIGN;
+    int rc = check_gain(gain, gain_type, type);
+    if (rc != QNN_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (rows == 0) return cudaMemsetAsync(dgain, 0, (size_t)width * sizeof(float), st) == cudaSuccess ? QNN_OK : QNN_E_CUDA;
+    if (!rstd) return QNN_E_ARG;
+    if ((rc = check_real(dy, type, lddy, width)) != QNN_OK || (rc = check_real(h, type, ldh, width)) != QNN_OK ||
+        (rc = check_real(dx, type, lddx, width)) != QNN_OK || (dh && (rc = check_real(dh, type, lddh, width)) != QNN_OK))
+        return rc;
+    if (!workspace || workspace_bytes < qnn_rms_norm_backward_workspace(rows, width)) return QNN_E_ARG;
+    if (!qnn_aligned(workspace, 256) || !qnn_aligned(rstd, 4)) return QNN_E_ALIGN;
+    const bool vec = width * g4_type_bytes(type) % 16 == 0 && in_packs(dy, type, lddy) && in_packs(h, type, ldh) && in_packs(dx, type, lddx) &&
+                     (!dh || in_packs(dh, type, lddh)) && qnn_aligned(gain, 16);
+    const NormBackParams p{dy, h, gain, dh, rstd, lddy, ldh, lddh, lddx, rows, width, dx, static_cast<float *>(workspace)};
+    return by_types(type, gain_type, [&](auto t, auto g) { return back_typed<decltype(t), decltype(g)>(p, vec, dgain, st); });
+}

@@ -3,8 +3,8 @@
 Argument marshalling only -- every step runs inside the library's CUDA kernels.  The
 library must have been built (``python -m paper_2106_09886_b200.build``); importing this
 module without it raises ImportError, and there is no CPU fallback.  The calls on 4-bit
-weights, which a decoding step makes by the hundred, are marshalled by a compiled module
-(csrc/binding.cpp) instead of ctypes.
+weights and on rows in 8 bits, the norm and the routing, which a decoding step makes by the
+hundred, are marshalled by a compiled module (csrc/binding.cpp) instead of ctypes.
 """
 from __future__ import annotations
 
@@ -30,6 +30,8 @@ EXPORTS = [
     "qnn_g4_codes_bytes", "qnn_g4_scales_bytes", "qnn_g4_pack_weights", "qnn_g4_matvec_workspace", "qnn_g4_matvec", "qnn_g4_expert_gemm_workspace",
     "qnn_g4_expert_gemm", "qnn_g4_expert_backward_data_workspace", "qnn_g4_expert_backward_data",
     "qnn_expert_backward_weights_workspace", "qnn_expert_backward_weights", "qnn_g4_plan",
+    "qnn_i8_quantize", "qnn_i8_decode", "qnn_i8_gemm", "qnn_i8_plan", "qnn_rms_norm", "qnn_rms_norm_backward_workspace",
+    "qnn_rms_norm_backward", "qnn_route_workspace", "qnn_route", "qnn_route_backward",
     "qnn_tensor_path_status", "qnn_last_device_status", "qnn_selftest_bounded_wait", "qnn_bgemm_int8_tensor_workspace", "qnn_bgemm_int8_tensor",
     "qnn_absmax_f32", "qnn_fc_forward_host", "qnn_fc_forward_host_pipelined", "qnn_fc_forward_noalloc", "qnn_probe_bitops", "qnn_probe_naive_sgemm", "qnn_probe_copy", "qnn_popcounts_per_output",
 ]
@@ -101,6 +103,18 @@ def _load() -> C.CDLL:
     lib.qnn_expert_backward_weights_workspace.argtypes = [p, p, i, i64, i64, i64, i, i, i]
     lib.qnn_expert_backward_weights.argtypes = [p, p, i, i64, i64, i64, p, i, i, i, p, p, sz, p]
     lib.qnn_g4_plan.argtypes = [i, i, i, i64, i, i, i, C.POINTER(i), C.POINTER(i)]
+    lib.qnn_i8_quantize.argtypes = [p, i, i64, i, i64, p, i64, p, p]
+    lib.qnn_i8_decode.argtypes = [p, p, i64, i, i64, i, p, i64, p]
+    lib.qnn_i8_gemm.argtypes = [p, p, i64, i64, p, p, i, i, i64, p, i, p, i64, p]
+    lib.qnn_i8_plan.argtypes = [i64, i, i, C.POINTER(i), C.POINTER(i)]
+    lib.qnn_rms_norm.argtypes = [p, i, i64, i, i64, p, i64, p, i, f, p, i64, p, i64, p, i64, p, p, p]
+    lib.qnn_rms_norm_backward_workspace.restype = sz
+    lib.qnn_rms_norm_backward_workspace.argtypes = [i64, i]
+    lib.qnn_rms_norm_backward.argtypes = [p, i, i64, i, i64, p, i64, p, i, p, p, i64, p, i64, p, p, sz, p]
+    lib.qnn_route_workspace.restype = sz
+    lib.qnn_route_workspace.argtypes = [i64, i, i]
+    lib.qnn_route.argtypes = [p, i, i64, i, i64, i, u, p, i, i, f, p, p, p, p, p, p, p, sz, p]
+    lib.qnn_route_backward.argtypes = [p, p, i, i64, i, i64, i, u, p, f, p, i64, p]
     lib.qnn_tensor_path_status.argtypes = [C.POINTER(C.c_uint)]
     lib.qnn_last_device_status.argtypes = [C.POINTER(C.c_uint)]
     lib.qnn_selftest_bounded_wait.argtypes = [u, p]
@@ -124,14 +138,14 @@ _binding = None
 
 
 def _load_binding():
-    """The compiled module of the 4-bit-weight calls, at the first of them: it holds for the Python and the torch that it was
+    """The compiled module of a decoding step's calls, at the first of them: it holds for the Python and the torch that it was
     built with, which nothing else here depends on."""
     global _binding
     if _binding is None:
         try:
             from . import _binding as module
         except ImportError as exc:
-            raise ImportError(f"the calls on 4-bit weights need their compiled module ({exc}); build it with "
+            raise ImportError(f"the calls of a decoding step need their compiled module ({exc}); build it with "
                               "python -m paper_2106_09886_b200.build") from exc
         _binding = module
     return _binding
@@ -469,6 +483,97 @@ def g4_plan(product: str, dtype: torch.dtype, rows: int, experts: int, n: int, k
     which = {"matvec": 0, "experts": 0, "data": 1, "weights": 2}[product]
     _check(lib.qnn_g4_plan(which, int(product == "matvec"), REAL_TYPES[dtype], rows, experts, n, k, C.byref(tile), C.byref(parts)), "qnn_g4_plan")
     return tile.value, parts.value
+
+
+class I8Rows(NamedTuple):
+    """Rows in 8 bits (tokens, or output features of a weight matrix): scales[r] * codes[r, i].  Rows of codes start on 16 bytes; the
+    calls that make them lay them out so.  Like the calls on 4-bit weights, those on rows in 8 bits, the norm and the routing are
+    not joined to torch's autograd and refuse operands that require grad while gradients are recorded."""
+    codes: torch.Tensor      # int8 [rows, k], rows a multiple of 16 bytes apart
+    scales: torch.Tensor     # fp32 [rows]
+
+
+def i8_quantize(x: torch.Tensor, stream=None) -> I8Rows:
+    """Real rows [rows, k] (tokens, or a weight matrix [features, k]) -> codes with a scale for each row, max|x| / 127."""
+    return I8Rows(*_result(_on_stream(stream, lambda: (_binding or _load_binding()).i8_quantize(x)), "qnn_i8_quantize"))
+
+
+def i8_decode(rows: I8Rows, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The numbers that rows in 8 bits stand for, [rows, k] of `dtype`."""
+    return _result(_on_stream(stream, lambda: (_binding or _load_binding()).i8_decode(*rows, dtype, out)), "qnn_i8_decode")
+
+
+def i8_gemm(x: I8Rows, w: I8Rows, dtype: torch.dtype = torch.bfloat16, bias: torch.Tensor | None = None,
+            out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Rows in 8 bits times weights in 8 bits (one scale for each token, one for each feature) -> [rows, features] of `dtype`."""
+    if stream is None:
+        return _result((_binding or _load_binding()).i8_gemm(*x, *w, dtype, bias, out), "qnn_i8_gemm")
+    return _result(_on_stream(stream, lambda: _load_binding().i8_gemm(*x, *w, dtype, bias, out)), "qnn_i8_gemm")
+
+
+def i8_plan(rows: int, n: int, k: int) -> tuple[int, int]:
+    """(tile, ranks) of the kernel that serves an i8_gemm of these sizes (include/qnn.h, qnn_i8_plan)."""
+    tile, ranks = C.c_int(), C.c_int()
+    _check(lib.qnn_i8_plan(rows, n, k, C.byref(tile), C.byref(ranks)), "qnn_i8_plan")
+    return tile.value, ranks.value
+
+
+def rms_norm(x: torch.Tensor, gain: torch.Tensor, eps: float = 1e-6, residual: torch.Tensor | None = None,
+             stream=None) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """h = x + residual (x itself without one), y = h / sqrt(mean h^2 + eps) * gain -> (y, h, rstd); rows [rows, width]."""
+    r = _result(_on_stream(stream, lambda: (_binding or _load_binding()).rms_norm(x, gain, eps, residual, True, False)), "qnn_rms_norm")
+    return r[0], r[3], r[4]
+
+
+def rms_norm_i8(x: torch.Tensor, gain: torch.Tensor, eps: float = 1e-6, residual: torch.Tensor | None = None, both: bool = False,
+                stream=None):
+    """rms_norm with its result in 8 bits -> (I8Rows, h, rstd); both=True: (I8Rows, y, h, rstd)."""
+    r = _result(_on_stream(stream, lambda: (_binding or _load_binding()).rms_norm(x, gain, eps, residual, both, True)), "qnn_rms_norm")
+    rows = I8Rows(r[1], r[2])
+    return (rows, r[0], r[3], r[4]) if both else (rows, r[3], r[4])
+
+
+def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, gain: torch.Tensor, rstd: torch.Tensor, dh: torch.Tensor | None = None,
+                      workspace: torch.Tensor | None = None, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
+    """Gradients of rms_norm: (dx, which is the residual's too, and dgain fp32); dh = the gradient that reaches h by another way."""
+    return _result(_on_stream(stream, lambda: (_binding or _load_binding()).rms_norm_backward(dy, h, gain, rstd, dh, workspace)),
+                   "qnn_rms_norm_backward")
+
+
+class Routes(NamedTuple):
+    """Where tokens go: their experts and weights, and the plan of the products grouped by expert."""
+    experts: torch.Tensor    # int32 [tokens, top], -1: none
+    weights: torch.Tensor    # fp32 [tokens, top]
+    order: torch.Tensor      # int32 [tokens * top]: slot (token * top + choice) of each row, -1 behind the last
+    place: torch.Tensor      # int32 [tokens, top]: row of each slot, -1: none
+    offsets: torch.Tensor    # int32 [experts + 1]: an expert's first row
+
+
+ROUTE_SIGMOID, ROUTE_RENORMALISE, ROUTE_GROUPS_BY_TWO = 1, 2, 4
+
+
+def _route_flags(score: str, renormalise: bool, group_score: str = "max") -> int:
+    if score not in ("softmax", "sigmoid") or group_score not in ("max", "top2"):
+        raise ValueError("score must be softmax or sigmoid, group_score max or top2")
+    return (ROUTE_SIGMOID if score == "sigmoid" else 0) | (ROUTE_RENORMALISE if renormalise else 0) | \
+        (ROUTE_GROUPS_BY_TWO if group_score == "top2" else 0)
+
+
+def route(logits: torch.Tensor, top: int, score: str = "softmax", bias: torch.Tensor | None = None, groups: int = 1,
+          top_groups: int = 1, group_score: str = "max", renormalise: bool = True, factor: float = 1.0,
+          mask: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None) -> Routes:
+    """logits [tokens, experts] -> the `top` experts of each token, their weights and the plan (include/qnn.h, qnn_route)."""
+    flags = _route_flags(score, renormalise, group_score)
+    return Routes(*_result(_on_stream(stream, lambda: (_binding or _load_binding()).route(
+        logits, top, flags, bias, groups, top_groups, factor, mask, workspace)), "qnn_route"))
+
+
+def route_backward(dweights: torch.Tensor, logits: torch.Tensor, experts: torch.Tensor, score: str = "softmax", renormalise: bool = True,
+                   factor: float = 1.0, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Gradient of route's weights with respect to the logits: dweights fp32 and experts int32 [tokens, top] -> [tokens, experts]."""
+    flags = _route_flags(score, renormalise)
+    return _result(_on_stream(stream, lambda: (_binding or _load_binding()).route_backward(dweights, logits, experts, flags, factor, out)),
+                   "qnn_route_backward")
 
 
 def unpack_codes_f32(planes: torch.Tensor, rows: int, k: int, bits: int, transpose: bool = False, stream=None) -> torch.Tensor:
