@@ -1,6 +1,7 @@
 // Rows of real numbers as the row-wise kernels (rms_norm.cu, route.cu, i8_gemm.cu) see them: element types, packs of elements
 // that move in one access, and the code of a value in 8 bits.
 #pragma once
+#include <type_traits>
 #include "g4_format.cuh"
 
 constexpr int64_t ROWS_MAX = (1ll << 31) - 1;      // rows of a call
@@ -17,6 +18,61 @@ template <> __device__ __forceinline__ float from_f32<float>(float v) { return v
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
 
+// 16 bytes of a row as fp32 numbers, and back.
+template <class T> struct Octets {
+    static constexpr int V = 8;
+    __device__ static __forceinline__ void get(const uint4 &w, float (&f)[8]) {
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+                f[2 * i] = __uint_as_float(u[i] << 16);
+                f[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+            } else {
+                const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(&u[i]));
+                f[2 * i] = v.x;
+                f[2 * i + 1] = v.y;
+            }
+        }
+    }
+    __device__ static __forceinline__ uint4 put(const float (&f)[8]) {
+        uint32_t u[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+                const __nv_bfloat162 v = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+                u[i] = *reinterpret_cast<const uint32_t *>(&v);
+            } else {
+                const __half2 v = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+                u[i] = *reinterpret_cast<const uint32_t *>(&v);
+            }
+        }
+        return make_uint4(u[0], u[1], u[2], u[3]);
+    }
+};
+template <> struct Octets<float> {
+    static constexpr int V = 4;
+    __device__ static __forceinline__ void get(const uint4 &w, float (&f)[4]) {
+        f[0] = __uint_as_float(w.x); f[1] = __uint_as_float(w.y); f[2] = __uint_as_float(w.z); f[3] = __uint_as_float(w.w);
+    }
+    __device__ static __forceinline__ uint4 put(const float (&f)[4]) {
+        return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    }
+};
+// Numbers of a gain of type G that go with pack i of rows of T.
+template <class T, class G> __device__ __forceinline__ void gain_of_pack(const void *gain, int i, float (&f)[Octets<T>::V]) {
+    if constexpr (std::is_same<T, G>::value) {
+        Octets<T>::get(static_cast<const uint4 *>(gain)[i], f);
+    } else {
+        const uint4 *g = static_cast<const uint4 *>(gain) + 2 * i;              // fp32 beside a 2-byte type
+        float lo[4], hi[4];
+        Octets<float>::get(g[0], lo);
+        Octets<float>::get(g[1], hi);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { f[e] = lo[e]; f[4 + e] = hi[e]; }
+    }
+}
+
 // The larger one; NaN if either is (fmaxf would drop it).
 __device__ __forceinline__ float max_or_nan(float a, float b) {
     float r;
@@ -26,6 +82,7 @@ __device__ __forceinline__ float max_or_nan(float a, float b) {
 
 // A row's scale from its largest magnitude m: m / 127, at least the smallest normal number, so that 1 / scale is finite and a row
 // of zeros decodes to zeros.  NaN for a row that holds an infinity or NaN.
+constexpr float TO_NEAREST = 12582912.0f;          // 1.5 * 2^23: a sum with it holds the nearest whole number in its low bits
 struct RowScale {
     float scale, inverse;
     __device__ __forceinline__ explicit RowScale(float m) {
@@ -40,5 +97,17 @@ struct RowScale {
         float r = rintf(t);
         if (fabsf(__fadd_rn(t, -r)) > 0.4999f) r = rintf(__fdiv_rn(v, scale));
         return min(max(__float2int_rn(r), -127), 127);
+    }
+    // The same as the low byte of a word; any byte where the scale is NaN.  (|v| <= 127 scale: no clamp is needed.)
+    __device__ __forceinline__ uint32_t code_byte(float v) const {
+        const float t = __fmul_rn(v, inverse);
+        float r = __fadd_rn(t, TO_NEAREST);
+        if (fabsf(__fadd_rn(t, -__fadd_rn(r, -TO_NEAREST))) > 0.4999f) r = __fadd_rn(rintf(__fdiv_rn(v, scale)), TO_NEAREST);
+        return __float_as_uint(r);
+    }
+    // Bytes of codes, zeros where the scale is NaN.
+    __device__ __forceinline__ uint32_t word(uint32_t a, uint32_t b, uint32_t c, uint32_t d) const {
+        const uint32_t w = __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+        return inverse != 0.0f ? w : 0u;
     }
 };

@@ -52,67 +52,68 @@ __device__ __forceinline__ float norm_factor(float sum, const NormParams &p) {
     return __frcp_rn(__fsqrt_rn(__fadd_rn(__fdiv_rn(sum, (float)p.width), p.eps)));
 }
 
+__device__ __forceinline__ uint32_t add_pair(uint32_t a, uint32_t b, __nv_bfloat16) {
+    const __nv_bfloat162 v = __hadd2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ uint32_t add_pair(uint32_t a, uint32_t b, __half) {
+    const __half2 v = __hadd2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ uint32_t add_pair(uint32_t a, uint32_t b, float) { return __float_as_uint(__fadd_rn(__uint_as_float(a), __uint_as_float(b))); }
+template <class T> __device__ __forceinline__ uint4 add_pack(uint4 a, uint4 b) {
+    return make_uint4(add_pair(a.x, b.x, T()), add_pair(a.y, b.y, T()), add_pair(a.z, b.z, T()), add_pair(a.w, b.w, T()));
+}
+
 // A row by `blockDim.x` threads (y: rows of a block, more than one for rows of a single warp).  Each thread holds NV packs of 16
-// bytes.  NORM = false: codes of the rows themselves.
+// bytes, as products with the gain.  NORM = false: codes of the rows themselves.
 template <class T, class G, int NV, bool NORM>
-__global__ void __launch_bounds__(NV == 1 ? 1024 : 512) norm_rows_kernel(const NormParams p) {
+__global__ void __launch_bounds__(NV == 1 ? 1024 : 512, NV == 2 ? 2 : 1) norm_rows_kernel(const NormParams p) {
     __shared__ float parts[2][32];
     start_next();
     wait_for_previous();
     const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
     if (row >= p.rows) return;                                      // (whole warps: blocks of several rows have one warp a row)
-    constexpr int V = 16 / sizeof(T);
+    typedef Octets<T> O;
+    constexpr int V = O::V;
     const int packs = p.width / V, step = blockDim.x;
-    typedef Pack<T, V> PT;
-    typedef Pack<G, V> PG;
-    PT v[NV], r[NV];
-    PG g[NV];
-    const T *x = static_cast<const T *>(p.x) + row * p.ldx;
+    const uint4 *x = reinterpret_cast<const uint4 *>(static_cast<const T *>(p.x) + row * p.ldx);
+    uint4 h[NV], r[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int i = threadIdx.x + j * step;
-        if (i < packs) v[j] = reinterpret_cast<const PT *>(x)[i];
+        h[j] = i < packs ? x[i] : make_uint4(0, 0, 0, 0);
     }
-    if constexpr (NORM) {
-        if (p.residual) {
-            const T *res = static_cast<const T *>(p.residual) + row * p.ldr;
+    if (NORM && p.residual) {
+        const uint4 *res = reinterpret_cast<const uint4 *>(static_cast<const T *>(p.residual) + row * p.ldr);
+        uint4 *out = reinterpret_cast<uint4 *>(static_cast<T *>(p.h) + row * p.ldh);
 #pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                const int i = threadIdx.x + j * step;
-                if (i < packs) r[j] = reinterpret_cast<const PT *>(res)[i];
-            }
+        for (int j = 0; j < NV; ++j) {
+            const int i = threadIdx.x + j * step;
+            r[j] = i < packs ? res[i] : make_uint4(0, 0, 0, 0);
         }
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int i = threadIdx.x + j * step;
-            if (i < packs) g[j] = static_cast<const PG *>(p.gain)[i];
-        }
-        if (p.residual) {
-            T *h = static_cast<T *>(p.h) + row * p.ldh;
-#pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                const int i = threadIdx.x + j * step;
-                if (i < packs) {
-#pragma unroll
-                    for (int e = 0; e < V; ++e) v[j].e[e] = from_f32<T>(__fadd_rn(to_f32(v[j].e[e]), to_f32(r[j].e[e])));
-                    reinterpret_cast<PT *>(h)[i] = v[j];
-                }
-            }
+            h[j] = add_pack<T>(h[j], r[j]);
+            if (i < packs) out[i] = h[j];
         }
     }
-    float sum = 0.0f, most = 0.0f;
+    float v[NV][V], sum = 0.0f, most = 0.0f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        if (threadIdx.x + j * step < packs)
+        O::get(h[j], v[j]);
+        if constexpr (NORM) {
+            float g[V];
+            gain_of_pack<T, G>(p.gain, min((int)threadIdx.x + j * step, packs - 1), g);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                float a = to_f32(v[j].e[e]);
-                if constexpr (NORM) {
-                    sum = __fmaf_rn(a, a, sum);
-                    a = __fmul_rn(a, to_f32(g[j].e[e]));
-                }
-                most = max_or_nan(most, fabsf(a));
+                sum = __fmaf_rn(v[j][e], v[j][e], sum);
+                v[j][e] = __fmul_rn(v[j][e], g[e]);
             }
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) most = max_or_nan(most, fabsf(v[j][e]));
     }
     block_sum_and_max<NORM>(sum, most, parts);
     float rstd = 1.0f;
@@ -121,35 +122,32 @@ __global__ void __launch_bounds__(NV == 1 ? 1024 : 512) norm_rows_kernel(const N
         if (p.rstd && threadIdx.x == 0) p.rstd[row] = rstd;
         most = __fmul_rn(most, rstd);
         if (p.y) {
-            T *y = static_cast<T *>(p.y) + row * p.ldy;
+            uint4 *y = reinterpret_cast<uint4 *>(static_cast<T *>(p.y) + row * p.ldy);
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 const int i = threadIdx.x + j * step;
-                if (i < packs) {
-                    PT o;
+                float o[V];
 #pragma unroll
-                    for (int e = 0; e < V; ++e) o.e[e] = from_f32<T>(__fmul_rn(__fmul_rn(to_f32(v[j].e[e]), to_f32(g[j].e[e])), rstd));
-                    reinterpret_cast<PT *>(y)[i] = o;
-                }
+                for (int e = 0; e < V; ++e) o[e] = __fmul_rn(v[j][e], rstd);
+                if (i < packs) y[i] = O::put(o);
             }
         }
     }
     if (!NORM || p.codes) {
         const RowScale s(most);
         if (threadIdx.x == 0) p.scales[row] = s.scale;
-        int8_t *codes = p.codes + row * p.ldc;
+        uint32_t *codes = reinterpret_cast<uint32_t *>(p.codes + row * p.ldc);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int i = threadIdx.x + j * step;
-            if (i < packs) {
-                Pack<int8_t, V> o;
+            uint32_t c[V];
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    float a = to_f32(v[j].e[e]);
-                    if constexpr (NORM) a = __fmul_rn(__fmul_rn(a, to_f32(g[j].e[e])), rstd);
-                    o.e[e] = (int8_t)s.code(a);
-                }
-                reinterpret_cast<Pack<int8_t, V> *>(codes)[i] = o;
+            for (int e = 0; e < V; ++e) c[e] = NORM ? __float_as_uint(__fmaf_rn(__fmul_rn(v[j][e], rstd), s.inverse, TO_NEAREST)) : s.code_byte(v[j][e]);
+            if (i < packs) {
+                if constexpr (V == 8)
+                    reinterpret_cast<uint2 *>(codes)[i] = make_uint2(s.word(c[0], c[1], c[2], c[3]), s.word(c[4], c[5], c[6], c[7]));
+                else
+                    codes[i] = s.word(c[0], c[1], c[2], c[3]);
             }
         }
     }
@@ -240,28 +238,64 @@ bool in_packs(const void *p, int type, int64_t ld) { return qnn_aligned(p, 16) &
 
 // ------------------------------------------------------------------------------------------------ codes back to numbers
 
-template <class T, int V>
+// A byte as a number: xor 128 makes it 0 .. 255, which the mantissa of 2^23 takes as it is.
+__device__ __forceinline__ float byte_value(uint32_t word, int i) {
+    return __fadd_rn(__uint_as_float(__byte_perm(word ^ 0x80808080u, 0x4B000000u, 0x7540 + i)), -8388736.0f);      // 2^23 + 128
+}
+// Sixteen codes of ROWS rows by a thread, all loaded first.
+template <class T, int ROWS>
 __global__ void __launch_bounds__(256) decode_kernel(const int8_t *codes, const float *scales, int64_t rows, int width, int64_t ldc, T *out, int64_t ldo) {
     start_next();
     wait_for_previous();
-    const int packs = width / V, i = blockIdx.x * 256 + threadIdx.x;
-    if (i >= packs) return;
-    for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
-        const Pack<int8_t, V> c = reinterpret_cast<const Pack<int8_t, V> *>(codes + row * ldc)[i];
-        const float s = scales[row];
-        Pack<T, V> o;
+    typedef Octets<T> O;
+    const int i = blockIdx.x * blockDim.x + threadIdx.x;
+    if (i * 16 >= width) return;
+    for (int64_t row = (int64_t)blockIdx.y * ROWS; row < rows; row += (int64_t)gridDim.y * ROWS) {
+        uint4 c[ROWS];
+        float s[ROWS];
 #pragma unroll
-        for (int e = 0; e < V; ++e) o.e[e] = from_f32<T>(__fmul_rn((float)c.e[e], s));
-        reinterpret_cast<Pack<T, V> *>(out + row * ldo)[i] = o;
+        for (int r = 0; r < ROWS; ++r) {
+            const int64_t at = row + r < rows ? row + r : rows - 1;
+            c[r] = reinterpret_cast<const uint4 *>(codes + at * ldc)[i];
+            s[r] = scales[at];
+        }
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            if (row + r >= rows) break;
+            const uint32_t w[4] = {c[r].x, c[r].y, c[r].z, c[r].w};
+            uint4 *dst = reinterpret_cast<uint4 *>(out + (row + r) * ldo) + i * (16 / O::V);
+#pragma unroll
+            for (int q = 0; q < 16 / O::V; ++q) {
+                float f[O::V];
+#pragma unroll
+                for (int e = 0; e < O::V; ++e) f[e] = __fmul_rn(byte_value(w[(q * O::V + e) / 4], (q * O::V + e) % 4), s[r]);
+                dst[q] = O::put(f);
+            }
+        }
+    }
+}
+template <class T>
+__global__ void __launch_bounds__(256) decode_any_kernel(const int8_t *codes, const float *scales, int64_t rows, int width, int64_t ldc, T *out, int64_t ldo) {
+    start_next();
+    wait_for_previous();
+    for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
+        const float s = scales[row];
+#pragma unroll 4
+        for (int i = blockIdx.x * 256 + threadIdx.x; i < width; i += gridDim.x * 256) out[row * ldo + i] = from_f32<T>(__fmul_rn((float)codes[row * ldc + i], s));
     }
 }
 template <class T>
 int decode(const int8_t *codes, const float *scales, int64_t rows, int width, int64_t ldc, void *out, int64_t ldo, bool vec, cudaStream_t st) {
-    constexpr int V = 16 / sizeof(T);
     T *o = static_cast<T *>(out);
-    const unsigned ys = (unsigned)(rows < 65535 ? rows : 65535);
-    if (vec) return launch_early(decode_kernel<T, V>, dim3((width / V + 255) / 256, ys), dim3(256), st, codes, scales, rows, width, ldc, o, ldo);
-    return launch_early(decode_kernel<T, 1>, dim3((width + 255) / 256, ys), dim3(256), st, codes, scales, rows, width, ldc, o, ldo);
+    if (!vec) {
+        const unsigned ys = (unsigned)(rows < 65535 ? rows : 65535);
+        return launch_early(decode_any_kernel<T>, dim3((width + 1023) / 1024, ys), dim3(256), st, codes, scales, rows, width, ldc, o, ldo);
+    }
+    const int packs = width / 16, threads = packs < 256 ? (packs + 31) / 32 * 32 : 256;
+    const unsigned xs = (unsigned)((packs + threads - 1) / threads);
+    if (rows < 4 * 148) return launch_early(decode_kernel<T, 1>, dim3(xs, (unsigned)rows), dim3(threads), st, codes, scales, rows, width, ldc, o, ldo);
+    const int64_t ys = (rows + 3) / 4;
+    return launch_early(decode_kernel<T, 4>, dim3(xs, (unsigned)(ys < 65535 ? ys : 65535)), dim3(threads), st, codes, scales, rows, width, ldc, o, ldo);
 }
 
 // ------------------------------------------------------------------------------------------------ backward products
@@ -276,82 +310,163 @@ struct NormBackParams {
     int width;
     void *dx;
     float *sums;                              // [gridDim.x][width]
+    unsigned int *err;
+    unsigned int wait_limit;
 };
 
+// What a pack of a row adds to the row's sum, and its u = h * rstd.
+template <class T> struct BackPack {
+    static constexpr int V = Octets<T>::V;
+    float dy[V], u[V];
+    __device__ __forceinline__ void get(const uint4 &d, const uint4 &h, float r) {
+        Octets<T>::get(d, dy);
+        Octets<T>::get(h, u);
+#pragma unroll
+        for (int e = 0; e < V; ++e) u[e] = __fmul_rn(u[e], r);
+    }
+    __device__ __forceinline__ void add(const float (&g)[V], float &dot, float (&sum)[V]) const {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            dot = __fmaf_rn(__fmul_rn(dy[e], g[e]), u[e], dot);
+            sum[e] = __fmaf_rn(dy[e], u[e], sum[e]);
+        }
+    }
+    __device__ __forceinline__ uint4 result(const float (&g)[V], float mean, float r, const uint4 &other) const {
+        float o[V], dh[V];
+        Octets<T>::get(other, dh);                              // (zeros where there is none)
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] = __fadd_rn(__fmul_rn(__fmaf_rn(-u[e], mean, __fmul_rn(dy[e], g[e])), r), dh[e]);
+        return Octets<T>::put(o);
+    }
+};
+
+// Rows of up to 32 * NV packs, a warp each: no barrier but the last, which adds the warps' sums of the gain in order.
+constexpr int BACK_WARPS = 8;
 template <class T, class G, int NV>
-__global__ void __launch_bounds__(NV == 1 ? 256 : 512) norm_back_kernel(const NormBackParams p) {
-    __shared__ float parts[2][32];
+__global__ void __launch_bounds__(BACK_WARPS * 32, 2) norm_back_warps_kernel(const NormBackParams p) {
+    __shared__ float all[BACK_WARPS][32 * NV * Octets<T>::V];
     start_next();
     wait_for_previous();
-    constexpr int V = 16 / sizeof(T);
-    typedef Pack<T, V> PT;
-    typedef Pack<G, V> PG;
-    const int packs = p.width / V, step = blockDim.x;
-    float sum[NV][V];
-    PG g[NV];
+    constexpr int V = Octets<T>::V;
+    const int packs = p.width / V, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    float g[NV][V], sum[NV][V];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        const int i = threadIdx.x + j * step;
-        if (i < packs) g[j] = static_cast<const PG *>(p.gain)[i];
+        gain_of_pack<T, G>(p.gain, min(lane + 32 * j, packs - 1), g[j]);
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum[j][e] = 0.0f;
+    }
+    for (int64_t row = (int64_t)blockIdx.x * BACK_WARPS + warp; row < p.rows; row += (int64_t)gridDim.x * BACK_WARPS) {
+        const uint4 *dys = reinterpret_cast<const uint4 *>(static_cast<const T *>(p.dy) + row * p.lddy);
+        const uint4 *hs = reinterpret_cast<const uint4 *>(static_cast<const T *>(p.h) + row * p.ldh);
+        const uint4 *dhs = reinterpret_cast<const uint4 *>(static_cast<const T *>(p.dh) + row * p.lddh);
+        uint4 *dxs = reinterpret_cast<uint4 *>(static_cast<T *>(p.dx) + row * p.lddx);
+        const float r = p.rstd[row];
+        uint4 dy[NV], h[NV], dh[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int i = lane + 32 * j;
+            dy[j] = i < packs ? dys[i] : zero;
+            h[j] = i < packs ? hs[i] : zero;
+            dh[j] = p.dh && i < packs ? dhs[i] : zero;
+        }
+        float dot = 0.0f;
+        BackPack<T> b[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            b[j].get(dy[j], h[j], r);
+            b[j].add(g[j], dot, sum[j]);
+        }
+        const float mean = __fdiv_rn(warp_sum(dot), (float)p.width);
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (lane + 32 * j < packs) dxs[lane + 32 * j] = b[j].result(g[j], mean, r, dh[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < V; ++e) all[warp][(lane + 32 * j) * V + e] = sum[j][e];
+    __syncthreads();
+    for (int c = threadIdx.x; c < p.width; c += BACK_WARPS * 32) {
+        float s = all[0][c];
+#pragma unroll
+        for (int w = 1; w < BACK_WARPS; ++w) s = __fadd_rn(s, all[w][c]);
+        p.sums[(int64_t)blockIdx.x * p.width + c] = s;
+    }
+}
+
+// Wider rows, a block each, NV packs a thread.  Rows come through a ring in shared memory by bulk copies, issued as soon as a stage
+// has been read, so that the next rows are under way while one is summed over the block's barrier.
+template <class T, class G, int NV>
+__global__ void __launch_bounds__(512) norm_back_kernel(const NormBackParams p, int stages, int stage_bytes) {
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ float parts[2][16];
+    __shared__ uint64_t full[8];
+    __shared__ uint32_t abort_word;
+    constexpr int V = Octets<T>::V;
+    const int packs = p.width / V, step = blockDim.x, row_bytes = p.width * (int)sizeof(T);
+    volatile uint32_t *abort_flag = &abort_word;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < stages; ++s) mbar_init(&full[s], 1);
+        *abort_flag = 0;
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    __syncthreads();
+    start_next();
+    wait_for_previous();
+    auto load = [&](int64_t row, int s) {                       // by one thread
+        uint8_t *dst = ring + s * stage_bytes;
+        mbar_expect_tx(&full[s], (p.dh ? 3 : 2) * row_bytes);
+        bulk_load(dst, static_cast<const T *>(p.dy) + row * p.lddy, row_bytes, &full[s]);
+        bulk_load(dst + row_bytes, static_cast<const T *>(p.h) + row * p.ldh, row_bytes, &full[s]);
+        if (p.dh) bulk_load(dst + 2 * row_bytes, static_cast<const T *>(p.dh) + row * p.lddh, row_bytes, &full[s]);
+    };
+    if (threadIdx.x == 0)
+        for (int s = 0; s < stages && blockIdx.x + (int64_t)s * gridDim.x < p.rows; ++s) load(blockIdx.x + (int64_t)s * gridDim.x, s);
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    float g[NV][V], sum[NV][V];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        gain_of_pack<T, G>(p.gain, min((int)threadIdx.x + j * step, packs - 1), g[j]);
 #pragma unroll
         for (int e = 0; e < V; ++e) sum[j][e] = 0.0f;
     }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    Ring at;
     int side = 0;
     for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, side ^= 1) {
-        PT dy[NV], h[NV], dh[NV];
-        const T *dys = static_cast<const T *>(p.dy) + row * p.lddy, *hs = static_cast<const T *>(p.h) + row * p.ldh;
+        const float r = p.rstd[row];
+        bool ok = short_wait(&full[at.s], at.ph, abort_flag, 1, p.err, p.wait_limit);
+        const uint32_t src = smem_u32(ring) + at.s * stage_bytes;
+        uint4 dh[NV];
+        BackPack<T> b[NV];
         float dot = 0.0f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int i = threadIdx.x + j * step;
-            if (i < packs) {
-                dy[j] = reinterpret_cast<const PT *>(dys)[i];
-                h[j] = reinterpret_cast<const PT *>(hs)[i];
-            }
+            const bool in = i < packs;
+            b[j].get(in ? lds_128(src + i * 16) : zero, in ? lds_128(src + row_bytes + i * 16) : zero, r);
+            dh[j] = in && p.dh ? lds_128(src + 2 * row_bytes + i * 16) : zero;
+            b[j].add(g[j], dot, sum[j]);
         }
-        if (p.dh) {
-            const T *dhs = static_cast<const T *>(p.dh) + row * p.lddh;
-#pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                const int i = threadIdx.x + j * step;
-                if (i < packs) dh[j] = reinterpret_cast<const PT *>(dhs)[i];
-            }
-        }
-        const float r = p.rstd[row];
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-            if (threadIdx.x + j * step < packs)
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float d = to_f32(dy[j].e[e]), u = __fmul_rn(to_f32(h[j].e[e]), r);
-                    dot = __fmaf_rn(__fmul_rn(d, to_f32(g[j].e[e])), u, dot);
-                    sum[j][e] = __fmaf_rn(d, u, sum[j][e]);
-                }
         dot = warp_sum(dot);
-        if (warps > 1) {
-            if (lane == 0) parts[side][warp] = dot;               // (two sides: the next row's sums do not wait for this one's readers)
-            __syncthreads();
-            dot = warp_sum(lane < warps ? parts[side][lane] : 0.0f);
-        }
-        const float mean = __fdiv_rn(dot, (float)p.width);
-        T *dxs = static_cast<T *>(p.dx) + row * p.lddx;
+        if (lane == 0) parts[side][warp] = dot;                 // (two sides: the next row's sums do not wait for this one's readers)
+        if (!__syncthreads_and(ok)) break;                      // all leave together; the copies in flight have been waited for or ...
+        if (threadIdx.x == 0 && row + (int64_t)stages * gridDim.x < p.rows) load(row + (int64_t)stages * gridDim.x, at.s);
+        at.next(stages);
+        const float mean = __fdiv_rn(warp_sum(lane < warps ? parts[side][lane] : 0.0f), (float)p.width);
+        uint4 *dxs = reinterpret_cast<uint4 *>(static_cast<T *>(p.dx) + row * p.lddx);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int i = threadIdx.x + j * step;
-            if (i < packs) {
-                PT o;
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float u = __fmul_rn(to_f32(h[j].e[e]), r);
-                    float d = __fmul_rn(__fmaf_rn(-u, mean, __fmul_rn(to_f32(dy[j].e[e]), to_f32(g[j].e[e]))), r);
-                    if (p.dh) d = __fadd_rn(d, to_f32(dh[j].e[e]));
-                    o.e[e] = from_f32<T>(d);
-                }
-                reinterpret_cast<PT *>(dxs)[i] = o;
-            }
+            if (i < packs) dxs[i] = b[j].result(g[j], mean, r, dh[j]);
         }
     }
+    // ... get some time to land
+    if (*abort_flag)
+#pragma unroll 1
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int i = threadIdx.x + j * step;
@@ -422,7 +537,24 @@ int back_blocks(int64_t rows) { return (int)(rows < 296 ? rows : 296); }
 
 template <class T, class G, int NV>
 int back_launch(const NormBackParams &p, int packs, cudaStream_t st) {
-    return launch_early(norm_back_kernel<T, G, NV>, dim3(back_blocks(p.rows)), dim3(whole_warps((packs + NV - 1) / NV)), st, p);
+    auto kernel = norm_back_kernel<T, G, NV>;
+    const int stage = (p.dh ? 3 : 2) * p.width * (int)sizeof(T), fit = 100 * 1024 / stage, stages = fit < 2 ? 2 : fit < 8 ? fit : 8;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024) != cudaSuccess) return QNN_E_CUDA;
+    LaunchAttrs attrs(1);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(back_blocks(p.rows));
+    cfg.blockDim = dim3(whole_warps((packs + NV - 1) / NV));
+    cfg.dynamicSmemBytes = stages * stage;
+    cfg.stream = st;
+    cfg.attrs = attrs.a;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, p, stages, stage) == cudaSuccess) return QNN_OK;
+    cudaGetLastError();
+    return QNN_E_CUDA;
+}
+template <class T, class G, int NV>
+int back_warps_launch(const NormBackParams &p, cudaStream_t st) {
+    return launch_early(norm_back_warps_kernel<T, G, NV>, dim3(back_blocks(p.rows)), dim3(BACK_WARPS * 32), st, p);
 }
 template <class T, class G>
 int back_any_launch(const NormBackParams &p, cudaStream_t st) {
@@ -446,7 +578,9 @@ int back_typed(const NormBackParams &p, bool vec, float *dgain, cudaStream_t st)
     const int packs = p.width / (16 / (int)sizeof(T));
     int rc;
     if (!vec || packs > 2048) rc = back_any_launch<T, G>(p, st);
-    else if (packs <= 256) rc = back_launch<T, G, 1>(p, packs, st);
+    else if (packs <= 32) rc = back_warps_launch<T, G, 1>(p, st);
+    else if (packs <= 64) rc = back_warps_launch<T, G, 2>(p, st);
+    else if (packs <= 128) rc = back_launch<T, G, 1>(p, packs, st);
     else if (packs <= 1024) rc = back_launch<T, G, 2>(p, packs, st);
     else rc = back_launch<T, G, 4>(p, packs, st);
     if (rc != QNN_OK) return rc;
@@ -508,7 +642,7 @@ extern "C" int qnn_i8_decode(const int8_t *codes, const float *scales, int64_t r
     int rc = check_codes(codes, scales, ldc, width);
     if (rc == QNN_OK) rc = check_real(out, type, ldo, width);
     if (rc != QNN_OK) return rc;
-    const bool vec = width * g4_type_bytes(type) % 16 == 0 && in_packs(out, type, ldo);
+    const bool vec = width % 16 == 0 && in_packs(out, type, ldo);
     return by_types(type, type, [&](auto t, auto) { return decode<decltype(t)>(codes, scales, rows, width, ldc, out, ldo, vec, static_cast<cudaStream_t>(stream)); });
 }
 
@@ -535,6 +669,7 @@ extern "C" int qnn_rms_norm_backward(const void *dy, int type, int64_t rows, int
     if (!qnn_aligned(workspace, 256) || !qnn_aligned(rstd, 4)) return QNN_E_ALIGN;
     const bool vec = width * g4_type_bytes(type) % 16 == 0 && in_packs(dy, type, lddy) && in_packs(h, type, ldh) && in_packs(dx, type, lddx) &&
                      (!dh || in_packs(dh, type, lddh)) && qnn_aligned(gain, 16);
-    const NormBackParams p{dy, h, gain, dh, rstd, lddy, ldh, lddh, lddx, rows, width, dx, static_cast<float *>(workspace)};
+    const NormBackParams p{dy, h, gain, dh, rstd, lddy, ldh, lddh, lddx, rows, width, dx, static_cast<float *>(workspace), qnn_tc_error_word(), WAIT_LIMIT};
+    if (!p.err) return QNN_E_CUDA;
     return by_types(type, gain_type, [&](auto t, auto g) { return back_typed<decltype(t), decltype(g)>(p, vec, dgain, st); });
 }

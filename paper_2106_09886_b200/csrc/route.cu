@@ -6,9 +6,9 @@
 // with a known error bound: whenever two keys whose order matters are nearer than that, the warp takes the token again with keys
 // in 64 bits.  The choice is therefore that of 64-bit scores, at the cost of fp32 ones.
 //
-// Plan.  A counting sort: a block takes a run of tokens, counts its slots by expert, and writes the counts; behind all of them,
-// the block that ranks the same slots adds up the counts of the runs ahead.  Slots of an expert keep their order, and nothing
-// depends on the order in which blocks run.  Few tokens: one block does both.
+// Plan.  A counting sort in three launches: a block takes a run of tokens and counts its slots by expert; the counts are added up
+// over the runs (few runs: by the last launch); a block ranks the slots of its run.  Slots of an expert keep their order, and nothing depends on the order in
+// which blocks run.  Few tokens: one block does it all.
 //
 // Bound: reading the logits and issue (some 50 instructions for each of a token's choices).
 #include "real_rows.cuh"
@@ -20,7 +20,10 @@ constexpr int ROUTE_MAX_EXPERTS = 1024, ROUTE_MAX_TOP = 32, ROUTE_MAX_GROUPS = 3
 constexpr int PLAN_THREADS = 1024;
 // Threads of a block whose lanes hold V experts each: V numbers of four kinds have to fit the registers.
 __host__ __device__ constexpr int choose_threads(int v) { return v <= 8 ? 1024 : 512; }
-constexpr int RANK_WARPS = 8;                                 // that rank a run's slots, each with its own counts
+// Warps that rank a run's slots, each with counts of its own.
+__host__ __device__ constexpr int rank_warps(int experts) { return experts <= 256 ? 32 : experts <= 512 ? 16 : 8; }
+constexpr int MAX_RUNS = 148;                                 // of tokens, a block each
+constexpr int SCANNED_RUNS = 32;                              // up to so many a block adds up the runs ahead of it itself
 constexpr int64_t ROUTE_MAX_SLOTS = (1ll << 31) - 1;
 
 struct RouteParams {
@@ -31,21 +34,30 @@ struct RouteParams {
     bool sigmoid, renormalise, by_sums;                       // by_sums: groups are judged by the sum of their two largest keys
     const float *bias;
     int groups, top_groups, each, lanes, pitch;               // experts, lanes and key pitch of a group
+    uint32_t group_of;                                        // ceil(2^20 / each): e / each = e * group_of >> 20 for e < 1024
+    bool whole;                                               // groups of 32: register v holds group v
     float factor;
     const uint8_t *mask;
     int32_t *chosen;
     float *weights;
     int32_t *order, *place, *offsets;                         // NULL: no plan
-    int32_t *counts;                                          // [runs][experts]
+    int32_t *counts;                                          // [experts][runs], behind them [experts] rows of each
     int runs, run;                                            // tokens of a run
 };
 
-// Keys as unsigned numbers of the same order; 0 is kept for "not to be chosen" (NaN and -infinity).
+// Numbers as unsigned ones of the same order (not for NaN).  An expert that is not to be chosen has key -infinity.
 __device__ __forceinline__ uint32_t ordered(float v) {
-    const uint32_t b = __float_as_uint(__fadd_rn(v, 0.0f));           // (-0 is 0)
-    return !(v > __int_as_float(0xFF800000)) ? 0u : (b & 0x80000000u) ? ~b : b | 0x80000000u;
+    const uint32_t b = __float_as_uint(v);
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
-__device__ __forceinline__ float from_ordered(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
+__device__ __forceinline__ float from_ordered(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+constexpr uint32_t NO_KEY = 0x007FFFFFu;                      // ordered(-infinity); below the key of any finite number whatever its lowest bits
+constexpr uint32_t INFINITE_KEY = 0xFF800000u;                // ordered(infinity); NaN (as max.NaN gives it) is above
+__device__ __forceinline__ float reciprocal(float v) {       // off by one step at most; 0 where the result would be subnormal
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
 __device__ __forceinline__ unsigned long long ordered(double v) {
     const unsigned long long b = (unsigned long long)__double_as_longlong(v + 0.0);
     return !(v > __longlong_as_double(0xFFF0000000000000ll)) ? 0ull : (b >> 63) ? ~b : b | 0x8000000000000000ull;
@@ -65,7 +77,6 @@ __device__ __forceinline__ float warp_most(float v) {
     for (int d = 16; d; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
     return v;
 }
-__device__ __forceinline__ uint32_t warp_max_key(uint32_t k) { return __reduce_max_sync(0xffffffffu, k); }
 __device__ __forceinline__ unsigned long long warp_max_key(unsigned long long k) {
     const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(k >> 32));
     const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
@@ -96,33 +107,55 @@ template <int V> __device__ __forceinline__ void load_row(const void *p, int typ
     }
 }
 
-// What decides between experts and groups, as numbers of type K (float, or double where fp32 is not enough).
-template <class K> struct Margin {                            // two keys nearer than this may be in the wrong order
+// Two fp32 keys nearer than this may be in the wrong order.
+struct Margin {
     float relative, bias;
-    __device__ __forceinline__ bool close(K a, K b) const {
-        if constexpr (sizeof(K) == 8) return false;
-        else return __fadd_rn(a, -b) <= __fmaf_rn(relative, __fadd_rn(fmaxf(fabsf(a), fabsf(b)), bias), 1e-37f);
+    __device__ __forceinline__ bool close(float a, float b) const {
+        return __fadd_rn(a, -b) <= __fmaf_rn(relative, __fadd_rn(fmaxf(fabsf(a), fabsf(b)), bias), 1e-37f);
     }
 };
+__device__ __forceinline__ int group_of(const RouteParams &p, int e) { return (int)((uint32_t)e * p.group_of >> 20); }
 
-// Experts of groups that are not among the best top_groups get key 0 in `keys`.  worth: keys[] as numbers, or the scores where
+// worth: of lane's group (-infinity in lanes without one), which lies at lane `at` of 32, every `stride`-th lane holding one.
+// Returns the lanes whose groups stay; `narrow` whether the worst of them is too close to the best of the others.
+template <class K> __device__ __forceinline__ unsigned best_groups(const RouteParams &p, K worth, bool holds, int stride, Margin margin, bool &narrow) {
+    const int lane = threadIdx.x & 31;
+    int better = 0;
+#pragma unroll 4
+    for (int g = 0; g < p.groups; ++g) {
+        const K other = __shfl_sync(0xffffffffu, worth, g * stride);
+        better += other > worth || (other == worth && g * stride < lane);
+    }
+    const unsigned stay = __ballot_sync(0xffffffffu, holds && better < p.top_groups);
+    narrow = false;
+    if constexpr (sizeof(K) == 4) {
+        const uint32_t key = holds ? ordered(__fadd_rn(worth, 0.0f)) : 0u;
+        const bool mine = stay >> lane & 1u;
+        const float worst = from_ordered(__reduce_min_sync(0xffffffffu, mine ? key : 0xffffffffu));
+        const uint32_t next = __reduce_max_sync(0xffffffffu, mine ? 0u : key);
+        margin.bias *= 2.0f;                                  // sums of two keys
+        margin.relative *= 2.0f;
+        narrow = next > NO_KEY && margin.close(worst, from_ordered(next));      // (else only groups without experts go)
+    }
+    return stay;
+}
+
+// Experts of groups that are not among the best top_groups get no_key in `keys`.  worth: the keys as numbers, or the scores where
 // sums of them decide and the keys are logits.  Returns whether the decision was too close.
 template <class K, class U, int V>
-__device__ __forceinline__ bool keep_groups(const RouteParams &p, const K (&worth)[V], U (&keys)[V], K *scratch, Margin<K> margin) {
+__device__ __forceinline__ bool keep_groups(const RouteParams &p, const K (&worth)[V], U (&keys)[V], U no_key, K *scratch, Margin margin) {
     const int lane = threadIdx.x & 31;
     const K none = -(K)__int_as_float(0x7F800000);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int e = lane + 32 * v;
-        if (e < p.experts) {
-            const int g = e / p.each;
-            scratch[g * p.pitch + e - g * p.each] = keys[v] ? worth[v] : none;
-        }
+        if (e < p.experts) scratch[e + group_of(p, e) * (p.pitch - p.each)] = keys[v] != no_key ? worth[v] : none;
     }
     __syncwarp();
     const int group = lane / p.lanes, sub = lane - group * p.lanes;
     K first = none, second = none;
     if (group < p.groups)
+#pragma unroll 4
         for (int i = sub; i < p.each; i += p.lanes) {
             const K k = scratch[group * p.pitch + i];
             second = k > first ? first : (k > second ? k : second);
@@ -136,55 +169,64 @@ __device__ __forceinline__ bool keep_groups(const RouteParams &p, const K (&wort
         second = low > second ? low : second;
         first = high;
     }
-    const K mine = p.by_sums ? first + second : first;
-    int better = 0;
-    bool close = false;
-    for (int g = 0; g < p.groups; ++g) {
-        const K other = __shfl_sync(0xffffffffu, mine, g * p.lanes);
-        better += other > mine || (other == mine && g < group);
-    }
-    const bool kept = group < p.groups && better < p.top_groups;
-    if constexpr (sizeof(K) == 4) {
-        // the worst group that stays against the best that goes
-        float worst = kept ? mine : __int_as_float(0x7F800000), best = group < p.groups && !kept ? mine : none;
+    bool close;
+    const unsigned stay = best_groups<K>(p, p.by_sums ? first + second : first, group < p.groups && sub == 0, p.lanes, margin, close);
 #pragma unroll
-        for (int d = 16; d; d >>= 1) {
-            worst = fminf(worst, __shfl_xor_sync(0xffffffffu, worst, d));
-            best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, d));
+    for (int v = 0; v < V; ++v)
+        if (lane + 32 * v < p.experts && !((stay >> (group_of(p, lane + 32 * v) * p.lanes)) & 1u)) keys[v] = no_key;
+    return close;
+}
+// The same for groups of 32 experts: register v of the lanes holds group v, worth as ordered numbers.  The two largest of every group
+// by one exchange that halves the registers at each of its first steps: lane l ends up with group l / (32 / V).
+template <int V>
+__device__ __forceinline__ bool keep_whole_groups(const RouteParams &p, const uint32_t (&worth)[V], uint32_t (&keys)[V], Margin margin) {
+    const int lane = threadIdx.x & 31;
+    uint32_t first[V], second[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) { first[v] = worth[v]; second[v] = NO_KEY; }
+#pragma unroll
+    for (int half = V / 2, d = 16; d >= 1; half /= 2, d /= 2) {
+        if (half >= 1) {
+            const bool upper = lane & d;
+#pragma unroll
+            for (int v = 0; v < half; ++v) {
+                const uint32_t a = upper ? first[v] : first[v + half], mine = upper ? first[v + half] : first[v], b = __shfl_xor_sync(0xffffffffu, a, d);
+                uint32_t low = min(mine, b);
+                if (d < 16) {                                 // (at the first step there is one number of each group)
+                    const uint32_t s = upper ? second[v] : second[v + half], own = upper ? second[v + half] : second[v];
+                    low = max(low, max(own, __shfl_xor_sync(0xffffffffu, s, d)));
+                }
+                first[v] = max(mine, b);
+                second[v] = low;
+            }
+        } else {
+            const uint32_t b = __shfl_xor_sync(0xffffffffu, first[0], d), t = __shfl_xor_sync(0xffffffffu, second[0], d);
+            second[0] = max(min(first[0], b), max(second[0], t));
+            first[0] = max(first[0], b);
         }
-        margin.bias *= 2.0f;                                  // sums of two keys
-        margin.relative *= 2.0f;
-        close = p.top_groups < p.groups && margin.close(worst, best);
     }
-    const unsigned stay = __ballot_sync(0xffffffffu, kept);
+    const float w = p.by_sums ? __fadd_rn(from_ordered(first[0]), from_ordered(second[0])) : from_ordered(first[0]);
+    constexpr int LANES = 32 / V;
+    bool close;
+    const unsigned stay = best_groups<float>(p, w, lane % LANES == 0 && lane / LANES < p.groups, LANES, margin, close);
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const int e = lane + 32 * v;
-        if (e < p.experts && !((stay >> (e / p.each * p.lanes)) & 1u)) keys[v] = 0;
-    }
+    for (int v = 0; v < V; ++v)
+        if (v < p.groups && !(stay >> (v * LANES) & 1u)) keys[v] = NO_KEY;
     return close;
 }
 
-// The `top` largest keys in order, ties to the lowest expert: lane i gets choice i (-1 where nothing is left).  CHECK: whether two
-// keys in a row, the first that was not chosen among them, are too close.
-template <bool CHECK, class U, int V>
-__device__ __forceinline__ bool take_top(int top, U (&keys)[V], int &mine, Margin<float> margin) {
+// The `top` largest keys in order, ties to the lowest expert: lane i gets choice i (-1 where nothing is left).
+template <class U, int V>
+__device__ __forceinline__ int take_top(int top, U (&keys)[V]) {
     const int lane = threadIdx.x & 31;
-    bool close = false;
-    U previous = 0;
-    mine = -1;
+    int mine = -1;
 #pragma unroll 1
-    for (int i = 0; i < top + (CHECK ? 1 : 0); ++i) {
+    for (int i = 0; i < top; ++i) {
         U best = keys[0];
 #pragma unroll
         for (int v = 1; v < V; ++v) best = keys[v] > best ? keys[v] : best;
         best = warp_max_key(best);
         if (best == 0) break;
-        if constexpr (CHECK) {
-            if (i > 0) close |= margin.close(from_ordered((uint32_t)previous), from_ordered((uint32_t)best));
-            previous = best;
-            if (i == top) break;
-        }
         int e = 0x7FFFFFFF;
 #pragma unroll
         for (int v = V - 1; v >= 0; --v) e = keys[v] == best ? lane + 32 * v : e;
@@ -193,7 +235,60 @@ __device__ __forceinline__ bool take_top(int top, U (&keys)[V], int &mine, Margi
         for (int v = 0; v < V; ++v) keys[v] = lane + 32 * v == e ? (U)0 : keys[v];
         if (lane == i) mine = e;
     }
-    return close;
+    return mine;
+}
+
+// Largest first.
+template <int V> __device__ __forceinline__ void sort_keys(uint32_t (&k)[V]) {
+    // odd-even merge sort of a power of two of numbers
+#pragma unroll
+    for (int p = 1; p < V; p *= 2)
+#pragma unroll
+        for (int q = p; q >= 1; q /= 2)
+#pragma unroll
+            for (int j = q % p; j + q < V; j += 2 * q)
+#pragma unroll
+                for (int i = 0; i < q; ++i)
+                    if (i + j + q < V && (i + j) / (2 * p) == (i + j + q) / (2 * p)) {
+                        const uint32_t a = k[i + j], b = k[i + j + q];
+                        k[i + j] = max(a, b);
+                        k[i + j + q] = min(a, b);
+                    }
+}
+
+// The same choice with V - 1 - v in the lowest bits of a key in place of its own: a lane sorts its keys once and then gives its head
+// away, which carries the expert with it.  close: whether two keys in a row (the first that was not chosen among them) are too near:
+// by the margin, or (BIAS false: keys are logits, exact up to the bits that were cut, which narrow types do not have) equal but for
+// those bits.
+template <bool BIAS, int V>
+__device__ __forceinline__ int take_top_sorted(const RouteParams &p, uint32_t (&keys)[V], Margin margin, bool &close) {
+    const int lane = threadIdx.x & 31;
+    constexpr uint32_t LOW = V - 1;
+#pragma unroll
+    for (int v = 0; v < V; ++v) keys[v] = (keys[v] & ~LOW) | (LOW - v);
+    sort_keys<V>(keys);
+    int from = 0;
+    uint32_t key = NO_KEY;
+    uint32_t best = __reduce_max_sync(0xffffffffu, keys[0]);
+#pragma unroll 1
+    for (int i = 0; i < p.top && best > NO_KEY; ++i) {
+        const int owner = __ffs(__ballot_sync(0xffffffffu, keys[0] == best)) - 1;
+        from = lane == i ? owner : from;
+        key = lane == i ? best : key;
+        const bool mine = lane == owner;
+#pragma unroll
+        for (int v = 0; v + 1 < V; ++v) keys[v] = mine ? keys[v + 1] : keys[v];
+        keys[V - 1] = mine ? NO_KEY : keys[V - 1];
+        best = __reduce_max_sync(0xffffffffu, keys[0]);
+    }
+    const uint32_t behind = __shfl_down_sync(0xffffffffu, key, 1), next = lane == p.top - 1 ? best : behind;
+    bool near = false;
+    if (lane < p.top && next > NO_KEY) {
+        if constexpr (BIAS) near = margin.close(from_ordered(key), from_ordered(next));
+        else near = p.type == QNN_F32 && (key & ~LOW) == (next & ~LOW);
+    }
+    close = __any_sync(0xffffffffu, near);
+    return key > NO_KEY ? from + 32 * (int)(LOW - (key & LOW)) : -1;
 }
 
 // The same decisions with 64-bit keys.
@@ -231,10 +326,8 @@ __device__ __noinline__ int choose_in_64_bits(const RouteParams &p, int64_t toke
             keys[v] = p.bias ? ordered(s[v]) : ordered((double)l[v]);
         }
     }
-    if (p.groups > 1) keep_groups<double, unsigned long long, V>(p, s, keys, scratch, Margin<double>{});
-    int mine;
-    take_top<false>(p.top, keys, mine, Margin<float>{});
-    return mine;
+    if (p.groups > 1) keep_groups<double, unsigned long long, V>(p, s, keys, 0ull, scratch, Margin{});
+    return take_top(p.top, keys);
 }
 
 // Choice and weights of one token, by a warp.  Lane i < top writes choice i and returns it (-1: none).
@@ -244,24 +337,22 @@ __device__ __forceinline__ int route_token(const RouteParams &p, int64_t token, 
     float l[V];
     load_row<V>(p.logits, p.type, token * p.ld, p.experts, l);
     const bool there = !p.mask || p.mask[token];
-    bool bad = false;
-    float most = __int_as_float(0xFF800000);
+    const float none = __int_as_float(0xFF800000);
+    float most = l[0];
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        bad |= l[v] != l[v];
-        most = fmaxf(most, l[v]);
-    }
-    most = warp_most(most);
-    bad = __any_sync(0xffffffffu, bad) || (!p.sigmoid && most == __int_as_float(0x7F800000));
+    for (int v = 1; v < V; ++v) most = max_or_nan(most, l[v]);
+    const uint32_t highest = __reduce_max_sync(0xffffffffu, ordered(max_or_nan(most, none)));
+    const bool bad = highest > INFINITE_KEY || (!p.sigmoid && highest == INFINITE_KEY);
+    most = from_ordered(highest);
     int mine = -1;
     float sum = 1.0f;
-    if (there && !bad && most > __int_as_float(0xFF800000)) {
+    if (there && !bad && highest > NO_KEY) {
         const bool scored = p.bias || (p.groups > 1 && p.by_sums);
         float s[V];
         if (scored || (!p.sigmoid && !p.renormalise)) {
             if (p.sigmoid) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) s[v] = __fdiv_rn(1.0f, __fadd_rn(1.0f, expf(-l[v])));
+                for (int v = 0; v < V; ++v) s[v] = reciprocal(__fadd_rn(1.0f, expf(-l[v])));
             } else {
                 sum = 0.0f;
 #pragma unroll
@@ -270,97 +361,117 @@ __device__ __forceinline__ int route_token(const RouteParams &p, int64_t token, 
                     sum = __fadd_rn(sum, s[v]);
                 }
                 sum = warp_add(sum);
+                const float scale = reciprocal(sum);
 #pragma unroll
-                for (int v = 0; v < V; ++v) s[v] = __fdiv_rn(s[v], sum);
+                for (int v = 0; v < V; ++v) s[v] = __fmul_rn(s[v], scale);
             }
         }
         uint32_t keys[V];
-        // fp32 scores: expf within 2 steps, a sum and a quotient rounded once each; softmax's exponent is rounded besides, by up to
-        // 2^-24 of a difference that matters up to some 88
-        const Margin<float> margin{p.sigmoid ? 9.5367431640625e-07f : 2.288818359375e-05f, bias_most};          // 2^-20, 1.5 * 2^-16
+        // A score is off by at most (sigmoid) expf's two steps, half a step of the sum and one of the quotient, 1.75 * 2^-22; (softmax)
+        // besides by the roundings of a difference of logits that matters up to some 88 and of a sum, 40 * 2^-22 in all.  The sum with
+        // the bias is off by 2^-24, and the key by the bits that the expert takes, V * 2^-23.  Two keys: twice that.
+        const Margin margin{(p.sigmoid ? 5.0f : 80.0f) * 2.384185791015625e-07f + V * 2.384185791015625e-07f, bias_most};
         bool close = false;
+        if (p.bias) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            if (p.bias) s[v] = __fadd_rn(s[v], bias[v]);
-            keys[v] = l[v] > __int_as_float(0xFF800000) ? ordered(p.bias ? s[v] : l[v]) : 0u;
+            for (int v = 0; v < V; ++v) {
+                s[v] = l[v] > none ? __fadd_rn(s[v], bias[v]) : none;
+                keys[v] = ordered(s[v]);
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) keys[v] = ordered(__fadd_rn(l[v], 0.0f));       // (-0 is 0)
         }
         if (p.groups > 1) {
-            if (scored) close = keep_groups<float, uint32_t, V>(p, s, keys, reinterpret_cast<float *>(scratch), margin);
-            else keep_groups<float, uint32_t, V>(p, l, keys, reinterpret_cast<float *>(scratch), margin);
+            float *floats = reinterpret_cast<float *>(scratch);
+            const bool sums_alone = scored && !p.bias;
+            if (p.whole) {
+                if (sums_alone) {
+                    uint32_t worth[V];
+#pragma unroll
+                    for (int v = 0; v < V; ++v) worth[v] = l[v] > none ? ordered(s[v]) : NO_KEY;
+                    close = keep_whole_groups<V>(p, worth, keys, margin);
+                } else {
+                    close = keep_whole_groups<V>(p, keys, keys, margin) && scored;
+                }
+            } else if (scored) {
+                close = keep_groups<float, uint32_t, V>(p, s, keys, NO_KEY, floats, margin);
+            } else {
+                keep_groups<float, uint32_t, V>(p, l, keys, NO_KEY, floats, margin);
+            }
         }
-        if (p.bias) close |= take_top<true>(p.top, keys, mine, margin);
-        else take_top<false>(p.top, keys, mine, margin);
-        if (close) mine = choose_in_64_bits<V>(p, token, scratch);
+        bool near;
+        mine = p.bias ? take_top_sorted<true, V>(p, keys, margin, near) : take_top_sorted<false, V>(p, keys, margin, near);
+        if (close || near) mine = choose_in_64_bits<V>(p, token, scratch);
+    }
+    const float x = mine >= 0 ? load_as_f32(p.logits, p.type, token * p.ld + mine) : none;
+    const float t = expf(-fabsf(x));                          // sigmoid: 1 / (1 + t), or t / (1 + t) below 0
+    float w = 0.0f;
+    if (p.renormalise) {
+        // shares of the chosen scores, with the largest one's power taken out, so that none underflows alone
+        const float high = __shfl_sync(0xffffffffu, p.bias ? warp_most(x) : x, 0);      // (without a bias the first is the largest)
+        float u = 0.0f;
+        if (mine >= 0) {
+            if (!p.sigmoid) u = expf(__fadd_rn(x, -high));
+            else u = __fmul_rn(x >= 0.0f ? 1.0f : high >= 0.0f ? t : expf(__fadd_rn(x, -high)), reciprocal(__fadd_rn(1.0f, t)));
+        }
+        const float total = warp_add(u);
+        if (mine >= 0) w = __fmul_rn(u, reciprocal(total));
+    } else if (mine >= 0) {
+        w = p.sigmoid ? __fmul_rn(x >= 0.0f ? 1.0f : t, reciprocal(__fadd_rn(1.0f, t))) : __fmul_rn(expf(__fadd_rn(x, -most)), reciprocal(sum));
     }
     if (lane < p.top) {
-        const float x = mine >= 0 ? load_as_f32(p.logits, p.type, token * p.ld + mine) : 0.0f;
-        float w = 0.0f;
-        const unsigned lanes = p.top == 32 ? 0xffffffffu : (1u << p.top) - 1u;
-        if (p.renormalise) {
-            // shares of the chosen scores, with the largest one's power taken out, so that none underflows alone
-            float high = mine >= 0 ? x : __int_as_float(0xFF800000), u = 0.0f, total = 0.0f;
-            for (int i = 0; i < p.top; ++i) high = fmaxf(high, __shfl_sync(lanes, high, i));
-            if (mine >= 0) {
-                if (!p.sigmoid) u = expf(__fadd_rn(x, -high));
-                else if (x >= 0.0f) u = __fdiv_rn(1.0f, __fadd_rn(1.0f, expf(-x)));
-                else u = __fdiv_rn(expf(__fadd_rn(x, -fminf(high, 0.0f))), __fadd_rn(1.0f, expf(x)));
-            }
-            for (int i = 0; i < p.top; ++i) total = __fadd_rn(total, __shfl_sync(lanes, u, i));
-            if (mine >= 0) w = __fdiv_rn(u, total);
-        } else if (mine >= 0) {
-            w = p.sigmoid ? __fdiv_rn(1.0f, __fadd_rn(1.0f, expf(-x))) : __fdiv_rn(expf(__fadd_rn(x, -most)), sum);
-        }
-        w = there && bad ? __int_as_float(0x7FC00000) : __fmul_rn(w, p.factor);
         p.chosen[token * p.top + lane] = mine;
-        p.weights[token * p.top + lane] = w;
+        p.weights[token * p.top + lane] = there && bad ? __int_as_float(0x7FC00000) : __fmul_rn(w, p.factor);
     }
     return mine;
 }
 
-// Places of the slots of one run.  base[e]: in, the first row of expert e for this run.  counts: [RANK_WARPS][experts].
+// Places of the slots of one run.  base[e]: in, the first row of expert e for this run.  counts: [warps][experts].
 __device__ void rank_run(const RouteParams &p, int run, int32_t *base, int32_t *counts) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = min(rank_warps(p.experts), (int)blockDim.x >> 5);
     const int64_t first = (int64_t)run * p.run * p.top, end_token = min((int64_t)p.tokens, (int64_t)(run + 1) * p.run);
-    const int64_t slots = end_token * p.top - first, segment = (slots + RANK_WARPS * 32 - 1) / (RANK_WARPS * 32) * 32;
-    for (int i = threadIdx.x; i < RANK_WARPS * p.experts; i += blockDim.x) counts[i] = 0;
+    const int64_t slots = end_token * p.top - first, segment = (slots + warps * 32 - 1) / (warps * 32) * 32;
+    const int64_t lo = warp * segment, hi = warp < warps ? min(slots, lo + segment) : lo;
+    // a run of up to 32 slots a warp is ranked in one step, whose slots stay in registers
+    const int e0 = lo + lane < hi ? p.chosen[first + lo + lane] : -1;
+    for (int i = threadIdx.x; i < warps * p.experts; i += blockDim.x) counts[i] = 0;
     __syncthreads();
-    const int64_t lo = warp * segment, hi = min(slots, lo + segment);
-    if (warp < RANK_WARPS)
-        for (int64_t i = lo; i < hi; i += 32) {
-            const int e = i + lane < hi ? p.chosen[first + i + lane] : -1;
-            const unsigned same = __match_any_sync(0xffffffffu, e);
-            if (e >= 0 && __ffs(same) - 1 == lane) counts[warp * p.experts + e] += __popc(same);
-            __syncwarp();
-        }
+    const unsigned same0 = __match_any_sync(0xffffffffu, e0);
+    for (int64_t i = lo; i < hi; i += 32) {
+        const int e = i == lo ? e0 : i + lane < hi ? p.chosen[first + i + lane] : -1;
+        const unsigned same = i == lo ? same0 : __match_any_sync(0xffffffffu, e);
+        if (e >= 0 && __ffs(same) - 1 == lane) counts[warp * p.experts + e] += __popc(same);
+        __syncwarp();
+    }
     __syncthreads();
     for (int e = threadIdx.x; e < p.experts; e += blockDim.x) {
         int at = base[e];
-#pragma unroll
-        for (int w = 0; w < RANK_WARPS; ++w) {
+#pragma unroll 8
+        for (int w = 0; w < warps; ++w) {
             const int c = counts[w * p.experts + e];
             counts[w * p.experts + e] = at;
             at += c;
         }
     }
     __syncthreads();
-    if (warp < RANK_WARPS)
-        for (int64_t i = lo; i < hi; i += 32) {
-            const bool in = i + lane < hi;
-            const int e = in ? p.chosen[first + i + lane] : -1;
-            const unsigned same = __match_any_sync(0xffffffffu, e);
-            const int at = e >= 0 ? counts[warp * p.experts + e] + __popc(same & ((1u << lane) - 1u)) : -1;
-            __syncwarp();
-            if (e >= 0 && __ffs(same) - 1 == lane) counts[warp * p.experts + e] += __popc(same);
-            __syncwarp();
-            if (in) p.place[first + i + lane] = at;
-            if (e >= 0) p.order[at] = (int32_t)(first + i + lane);
-        }
+    for (int64_t i = lo; i < hi; i += 32) {
+        const bool in = i + lane < hi;
+        const int e = i == lo ? e0 : in ? p.chosen[first + i + lane] : -1;
+        const unsigned same = i == lo ? same0 : __match_any_sync(0xffffffffu, e);
+        const int at = e >= 0 ? counts[warp * p.experts + e] + __popc(same & ((1u << lane) - 1u)) : -1;
+        __syncwarp();
+        if (e >= 0 && __ffs(same) - 1 == lane) counts[warp * p.experts + e] += __popc(same);
+        __syncwarp();
+        if (in) p.place[first + i + lane] = at;
+        if (e >= 0) p.order[at] = (int32_t)(first + i + lane);
+    }
 }
 
 // counts[e] of every expert -> the experts' first rows, into offsets too where that is given; returns the rows in all.  warp_sums: 33
 // numbers of shared memory.
 __device__ __forceinline__ int scan_experts(int32_t *counts, int experts, int32_t *warp_sums, int32_t *offsets) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, each = (experts + blockDim.x - 1) / blockDim.x;      // (1 or 2)
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, each = (experts + blockDim.x - 1) / blockDim.x;
     const int first = threadIdx.x * each;
     int v = 0;
     for (int e = first; e < min(first + each, experts); ++e) v += counts[e];
@@ -399,8 +510,8 @@ __device__ __forceinline__ int scan_experts(int32_t *counts, int experts, int32_
 // A block's shared memory: counts of its run, the ranks' counts, sums; then each warp's keys.
 struct RouteSmem {
     static __host__ __device__ int ranks(int experts) { return experts; }
-    static __host__ __device__ int sums(int experts) { return (1 + RANK_WARPS) * experts; }
-    static __host__ __device__ int keys(int experts) { return ((1 + RANK_WARPS) * experts + 40 + 3) / 4 * 4; }      // in words
+    static __host__ __device__ int sums(int experts) { return (1 + rank_warps(experts)) * experts; }
+    static __host__ __device__ int keys(int experts) { return ((1 + rank_warps(experts)) * experts + 40 + 3) / 4 * 4; }      // in words
 };
 
 // Choices of a run of tokens; ALONE: the plan as well (one run).
@@ -415,20 +526,21 @@ __global__ void __launch_bounds__(choose_threads(V)) route_choose_kernel(const _
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         bias[v] = p.bias && lane + 32 * v < p.experts ? p.bias[lane + 32 * v] : 0.0f;
+        if (bias[v] != bias[v]) bias[v] = __int_as_float(0xFF800000);
         if (fabsf(bias[v]) <= 3.402823466e38f) bias_most = fmaxf(bias_most, fabsf(bias[v]));
     }
     bias_most = warp_most(bias_most);
     double *scratch = reinterpret_cast<double *>(words + RouteSmem::keys(p.experts)) + warp * (p.groups > 1 ? p.groups * p.pitch : 0);
     __syncthreads();
     const int64_t first = (int64_t)blockIdx.x * p.run, last = min((int64_t)p.tokens, first + p.run);
-    for (int64_t t = first + warp; t < last; t += choose_threads(V) / 32) {
+    for (int64_t t = first + warp; t < last; t += blockDim.x >> 5) {
         const int e = route_token<V>(p, t, bias, bias_most, scratch);
         if (lane < p.top && e >= 0) atomicAdd(&words[e], 1);
     }
     if (!p.order) return;
     __syncthreads();
     if constexpr (!ALONE) {
-        for (int e = threadIdx.x; e < p.experts; e += blockDim.x) p.counts[(int64_t)blockIdx.x * p.experts + e] = words[e];
+        for (int e = threadIdx.x; e < p.experts; e += blockDim.x) p.counts[(int64_t)e * p.runs + blockIdx.x] = words[e];
     } else {
         const int total = scan_experts(words, p.experts, words + RouteSmem::sums(p.experts), p.offsets);
         for (int i = total + threadIdx.x; i < p.tokens * p.top; i += blockDim.x) p.order[i] = -1;
@@ -437,26 +549,56 @@ __global__ void __launch_bounds__(choose_threads(V)) route_choose_kernel(const _
     }
 }
 
-// The plan of a run, behind the counts of all.
+// counts of an expert's runs -> its rows in the runs ahead, and in all; a warp takes an expert, a lane up to five runs in a row.
+__global__ void __launch_bounds__(256) route_scan_kernel(const __grid_constant__ RouteParams p) {
+    start_next();
+    wait_for_previous();
+    const int e = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (e >= p.experts) return;
+    int32_t *counts = p.counts + (int64_t)e * p.runs;
+    int c[MAX_RUNS / 32 + 1], sum = 0;
+    constexpr int EACH = MAX_RUNS / 32 + 1;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        c[i] = lane * EACH + i < p.runs ? counts[lane * EACH + i] : 0;
+        sum += c[i];
+    }
+    int incl = sum;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += o;
+    }
+    int at = incl - sum;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        if (lane * EACH + i < p.runs) counts[lane * EACH + i] = at;
+        at += c[i];
+    }
+    if (lane == 31) p.counts[(int64_t)p.experts * p.runs + e] = incl;
+}
+
+// The plan of a run.
 __global__ void __launch_bounds__(PLAN_THREADS) route_plan_kernel(const __grid_constant__ RouteParams p) {
     extern __shared__ __align__(16) int32_t words[];
     start_next();
     wait_for_previous();
-    // counts of an expert in all runs and in those ahead, by as many threads as fit
     int32_t *ahead = words, *all = words + RouteSmem::ranks(p.experts);
-    for (int e = threadIdx.x; e < p.experts; e += blockDim.x) ahead[e] = all[e] = 0;
-    __syncthreads();
-    const int width = (p.experts + 31) / 32 * 32, parts = PLAN_THREADS / width, part = threadIdx.x / width, expert = threadIdx.x - part * width;
-    if (part < parts && expert < p.experts) {
-        int a = 0, b = 0;
-#pragma unroll 16
-        for (int r = part; r < p.runs; r += parts) {
-            const int c = p.counts[(int64_t)r * p.experts + expert];
-            b += c;
-            a += r < (int)blockIdx.x ? c : 0;
+    for (int e = threadIdx.x; e < p.experts; e += blockDim.x) {
+        const int32_t *counts = p.counts + (int64_t)e * p.runs;
+        if (p.runs > SCANNED_RUNS) {
+            ahead[e] = counts[blockIdx.x];
+            all[e] = p.counts[(int64_t)p.experts * p.runs + e];
+        } else {
+            int a = 0, b = 0;
+#pragma unroll 8
+            for (int r = 0; r < p.runs; ++r) {
+                b += counts[r];
+                a += r < (int)blockIdx.x ? counts[r] : 0;
+            }
+            ahead[e] = a;
+            all[e] = b;
         }
-        atomicAdd(&ahead[expert], a);
-        atomicAdd(&all[expert], b);
     }
     __syncthreads();
     const int total = scan_experts(all, p.experts, words + RouteSmem::sums(p.experts), blockIdx.x == 0 ? p.offsets : nullptr);
@@ -554,7 +696,7 @@ __global__ void __launch_bounds__(256) route_back_kernel(const RouteBackParams p
 // SMs, of at least 32 tokens.  Sized for 148 SMs, so that workspace queries and calls agree.
 int route_run(int64_t tokens) {
     if (tokens <= 64) return 64;
-    const int64_t each = (tokens + 147) / 148;
+    const int64_t each = (tokens + MAX_RUNS - 1) / MAX_RUNS;
     return (int)(each < 32 ? 32 : each);
 }
 int route_runs(int64_t tokens) { return (int)((tokens + route_run(tokens) - 1) / route_run(tokens)); }
@@ -576,9 +718,15 @@ template <class K> int launch_route(K kernel, int blocks, int threads, int smem,
 template <int V> int route_launch(const RouteParams &p, cudaStream_t st) {
     constexpr int threads = choose_threads(V);
     const int fixed = RouteSmem::keys(p.experts) * 4, smem = fixed + (p.groups > 1 ? threads / 32 * p.groups * p.pitch * 8 : 0);
-    if (p.runs == 1) return launch_route(route_choose_kernel<V, true>, 1, threads, smem, st, p);
+    if (p.runs == 1) {
+        // a warp for each token, and at least half a thread for each expert: barriers of idle warps take longer than their work
+        const int some = max(p.tokens, (p.experts + 63) / 64) * 32;
+        return launch_route(route_choose_kernel<V, true>, 1, some < threads ? some : threads, smem, st, p);
+    }
     const int rc = launch_route(route_choose_kernel<V, false>, p.runs, threads, smem, st, p);
-    return rc != QNN_OK || !p.order ? rc : launch_route(route_plan_kernel, p.runs, PLAN_THREADS, fixed, st, p);
+    if (rc != QNN_OK || !p.order) return rc;
+    const int scanned = p.runs > SCANNED_RUNS ? launch_early(route_scan_kernel, dim3((p.experts + 7) / 8), dim3(256), st, p) : QNN_OK;
+    return scanned != QNN_OK ? scanned : launch_route(route_plan_kernel, p.runs, PLAN_THREADS, fixed, st, p);
 }
 template <class T, int V> int back_launch(const RouteBackParams &p, cudaStream_t st) {
     const int64_t blocks = ((int64_t)p.tokens + 7) / 8;
@@ -598,7 +746,7 @@ bool route_sizes_ok(int64_t tokens, int experts, int top) {
 
 extern "C" size_t qnn_route_workspace(int64_t tokens, int experts, int top) {
     if (!route_sizes_ok(tokens, experts, top) || tokens == 0 || tokens * top > ROUTE_MAX_SLOTS || route_runs(tokens) == 1) return 0;
-    return ((size_t)route_runs(tokens) * (size_t)experts * sizeof(int32_t) + 255) / 256 * 256;
+    return ((size_t)(route_runs(tokens) + 1) * (size_t)experts * sizeof(int32_t) + 255) / 256 * 256;
 }
 
 extern "C" int qnn_route(const void *logits, int type, int64_t tokens, int experts, int64_t ld, int top, unsigned flags, const float *bias,
@@ -629,6 +777,8 @@ extern "C" int qnn_route(const void *logits, int type, int64_t tokens, int exper
     p.lanes = 1;
     while (p.lanes * 2 * groups <= 32) p.lanes *= 2;
     p.pitch = p.each | 1;                                      // (odd: lanes that walk along groups of their own meet no bank conflicts)
+    p.group_of = (uint32_t)(((1u << 20) + p.each - 1) / p.each);
+    p.whole = p.each == 32;
     p.factor = factor; p.mask = mask; p.chosen = chosen; p.weights = weights;
     p.order = order; p.place = place; p.offsets = offsets;
     p.counts = static_cast<int32_t *>(workspace);
