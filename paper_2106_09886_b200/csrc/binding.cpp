@@ -10,6 +10,7 @@
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <c10/core/GradMode.h>
+#include <c10/core/TensorImpl.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -210,6 +211,53 @@ float float_of(PyObject *o) {
 }
 void *pointer(const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
 
+// The results of one call.  Small ones lie in one allocation, each on 16 bytes: an allocation takes half a microsecond, and a decoding
+// step's results are small.  Large ones have their own, so that none keeps another's memory alive.
+class Results {
+  public:
+    Results(const at::Tensor &like) : like_(like) {}
+    // an array of rows x width elements, rows `ld` apart; 0 rows of anything is an empty array
+    void add(at::Tensor &t, at::ScalarType type, int64_t rows, int64_t width, int64_t ld) { parts_[count_++] = {&t, type, rows, width, ld, false}; }
+    void add(at::Tensor &t, at::ScalarType type, int64_t size) { parts_[count_++] = {&t, type, size, 1, 1, true}; }
+    void make() {
+        int64_t total = 0;
+        for (int i = 0; i < count_; ++i) total += bytes(parts_[i]);
+        if (total > TOGETHER || count_ == 1) {
+            for (int i = 0; i < count_; ++i) {
+                const Part &p = parts_[i];
+                const auto options = like_.options().dtype(p.type);
+                *p.t = p.flat ? at::empty({p.rows}, options) : p.ld == p.width ? at::empty({p.rows, p.width}, options) : at::empty_strided({p.rows, p.width}, {p.ld, 1}, options);
+            }
+            return;
+        }
+        const at::Tensor all = at::empty({total}, like_.options().dtype(at::kByte));
+        int64_t at_byte = 0;
+        for (int i = 0; i < count_; ++i) {
+            const Part &p = parts_[i];
+            *p.t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(), c10::scalarTypeToTypeMeta(p.type));
+            c10::TensorImpl *impl = p.t->unsafeGetTensorImpl();
+            const int64_t size = (int64_t)c10::elementSize(p.type);
+            const std::array<int64_t, 2> sizes{p.rows, p.width}, strides{p.flat ? 1 : p.ld, 1};
+            const size_t dims = p.flat ? 1 : 2;
+            impl->set_sizes_and_strides(at::IntArrayRef(sizes.data(), dims), at::IntArrayRef(strides.data(), dims), at_byte / size);
+            at_byte += bytes(p);
+        }
+    }
+
+  private:
+    static constexpr int64_t TOGETHER = 256 * 1024;
+    struct Part {
+        at::Tensor *t;
+        at::ScalarType type;
+        int64_t rows, width, ld;
+        bool flat;
+    };
+    static int64_t bytes(const Part &p) { return whole_units(p.rows * p.ld * (int64_t)c10::elementSize(p.type)); }
+    const at::Tensor &like_;
+    Part parts_[6];
+    int count_ = 0;
+};
+
 // A tuple of results, or the status.
 PyObject *answers(int status, std::initializer_list<at::Tensor *> results) {
     if (status != QNN_OK) return PyLong_FromLong(status);
@@ -248,10 +296,6 @@ Codes codes_of(PyObject *const *a) {
     check_int(c.k);
     return c;
 }
-// Room for rows in 8 bits, each starting on 16 bytes.
-at::Tensor new_codes(const at::Tensor &like, int64_t rows, int64_t k) {
-    return at::empty_strided({rows, k}, {whole_units(k), 1}, like.options().dtype(at::kChar));
-}
 void check_like(const at::Tensor &t, const Rows &r, const at::Tensor &like, const Rows &l) {
     if (r.type != l.type || r.rows != l.rows || t.size(1) != like.size(1)) throw Refused("all rows must have the same type and shape");
 }
@@ -263,7 +307,11 @@ PyObject *i8_quantize(PyObject *const *a) {
     const int64_t k = x.size(1);
     check_int(k);
     void *stream = stream_for(x, {});
-    at::Tensor codes = new_codes(x, r.rows, k), scales = at::empty({r.rows}, x.options().dtype(at::kFloat));
+    at::Tensor codes, scales;
+    Results results(x);
+    results.add(codes, at::kChar, r.rows, k, whole_units(k));
+    results.add(scales, at::kFloat, r.rows);
+    results.make();
     const int status = qnn_i8_quantize(x.data_ptr(), r.type, r.rows, (int)k, r.ld, (int8_t *)codes.data_ptr(), whole_units(k), (float *)scales.data_ptr(), stream);
     return answers(status, {&codes, &scales});
 }
@@ -337,7 +385,8 @@ PyObject *rms_norm(PyObject *const *a) {
     const at::Tensor &gain = gain_of(a[1], r, k, &gain_type);
     const float eps = float_of(a[2]);
     const bool real = PyObject_IsTrue(a[4]) == 1, eight = PyObject_IsTrue(a[5]) == 1;
-    at::Tensor residual, h, y, codes, scales;
+    at::Tensor residual, h, y, codes, scales, rstd;
+    Results results(x);
     int64_t ldr = 0;
     void *stream;
     if (given(a[3])) {
@@ -346,16 +395,17 @@ PyObject *rms_norm(PyObject *const *a) {
         check_like(residual, q, x, r);
         ldr = q.ld;
         stream = stream_for(x, {&gain, &residual});
-        h = at::empty({r.rows, k}, x.options());
+        results.add(h, x.scalar_type(), r.rows, k, k);
     } else {
         stream = stream_for(x, {&gain});
     }
-    if (real) y = at::empty({r.rows, k}, x.options());
+    if (real) results.add(y, x.scalar_type(), r.rows, k, k);
     if (eight) {
-        codes = new_codes(x, r.rows, k);
-        scales = at::empty({r.rows}, x.options().dtype(at::kFloat));
+        results.add(codes, at::kChar, r.rows, k, whole_units(k));
+        results.add(scales, at::kFloat, r.rows);
     }
-    at::Tensor rstd = at::empty({r.rows}, x.options().dtype(at::kFloat));
+    results.add(rstd, at::kFloat, r.rows);
+    results.make();
     const int status = qnn_rms_norm(x.data_ptr(), r.type, r.rows, (int)k, r.ld, pointer(residual), ldr, gain.data_ptr(), gain_type, eps, pointer(h), k,
                                     pointer(y), k, (int8_t *)pointer(codes), whole_units(k), (float *)pointer(scales), (float *)rstd.data_ptr(), stream);
     if (!h.defined()) h = x;
@@ -385,7 +435,11 @@ PyObject *rms_norm_backward(PyObject *const *a) {
     } else {
         stream = stream_for(dy, {&h, &gain, &rstd});
     }
-    at::Tensor dx = at::empty({r.rows, k}, dy.options()), dgain = at::empty({k}, dy.options().dtype(at::kFloat));
+    at::Tensor dx, dgain;
+    Results results(dy);
+    results.add(dx, dy.scalar_type(), r.rows, k, k);
+    results.add(dgain, at::kFloat, k);
+    results.make();
     const at::Tensor ws = workspace_for(a[5], qnn_rms_norm_backward_workspace(r.rows, (int)k), dy);
     const int status = qnn_rms_norm_backward(dy.data_ptr(), r.type, r.rows, (int)k, r.ld, h.data_ptr(), q.ld, gain.data_ptr(), gain_type,
                                              (const float *)rstd.data_ptr(), pointer(dh), lddh, dx.data_ptr(), k, (float *)dgain.data_ptr(), pointer(ws),
@@ -409,9 +463,14 @@ PyObject *route(PyObject *const *a) {
     void *stream = stream_for(logits, {});
     for (const at::Tensor *t : std::initializer_list<const at::Tensor *>{&bias, &mask})
         if (t->defined()) stream_for(*t, {&logits});
-    const auto whole = logits.options().dtype(at::kInt);
-    at::Tensor chosen = at::empty({r.rows, top}, whole), weights = at::empty({r.rows, top}, logits.options().dtype(at::kFloat));
-    at::Tensor order = at::empty({r.rows * top}, whole), place = at::empty({r.rows, top}, whole), offsets = at::empty({experts + 1}, whole);
+    at::Tensor chosen, weights, order, place, offsets;
+    Results results(logits);
+    results.add(chosen, at::kInt, r.rows, top, top);
+    results.add(weights, at::kFloat, r.rows, top, top);
+    results.add(order, at::kInt, r.rows * top);
+    results.add(place, at::kInt, r.rows, top, top);
+    results.add(offsets, at::kInt, experts + 1);
+    results.make();
     const at::Tensor ws = workspace_for(a[8], qnn_route_workspace(r.rows, (int)experts, (int)top), logits);
     const int status = qnn_route(logits.data_ptr(), r.type, r.rows, (int)experts, r.ld, (int)top, (unsigned)int_of(a[2]), (const float *)pointer(bias),
                                  (int)groups, (int)top_groups, float_of(a[6]), (const uint8_t *)pointer(mask), (int32_t *)chosen.data_ptr(),

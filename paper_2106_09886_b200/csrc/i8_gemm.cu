@@ -32,9 +32,9 @@ I8Plan i8_plan(int64_t rows, int n, int k) {
     return {tile, ranks};
 }
 
-template <class K, class... A>
-int i8_launch(K kernel, dim3 grid, int threads, int smem, int cluster, cudaStream_t st, A... args) {
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return QNN_E_CUDA;
+template <auto KERNEL, class... A>
+int i8_launch(dim3 grid, int threads, int smem, int cluster, cudaStream_t st, A... args) {
+    if (!allow_shared_memory<KERNEL>(smem)) return QNN_E_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
@@ -43,7 +43,7 @@ int i8_launch(K kernel, dim3 grid, int threads, int smem, int cluster, cudaStrea
     LaunchAttrs attrs(cluster);
     cfg.attrs = attrs.a;
     cfg.numAttrs = cluster > 1 ? 2 : 1;
-    if (cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess) return QNN_OK;
+    if (cudaLaunchKernelEx(&cfg, KERNEL, args...) == cudaSuccess) return QNN_OK;
     cudaGetLastError();
     return QNN_E_CUDA;
 }
@@ -56,7 +56,7 @@ template <int TN, class T> int run_split(const I8Operands &o, const I8Params &p,
     if (ttiles > 65535) return QNN_E_RANGE;
     int log_ranks = 0;
     while (1 << log_ranks < ranks) ++log_ranks;
-    return i8_launch(i8_split_kernel<TN, T>, dim3((p.n + 127) / 128 << log_ranks, (unsigned)ttiles), L::THREADS, L::TOTAL, ranks, st, w, x, p, log_ranks);
+    return i8_launch<i8_split_kernel<TN, T>>(dim3((p.n + 127) / 128 << log_ranks, (unsigned)ttiles), L::THREADS, L::TOTAL, ranks, st, w, x, p, log_ranks);
 }
 template <int TN, class T> int run_pair(const I8Operands &o, I8Params p, cudaStream_t st) {
     using L = I8Pair<TN, T>;
@@ -69,7 +69,7 @@ template <int TN, class T> int run_pair(const I8Operands &o, I8Params p, cudaStr
     if (items > 0x3FFFFFFF || (int64_t)p.band * p.ftiles > 0x3FFFFFFF) return QNN_E_RANGE;
     const int sms = sm_count(), most = sms / 2;
     if (most < 1) return QNN_E_CUDA;
-    return i8_launch(i8_pair_kernel<TN, T>, dim3((unsigned)(items < most ? items : most) * 2), L::THREADS, L::TOTAL, 2, st, w, x, p);
+    return i8_launch<i8_pair_kernel<TN, T>>(dim3((unsigned)(items < most ? items : most) * 2), L::THREADS, L::TOTAL, 2, st, w, x, p);
 }
 template <class T> int run(const I8Operands &o, const I8Params &p, cudaStream_t st) {
     const I8Plan plan = i8_plan(p.rows, p.n, o.k);

@@ -537,9 +537,8 @@ int back_blocks(int64_t rows) { return (int)(rows < 296 ? rows : 296); }
 
 template <class T, class G, int NV>
 int back_launch(const NormBackParams &p, int packs, cudaStream_t st) {
-    auto kernel = norm_back_kernel<T, G, NV>;
     const int stage = (p.dh ? 3 : 2) * p.width * (int)sizeof(T), fit = 100 * 1024 / stage, stages = fit < 2 ? 2 : fit < 8 ? fit : 8;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024) != cudaSuccess) return QNN_E_CUDA;
+    if (!allow_shared_memory<norm_back_kernel<T, G, NV>>(200 * 1024)) return QNN_E_CUDA;
     LaunchAttrs attrs(1);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(back_blocks(p.rows));
@@ -548,7 +547,7 @@ int back_launch(const NormBackParams &p, int packs, cudaStream_t st) {
     cfg.stream = st;
     cfg.attrs = attrs.a;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, kernel, p, stages, stage) == cudaSuccess) return QNN_OK;
+    if (cudaLaunchKernelEx(&cfg, norm_back_kernel<T, G, NV>, p, stages, stage) == cudaSuccess) return QNN_OK;
     cudaGetLastError();
     return QNN_E_CUDA;
 }
@@ -558,9 +557,8 @@ int back_warps_launch(const NormBackParams &p, cudaStream_t st) {
 }
 template <class T, class G>
 int back_any_launch(const NormBackParams &p, cudaStream_t st) {
-    auto kernel = norm_back_any_kernel<T, G>;
     const int smem = p.width * (int)sizeof(float);
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NORM_MAX_WIDTH * (int)sizeof(float)) != cudaSuccess) return QNN_E_CUDA;
+    if (!allow_shared_memory<norm_back_any_kernel<T, G>>(NORM_MAX_WIDTH * (int)sizeof(float))) return QNN_E_CUDA;
     LaunchAttrs attrs(1);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(back_blocks(p.rows));
@@ -569,7 +567,7 @@ int back_any_launch(const NormBackParams &p, cudaStream_t st) {
     cfg.stream = st;
     cfg.attrs = attrs.a;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess) return QNN_OK;
+    if (cudaLaunchKernelEx(&cfg, norm_back_any_kernel<T, G>, p) == cudaSuccess) return QNN_OK;
     cudaGetLastError();
     return QNN_E_CUDA;
 }

@@ -701,8 +701,8 @@ int route_run(int64_t tokens) {
 }
 int route_runs(int64_t tokens) { return (int)((tokens + route_run(tokens) - 1) / route_run(tokens)); }
 
-template <class K> int launch_route(K kernel, int blocks, int threads, int smem, cudaStream_t st, const RouteParams &p) {
-    if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return QNN_E_CUDA;
+template <auto KERNEL> int launch_route(int blocks, int threads, int smem, cudaStream_t st, const RouteParams &p) {
+    if (smem > 48 * 1024 && !allow_shared_memory<KERNEL>(200 * 1024)) return QNN_E_CUDA;
     LaunchAttrs attrs(1);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(blocks);
@@ -711,7 +711,7 @@ template <class K> int launch_route(K kernel, int blocks, int threads, int smem,
     cfg.stream = st;
     cfg.attrs = attrs.a;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess) return QNN_OK;
+    if (cudaLaunchKernelEx(&cfg, KERNEL, p) == cudaSuccess) return QNN_OK;
     cudaGetLastError();
     return QNN_E_CUDA;
 }
@@ -721,12 +721,12 @@ template <int V> int route_launch(const RouteParams &p, cudaStream_t st) {
     if (p.runs == 1) {
         // a warp for each token, and at least half a thread for each expert: barriers of idle warps take longer than their work
         const int some = max(p.tokens, (p.experts + 63) / 64) * 32;
-        return launch_route(route_choose_kernel<V, true>, 1, some < threads ? some : threads, smem, st, p);
+        return launch_route<route_choose_kernel<V, true>>(1, some < threads ? some : threads, smem, st, p);
     }
-    const int rc = launch_route(route_choose_kernel<V, false>, p.runs, threads, smem, st, p);
+    const int rc = launch_route<route_choose_kernel<V, false>>(p.runs, threads, smem, st, p);
     if (rc != QNN_OK || !p.order) return rc;
     const int scanned = p.runs > SCANNED_RUNS ? launch_early(route_scan_kernel, dim3((p.experts + 7) / 8), dim3(256), st, p) : QNN_OK;
-    return scanned != QNN_OK ? scanned : launch_route(route_plan_kernel, p.runs, PLAN_THREADS, fixed, st, p);
+    return scanned != QNN_OK ? scanned : launch_route<route_plan_kernel>(p.runs, PLAN_THREADS, fixed, st, p);
 }
 template <class T, int V> int back_launch(const RouteBackParams &p, cudaStream_t st) {
     const int64_t blocks = ((int64_t)p.tokens + 7) / 8;

@@ -1,6 +1,7 @@
 // Thin wrappers of the PTX that the tensor-memory kernels are built from, their bounded waits, and the host-side entry
 // point of tensor maps.  Everything is in an anonymous namespace.
 #pragma once
+#include <atomic>
 #include <cuda.h>
 #include "qnn_internal.cuh"
 
@@ -212,6 +213,22 @@ struct LaunchAttrs {
         a[1].val.clusterDim.y = a[1].val.clusterDim.z = 1;
     }
 };
+
+// Lets KERNEL use up to `bytes` of dynamic shared memory on the current device; asked of the runtime once a device, which takes longer
+// than the rest of a small call's checks.
+template <auto KERNEL> bool allow_shared_memory(int bytes) {
+    static std::atomic<uint64_t> allowed{0};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return false;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (dev < 64 && (allowed.load(std::memory_order_relaxed) & bit)) return true;
+    if (cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) {
+        cudaGetLastError();
+        return false;
+    }
+    allowed.fetch_or(bit, std::memory_order_relaxed);
+    return true;
+}
 
 // A launch without clusters that may start early.
 template <class... P, class... A>

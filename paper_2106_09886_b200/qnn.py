@@ -495,12 +495,16 @@ class I8Rows(NamedTuple):
 
 def i8_quantize(x: torch.Tensor, stream=None) -> I8Rows:
     """Real rows [rows, k] (tokens, or a weight matrix [features, k]) -> codes with a scale for each row, max|x| / 127."""
-    return I8Rows(*_result(_on_stream(stream, lambda: (_binding or _load_binding()).i8_quantize(x)), "qnn_i8_quantize"))
+    if stream is None:
+        return I8Rows(*_result((_binding or _load_binding()).i8_quantize(x), "qnn_i8_quantize"))
+    return I8Rows(*_result(_on_stream(stream, lambda: _load_binding().i8_quantize(x)), "qnn_i8_quantize"))
 
 
 def i8_decode(rows: I8Rows, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """The numbers that rows in 8 bits stand for, [rows, k] of `dtype`."""
-    return _result(_on_stream(stream, lambda: (_binding or _load_binding()).i8_decode(*rows, dtype, out)), "qnn_i8_decode")
+    if stream is None:
+        return _result((_binding or _load_binding()).i8_decode(*rows, dtype, out), "qnn_i8_decode")
+    return _result(_on_stream(stream, lambda: _load_binding().i8_decode(*rows, dtype, out)), "qnn_i8_decode")
 
 
 def i8_gemm(x: I8Rows, w: I8Rows, dtype: torch.dtype = torch.bfloat16, bias: torch.Tensor | None = None,
@@ -521,14 +525,20 @@ def i8_plan(rows: int, n: int, k: int) -> tuple[int, int]:
 def rms_norm(x: torch.Tensor, gain: torch.Tensor, eps: float = 1e-6, residual: torch.Tensor | None = None,
              stream=None) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """h = x + residual (x itself without one), y = h / sqrt(mean h^2 + eps) * gain -> (y, h, rstd); rows [rows, width]."""
-    r = _result(_on_stream(stream, lambda: (_binding or _load_binding()).rms_norm(x, gain, eps, residual, True, False)), "qnn_rms_norm")
+    if stream is None:
+        r = _result((_binding or _load_binding()).rms_norm(x, gain, eps, residual, True, False), "qnn_rms_norm")
+    else:
+        r = _result(_on_stream(stream, lambda: _load_binding().rms_norm(x, gain, eps, residual, True, False)), "qnn_rms_norm")
     return r[0], r[3], r[4]
 
 
 def rms_norm_i8(x: torch.Tensor, gain: torch.Tensor, eps: float = 1e-6, residual: torch.Tensor | None = None, both: bool = False,
                 stream=None):
     """rms_norm with its result in 8 bits -> (I8Rows, h, rstd); both=True: (I8Rows, y, h, rstd)."""
-    r = _result(_on_stream(stream, lambda: (_binding or _load_binding()).rms_norm(x, gain, eps, residual, both, True)), "qnn_rms_norm")
+    if stream is None:
+        r = _result((_binding or _load_binding()).rms_norm(x, gain, eps, residual, both, True), "qnn_rms_norm")
+    else:
+        r = _result(_on_stream(stream, lambda: _load_binding().rms_norm(x, gain, eps, residual, both, True)), "qnn_rms_norm")
     rows = I8Rows(r[1], r[2])
     return (rows, r[0], r[3], r[4]) if both else (rows, r[3], r[4])
 
@@ -564,7 +574,10 @@ def route(logits: torch.Tensor, top: int, score: str = "softmax", bias: torch.Te
           mask: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None) -> Routes:
     """logits [tokens, experts] -> the `top` experts of each token, their weights and the plan (include/qnn.h, qnn_route)."""
     flags = _route_flags(score, renormalise, group_score)
-    return Routes(*_result(_on_stream(stream, lambda: (_binding or _load_binding()).route(
+    if stream is None:
+        return Routes(*_result((_binding or _load_binding()).route(logits, top, flags, bias, groups, top_groups, factor, mask, workspace),
+                               "qnn_route"))
+    return Routes(*_result(_on_stream(stream, lambda: _load_binding().route(
         logits, top, flags, bias, groups, top_groups, factor, mask, workspace)), "qnn_route"))
 
 
