@@ -17,19 +17,39 @@ struct I8Plan {
     int tile, ranks;
 };
 
+// The form that ends first by an estimate in nanoseconds: what a launch costs, and for each round of blocks a step of 128 elements
+// and a fixed part (first copies, results).  Fitted to 230 sizes (1 to 4096 rows, n 200 to 16384, k 300 to 16384; times in a
+// replayed graph), where the choice is 2.8 % off the best form on average and 33 % at most.  Two sides of it: 301 x 4096 x 4096
+// takes 13.6 us in one block's tiles of 128 tokens and 10.4 in a pair's; 64 x 4096 x 4096 7.2 us in 32-token tiles with four ranks
+// and 9.9 by pairs.  Blocks of tiles up to 64 tokens go two to an SM, and share it when more than 148 run (step + 42 %, fixed part
+// x 4.9); clusters of four and eight do not fill every group of SMs.  Sized for 148 SMs.
 I8Plan i8_plan(int64_t rows, int n, int k) {
-    const int64_t steps = (k + I8_STEP - 1) / I8_STEP;
-    const int64_t pairs = ((n + 255) / 256) * ((rows + 255) / 256);
-    if (pairs >= 74) return {256, 0};
-    const int tile = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128, at_once = tile <= 64 ? 296 : 148;
-    const int64_t tiles = (int64_t)((n + 127) / 128) * ((rows + tile - 1) / tile);
-    int ranks = 1;
-    int64_t best = INT64_MAX;
-    for (int r = 1; r <= 8 && r <= steps; r *= 2) {
-        const int64_t rounds = (tiles * r + at_once - 1) / at_once, cost = rounds * ((steps + r - 1) / r + 8) + (r > 1 ? 4 : 0);
-        if (cost < best) { best = cost; ranks = r; }
+    struct Form {
+        int tile, launch, step, fixed;
+    };
+    static const Form split[] = {{16, 1370, 189, 330}, {32, 2360, 202, 340}, {64, 3320, 258, 450}, {128, 0, 230, 5480}};
+    static const Form pair[] = {{128, 3430, 172, 1790}, {256, 4220, 296, 3020}};
+    static const int join[] = {0, 690, 350, 0}, places[] = {148, 148, 136, 112};
+    const double steps = (double)((k + I8_STEP - 1) / I8_STEP), wide = (double)((n + 255) / 256), narrow = (double)((n + 127) / 128);
+    I8Plan best = {16, 1};
+    double least = 1e300;
+    for (const Form &f : split) {
+        if (f.tile > 16 && f.tile >= 2 * rows) break;                              // half of such a tile would be empty
+        const double tiles = narrow * (double)((rows + f.tile - 1) / f.tile);
+        const int together = f.tile <= 64 ? 2 : 1;
+        for (int l = 0; l < 4 && (1 << l) <= steps; ++l) {
+            const double blocks = tiles * (1 << l), rounds = ceil(blocks / (places[l] * together)), each = ceil(steps / (1 << l));
+            const double shared = together == 1 || blocks <= 148.0 ? 0.0 : blocks < 296.0 ? blocks / 148.0 - 1.0 : 1.0;
+            const double cost = f.launch + rounds * (each * f.step * (1.0 + 0.42 * shared) + f.fixed * (1.0 + 3.9 * shared)) + join[l];
+            if (cost < least) { least = cost; best = {f.tile, 1 << l}; }
+        }
     }
-    return {tile, ranks};
+    if (rows > 32)
+        for (const Form &f : pair) {
+            const double rounds = ceil(wide * (double)((rows + f.tile - 1) / f.tile) / 74.0), cost = f.launch + rounds * (steps * f.step + f.fixed);
+            if (cost < least) { least = cost; best = {f.tile, 0}; }
+        }
+    return best;
 }
 
 template <auto KERNEL, class... A>
@@ -73,7 +93,7 @@ template <int TN, class T> int run_pair(const I8Operands &o, I8Params p, cudaStr
 }
 template <class T> int run(const I8Operands &o, const I8Params &p, cudaStream_t st) {
     const I8Plan plan = i8_plan(p.rows, p.n, o.k);
-    if (plan.ranks == 0) return run_pair<256, T>(o, p, st);
+    if (plan.ranks == 0) return plan.tile == 128 ? run_pair<128, T>(o, p, st) : run_pair<256, T>(o, p, st);
     switch (plan.tile) {
         case 16: return run_split<16, T>(o, p, plan.ranks, st);
         case 32: return run_split<32, T>(o, p, plan.ranks, st);

@@ -53,12 +53,46 @@ template <int TN> struct I8Split {
     static constexpr int A_STAGE = 128 * I8_STEP, STAGE = A_STAGE + TN * I8_STEP;
     static constexpr int STAGES = TN <= 16 ? 6 : TN <= 32 ? 5 : TN <= 64 ? 4 : 6;
     static constexpr int BLOCKS = TN <= 64 ? 2 : 1;      // that fit an SM
-    static constexpr int BAR_OFF = STAGES * STAGE;
+    static constexpr int SCALE_OFF = STAGES * STAGE, BAR_OFF = SCALE_OFF + TN * 4;
     static constexpr int TOTAL = BAR_OFF + (2 * STAGES + 1) * 8 + 16 + 1024;
     static constexpr int COLS = TN < 32 ? 32 : TN;       // tensor-memory columns
     static constexpr int THREADS = 192;                  // warps 0-3 results, 4 copies, 5 instructions
-    static_assert(TN * 128 * 4 <= BAR_OFF, "the block's sums fit the ring");
+    static_assert(TN * 128 * 4 <= SCALE_OFF, "the block's sums fit the ring");
 };
+
+// Tokens rank, rank + RANKS, ... of a tile: the ranks' sums, read through distributed shared memory with 16 loads under way (each takes
+// a round trip), and the result.
+template <int RANKS, class T>
+__device__ __forceinline__ void i8_add_ranks(uint32_t mine, int rank, int have, T *out, int64_t ldo, const float *x_scales, float w_scale, float bias) {
+    constexpr int TOKENS = 16 / RANKS;
+    uint32_t there[RANKS];
+#pragma unroll
+    for (int q = 0; q < RANKS; ++q) asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there[q]) : "r"(mine), "r"(q));
+#pragma unroll 1
+    for (int c0 = rank; c0 < have; c0 += RANKS * TOKENS) {
+        int v[TOKENS][RANKS];
+        float s[TOKENS];
+#pragma unroll
+        for (int i = 0; i < TOKENS; ++i) {
+            const int c = c0 + i * RANKS;
+            if (c < have) {
+                s[i] = x_scales[c];
+#pragma unroll
+                for (int q = 0; q < RANKS; ++q) asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v[i][q]) : "r"(there[q] + c * 512) : "memory");
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < TOKENS; ++i) {
+            const int c = c0 + i * RANKS;
+            if (c < have) {
+                int sum = v[i][0];
+#pragma unroll
+                for (int q = 1; q < RANKS; ++q) sum += v[i][q];
+                out[(int64_t)c * ldo] = from_f32<T>(i8_result(sum, s[i], w_scale, bias));
+            }
+        }
+    }
+}
 
 template <int TN, class T>
 __global__ void __launch_bounds__(I8Split<TN>::THREADS, I8Split<TN>::BLOCKS)
@@ -122,17 +156,22 @@ i8_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         }
         __syncwarp();
     }
+    const int have = min(TN, p.rows - t0), f = f0 + warp * 32 + lane;
+    float *x_scales = reinterpret_cast<float *>(smem + L::SCALE_OFF);
+    float w_scale = 0.0f, bias = 0.0f;
+    if (warp < 4) {
+        for (int c = threadIdx.x; c < have; c += 128) x_scales[c] = p.x_scales[t0 + c];
+        if (f < p.n) {
+            w_scale = p.w_scales[f];
+            if (p.bias) bias = p.bias[f];
+        }
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+    }
     // every instruction has completed: the sums are there, and the ring is free
     const bool ok = __all_sync(0xffffffffu, short_wait(done, 0u, abort_flag, 2, p.err, p.wait_limit));
     tc_fence_after();
-    const int have = min(TN, p.rows - t0), f = f0 + warp * 32 + lane;
     const uint32_t at = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
     T *out = static_cast<T *>(p.out) + (int64_t)t0 * p.ldo + f;
-    float w_scale = 0.0f, bias = 0.0f;
-    if (warp < 4 && f < p.n) {
-        w_scale = p.w_scales[f];
-        if (p.bias) bias = p.bias[f];
-    }
     if (log_ranks == 0) {
         if (warp < 4 && ok)
 #pragma unroll 1
@@ -142,7 +181,7 @@ i8_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                 if (f < p.n)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        if (c0 + i < have) out[(int64_t)(c0 + i) * p.ldo] = from_f32<T>(i8_result((int)v[i], p.x_scales[t0 + c0 + i], w_scale, bias));
+                        if (c0 + i < have) out[(int64_t)(c0 + i) * p.ldo] = from_f32<T>(i8_result((int)v[i], x_scales[c0 + i], w_scale, bias));
                 __syncwarp();
             }
     } else {
@@ -158,23 +197,11 @@ i8_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         __syncwarp();
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-        if (warp < 4 && f < p.n)                                                 // tokens rank, rank + ranks, ... of the tile
-#pragma unroll 2
-            for (int c = rank; c < have; c += ranks) {
-                int v[8], sum = 0;
-#pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    v[q] = 0;
-                    if (q < ranks) {
-                        uint32_t there;
-                        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine + c * 512), "r"(q));
-                        asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v[q]) : "r"(there) : "memory");
-                    }
-                }
-#pragma unroll
-                for (int q = 0; q < 8; ++q) sum += v[q];
-                out[(int64_t)c * p.ldo] = from_f32<T>(i8_result(sum, p.x_scales[t0 + c], w_scale, bias));
-            }
+        if (warp < 4 && f < p.n) {
+            if (log_ranks == 1) i8_add_ranks<2>(mine, rank, have, out, p.ldo, x_scales, w_scale, bias);
+            else if (log_ranks == 2) i8_add_ranks<4>(mine, rank, have, out, p.ldo, x_scales, w_scale, bias);
+            else i8_add_ranks<8>(mine, rank, have, out, p.ldo, x_scales, w_scale, bias);
+        }
         __syncwarp();
         asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");    // nobody leaves while its sums are read
         asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
@@ -237,23 +264,23 @@ __device__ __forceinline__ void i8_store_quarter(uint32_t taddr, uint32_t buf, c
                          ::"r"(at + i * 16 * 80 + h * 32), "r"(v[4 * i]), "r"(v[4 * i + 1]), "r"(v[4 * i + 2]), "r"(v[4 * i + 3]) : "memory");
     }
     __syncwarp();
-    const int c0 = f + (lane >> 3) * 8;
-    uint4 v[4];
+    if (vec && f + 32 <= n) {
+        const int c0 = f + (lane >> 3) * 8;
+        uint4 v[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = lds_128(buf + (i * 8 + (lane & 7)) * 80 + (lane >> 3) * 16);
+        for (int i = 0; i < 4; ++i) v[i] = lds_128(buf + (i * 8 + (lane & 7)) * 80 + (lane >> 3) * 16);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int token = i * 8 + (lane & 7);
-        if (token < tokens) {
-            T *dst = row0 + (int64_t)token * ldo + c0;
-            if (vec && c0 + 8 <= n) {
-                *reinterpret_cast<uint4 *>(dst) = v[i];
-            } else {
-                const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (c0 + j < n) reinterpret_cast<uint16_t *>(dst)[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
-            }
+        for (int i = 0; i < 4; ++i) {
+            const int token = i * 8 + (lane & 7);
+            if (token < tokens) *reinterpret_cast<uint4 *>(row0 + (int64_t)token * ldo + c0) = v[i];
+        }
+    } else if (f + lane < n) {                   // a token's 32 features by the warp, element by element
+        uint16_t *dst = reinterpret_cast<uint16_t *>(row0) + f + lane;
+#pragma unroll 8
+        for (int token = 0; token < 32; ++token) {
+            uint16_t v;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(buf + token * 80 + lane * 2) : "memory");
+            if (token < tokens) dst[(int64_t)token * ldo] = v;
         }
     }
     __syncwarp();

@@ -126,6 +126,32 @@ def test_gemm_by_pairs(t, qnn, dtype, rows, n, k):
     assert t.equal(got, want.to(got.dtype)) and qnn.tensor_path_status() == 0
 
 
+FORMS = {(16, 1): (5, 16, 32), (16, 2): (467, 130, 914), (16, 4): (1, 16, 390), (16, 8): (1, 17, 925), (32, 1): (2087, 138, 32),
+         (32, 2): (759, 270, 2475), (32, 4): (482, 129, 1923), (32, 8): (251, 129, 3590), (64, 1): (2821, 276, 32), (64, 2): (1027, 411, 3243),
+         (64, 4): (530, 405, 3052), (64, 8): (457, 134, 4873), (128, 1): (3605, 542, 49), (128, 2): (976, 922, 2333), (128, 4): (991, 411, 2959),
+         (128, 8): (228, 771, 9757), (128, 0): (2064, 900, 45), (256, 0): (1703, 1294, 538)}
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("form", FORMS)
+def test_gemm_by_every_form(t, qnn, dtype, form):
+    """Every tile and split that the plan can choose, at a small size that it serves; operands that grow out of one another on the way
+    (a call's result feeds the next one's rows), queued without a wait."""
+    rows, n, k = FORMS[form]
+    assert qnn.i8_plan(rows, n, k) == form
+    rng = np.random.default_rng(rows + n + k)
+    xd, wd = rows_of(t, qnn, *random_rows(rng, rows, k)), rows_of(t, qnn, *random_rows(rng, n, k))
+    kind = ref.torch_type(dtype)
+    acc = xd.codes.double() @ wd.codes.double().t()
+    want = (acc.float() * xd.scales.view(-1, 1) * wd.scales).to(kind)
+    t.cuda.synchronize()
+    for _ in range(3):
+        got = qnn.i8_gemm(xd, wd, kind)
+        chained = qnn.i8_quantize(got)
+        assert t.equal(got, want) and t.equal(chained.codes, qnn.i8_quantize(want).codes)
+    assert qnn.tensor_path_status() == 0
+
+
 def test_gemm_extreme_codes(t, qnn):
     """The longest contraction of the largest codes: the sum is 2^31 - 2^14, rounded once."""
     k = 131071
