@@ -6,6 +6,7 @@
     python -m paper_2106_09886_b200.run_case backward_conv --N 32 --H 14 --W 14 --C 256 --Cout 256
     python -m paper_2106_09886_b200.run_case stack  --net vgg16 [--batch 64] [--layers 0,1] [--table]
     python -m paper_2106_09886_b200.run_case experts --tokens 512 --experts 8 --top 2 --hidden 1024 --inner 2048
+    python -m paper_2106_09886_b200.run_case block  --tokens 512 --experts 32 --top 4 --groups 4 --hidden 1024 --inner 512
 
 Inputs are drawn on the device (half-normal activations, normal weights); this is a timing and
 profiling driver, correctness is the business of the test-suite.  Times are CUDA-event times of
@@ -306,6 +307,97 @@ def time_experts(tokens, experts, top, hidden, inner, group=128, dtype="bf16", r
             "last_loss": losses[-1], "status": qnn.tensor_path_status()}
 
 
+class FeedForwardBlock:
+    """The feed-forward half of a decoder block: norm of x + residual, then a dense branch with weights and activations in 8 bits and,
+    beside it, a layer of experts on 4-bit weights that sigmoid scores route to, balanced by a bias and limited to the best half of
+    the groups:
+
+        h = x + residual     y = rms_norm(h)     out = h + down(silu(up(y))) + sum of weight * W2_e silu(W1_e y)
+
+    The real weights are kept for training: backward gives the gradients of the decoded ones, straight through every rounding."""
+
+    def __init__(self, hidden, inner, experts, top, groups=1, group=64, dtype=torch.bfloat16, seed=0, dev="cuda:0"):
+        g = torch.Generator(device=dev).manual_seed(seed)
+        normal = lambda *shape: torch.randn(shape, device=dev, generator=g)
+        self.top, self.groups, self.group, self.dtype, self.factor, self.eps = top, groups, group, dtype, 2.0, 1e-6
+        self.gain = (1.0 + 0.1 * normal(hidden)).to(dtype)
+        self.router, self.bias = normal(experts, hidden) * hidden ** -0.5, normal(experts) * 0.05
+        self.w1, self.w2 = normal(experts, inner, hidden) * hidden ** -0.5, normal(experts, hidden, inner) * inner ** -0.5
+        self.up, self.down = normal(2 * inner, hidden) * hidden ** -0.5, normal(hidden, 2 * inner) * (2 * inner) ** -0.5
+        self.pack()
+
+    def pack(self):
+        self.q1, self.q2 = qnn.g4_pack_weights(self.w1, self.group), qnn.g4_pack_weights(self.w2, self.group)
+        self.q_up, self.q_down = qnn.i8_quantize(self.up), qnn.i8_quantize(self.down)
+
+    def forward(self, x, residual, mask=None):
+        """x, residual [tokens, hidden]; mask (optional) [tokens], False for padding, which no expert sees.  Returns out and what
+        backward needs."""
+        silu = torch.nn.functional.silu
+        rows, y, h, rstd = qnn.rms_norm_i8(x, self.gain, self.eps, residual, both=True)
+        a = qnn.i8_gemm(rows, self.q_up, self.dtype)
+        act = qnn.i8_quantize(silu(a))
+        dense = qnn.i8_gemm(act, self.q_down, self.dtype)
+        logits = y.float() @ self.router.t()
+        routes = qnn.route(logits, self.top, "sigmoid", self.bias, self.groups, max(1, self.groups // 2), "top2", True, self.factor, mask)
+        expert_rows = y[routes.order.clamp(min=0) // self.top]
+        b = qnn.g4_expert_gemm(expert_rows, self.q1, routes.offsets)
+        z = qnn.g4_expert_gemm(silu(b), self.q2, routes.offsets)
+        there = (routes.place >= 0).unsqueeze(2)
+        picked = torch.where(there, z[routes.place.clamp(min=0)].float(), 0.0)                # [tokens, top, hidden]
+        out = h.float() + dense.float() + (picked * routes.weights.unsqueeze(2)).sum(1)
+        return out.to(x.dtype), (rows, y, h, rstd, a, act, logits, routes, expert_rows, b, picked)
+
+    def backward(self, dout, saved):
+        """Gradients of sum(dout * out) with respect to x (the residual's too) and the weights."""
+        rows, y, h, rstd, a, act, logits, routes, expert_rows, b, picked = saved
+        everything = torch.tensor([0, y.shape[0]], dtype=torch.int32, device=y.device)
+        dsilu = lambda v: (lambda s: s * (1 + v.float() * (1 - s)))(torch.sigmoid(v.float()))
+        d = dout.to(self.dtype)
+        grads = {"down": qnn.expert_gemm_backward_weights(d, qnn.i8_decode(act, self.dtype), everything)[0]}
+        da = ((d.float() @ qnn.i8_decode(self.q_down, torch.float32)) * dsilu(a)).to(self.dtype)
+        grads["up"] = qnn.expert_gemm_backward_weights(da, qnn.i8_decode(rows, self.dtype), everything)[0]
+        dy = da.float() @ qnn.i8_decode(self.q_up, torch.float32)
+        slot = routes.order.clamp(min=0)
+        dz = (d.float()[slot // self.top] * routes.weights.reshape(-1)[slot].unsqueeze(1)).to(self.dtype)
+        grads["w2"] = qnn.expert_gemm_backward_weights(dz, torch.nn.functional.silu(b), routes.offsets)
+        db = (qnn.g4_expert_gemm_backward_data(dz, self.q2, routes.offsets).float() * dsilu(b)).to(self.dtype)
+        grads["w1"] = qnn.expert_gemm_backward_weights(db, expert_rows, routes.offsets)
+        drows = qnn.g4_expert_gemm_backward_data(db, self.q1, routes.offsets)
+        dy += torch.where((routes.place >= 0).unsqueeze(2), drows[routes.place.clamp(min=0)].float(), 0.0).sum(1)
+        dlogits = qnn.route_backward((picked * d.float().unsqueeze(1)).sum(2), logits, routes.experts, "sigmoid", True, self.factor)
+        grads["router"] = dlogits.t() @ y.float()
+        dy += dlogits @ self.router
+        grads["x"], grads["gain"] = qnn.rms_norm_backward(dy.to(self.dtype), h, self.gain, rstd, d)
+        return grads
+
+    def train_step(self, x, residual, target, rate):
+        """One step of gradient descent on 0.5 * mean squared error.  Returns the loss."""
+        out, saved = self.forward(x, residual)
+        diff = out.float() - target
+        grads = self.backward(diff / x.shape[0], saved)
+        for name in ("w1", "w2", "up", "down", "router"):
+            getattr(self, name).sub_(rate * grads[name])
+        self.gain = (self.gain.float() - rate * grads["gain"]).to(self.dtype)
+        self.pack()
+        return float(0.5 * diff.square().sum(1).mean())
+
+
+def time_block(tokens, experts, top, groups, hidden, inner, dtype="bf16", reps=5, warmup=3, dev="cuda:0"):
+    kind = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}[dtype]
+    block = FeedForwardBlock(hidden, inner, experts, top, groups, dtype=kind, dev=dev)
+    g = torch.Generator(device=dev).manual_seed(1)
+    x, residual = (torch.randn((tokens, hidden), device=dev, generator=g).to(kind) for _ in range(2))
+    target = torch.randn((tokens, hidden), device=dev, generator=g)
+    prompt = statistics.median(_time_calls(lambda i: block.forward(x, residual), reps, warmup))
+    token = statistics.median(_time_calls(lambda i: block.forward(x[:1], residual[:1]), reps, warmup))
+    losses = []
+    step = statistics.median(_time_calls(lambda i: losses.append(block.train_step(x, residual, target, 0.05)), reps, warmup))
+    return {"call": "block", "tokens": tokens, "experts": experts, "top": top, "groups": groups, "hidden": hidden, "inner": inner,
+            "dtype": dtype, "forward_ms": prompt, "one_token_ms": token, "train_step_ms": step, "first_loss": losses[0],
+            "last_loss": losses[-1], "status": qnn.tensor_path_status()}
+
+
 def _report(call, Mg, Ng, Kg, ab, wb, times):
     ms = statistics.median(times)
     macs = float(Mg) * Ng * Kg
@@ -349,7 +441,11 @@ def main():
     for name, default in (("tokens", 512), ("experts", 8), ("top", 2), ("hidden", 1024), ("inner", 2048), ("group", 128)):
         x.add_argument(f"--{name}", type=int, default=default)
     x.add_argument("--dtype", choices=["bf16", "fp16", "fp32"], default="bf16")
-    for s in (g, c, e, k, mb, bw, bc, x):
+    fb = sub.add_parser("block")
+    for name, default in (("tokens", 512), ("experts", 32), ("top", 4), ("groups", 4), ("hidden", 1024), ("inner", 512)):
+        fb.add_argument(f"--{name}", type=int, default=default)
+    fb.add_argument("--dtype", choices=["bf16", "fp16", "fp32"], default="bf16")
+    for s in (g, c, e, k, mb, bw, bc, x, fb):
         s.add_argument("--reps", type=int, default=5)
         s.add_argument("--warmup", type=int, default=3)
         s.add_argument("--sets", type=int, default=3)
@@ -364,6 +460,8 @@ def main():
         r = time_backward_conv(a.N, a.H, a.W, a.C, a.Cout, a.R, a.S, a.stride, a.pad, a.ab, a.wb, a.reps, a.warmup)
     elif a.case == "experts":
         r = time_experts(a.tokens, a.experts, a.top, a.hidden, a.inner, a.group, a.dtype, a.reps, a.warmup)
+    elif a.case == "block":
+        r = time_block(a.tokens, a.experts, a.top, a.groups, a.hidden, a.inner, a.dtype, a.reps, a.warmup)
     elif a.case == "mbit":
         r = time_mbit(a.n, a.bits, a.reps, a.warmup)
     elif a.case == "stack":
