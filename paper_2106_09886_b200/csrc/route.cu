@@ -23,6 +23,7 @@ __host__ __device__ constexpr int choose_threads(int v) { return v <= 8 ? 1024 :
 // Warps that rank a run's slots, each with counts of its own.
 __host__ __device__ constexpr int rank_warps(int experts) { return experts <= 256 ? 32 : experts <= 512 ? 16 : 8; }
 constexpr int MAX_RUNS = 148;                                 // of tokens, a block each
+constexpr int ALONE_TOKENS = 16;                              // up to so many make one run, whose block makes the plan as well
 constexpr int SCANNED_RUNS = 32;                              // up to so many a block adds up the runs ahead of it itself
 constexpr int64_t ROUTE_MAX_SLOTS = (1ll << 31) - 1;
 
@@ -33,7 +34,7 @@ struct RouteParams {
     int tokens, experts, top;
     bool sigmoid, renormalise, by_sums;                       // by_sums: groups are judged by the sum of their two largest keys
     const float *bias;
-    int groups, top_groups, each, lanes, pitch;               // experts, lanes and key pitch of a group
+    int groups, top_groups, each, log_lanes, pitch;           // experts, lanes (a power of two) and key pitch of a group
     uint32_t group_of;                                        // ceil(2^20 / each): e / each = e * group_of >> 20 for e < 1024
     bool whole;                                               // groups of 32: register v holds group v
     float factor;
@@ -152,17 +153,17 @@ __device__ __forceinline__ bool keep_groups(const RouteParams &p, const K (&wort
         if (e < p.experts) scratch[e + group_of(p, e) * (p.pitch - p.each)] = keys[v] != no_key ? worth[v] : none;
     }
     __syncwarp();
-    const int group = lane / p.lanes, sub = lane - group * p.lanes;
+    const int lanes = 1 << p.log_lanes, group = lane >> p.log_lanes, sub = lane & (lanes - 1);
     K first = none, second = none;
     if (group < p.groups)
 #pragma unroll 4
-        for (int i = sub; i < p.each; i += p.lanes) {
+        for (int i = sub; i < p.each; i += lanes) {
             const K k = scratch[group * p.pitch + i];
             second = k > first ? first : (k > second ? k : second);
             first = k > first ? k : first;
         }
     __syncwarp();
-    for (int d = 1; d < p.lanes; d <<= 1) {
+    for (int d = 1; d < lanes; d <<= 1) {
         const K a = __shfl_xor_sync(0xffffffffu, first, d), b = __shfl_xor_sync(0xffffffffu, second, d);
         const K low = a > first ? first : a, high = a > first ? a : first;
         second = b > second ? b : second;
@@ -170,10 +171,10 @@ __device__ __forceinline__ bool keep_groups(const RouteParams &p, const K (&wort
         first = high;
     }
     bool close;
-    const unsigned stay = best_groups<K>(p, p.by_sums ? first + second : first, group < p.groups && sub == 0, p.lanes, margin, close);
+    const unsigned stay = best_groups<K>(p, p.by_sums ? first + second : first, group < p.groups && sub == 0, lanes, margin, close);
 #pragma unroll
     for (int v = 0; v < V; ++v)
-        if (lane + 32 * v < p.experts && !((stay >> (group_of(p, lane + 32 * v) * p.lanes)) & 1u)) keys[v] = no_key;
+        if (lane + 32 * v < p.experts && !((stay >> (group_of(p, lane + 32 * v) << p.log_lanes)) & 1u)) keys[v] = no_key;
     return close;
 }
 // The same for groups of 32 experts: register v of the lanes holds group v, worth as ordered numbers.  The two largest of every group
@@ -429,16 +430,17 @@ __device__ __forceinline__ int route_token(const RouteParams &p, int64_t token, 
 
 // Places of the slots of one run.  base[e]: in, the first row of expert e for this run.  counts: [warps][experts].
 __device__ void rank_run(const RouteParams &p, int run, int32_t *base, int32_t *counts) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = min(rank_warps(p.experts), (int)blockDim.x >> 5);
-    const int64_t first = (int64_t)run * p.run * p.top, end_token = min((int64_t)p.tokens, (int64_t)(run + 1) * p.run);
-    const int64_t slots = end_token * p.top - first, segment = (slots + warps * 32 - 1) / (warps * 32) * 32;
-    const int64_t lo = warp * segment, hi = warp < warps ? min(slots, lo + segment) : lo;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, all = (int)blockDim.x >> 5;
+    const int log_warps = 31 - __clz(min(rank_warps(p.experts), all)), warps = 1 << log_warps;
+    const int first = run * p.run * p.top, slots = min(p.tokens - run * p.run, p.run) * p.top;               // (fewer than 2^31 in all)
+    const int segment = ((slots - 1) >> (log_warps + 5)) + 1 << 5;                                            // whole 32s
+    const int lo = min(slots, warp * segment), hi = warp < warps ? min(slots - lo, segment) + lo : lo;
     // a run of up to 32 slots a warp is ranked in one step, whose slots stay in registers
     const int e0 = lo + lane < hi ? p.chosen[first + lo + lane] : -1;
     for (int i = threadIdx.x; i < warps * p.experts; i += blockDim.x) counts[i] = 0;
     __syncthreads();
     const unsigned same0 = __match_any_sync(0xffffffffu, e0);
-    for (int64_t i = lo; i < hi; i += 32) {
+    for (int i = lo; i < hi; i += 32) {
         const int e = i == lo ? e0 : i + lane < hi ? p.chosen[first + i + lane] : -1;
         const unsigned same = i == lo ? same0 : __match_any_sync(0xffffffffu, e);
         if (e >= 0 && __ffs(same) - 1 == lane) counts[warp * p.experts + e] += __popc(same);
@@ -455,7 +457,7 @@ __device__ void rank_run(const RouteParams &p, int run, int32_t *base, int32_t *
         }
     }
     __syncthreads();
-    for (int64_t i = lo; i < hi; i += 32) {
+    for (int i = lo; i < hi; i += 32) {
         const bool in = i + lane < hi;
         const int e = i == lo ? e0 : in ? p.chosen[first + i + lane] : -1;
         const unsigned same = i == lo ? same0 : __match_any_sync(0xffffffffu, e);
@@ -464,7 +466,7 @@ __device__ void rank_run(const RouteParams &p, int run, int32_t *base, int32_t *
         if (e >= 0 && __ffs(same) - 1 == lane) counts[warp * p.experts + e] += __popc(same);
         __syncwarp();
         if (in) p.place[first + i + lane] = at;
-        if (e >= 0) p.order[at] = (int32_t)(first + i + lane);
+        if (e >= 0) p.order[at] = first + i + lane;
     }
 }
 
@@ -532,8 +534,8 @@ __global__ void __launch_bounds__(choose_threads(V)) route_choose_kernel(const _
     bias_most = warp_most(bias_most);
     double *scratch = reinterpret_cast<double *>(words + RouteSmem::keys(p.experts)) + warp * (p.groups > 1 ? p.groups * p.pitch : 0);
     __syncthreads();
-    const int64_t first = (int64_t)blockIdx.x * p.run, last = min((int64_t)p.tokens, first + p.run);
-    for (int64_t t = first + warp; t < last; t += blockDim.x >> 5) {
+    const int first = blockIdx.x * p.run, last = first + min(p.tokens - first, p.run);
+    for (int t = first + warp; t < last; t += blockDim.x >> 5) {
         const int e = route_token<V>(p, t, bias, bias_most, scratch);
         if (lane < p.top && e >= 0) atomicAdd(&words[e], 1);
     }
@@ -692,12 +694,13 @@ __global__ void __launch_bounds__(256) route_back_kernel(const RouteBackParams p
 
 // ------------------------------------------------------------------------------------------------ host side
 
-// Runs of tokens: one for so few that a block's warps take two each (a second launch costs more than that), else as many as there are
-// SMs, of at least 32 tokens.  Sized for 148 SMs, so that workspace queries and calls agree.
+// Runs of tokens: one for so few that the warps of a block take less time than a second launch (50 x 144 in groups: 12 us in one
+// block, 8 by runs), else as many as there are SMs, of at least eight tokens.  Sized for 148 SMs, so that workspace queries and
+// calls agree.
 int route_run(int64_t tokens) {
-    if (tokens <= 64) return 64;
+    if (tokens <= ALONE_TOKENS) return ALONE_TOKENS;
     const int64_t each = (tokens + MAX_RUNS - 1) / MAX_RUNS;
-    return (int)(each < 32 ? 32 : each);
+    return (int)(each < 8 ? 8 : each);
 }
 int route_runs(int64_t tokens) { return (int)((tokens + route_run(tokens) - 1) / route_run(tokens)); }
 
@@ -723,10 +726,11 @@ template <int V> int route_launch(const RouteParams &p, cudaStream_t st) {
         const int some = max(p.tokens, (p.experts + 63) / 64) * 32;
         return launch_route<route_choose_kernel<V, true>>(1, some < threads ? some : threads, smem, st, p);
     }
-    const int rc = launch_route<route_choose_kernel<V, false>>(p.runs, threads, smem, st, p);
+    const int some = p.run * 32;
+    const int rc = launch_route<route_choose_kernel<V, false>>(p.runs, some < threads ? some : threads, smem, st, p);
     if (rc != QNN_OK || !p.order) return rc;
     const int scanned = p.runs > SCANNED_RUNS ? launch_early(route_scan_kernel, dim3((p.experts + 7) / 8), dim3(256), st, p) : QNN_OK;
-    return scanned != QNN_OK ? scanned : launch_route<route_plan_kernel>(p.runs, PLAN_THREADS, fixed, st, p);
+    return scanned != QNN_OK ? scanned : launch_route<route_plan_kernel>(p.runs, p.run * p.top <= 256 ? 256 : PLAN_THREADS, fixed, st, p);
 }
 template <class T, int V> int back_launch(const RouteBackParams &p, cudaStream_t st) {
     const int64_t blocks = ((int64_t)p.tokens + 7) / 8;
@@ -774,8 +778,7 @@ extern "C" int qnn_route(const void *logits, int type, int64_t tokens, int exper
     p.renormalise = flags & QNN_ROUTE_RENORMALISE;
     p.by_sums = flags & QNN_ROUTE_GROUPS_BY_TWO;
     p.bias = bias; p.groups = groups; p.top_groups = top_groups; p.each = experts / groups;
-    p.lanes = 1;
-    while (p.lanes * 2 * groups <= 32) p.lanes *= 2;
+    while ((2 << p.log_lanes) * groups <= 32) ++p.log_lanes;
     p.pitch = p.each | 1;                                      // (odd: lanes that walk along groups of their own meet no bank conflicts)
     p.group_of = (uint32_t)(((1u << 20) + p.each - 1) / p.each);
     p.whole = p.each == 32;
