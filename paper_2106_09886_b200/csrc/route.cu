@@ -18,8 +18,9 @@ namespace {
 
 constexpr int ROUTE_MAX_EXPERTS = 1024, ROUTE_MAX_TOP = 32, ROUTE_MAX_GROUPS = 32;
 constexpr int PLAN_THREADS = 1024;
-// Threads of a block whose lanes hold V experts each: V numbers of four kinds have to fit the registers.
-__host__ __device__ constexpr int choose_threads(int v) { return v <= 8 ? 1024 : 512; }
+// Threads of a block whose lanes hold V experts each: V numbers of four kinds have to fit the registers (256 experts in groups, one token:
+// 5.2 us with 512 threads of 128 registers, 5.8 with 1024 of 64; 16384 tokens: the same).
+__host__ __device__ constexpr int choose_threads(int v) { return v <= 4 ? 1024 : 512; }
 // Warps that rank a run's slots, each with counts of its own.
 __host__ __device__ constexpr int rank_warps(int experts) { return experts <= 256 ? 32 : experts <= 512 ? 16 : 8; }
 constexpr int MAX_RUNS = 148;                                 // of tokens, a block each
@@ -141,16 +142,16 @@ template <class K> __device__ __forceinline__ unsigned best_groups(const RoutePa
     return stay;
 }
 
-// Experts of groups that are not among the best top_groups get no_key in `keys`.  worth: the keys as numbers, or the scores where
-// sums of them decide and the keys are logits.  Returns whether the decision was too close.
-template <class K, class U, int V>
-__device__ __forceinline__ bool keep_groups(const RouteParams &p, const K (&worth)[V], U (&keys)[V], U no_key, K *scratch, Margin margin) {
+// The worth of lane >> log_lanes' group: its largest number, or the sum of its two largest.  worth: -infinity where an expert is not to
+// be chosen.  By way of shared memory, for groups of any size.
+template <class K, int V>
+__device__ __forceinline__ K group_worth(const RouteParams &p, const K (&worth)[V], K *scratch) {
     const int lane = threadIdx.x & 31;
     const K none = -(K)__int_as_float(0x7F800000);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int e = lane + 32 * v;
-        if (e < p.experts) scratch[e + group_of(p, e) * (p.pitch - p.each)] = keys[v] != no_key ? worth[v] : none;
+        if (e < p.experts) scratch[e + group_of(p, e) * (p.pitch - p.each)] = worth[v];
     }
     __syncwarp();
     const int lanes = 1 << p.log_lanes, group = lane >> p.log_lanes, sub = lane & (lanes - 1);
@@ -170,17 +171,11 @@ __device__ __forceinline__ bool keep_groups(const RouteParams &p, const K (&wort
         second = low > second ? low : second;
         first = high;
     }
-    bool close;
-    const unsigned stay = best_groups<K>(p, p.by_sums ? first + second : first, group < p.groups && sub == 0, lanes, margin, close);
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-        if (lane + 32 * v < p.experts && !((stay >> (group_of(p, lane + 32 * v) << p.log_lanes)) & 1u)) keys[v] = no_key;
-    return close;
+    return p.by_sums ? first + second : first;
 }
-// The same for groups of 32 experts: register v of the lanes holds group v, worth as ordered numbers.  The two largest of every group
-// by one exchange that halves the registers at each of its first steps: lane l ends up with group l / (32 / V).
-template <int V>
-__device__ __forceinline__ bool keep_whole_groups(const RouteParams &p, const uint32_t (&worth)[V], uint32_t (&keys)[V], Margin margin) {
+// The same for groups of 32 experts: register v of the lanes holds group v, as ordered numbers.  The two largest of every group by
+// one exchange that halves the registers at each of its first steps: lane l ends up with group l / (32 / V), where group_worth has it.
+template <int V> __device__ __forceinline__ float whole_group_worth(const RouteParams &p, const uint32_t (&worth)[V]) {
     const int lane = threadIdx.x & 31;
     uint32_t first[V], second[V];
 #pragma unroll
@@ -206,14 +201,20 @@ __device__ __forceinline__ bool keep_whole_groups(const RouteParams &p, const ui
             first[0] = max(first[0], b);
         }
     }
-    const float w = p.by_sums ? __fadd_rn(from_ordered(first[0]), from_ordered(second[0])) : from_ordered(first[0]);
-    constexpr int LANES = 32 / V;
-    bool close;
-    const unsigned stay = best_groups<float>(p, w, lane % LANES == 0 && lane / LANES < p.groups, LANES, margin, close);
+    return p.by_sums ? __fadd_rn(from_ordered(first[0]), from_ordered(second[0])) : from_ordered(first[0]);
+}
+// Lanes whose group is at bit group << log_lanes of a warp's mask.
+__device__ __forceinline__ bool holds_group(const RouteParams &p) {
+    const int lane = threadIdx.x & 31;
+    return lane >> p.log_lanes < p.groups && (lane & ((1 << p.log_lanes) - 1)) == 0;
+}
+template <class U, int V> __device__ __forceinline__ void keep_groups(const RouteParams &p, unsigned stay, U (&keys)[V], U no_key) {
+    const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-        if (v < p.groups && !(stay >> (v * LANES) & 1u)) keys[v] = NO_KEY;
-    return close;
+    for (int v = 0; v < V; ++v) {
+        const int e = lane + 32 * v;
+        if (e < p.experts && !(stay >> ((p.whole ? v : group_of(p, e)) << p.log_lanes) & 1u)) keys[v] = no_key;
+    }
 }
 
 // The `top` largest keys in order, ties to the lowest expert: lane i gets choice i (-1 where nothing is left).
@@ -257,52 +258,40 @@ template <int V> __device__ __forceinline__ void sort_keys(uint32_t (&k)[V]) {
                     }
 }
 
-// The same choice with V - 1 - v in the lowest bits of a key in place of its own: a lane sorts its keys once and then gives its head
-// away, which carries the expert with it.  close: whether two keys in a row (the first that was not chosen among them) are too near:
-// by the margin, or (BIAS false: keys are logits, exact up to the bits that were cut, which narrow types do not have) equal but for
-// those bits.
-template <bool BIAS, int V>
-__device__ __forceinline__ int take_top_sorted(const RouteParams &p, uint32_t (&keys)[V], Margin margin, bool &close) {
+// Choices lo .. hi - 1 with V - 1 - v in the lowest bits of a key in place of its own: the lanes' keys are sorted, and each round a lane
+// gives its head away, which carries the expert with it.  Lane i gets choice i (-1 where nothing is left); best: the next head.
+template <int V> __device__ __forceinline__ void take_sorted(uint32_t (&keys)[V], int lo, int hi, int &mine, uint32_t &best) {
     const int lane = threadIdx.x & 31;
     constexpr uint32_t LOW = V - 1;
-#pragma unroll
-    for (int v = 0; v < V; ++v) keys[v] = (keys[v] & ~LOW) | (LOW - v);
-    sort_keys<V>(keys);
     int from = 0;
     uint32_t key = NO_KEY;
-    uint32_t best = __reduce_max_sync(0xffffffffu, keys[0]);
 #pragma unroll 1
-    for (int i = 0; i < p.top && best > NO_KEY; ++i) {
+    for (int i = lo; i < hi && best > NO_KEY; ++i) {
         const int owner = __ffs(__ballot_sync(0xffffffffu, keys[0] == best)) - 1;
         from = lane == i ? owner : from;
         key = lane == i ? best : key;
-        const bool mine = lane == owner;
+        const bool gives = lane == owner;
 #pragma unroll
-        for (int v = 0; v + 1 < V; ++v) keys[v] = mine ? keys[v + 1] : keys[v];
-        keys[V - 1] = mine ? NO_KEY : keys[V - 1];
+        for (int v = 0; v + 1 < V; ++v) keys[v] = gives ? keys[v + 1] : keys[v];
+        keys[V - 1] = gives ? NO_KEY : keys[V - 1];
         best = __reduce_max_sync(0xffffffffu, keys[0]);
     }
-    const uint32_t behind = __shfl_down_sync(0xffffffffu, key, 1), next = lane == p.top - 1 ? best : behind;
-    bool near = false;
-    if (lane < p.top && next > NO_KEY) {
-        if constexpr (BIAS) near = margin.close(from_ordered(key), from_ordered(next));
-        else near = p.type == QNN_F32 && (key & ~LOW) == (next & ~LOW);
-    }
-    close = __any_sync(0xffffffffu, near);
-    return key > NO_KEY ? from + 32 * (int)(LOW - (key & LOW)) : -1;
+    if (key > NO_KEY) mine = from + 32 * (int)(LOW - (key & LOW));
 }
 
-// The same decisions with 64-bit keys.
-template <int V>
-__device__ __noinline__ int choose_in_64_bits(const RouteParams &p, int64_t token, double *scratch) {
-    const int lane = threadIdx.x & 31;
-    float l[V];
-    load_row<V>(p.logits, p.type, token * p.ld, p.experts, l);
-    double s[V];
-    unsigned long long keys[V];
+// 1 / (1 + exp(-x)): for the exponential t of -|x| one over 1 + t, which is between 1 and 2, by Newton's iteration from fp32's.
+__device__ __forceinline__ double sigmoid_64(double x) {
+    const double t = exp(-fabs(x)), y = 1.0 + t;
+    double r = (double)reciprocal((float)y);
+    r = fma(r, fma(-y, r, 1.0), r);
+    r = fma(r, fma(-y, r, 1.0), r);
+    return x >= 0.0 ? r : t * r;
+}
+// Scores of a token's experts in 64 bits.
+template <int V> __device__ __forceinline__ void scores_64(const RouteParams &p, const float (&l)[V], double (&s)[V]) {
     if (p.sigmoid) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) s[v] = 1.0 / (1.0 + exp(-(double)l[v]));
+        for (int v = 0; v < V; ++v) s[v] = sigmoid_64((double)l[v]);
     } else {
         float most = l[0];
 #pragma unroll
@@ -318,6 +307,33 @@ __device__ __noinline__ int choose_in_64_bits(const RouteParams &p, int64_t toke
 #pragma unroll
         for (int v = 0; v < V; ++v) s[v] /= sum;
     }
+}
+// The groups that stay, by 64-bit keys: a mask for keep_groups.
+template <int V>
+__device__ __noinline__ unsigned groups_in_64_bits(const RouteParams &p, int64_t token, double *scratch) {
+    const int lane = threadIdx.x & 31;
+    float l[V];
+    load_row<V>(p.logits, p.type, token * p.ld, p.experts, l);
+    double s[V];
+    scores_64<V>(p, l, s);
+    const double none = -(double)__int_as_float(0x7F800000);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const float b = p.bias && lane + 32 * v < p.experts ? p.bias[lane + 32 * v] : 0.0f;
+        s[v] = l[v] > __int_as_float(0xFF800000) && b == b ? s[v] + (double)b : none;
+    }
+    bool close;
+    return best_groups<double>(p, group_worth<double, V>(p, s, scratch), holds_group(p), 1 << p.log_lanes, Margin{}, close);
+}
+// All decisions with 64-bit keys; stay: the groups.
+template <int V>
+__device__ __noinline__ int choose_in_64_bits(const RouteParams &p, int64_t token, unsigned stay) {
+    const int lane = threadIdx.x & 31;
+    float l[V];
+    load_row<V>(p.logits, p.type, token * p.ld, p.experts, l);
+    double s[V];
+    unsigned long long keys[V];
+    if (p.bias) scores_64<V>(p, l, s);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int e = lane + 32 * v;
@@ -327,8 +343,54 @@ __device__ __noinline__ int choose_in_64_bits(const RouteParams &p, int64_t toke
             keys[v] = p.bias ? ordered(s[v]) : ordered((double)l[v]);
         }
     }
-    if (p.groups > 1) keep_groups<double, unsigned long long, V>(p, s, keys, 0ull, scratch, Margin{});
+    if (p.groups > 1) keep_groups<unsigned long long, V>(p, stay, keys, 0ull);
     return take_top(p.top, keys);
+}
+
+// The same by candidates alone: those in lanes 0 .. count - 1 are put in order by 64-bit keys; the keys of all others are
+// at most `rest` (NO_KEY: there are none), and where that is too near all decisions are taken so.
+template <int V>
+__device__ __noinline__ int order_in_64_bits(const RouteParams &p, int64_t token, int candidate, int count, uint32_t rest, Margin margin, unsigned stay) {
+    const int lane = threadIdx.x & 31;
+    const bool valid = lane < count && candidate >= 0;
+    const double none = -(double)__int_as_float(0x7F800000);
+    const double x = valid ? (double)load_as_f32(p.logits, p.type, token * p.ld + candidate) : none;
+    double key = x;
+    if (p.bias) {
+        if (p.sigmoid) {
+            key = sigmoid_64(x);
+        } else {
+            float l[V];
+            load_row<V>(p.logits, p.type, token * p.ld, p.experts, l);
+            float most = l[0];
+#pragma unroll
+            for (int v = 1; v < V; ++v) most = fmaxf(most, l[v]);
+            most = warp_most(most);
+            double sum = 0.0;
+#pragma unroll 1
+            for (int v = 0; v < V; ++v) sum += exp((double)l[v] - (double)most);
+            key = exp(x - (double)most) / warp_add(sum);
+        }
+        key = valid ? key + (double)p.bias[candidate] : none;
+    }
+    int rank = 0, mine = -1;
+#pragma unroll 4
+    for (int j = 0; j < count; ++j) {
+        const double k = __shfl_sync(0xffffffffu, key, j);
+        const int e = __shfl_sync(0xffffffffu, candidate, j);
+        rank += e >= 0 && (k > key || (k == key && e < candidate));
+    }
+#pragma unroll 4
+    for (int j = 0; j < count; ++j) {
+        const int r = __shfl_sync(0xffffffffu, rank, j), e = __shfl_sync(0xffffffffu, candidate, j);
+        if (e >= 0 && r == lane && lane < p.top) mine = e;
+    }
+    if (rest > NO_KEY) {
+        const unsigned last = __ballot_sync(0xffffffffu, valid && rank == p.top - 1);
+        const double least = __shfl_sync(0xffffffffu, key, __ffs(last) - 1), most = (double)from_ordered(rest);
+        if (p.bias ? margin.close((float)least, (float)most) : !(least > most)) return choose_in_64_bits<V>(p, token, stay);
+    }
+    return mine;
 }
 
 // Choice and weights of one token, by a warp.  Lane i < top writes choice i and returns it (-1: none).
@@ -346,7 +408,7 @@ __device__ __forceinline__ int route_token(const RouteParams &p, int64_t token, 
     const bool bad = highest > INFINITE_KEY || (!p.sigmoid && highest == INFINITE_KEY);
     most = from_ordered(highest);
     int mine = -1;
-    float sum = 1.0f;
+    float x = none, scale = 1.0f;                             // the chosen logit, one over softmax's sum
     if (there && !bad && highest > NO_KEY) {
         const bool scored = p.bias || (p.groups > 1 && p.by_sums);
         float s[V];
@@ -355,14 +417,13 @@ __device__ __forceinline__ int route_token(const RouteParams &p, int64_t token, 
 #pragma unroll
                 for (int v = 0; v < V; ++v) s[v] = reciprocal(__fadd_rn(1.0f, expf(-l[v])));
             } else {
-                sum = 0.0f;
+                float sum = 0.0f;
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
                     s[v] = expf(__fadd_rn(l[v], -most));
                     sum = __fadd_rn(sum, s[v]);
                 }
-                sum = warp_add(sum);
-                const float scale = reciprocal(sum);
+                scale = reciprocal(warp_add(sum));
 #pragma unroll
                 for (int v = 0; v < V; ++v) s[v] = __fmul_rn(s[v], scale);
             }
@@ -370,9 +431,9 @@ __device__ __forceinline__ int route_token(const RouteParams &p, int64_t token, 
         uint32_t keys[V];
         // A score is off by at most (sigmoid) expf's two steps, half a step of the sum and one of the quotient, 1.75 * 2^-22; (softmax)
         // besides by the roundings of a difference of logits that matters up to some 88 and of a sum, 40 * 2^-22 in all.  The sum with
-        // the bias is off by 2^-24, and the key by the bits that the expert takes, V * 2^-23.  Two keys: twice that.
-        const Margin margin{(p.sigmoid ? 5.0f : 80.0f) * 2.384185791015625e-07f + V * 2.384185791015625e-07f, bias_most};
-        bool close = false;
+        // the bias is off by 2^-24.  Two keys: twice that.
+        const Margin margin{(p.sigmoid ? 5.0f : 80.0f) * 2.384185791015625e-07f, bias_most};
+        unsigned stay = 0;
         if (p.bias) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -384,28 +445,56 @@ __device__ __forceinline__ int route_token(const RouteParams &p, int64_t token, 
             for (int v = 0; v < V; ++v) keys[v] = ordered(__fadd_rn(l[v], 0.0f));       // (-0 is 0)
         }
         if (p.groups > 1) {
-            float *floats = reinterpret_cast<float *>(scratch);
-            const bool sums_alone = scored && !p.bias;
-            if (p.whole) {
-                if (sums_alone) {
-                    uint32_t worth[V];
+            float worth;
+            if (p.whole && scored && !p.bias) {
+                uint32_t by_scores[V];
 #pragma unroll
-                    for (int v = 0; v < V; ++v) worth[v] = l[v] > none ? ordered(s[v]) : NO_KEY;
-                    close = keep_whole_groups<V>(p, worth, keys, margin);
-                } else {
-                    close = keep_whole_groups<V>(p, keys, keys, margin) && scored;
-                }
-            } else if (scored) {
-                close = keep_groups<float, uint32_t, V>(p, s, keys, NO_KEY, floats, margin);
+                for (int v = 0; v < V; ++v) by_scores[v] = l[v] > none ? ordered(s[v]) : NO_KEY;
+                worth = whole_group_worth<V>(p, by_scores);
+            } else if (p.whole) {
+                worth = whole_group_worth<V>(p, keys);
             } else {
-                keep_groups<float, uint32_t, V>(p, l, keys, NO_KEY, floats, margin);
+                float numbers[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) numbers[v] = scored && l[v] > none ? s[v] : l[v];
+                worth = group_worth<float, V>(p, numbers, reinterpret_cast<float *>(scratch));
             }
+            bool close;
+            stay = best_groups<float>(p, worth, holds_group(p), 1 << p.log_lanes, margin, close);
+            if (close && scored) stay = groups_in_64_bits<V>(p, token, scratch);       // (logits are compared exactly)
+            keep_groups<uint32_t, V>(p, stay, keys, NO_KEY);
         }
+        constexpr uint32_t LOW = V - 1;
+#pragma unroll
+        for (int v = 0; v < V; ++v) keys[v] = (keys[v] & ~LOW) | (LOW - v);
+        sort_keys<V>(keys);
+        uint32_t best = __reduce_max_sync(0xffffffffu, keys[0]);
+        take_sorted<V>(keys, 0, p.top, mine, best);
+        // Is that order certain?  The keys again, whole, each against the one behind it; the last against the most that any other can be.
+        if (mine >= 0) x = load_as_f32(p.logits, p.type, token * p.ld + mine);
+        float key = x;
+        if (p.bias && mine >= 0)
+            key = __fadd_rn(p.sigmoid ? reciprocal(__fadd_rn(1.0f, expf(-x))) : __fmul_rn(expf(__fadd_rn(x, -most)), scale), p.bias[mine]);
+        float behind = __shfl_down_sync(0xffffffffu, key, 1);
+        int expert = __shfl_down_sync(0xffffffffu, mine, 1);
         bool near;
-        mine = p.bias ? take_top_sorted<true, V>(p, keys, margin, near) : take_top_sorted<false, V>(p, keys, margin, near);
-        if (close || near) mine = choose_in_64_bits<V>(p, token, scratch);
+        if (p.bias) {
+            if (lane == p.top - 1) {
+                behind = from_ordered(best | LOW);
+                expert = best > NO_KEY ? 0 : -1;
+            }
+            near = lane < p.top && mine >= 0 && expert >= 0 && margin.close(key, behind);
+        } else {                                              // (narrow types lose nothing with the lowest bits)
+            near = lane < p.top - 1 ? expert >= 0 && (key < behind || (key == behind && mine > expert))
+                                    : lane == p.top - 1 && mine >= 0 && p.type == QNN_F32 && ordered(__fadd_rn(key, 0.0f)) <= (best | LOW) && best > NO_KEY;
+        }
+        if (__any_sync(0xffffffffu, near)) {
+            const int count = min(32, p.top + 8);
+            take_sorted<V>(keys, p.top, count, mine, best);
+            mine = order_in_64_bits<V>(p, token, mine, count, best > NO_KEY ? best | LOW : NO_KEY, margin, stay);
+            x = mine >= 0 ? load_as_f32(p.logits, p.type, token * p.ld + mine) : none;
+        }
     }
-    const float x = mine >= 0 ? load_as_f32(p.logits, p.type, token * p.ld + mine) : none;
     const float t = expf(-fabsf(x));                          // sigmoid: 1 / (1 + t), or t / (1 + t) below 0
     float w = 0.0f;
     if (p.renormalise) {
@@ -419,7 +508,7 @@ __device__ __forceinline__ int route_token(const RouteParams &p, int64_t token, 
         const float total = warp_add(u);
         if (mine >= 0) w = __fmul_rn(u, reciprocal(total));
     } else if (mine >= 0) {
-        w = p.sigmoid ? __fmul_rn(x >= 0.0f ? 1.0f : t, reciprocal(__fadd_rn(1.0f, t))) : __fmul_rn(expf(__fadd_rn(x, -most)), reciprocal(sum));
+        w = p.sigmoid ? __fmul_rn(x >= 0.0f ? 1.0f : t, reciprocal(__fadd_rn(1.0f, t))) : __fmul_rn(expf(__fadd_rn(x, -most)), scale);
     }
     if (lane < p.top) {
         p.chosen[token * p.top + lane] = mine;
@@ -533,11 +622,15 @@ __global__ void __launch_bounds__(choose_threads(V)) route_choose_kernel(const _
     }
     bias_most = warp_most(bias_most);
     double *scratch = reinterpret_cast<double *>(words + RouteSmem::keys(p.experts)) + warp * (p.groups > 1 ? p.groups * p.pitch : 0);
-    __syncthreads();
     const int first = blockIdx.x * p.run, last = first + min(p.tokens - first, p.run);
-    for (int t = first + warp; t < last; t += blockDim.x >> 5) {
+    int32_t *next = words + RouteSmem::sums(p.experts) + 36;     // warps fetch their tokens: one that took a decision again falls behind
+    if (threadIdx.x == 0) *next = first + (int)(blockDim.x >> 5);
+    __syncthreads();
+    for (int t = first + warp; t < last;) {
         const int e = route_token<V>(p, t, bias, bias_most, scratch);
         if (lane < p.top && e >= 0) atomicAdd(&words[e], 1);
+        if (lane == 0) t = atomicAdd(next, 1);
+        t = __shfl_sync(0xffffffffu, t, 0);
     }
     if (!p.order) return;
     __syncthreads();

@@ -92,6 +92,29 @@ def test_keys_nearer_than_fp32_can_tell(t, qnn, score, groups):
         check(t, qnn, logits, top, bias=bias, score=score, groups=groups, top_groups=max(1, groups // 2), group_score=group_score)
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("experts,top", [(64, 8), (256, 8), (256, 31), (256, 32), (40, 1), (20, 12), (1000, 6)])
+def test_keys_near_one_another_in_places(t, qnn, score, experts, top):
+    """Keys that fp32 cannot tell apart in pairs, in fours, and in one run of twenty, among keys that it can; with and without a bias."""
+    rng = np.random.default_rng(experts + top)
+    for size in (2, 4, 20):
+        if size > experts:
+            continue
+        rows, biases = [], []
+        row = rng.standard_normal(experts).astype(np.float32)
+        s = ref.scores(row[None].astype(np.float64), score)[0]
+        place = rng.permutation(experts)
+        target = 0.2 + 0.6 * np.arange((experts + size - 1) // size)[np.argsort(np.argsort(place)) // size] / experts
+        bias = (target - s).astype(np.float32)
+        check(t, qnn, t.from_numpy(np.repeat(row[None], 40, 0)).to(DEV), top, bias=bias, score=score)
+        check(t, qnn, t.from_numpy(np.repeat(row[None], 40, 0)).to(DEV), top, bias=bias, score=score, groups=4, top_groups=4, group_score="top2")
+        # without a bias: logits that differ in their lowest bits only
+        base = np.repeat(rng.standard_normal((40, (experts + size - 1) // size)), size, 1)[:, :experts].astype(np.float32)
+        bits = base.view(np.int32) + rng.integers(0, 6, base.shape).astype(np.int32)
+        l = np.take_along_axis(bits.view(np.float32), rng.permuted(np.tile(np.arange(experts), (40, 1)), axis=1), 1)
+        check(t, qnn, t.from_numpy(np.ascontiguousarray(l)).to(DEV), top, score=score)
+
+
 def test_excluded_experts_and_tokens(t, qnn):
     """Masked experts, rows that a mask leaves nothing of, NaN and infinities."""
     rng = np.random.default_rng(13)
