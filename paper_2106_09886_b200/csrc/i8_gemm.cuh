@@ -178,10 +178,16 @@ i8_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             for (int c0 = 0; c0 < have; c0 += 16) {
                 uint32_t v[16];
                 tmem_load_lane_16(at + c0, v);
-                if (f < p.n)
+                if (f < p.n) {
+                    if (have - c0 >= 16) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (c0 + i < have) out[(int64_t)(c0 + i) * p.ldo] = from_f32<T>(i8_result((int)v[i], x_scales[c0 + i], w_scale, bias));
+                        for (int i = 0; i < 16; ++i, out += p.ldo) *out = from_f32<T>(i8_result((int)v[i], x_scales[c0 + i], w_scale, bias));
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i, out += p.ldo)
+                            if (c0 + i < have) *out = from_f32<T>(i8_result((int)v[i], x_scales[c0 + i], w_scale, bias));
+                    }
+                }
                 __syncwarp();
             }
     } else {
@@ -220,11 +226,13 @@ template <int TN, class T> struct I8Pair {
     static constexpr int XROWS = TN / 2;                                         // tokens that a block stages
     static constexpr int A_STAGE = 128 * I8_STEP, STAGE = A_STAGE + XROWS * I8_STEP;
     static constexpr int OUT_WARP = sizeof(T) == 2 ? 32 * 80 : 0;                // transposing buffer of a result warp
-    static constexpr int FIXED = 4 * (OUT_WARP + TN * 4) + 2048;
+    static constexpr int FIXED = 8 * (OUT_WARP + TN * 4) + 2048;
     static constexpr int STAGES = (227 * 1024 - FIXED) / STAGE < 8 ? (227 * 1024 - FIXED) / STAGE : 8;
-    static constexpr int OUT_OFF = STAGES * STAGE, SCALE_OFF = OUT_OFF + 4 * OUT_WARP, BAR_OFF = SCALE_OFF + 4 * TN * 4;
+    static constexpr int OUT_OFF = STAGES * STAGE, SCALE_OFF = OUT_OFF + 8 * OUT_WARP, BAR_OFF = SCALE_OFF + 8 * TN * 4;
     static constexpr int TOTAL = BAR_OFF + (2 * STAGES + 5) * 8 + 16 + 1024;
-    static constexpr int THREADS = 256;       // warps: 0 copies, 1 instructions, 2 owner of the tensor memory, 3 idle, 4-7 results
+    // warps: 0 copies, 1 instructions, 2 owner of the tensor memory, 3 idle, 4-11 results (two for each quarter of the lanes, whose
+    // latencies cover one another: 4096 x 5000 x 700 takes 25 us, 28.6 with one)
+    static constexpr int THREADS = 384;
     static_assert(TOTAL <= 227 * 1024, "shared memory");
 };
 
@@ -248,16 +256,17 @@ __device__ __forceinline__ void i8_store_quarter(uint32_t taddr, uint32_t buf, c
     float2 s[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[i] = *reinterpret_cast<const float2 *>(scales + 8 * i + 2 * (lane & 3));
+    uint32_t r[2][16];
+    tmem_load_16x32(taddr, r[0]);
+    tmem_load_16x32(taddr + (16u << 16), r[1]);
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        uint32_t r[16];
-        tmem_load_16x32(taddr + ((uint32_t)(16 * h) << 16), r);
-        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
         uint32_t v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i)              // register pair i: features 16h + 8 (i % 2) + lane / 4, tokens 8 (i / 2) + 2 (lane % 4) + {0, 1}
-            v[i] = pack_pair<T>(i8_result((int)r[2 * i], s[i >> 1].x, w_scale[2 * h + (i & 1)], bias[2 * h + (i & 1)]),
-                                i8_result((int)r[2 * i + 1], s[i >> 1].y, w_scale[2 * h + (i & 1)], bias[2 * h + (i & 1)]));
+            v[i] = pack_pair<T>(i8_result((int)r[h][2 * i], s[i >> 1].x, w_scale[2 * h + (i & 1)], bias[2 * h + (i & 1)]),
+                                i8_result((int)r[h][2 * i + 1], s[i >> 1].y, w_scale[2 * h + (i & 1)], bias[2 * h + (i & 1)]));
 #pragma unroll
         for (int i = 0; i < 2; ++i)
             asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};"
@@ -274,13 +283,22 @@ __device__ __forceinline__ void i8_store_quarter(uint32_t taddr, uint32_t buf, c
             const int token = i * 8 + (lane & 7);
             if (token < tokens) *reinterpret_cast<uint4 *>(row0 + (int64_t)token * ldo + c0) = v[i];
         }
-    } else if (f + lane < n) {                   // a token's 32 features by the warp, element by element
-        uint16_t *dst = reinterpret_cast<uint16_t *>(row0) + f + lane;
-#pragma unroll 8
-        for (int token = 0; token < 32; ++token) {
-            uint16_t v;
-            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(buf + token * 80 + lane * 2) : "memory");
-            if (token < tokens) dst[(int64_t)token * ldo] = v;
+    } else if (f + lane < n) {                   // a token's 32 features by the warp, element by element (pairs of them at even
+        uint16_t *dst = reinterpret_cast<uint16_t *>(row0) + f + lane;      // addresses, half a warp a token, took a third longer)
+        const uint32_t src = buf + lane * 2;
+#pragma unroll 1
+        for (int t0 = 0; t0 < min(tokens, 32); t0 += 8) {
+            uint16_t v[8];
+#pragma unroll
+            for (int t = 0; t < 8; ++t) asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v[t]) : "r"(src + (t0 + t) * 80) : "memory");
+            if (tokens - t0 >= 8) {
+#pragma unroll
+                for (int t = 0; t < 8; ++t, dst += ldo) *dst = v[t];
+            } else {
+#pragma unroll
+                for (int t = 0; t < 8; ++t, dst += ldo)
+                    if (t0 + t < tokens) *dst = v[t];
+            }
         }
     }
     __syncwarp();
@@ -305,7 +323,7 @@ i8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < L::STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 8); }
+        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 16); }
         mbar_init(finish, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -378,9 +396,9 @@ i8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
             __syncwarp();
         }
     } else if (warp >= 4) {
-        const int q = warp & 3;
+        const int q = warp & 3, w = warp - 4;                    // quarter of the lanes; warps w and w + 4 share it
         const uint32_t lanes = (uint32_t)(q * 32) << 16;
-        float *scales = reinterpret_cast<float *>(smem + L::SCALE_OFF) + q * TN;
+        float *scales = reinterpret_cast<float *>(smem + L::SCALE_OFF) + w * TN;
         Ring acc;
 #pragma unroll 1
         for (int t = first; t < items && !__any_sync(0xffffffffu, stop()); t += stride) {
@@ -405,17 +423,24 @@ i8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
             tc_fence_after();
             const uint32_t from = tmem_base + lanes + (uint32_t)(acc.s * TN);
 #pragma unroll 1
-            for (int c0 = 0; c0 < have; c0 += 32) {
+            for (int c0 = (w >> 2) * 32; c0 < have; c0 += 64) {
                 if constexpr (sizeof(T) == 2) {
-                    i8_store_quarter<T>(from + c0, smem_at + L::OUT_OFF + q * L::OUT_WARP, scales + c0, dst + (int64_t)c0 * p.ldo, p.ldo, have - c0, f,
+                    i8_store_quarter<T>(from + c0, smem_at + L::OUT_OFF + w * L::OUT_WARP, scales + c0, dst + (int64_t)c0 * p.ldo, p.ldo, have - c0, f,
                                         p.n, w_scale, bias, p.out_vec);
                 } else {
                     uint32_t v[32];
                     tmem_load_32(from + c0, v);
-                    if (f + lane < p.n)
+                    if (f + lane < p.n) {
+                        T *to = dst + (int64_t)c0 * p.ldo + f + lane;
+                        if (have - c0 >= 32) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (c0 + i < have) dst[(int64_t)(c0 + i) * p.ldo + f + lane] = i8_result((int)v[i], scales[c0 + i], w_scale[0], bias[0]);
+                            for (int i = 0; i < 32; ++i, to += p.ldo) *to = i8_result((int)v[i], scales[c0 + i], w_scale[0], bias[0]);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i, to += p.ldo)
+                                if (c0 + i < have) *to = i8_result((int)v[i], scales[c0 + i], w_scale[0], bias[0]);
+                        }
+                    }
                     __syncwarp();
                 }
             }

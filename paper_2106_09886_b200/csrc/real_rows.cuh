@@ -90,15 +90,9 @@ struct RowScale {
         scale = finite ? fmaxf(__fdiv_rn(m, 127.0f), 1.17549435e-38f) : __int_as_float(0x7FC00000);
         inverse = finite ? __frcp_rn(scale) : 0.0f;
     }
-    // rint(v / scale), the quotient rounded to fp32: the product with the inverse is off by at most 2^-23 of 127, so that only a
-    // quotient next to a half needs the division itself.  0 where the scale is NaN.
-    __device__ __forceinline__ int code(float v) const {
-        const float t = __fmul_rn(v, inverse);
-        float r = rintf(t);
-        if (fabsf(__fadd_rn(t, -r)) > 0.4999f) r = rintf(__fdiv_rn(v, scale));
-        return min(max(__float2int_rn(r), -127), 127);
-    }
-    // The same as the low byte of a word; any byte where the scale is NaN.  (|v| <= 127 scale: no clamp is needed.)
+    // rint(v / scale), the quotient rounded to fp32, as the low byte of a word; any byte where the scale is NaN.  The product with the
+    // inverse is off by at most 2^-23 of 127, so that only a quotient next to a half needs the division itself.  (|v| <= 127 scale:
+    // no clamp is needed.)
     __device__ __forceinline__ uint32_t code_byte(float v) const {
         const float t = __fmul_rn(v, inverse);
         float r = __fadd_rn(t, TO_NEAREST);

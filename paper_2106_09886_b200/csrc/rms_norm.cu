@@ -153,39 +153,41 @@ __global__ void __launch_bounds__(NV == 1 ? 1024 : 512, NV == 2 ? 2 : 1) norm_ro
     }
 }
 
-// Rows whose start, stride or width is not a multiple of 16 bytes: element by element, read again (from the caches) where the
-// packs above stay in registers.
-template <class T, class G, bool NORM>
-__global__ void __launch_bounds__(512) norm_any_kernel(const NormParams p) {
+// Rows whose start, stride or width is not a multiple of 16 bytes: element by element, NE of them a thread, `blockDim.x` apart, so that
+// a warp's accesses lie together whatever the row's alignment.
+template <class T, class G, int NE, bool NORM>
+__global__ void __launch_bounds__(512, NE <= 16 ? 2 : 1) norm_elements_kernel(const NormParams p) {
     __shared__ float parts[2][32];
     start_next();
     wait_for_previous();
-    const int64_t row = blockIdx.x;
-    const T *x = static_cast<const T *>(p.x) + row * p.ldx;
-    const G *gain = static_cast<const G *>(p.gain);
-    float sum = 0.0f, most = 0.0f;
+    const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    if (row >= p.rows) return;                                      // (whole warps: blocks of several rows have one warp a row)
+    const int step = blockDim.x, width = p.width, first = threadIdx.x;
+    const T *x = static_cast<const T *>(p.x) + row * p.ldx + first;
+    const G *gain = static_cast<const G *>(p.gain) + first;
+    T h[NE], r[NE];
+    float v[NE], sum = 0.0f, most = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NE; ++j) h[j] = first + j * step < width ? x[j * step] : from_f32<T>(0.0f);
     if (NORM && p.residual) {
-        const T *res = static_cast<const T *>(p.residual) + row * p.ldr;
-        T *h = static_cast<T *>(p.h) + row * p.ldh;
-#pragma unroll 8
-        for (int i = threadIdx.x; i < p.width; i += blockDim.x) {
-            const T v = from_f32<T>(__fadd_rn(to_f32(x[i]), to_f32(res[i])));
-            const float a = to_f32(v);
-            h[i] = v;
-            sum = __fmaf_rn(a, a, sum);
-            most = max_or_nan(most, fabsf(__fmul_rn(a, to_f32(gain[i]))));
+        const T *res = static_cast<const T *>(p.residual) + row * p.ldr + first;
+        T *out = static_cast<T *>(p.h) + row * p.ldh + first;
+#pragma unroll
+        for (int j = 0; j < NE; ++j) r[j] = first + j * step < width ? res[j * step] : from_f32<T>(0.0f);
+#pragma unroll
+        for (int j = 0; j < NE; ++j) {
+            h[j] = from_f32<T>(__fadd_rn(to_f32(h[j]), to_f32(r[j])));
+            if (first + j * step < width) out[j * step] = h[j];
         }
-        x = h;                                                      // (each thread reads what it has written itself)
-    } else {
-#pragma unroll 8
-        for (int i = threadIdx.x; i < p.width; i += blockDim.x) {
-            float a = to_f32(x[i]);
-            if constexpr (NORM) {
-                sum = __fmaf_rn(a, a, sum);
-                a = __fmul_rn(a, to_f32(gain[i]));
-            }
-            most = max_or_nan(most, fabsf(a));
+    }
+#pragma unroll
+    for (int j = 0; j < NE; ++j) {
+        v[j] = to_f32(h[j]);
+        if constexpr (NORM) {
+            sum = __fmaf_rn(v[j], v[j], sum);
+            v[j] = first + j * step < width ? __fmul_rn(v[j], to_f32(gain[j * step])) : 0.0f;
         }
+        most = max_or_nan(most, fabsf(v[j]));
     }
     block_sum_and_max<NORM>(sum, most, parts);
     float rstd = 1.0f;
@@ -193,18 +195,22 @@ __global__ void __launch_bounds__(512) norm_any_kernel(const NormParams p) {
         rstd = norm_factor(sum, p);
         if (p.rstd && threadIdx.x == 0) p.rstd[row] = rstd;
         most = __fmul_rn(most, rstd);
+        if (p.y) {
+            T *y = static_cast<T *>(p.y) + row * p.ldy + first;
+#pragma unroll
+            for (int j = 0; j < NE; ++j)
+                if (first + j * step < width) y[j * step] = from_f32<T>(__fmul_rn(v[j], rstd));
+        }
     }
-    const bool coded = !NORM || p.codes;
-    const RowScale s(most);
-    if (coded && threadIdx.x == 0) p.scales[row] = s.scale;
-    int8_t *codes = p.codes + row * p.ldc;
-    T *y = static_cast<T *>(p.y) + row * p.ldy;
-#pragma unroll 8
-    for (int i = threadIdx.x; i < p.width; i += blockDim.x) {
-        float a = to_f32(x[i]);
-        if constexpr (NORM) a = __fmul_rn(__fmul_rn(a, to_f32(gain[i])), rstd);
-        if (NORM && p.y) y[i] = from_f32<T>(a);
-        if (coded) codes[i] = (int8_t)s.code(a);
+    if (!NORM || p.codes) {
+        const RowScale s(most);
+        if (threadIdx.x == 0) p.scales[row] = s.scale;
+        int8_t *codes = p.codes + row * p.ldc + first;
+#pragma unroll
+        for (int j = 0; j < NE; ++j) {
+            const uint32_t c = NORM ? __float_as_uint(__fmaf_rn(__fmul_rn(v[j], rstd), s.inverse, TO_NEAREST)) : s.code_byte(v[j]);
+            if (first + j * step < width) codes[j * step] = (int8_t)(s.inverse != 0.0f ? c : 0u);
+        }
     }
 }
 
@@ -215,9 +221,18 @@ int norm_launch(const NormParams &p, int packs, cudaStream_t st) {
     const int64_t blocks = (p.rows + together - 1) / together;
     return launch_early(norm_rows_kernel<T, G, NV, NORM>, dim3((unsigned)blocks), dim3(threads, together), st, p);
 }
+template <class T, class G, int NE, bool NORM>
+int norm_elements_launch(const NormParams &p, cudaStream_t st) {
+    const int threads = whole_warps((p.width + NE - 1) / NE), together = threads == 32 ? 4 : 1;
+    return launch_early(norm_elements_kernel<T, G, NE, NORM>, dim3((unsigned)((p.rows + together - 1) / together)), dim3(threads, together), st, p);
+}
 template <class T, class G, bool NORM>
 int norm_typed(const NormParams &p, bool vec, cudaStream_t st) {
-    if (!vec) return launch_early(norm_any_kernel<T, G, NORM>, dim3((unsigned)p.rows), dim3(p.width <= 256 ? whole_warps(p.width) : p.width <= 4096 ? 256 : 512), st, p);
+    if (!vec) {
+        if (p.width <= 4096) return norm_elements_launch<T, G, 8, NORM>(p, st);
+        if (p.width <= 8192) return norm_elements_launch<T, G, 16, NORM>(p, st);
+        return norm_elements_launch<T, G, 32, NORM>(p, st);
+    }
     const int packs = p.width / (16 / (int)sizeof(T));
     if (packs <= 1024 && (p.rows <= 296 || packs <= 32)) return norm_launch<T, G, 1, NORM>(p, packs, st);
     if (packs <= 1024) return norm_launch<T, G, 2, NORM>(p, packs, st);
@@ -476,7 +491,60 @@ __global__ void __launch_bounds__(512) norm_back_kernel(const NormBackParams p, 
     }
 }
 
-// The same element by element, for rows that cannot be accessed in packs; a thread's sums are in shared memory.
+// Rows that cannot be accessed in packs, element by element, NE of them a thread, blockDim.x apart.
+template <class T, class G, int NE>
+__global__ void __launch_bounds__(512, NE <= 8 ? 2 : 1) norm_back_elements_kernel(const NormBackParams p) {
+    __shared__ float parts[2][16];
+    start_next();
+    wait_for_previous();
+    const int step = blockDim.x, width = p.width, first = threadIdx.x;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    const G *gain = static_cast<const G *>(p.gain) + first;
+    float g[NE], sum[NE];
+#pragma unroll
+    for (int j = 0; j < NE; ++j) {
+        g[j] = first + j * step < width ? to_f32(gain[j * step]) : 0.0f;
+        sum[j] = 0.0f;
+    }
+    int side = 0;
+    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, side ^= 1) {
+        const T *dys = static_cast<const T *>(p.dy) + row * p.lddy + first, *hs = static_cast<const T *>(p.h) + row * p.ldh + first;
+        const T *dhs = static_cast<const T *>(p.dh) + row * p.lddh + first;
+        T *dxs = static_cast<T *>(p.dx) + row * p.lddx + first;
+        const float r = p.rstd[row];
+        const T zero = from_f32<T>(0.0f);
+        T dy[NE], h[NE], dh[NE];
+#pragma unroll
+        for (int j = 0; j < NE; ++j) {
+            const bool in = first + j * step < width;
+            dy[j] = in ? dys[j * step] : zero;
+            h[j] = in ? hs[j * step] : zero;
+            dh[j] = in && p.dh ? dhs[j * step] : zero;
+        }
+        float dot = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NE; ++j) {
+            const float d = to_f32(dy[j]), u = __fmul_rn(to_f32(h[j]), r);
+            dot = __fmaf_rn(__fmul_rn(d, g[j]), u, dot);
+            sum[j] = __fmaf_rn(d, u, sum[j]);
+        }
+        dot = warp_sum(dot);
+        if (lane == 0) parts[side][warp] = dot;                 // (two sides: the next row's sums do not wait for this one's readers)
+        __syncthreads();
+        const float mean = __fdiv_rn(warp_sum(lane < warps ? parts[side][lane] : 0.0f), (float)width);
+#pragma unroll
+        for (int j = 0; j < NE; ++j) {
+            const float u = __fmul_rn(to_f32(h[j]), r);
+            const float d = __fadd_rn(__fmul_rn(__fmaf_rn(-u, mean, __fmul_rn(to_f32(dy[j]), g[j])), r), to_f32(dh[j]));
+            if (first + j * step < width) dxs[j * step] = from_f32<T>(d);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NE; ++j)
+        if (first + j * step < width) p.sums[(int64_t)blockIdx.x * width + first + j * step] = sum[j];
+}
+
+// Wider ones than that has registers for: a thread's sums are in shared memory, and rows are read twice.
 template <class T, class G>
 __global__ void __launch_bounds__(512) norm_back_any_kernel(const NormBackParams p) {
     extern __shared__ float sums[];
@@ -555,6 +623,10 @@ template <class T, class G, int NV>
 int back_warps_launch(const NormBackParams &p, cudaStream_t st) {
     return launch_early(norm_back_warps_kernel<T, G, NV>, dim3(back_blocks(p.rows)), dim3(BACK_WARPS * 32), st, p);
 }
+template <class T, class G, int NE>
+int back_elements_launch(const NormBackParams &p, cudaStream_t st) {
+    return launch_early(norm_back_elements_kernel<T, G, NE>, dim3(back_blocks(p.rows)), dim3(whole_warps((p.width + NE - 1) / NE)), st, p);
+}
 template <class T, class G>
 int back_any_launch(const NormBackParams &p, cudaStream_t st) {
     const int smem = p.width * (int)sizeof(float);
@@ -575,7 +647,9 @@ template <class T, class G>
 int back_typed(const NormBackParams &p, bool vec, float *dgain, cudaStream_t st) {
     const int packs = p.width / (16 / (int)sizeof(T));
     int rc;
-    if (!vec || packs > 2048) rc = back_any_launch<T, G>(p, st);
+    if (!vec && p.width <= 4096) rc = back_elements_launch<T, G, 8>(p, st);
+    else if (!vec && p.width <= 8192) rc = back_elements_launch<T, G, 16>(p, st);
+    else if (!vec || packs > 2048) rc = back_any_launch<T, G>(p, st);
     else if (packs <= 32) rc = back_warps_launch<T, G, 1>(p, st);
     else if (packs <= 64) rc = back_warps_launch<T, G, 2>(p, st);
     else if (packs <= 128) rc = back_launch<T, G, 1>(p, packs, st);
