@@ -7,7 +7,7 @@
 // in 64 bits.  The choice is therefore that of 64-bit scores, at the cost of fp32 ones.
 //
 // Plan.  A counting sort in three launches: a block takes a run of tokens and counts its slots by expert; the counts are added up
-// over the runs (few runs: by the last launch); a block ranks the slots of its run.  Slots of an expert keep their order, and nothing depends on the order in
+// over the runs (few of them: by the last launch); a block ranks the slots of its run.  Slots of an expert keep their order, and nothing depends on the order in
 // which blocks run.  Few tokens: one block does it all.
 //
 // Bound: reading the logits and issue (some 50 instructions for each of a token's choices).
@@ -25,7 +25,6 @@ __host__ __device__ constexpr int choose_threads(int v) { return v <= 4 ? 1024 :
 __host__ __device__ constexpr int rank_warps(int experts) { return experts <= 256 ? 32 : experts <= 512 ? 16 : 8; }
 constexpr int MAX_RUNS = 148;                                 // of tokens, a block each
 constexpr int ALONE_TOKENS = 16;                              // up to so many make one run, whose block makes the plan as well
-constexpr int SCANNED_RUNS = 32;                              // up to so many a block adds up the runs ahead of it itself
 constexpr int64_t ROUTE_MAX_SLOTS = (1ll << 31) - 1;
 
 struct RouteParams {
@@ -45,6 +44,7 @@ struct RouteParams {
     int32_t *order, *place, *offsets;                         // NULL: no plan
     int32_t *counts;                                          // [experts][runs], behind them [experts] rows of each
     int runs, run;                                            // tokens of a run
+    bool scanned;                                             // counts are added up over the runs by a launch of its own
 };
 
 // Numbers as unsigned ones of the same order (not for NaN).  An expert that is not to be chosen has key -infinity.
@@ -679,20 +679,25 @@ __global__ void __launch_bounds__(PLAN_THREADS) route_plan_kernel(const __grid_c
     start_next();
     wait_for_previous();
     int32_t *ahead = words, *all = words + RouteSmem::ranks(p.experts);
-    for (int e = threadIdx.x; e < p.experts; e += blockDim.x) {
-        const int32_t *counts = p.counts + (int64_t)e * p.runs;
-        if (p.runs > SCANNED_RUNS) {
-            ahead[e] = counts[blockIdx.x];
+    if (p.scanned) {
+        for (int e = threadIdx.x; e < p.experts; e += blockDim.x) {
+            ahead[e] = p.counts[(int64_t)e * p.runs + blockIdx.x];
             all[e] = p.counts[(int64_t)p.experts * p.runs + e];
-        } else {
+        }
+    } else {                                                  // a warp adds up an expert's runs
+        const int lane = threadIdx.x & 31;
+#pragma unroll 4
+        for (int e = threadIdx.x >> 5; e < p.experts; e += blockDim.x >> 5) {
+            const int32_t *counts = p.counts + (int64_t)e * p.runs;
             int a = 0, b = 0;
-#pragma unroll 8
-            for (int r = 0; r < p.runs; ++r) {
-                b += counts[r];
-                a += r < (int)blockIdx.x ? counts[r] : 0;
+            for (int r = lane; r < p.runs; r += 32) {
+                const int c = counts[r];
+                b += c;
+                a += r < (int)blockIdx.x ? c : 0;
             }
-            ahead[e] = a;
-            all[e] = b;
+            a = __reduce_add_sync(0xffffffffu, a);
+            b = __reduce_add_sync(0xffffffffu, b);
+            if (lane == 0) { ahead[e] = a; all[e] = b; }
         }
     }
     __syncthreads();
@@ -811,6 +816,10 @@ template <auto KERNEL> int launch_route(int blocks, int threads, int smem, cudaS
     cudaGetLastError();
     return QNN_E_CUDA;
 }
+// Threads of the blocks that rank runs, and whether a launch of its own adds up the counts ahead of them: where a warp would have
+// more than 32 loads of them to make.
+int plan_threads(const RouteParams &p) { return p.run * p.top <= 256 ? 256 : PLAN_THREADS; }
+bool plan_scanned(const RouteParams &p) { return (int64_t)p.experts * ((p.runs + 31) / 32) > plan_threads(p); }
 template <int V> int route_launch(const RouteParams &p, cudaStream_t st) {
     constexpr int threads = choose_threads(V);
     const int fixed = RouteSmem::keys(p.experts) * 4, smem = fixed + (p.groups > 1 ? threads / 32 * p.groups * p.pitch * 8 : 0);
@@ -822,8 +831,8 @@ template <int V> int route_launch(const RouteParams &p, cudaStream_t st) {
     const int some = p.run * 32;
     const int rc = launch_route<route_choose_kernel<V, false>>(p.runs, some < threads ? some : threads, smem, st, p);
     if (rc != QNN_OK || !p.order) return rc;
-    const int scanned = p.runs > SCANNED_RUNS ? launch_early(route_scan_kernel, dim3((p.experts + 7) / 8), dim3(256), st, p) : QNN_OK;
-    return scanned != QNN_OK ? scanned : launch_route<route_plan_kernel>(p.runs, p.run * p.top <= 256 ? 256 : PLAN_THREADS, fixed, st, p);
+    const int scanned = p.scanned ? launch_early(route_scan_kernel, dim3((p.experts + 7) / 8), dim3(256), st, p) : QNN_OK;
+    return scanned != QNN_OK ? scanned : launch_route<route_plan_kernel>(p.runs, plan_threads(p), fixed, st, p);
 }
 template <class T, int V> int back_launch(const RouteBackParams &p, cudaStream_t st) {
     const int64_t blocks = ((int64_t)p.tokens + 7) / 8;
@@ -880,6 +889,7 @@ extern "C" int qnn_route(const void *logits, int type, int64_t tokens, int exper
     p.counts = static_cast<int32_t *>(workspace);
     p.run = route_run(tokens);
     p.runs = route_runs(tokens);
+    p.scanned = plan_scanned(p);
     if (experts <= 32) return route_launch<1>(p, st);
     if (experts <= 64) return route_launch<2>(p, st);
     if (experts <= 128) return route_launch<4>(p, st);
