@@ -19,17 +19,17 @@ struct I8Plan {
 
 // The form that ends first by an estimate in nanoseconds: what a launch costs, and for each round of blocks a step of 128 elements
 // and a fixed part (first copies, results).  Fitted to 323 sizes (1 to 8192 rows, n 200 to 16384, k 192 to 16384; times in a
-// replayed graph), where the choice is 1.9 % off the best form on average and 32 % at most.  Two sides of it: 301 x 4096 x 4096
+// replayed graph), where the choice is 1.9 % off the best form on average and 22 % at most.  Two sides of it: 301 x 4096 x 4096
 // takes 13.6 us in one block's tiles of 128 tokens and 10.4 in a pair's; 64 x 4096 x 4096 7.2 us in 32-token tiles with four ranks
-// and 9.9 by pairs.  Blocks of tiles up to 64 tokens go two to an SM, and share it when more than 148 run (step + 33 %, fixed part
-// x 4.6); clusters of four and eight do not fill every group of SMs.  Sized for 148 SMs.
+// and 9.9 by pairs.  Blocks of tiles up to 64 tokens go two to an SM, and share it when more than 148 run (step + 31 %, fixed part
+// x 4.5); clusters of four and eight do not fill every group of SMs.  Sized for 148 SMs.
 I8Plan i8_plan(int64_t rows, int n, int k) {
     struct Form {
         int tile, launch, step, fixed;
     };
-    static const Form split[] = {{16, 1290, 194, 355}, {32, 2240, 202, 366}, {64, 3120, 254, 497}, {128, 0, 220, 5370}};
-    static const Form pair[] = {{128, 2450, 174, 1830}, {256, 1970, 304, 3350}};
-    static const int join[] = {0, 790, 480, 0}, places[] = {148, 148, 136, 112};
+    static const Form split[] = {{16, 1330, 200, 368}, {32, 2260, 209, 375}, {64, 3170, 260, 499}, {128, 0, 222, 5390}};
+    static const Form pair[] = {{128, 2950, 181, 1340}, {256, 2970, 318, 2280}};
+    static const int join[] = {0, 740, 470, 0}, places[] = {148, 148, 136, 112};
     const double steps = (double)((k + I8_STEP - 1) / I8_STEP), wide = (double)((n + 255) / 256), narrow = (double)((n + 127) / 128);
     I8Plan best = {16, 1};
     double least = 1e300;
@@ -40,7 +40,7 @@ I8Plan i8_plan(int64_t rows, int n, int k) {
         for (int l = 0; l < 4 && (1 << l) <= steps; ++l) {
             const double blocks = tiles * (1 << l), rounds = ceil(blocks / (places[l] * together)), each = ceil(steps / (1 << l));
             const double shared = together == 1 || blocks <= 148.0 ? 0.0 : blocks < 296.0 ? blocks / 148.0 - 1.0 : 1.0;
-            const double cost = f.launch + rounds * (each * f.step * (1.0 + 0.33 * shared) + f.fixed * (1.0 + 3.6 * shared)) + join[l];
+            const double cost = f.launch + rounds * (each * f.step * (1.0 + 0.31 * shared) + f.fixed * (1.0 + 3.5 * shared)) + join[l];
             if (cost < least) { least = cost; best = {f.tile, 1 << l}; }
         }
     }

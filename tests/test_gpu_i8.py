@@ -127,8 +127,8 @@ def test_gemm_by_pairs(t, qnn, dtype, rows, n, k):
 
 
 FORMS = {(16, 1): (5, 16, 32), (16, 2): (474, 130, 1201), (16, 4): (1, 16, 390), (16, 8): (1, 17, 925), (32, 1): (2087, 138, 32),
-         (32, 2): (566, 407, 2598), (32, 4): (482, 129, 1923), (32, 8): (251, 129, 3590), (64, 1): (2821, 276, 32), (64, 2): (1027, 411, 3243),
-         (64, 4): (530, 405, 3052), (64, 8): (457, 134, 4873), (128, 1): (3605, 542, 49), (128, 2): (798, 949, 4004), (128, 4): (991, 411, 2959),
+         (32, 2): (566, 407, 2598), (32, 4): (482, 129, 1923), (32, 8): (251, 129, 3590), (64, 1): (2821, 276, 32), (64, 2): (1062, 390, 2984),
+         (64, 4): (530, 405, 3052), (64, 8): (457, 134, 4873), (128, 1): (2504, 777, 161), (128, 2): (798, 949, 4004), (128, 4): (991, 411, 2959),
          (128, 8): (204, 811, 10283), (128, 0): (2064, 900, 45), (256, 0): (1703, 1294, 538)}
 
 
