@@ -257,35 +257,38 @@ bool in_packs(const void *p, int type, int64_t ld) { return qnn_aligned(p, 16) &
 __device__ __forceinline__ float byte_value(uint32_t word, int i) {
     return __fadd_rn(__uint_as_float(__byte_perm(word ^ 0x80808080u, 0x4B000000u, 0x7540 + i)), -8388736.0f);      // 2^23 + 128
 }
-// Sixteen codes of ROWS rows by a thread, all loaded first.
+// The codes of one 16-byte pack of results in each of ROWS rows by a thread, all loaded first.  (A pack a thread: with two, a warp's
+// stores cover half sectors, and 16384 x 4096 take 43 us instead of 31.)
 template <class T, int ROWS>
 __global__ void __launch_bounds__(256) decode_kernel(const int8_t *codes, const float *scales, int64_t rows, int width, int64_t ldc, T *out, int64_t ldo) {
     start_next();
     wait_for_previous();
     typedef Octets<T> O;
     const int i = blockIdx.x * blockDim.x + threadIdx.x;
-    if (i * 16 >= width) return;
+    if (i * O::V >= width) return;
     for (int64_t row = (int64_t)blockIdx.y * ROWS; row < rows; row += (int64_t)gridDim.y * ROWS) {
-        uint4 c[ROWS];
+        uint32_t c[ROWS][O::V / 4];
         float s[ROWS];
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             const int64_t at = row + r < rows ? row + r : rows - 1;
-            c[r] = reinterpret_cast<const uint4 *>(codes + at * ldc)[i];
+            const uint32_t *src = reinterpret_cast<const uint32_t *>(codes + at * ldc);
+            if constexpr (O::V == 8) {
+                const uint2 w = reinterpret_cast<const uint2 *>(src)[i];
+                c[r][0] = w.x;
+                c[r][1] = w.y;
+            } else {
+                c[r][0] = src[i];
+            }
             s[r] = scales[at];
         }
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             if (row + r >= rows) break;
-            const uint32_t w[4] = {c[r].x, c[r].y, c[r].z, c[r].w};
-            uint4 *dst = reinterpret_cast<uint4 *>(out + (row + r) * ldo) + i * (16 / O::V);
+            float f[O::V];
 #pragma unroll
-            for (int q = 0; q < 16 / O::V; ++q) {
-                float f[O::V];
-#pragma unroll
-                for (int e = 0; e < O::V; ++e) f[e] = __fmul_rn(byte_value(w[(q * O::V + e) / 4], (q * O::V + e) % 4), s[r]);
-                dst[q] = O::put(f);
-            }
+            for (int e = 0; e < O::V; ++e) f[e] = __fmul_rn(byte_value(c[r][e / 4], e % 4), s[r]);
+            reinterpret_cast<uint4 *>(out + (row + r) * ldo)[i] = O::put(f);
         }
     }
 }
@@ -306,7 +309,7 @@ int decode(const int8_t *codes, const float *scales, int64_t rows, int width, in
         const unsigned ys = (unsigned)(rows < 65535 ? rows : 65535);
         return launch_early(decode_any_kernel<T>, dim3((width + 1023) / 1024, ys), dim3(256), st, codes, scales, rows, width, ldc, o, ldo);
     }
-    const int packs = width / 16, threads = packs < 256 ? (packs + 31) / 32 * 32 : 256;
+    const int packs = width / Octets<T>::V, threads = packs < 256 ? (packs + 31) / 32 * 32 : 256;
     const unsigned xs = (unsigned)((packs + threads - 1) / threads);
     if (rows < 4 * 148) return launch_early(decode_kernel<T, 1>, dim3(xs, (unsigned)rows), dim3(threads), st, codes, scales, rows, width, ldc, o, ldo);
     const int64_t ys = (rows + 3) / 4;
@@ -582,26 +585,31 @@ __global__ void __launch_bounds__(512) norm_back_any_kernel(const NormBackParams
     for (int i = threadIdx.x; i < p.width; i += blockDim.x) p.sums[(int64_t)blockIdx.x * p.width + i] = sums[i];
 }
 
-// dgain[c] = sum over `parts` rows of sums.  Eight threads a column, whose sums are added in order.
-__global__ void __launch_bounds__(256) norm_gain_kernel(const float *sums, int parts, int width, float *dgain) {
-    __shared__ float part[8][32];
+// dgain[c] = sum over `parts` rows of sums.  A thread adds every 32nd of them, with all loads under way; 32 threads a column, whose sums
+// are added in order.
+constexpr int BACK_PARTS = 296;
+__global__ void __launch_bounds__(1024) norm_gain_kernel(const float *sums, int parts, int width, float *dgain) {
+    __shared__ float part[32][33];
     start_next();
     wait_for_previous();
     const int c = blockIdx.x * 32 + threadIdx.x;
-    float sum = 0.0f;
-    if (c < width)
-#pragma unroll 8
-        for (int q = threadIdx.y; q < parts; q += 8) sum = __fadd_rn(sum, sums[(int64_t)q * width + c]);
+    constexpr int EACH = (BACK_PARTS + 31) / 32;
+    float v[EACH], sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int q = threadIdx.y + 32 * i;
+        v[i] = c < width && q < parts ? sums[(int64_t)q * width + c] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) sum = __fadd_rn(sum, v[i]);
     part[threadIdx.y][threadIdx.x] = sum;
     __syncthreads();
-    if (threadIdx.y == 0 && c < width) {
-        for (int q = 1; q < 8; ++q) sum = __fadd_rn(sum, part[q][threadIdx.x]);
-        dgain[c] = sum;
-    }
+    const float total = warp_sum(part[threadIdx.x][threadIdx.y]);         // warp y takes column y
+    if (threadIdx.x == 0 && blockIdx.x * 32 + threadIdx.y < width) dgain[blockIdx.x * 32 + threadIdx.y] = total;
 }
 
 // Blocks of the backward kernel; sized for 148 SMs, so that workspace queries and calls agree.
-int back_blocks(int64_t rows) { return (int)(rows < 296 ? rows : 296); }
+int back_blocks(int64_t rows) { return (int)(rows < BACK_PARTS ? rows : BACK_PARTS); }
 
 template <class T, class G, int NV>
 int back_launch(const NormBackParams &p, int packs, cudaStream_t st) {
@@ -656,7 +664,7 @@ int back_typed(const NormBackParams &p, bool vec, float *dgain, cudaStream_t st)
     else if (packs <= 1024) rc = back_launch<T, G, 2>(p, packs, st);
     else rc = back_launch<T, G, 4>(p, packs, st);
     if (rc != QNN_OK) return rc;
-    return launch_early(norm_gain_kernel, dim3((p.width + 31) / 32), dim3(32, 8), st, p.sums, back_blocks(p.rows), p.width, dgain);
+    return launch_early(norm_gain_kernel, dim3((p.width + 31) / 32), dim3(32, 32), st, p.sums, back_blocks(p.rows), p.width, dgain);
 }
 
 // f(T, G) for the element type and the gain's (that type or fp32)
@@ -714,7 +722,7 @@ extern "C" int qnn_i8_decode(const int8_t *codes, const float *scales, int64_t r
     int rc = check_codes(codes, scales, ldc, width);
     if (rc == QNN_OK) rc = check_real(out, type, ldo, width);
     if (rc != QNN_OK) return rc;
-    const bool vec = width % 16 == 0 && in_packs(out, type, ldo);
+    const bool vec = width * g4_type_bytes(type) % 16 == 0 && in_packs(out, type, ldo);
     return by_types(type, type, [&](auto t, auto) { return decode<decltype(t)>(codes, scales, rows, width, ldc, out, ldo, vec, static_cast<cudaStream_t>(stream)); });
 }
 
