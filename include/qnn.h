@@ -373,7 +373,7 @@ int qnn_g4_plan(int product, int one, int type, int64_t rows, int experts, int n
  * from `width` on are never read nor written.
  *   scale = max(max|x| / 127, 2^-126)      code = x / scale, the fp32 quotient rounded to nearest, half to even
  * A row that holds an infinity or NaN gets scale NaN and codes 0: all of it, and every product with it, is NaN.
- * width is at most 16384, rows below 2^31.  rows = 0 is allowed and does nothing.
+ * width is at most 131072, rows below 2^31.  rows = 0 is allowed and does nothing.
  *   x, out     [rows][ld] of `type`, ld >= width, any alignment of the element size (rows on 16 bytes are faster)
  */
 int qnn_i8_quantize(const void *x, int type, int64_t rows, int width, int64_t ldx, int8_t *codes, int64_t ldc, float *scales, void *stream);
@@ -406,7 +406,7 @@ int qnn_i8_plan(int64_t rows, int n, int k, int *tile, int *ranks);
  *   y          out, optional; it may be x where there is no residual
  *   codes, scales   out, optional: the rows y, before any rounding to `type`, in 8 bits as above.  One of y and codes is given.
  *   rstd       out, optional fp32 [rows], for the backward products
- * eps >= 0; sizes, alignment and rows = 0 as above.
+ * eps >= 0 (with 0 a row of zeros gives NaN); width at most 32768; alignment and rows = 0 as above.
  *
  * Backward, given dy = dC/dy (through codes: straight through) and, optional, dh = what reaches h by another way:
  *   dx = rstd * (dy * gain - u * mean(dy * gain * u)) + dh with u = h * rstd     (also the residual's gradient)
@@ -439,7 +439,7 @@ int qnn_rms_norm_backward(const void *dy, int type, int64_t rows, int width, int
  *   place    int32 [tokens][top]: the row of each slot, -1 where it has no expert
  *   logits   [tokens][ld] of `type`, ld >= experts;  chosen int32, weights fp32 [tokens][top]
  * experts at most 1024, top at most 32, groups at most 32 and a divisor of experts, top <= top_groups * experts / groups,
- * tokens * top < 2^31.  tokens = 0 is allowed (offsets become 0).  workspace: device scratch owned by the caller, 256-byte aligned,
+ * tokens * top < 2^30.  tokens = 0 is allowed (offsets become 0).  workspace: device scratch owned by the caller, 256-byte aligned,
  * qnn_route_workspace(...) bytes (0: it may be NULL), needed with a plan only.
  *
  * Backward: dlogits [tokens][ldd] of `type`, fully written, from dweights fp32 [tokens][top], the logits and the choice (experts

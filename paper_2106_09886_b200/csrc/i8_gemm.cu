@@ -31,10 +31,11 @@ I8Plan i8_plan(int64_t rows, int n, int k) {
     static const Form pair[] = {{128, 2950, 181, 1340}, {256, 2970, 318, 2280}};
     static const int join[] = {0, 740, 470, 0}, places[] = {148, 148, 136, 112};
     const double steps = (double)((k + I8_STEP - 1) / I8_STEP), wide = (double)((n + 255) / 256), narrow = (double)((n + 127) / 128);
-    I8Plan best = {16, 1};
+    I8Plan best = {256, 0};
     double least = 1e300;
     for (const Form &f : split) {
         if (f.tile > 16 && f.tile >= 2 * rows) break;                              // half of such a tile would be empty
+        if (rows > (int64_t)f.tile * 65535) continue;                              // (tiles of tokens are a grid's second dimension)
         const double tiles = narrow * (double)((rows + f.tile - 1) / f.tile);
         const int together = f.tile <= 64 ? 2 : 1;
         for (int l = 0; l < 4 && (1 << l) <= steps; ++l) {
@@ -73,7 +74,6 @@ template <int TN, class T> int run_split(const I8Operands &o, const I8Params &p,
     CUtensorMap w, x;
     if (!make_map_i8(&w, o.w, p.n, o.k, o.ldw, 128) || !make_map_i8(&x, o.x, p.rows, o.k, o.ldx, TN)) return QNN_E_CUDA;
     const int64_t ttiles = ((int64_t)p.rows + TN - 1) / TN;
-    if (ttiles > 65535) return QNN_E_RANGE;
     int log_ranks = 0;
     while (1 << log_ranks < ranks) ++log_ranks;
     return i8_launch<i8_split_kernel<TN, T>>(dim3((p.n + 127) / 128 << log_ranks, (unsigned)ttiles), L::THREADS, L::TOTAL, ranks, st, w, x, p, log_ranks);

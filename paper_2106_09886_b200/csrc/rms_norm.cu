@@ -12,7 +12,7 @@
 
 namespace {
 
-constexpr int NORM_MAX_WIDTH = 16384;
+constexpr int NORM_MAX_WIDTH = 32768, CODES_MAX_WIDTH = 131072;
 
 struct NormParams {
     const void *x, *residual, *gain;          // residual NULL: h is x.  gain NULL: no norm (y = x)
@@ -214,6 +214,60 @@ __global__ void __launch_bounds__(512, NE <= 16 ? 2 : 1) norm_elements_kernel(co
     }
 }
 
+// Rows that do not fit the registers of a block: element by element, read again (from the caches) for the results.
+template <class T, class G, bool NORM>
+__global__ void __launch_bounds__(1024) norm_wide_kernel(const NormParams p) {
+    __shared__ float parts[2][32];
+    start_next();
+    wait_for_previous();
+    const int64_t row = blockIdx.x;
+    const T *x = static_cast<const T *>(p.x) + row * p.ldx;
+    const G *gain = static_cast<const G *>(p.gain);
+    float sum = 0.0f, most = 0.0f;
+    if (NORM && p.residual) {
+        const T *res = static_cast<const T *>(p.residual) + row * p.ldr;
+        T *h = static_cast<T *>(p.h) + row * p.ldh;
+#pragma unroll 8
+        for (int i = threadIdx.x; i < p.width; i += blockDim.x) {
+            const T v = from_f32<T>(__fadd_rn(to_f32(x[i]), to_f32(res[i])));
+            const float a = to_f32(v);
+            h[i] = v;
+            sum = __fmaf_rn(a, a, sum);
+            most = max_or_nan(most, fabsf(__fmul_rn(a, to_f32(gain[i]))));
+        }
+        x = h;                                                      // (each thread reads what it has written itself)
+    } else {
+#pragma unroll 8
+        for (int i = threadIdx.x; i < p.width; i += blockDim.x) {
+            float a = to_f32(x[i]);
+            if constexpr (NORM) {
+                sum = __fmaf_rn(a, a, sum);
+                a = __fmul_rn(a, to_f32(gain[i]));
+            }
+            most = max_or_nan(most, fabsf(a));
+        }
+    }
+    block_sum_and_max<NORM>(sum, most, parts);
+    float rstd = 1.0f;
+    if constexpr (NORM) {
+        rstd = norm_factor(sum, p);
+        if (p.rstd && threadIdx.x == 0) p.rstd[row] = rstd;
+        most = __fmul_rn(most, rstd);
+    }
+    const bool coded = !NORM || p.codes;
+    const RowScale s(most);
+    if (coded && threadIdx.x == 0) p.scales[row] = s.scale;
+    int8_t *codes = p.codes + row * p.ldc;
+    T *y = static_cast<T *>(p.y) + row * p.ldy;
+#pragma unroll 8
+    for (int i = threadIdx.x; i < p.width; i += blockDim.x) {
+        float a = to_f32(x[i]);
+        if constexpr (NORM) a = __fmul_rn(__fmul_rn(a, to_f32(gain[i])), rstd);
+        if (NORM && p.y) y[i] = from_f32<T>(a);
+        if (coded) codes[i] = (int8_t)(s.inverse != 0.0f ? (NORM ? __float_as_uint(__fmaf_rn(a, s.inverse, TO_NEAREST)) : s.code_byte(a)) : 0u);
+    }
+}
+
 static inline int whole_warps(int threads) { return (threads + 31) / 32 * 32; }
 template <class T, class G, int NV, bool NORM>
 int norm_launch(const NormParams &p, int packs, cudaStream_t st) {
@@ -231,9 +285,11 @@ int norm_typed(const NormParams &p, bool vec, cudaStream_t st) {
     if (!vec) {
         if (p.width <= 4096) return norm_elements_launch<T, G, 8, NORM>(p, st);
         if (p.width <= 8192) return norm_elements_launch<T, G, 16, NORM>(p, st);
-        return norm_elements_launch<T, G, 32, NORM>(p, st);
+        if (p.width <= 16384) return norm_elements_launch<T, G, 32, NORM>(p, st);
+        return launch_early(norm_wide_kernel<T, G, NORM>, dim3((unsigned)p.rows), dim3(1024), st, p);
     }
     const int packs = p.width / (16 / (int)sizeof(T));
+    if (packs > 4096) return launch_early(norm_wide_kernel<T, G, NORM>, dim3((unsigned)p.rows), dim3(1024), st, p);
     if (packs <= 1024 && (p.rows <= 296 || packs <= 32)) return norm_launch<T, G, 1, NORM>(p, packs, st);
     if (packs <= 1024) return norm_launch<T, G, 2, NORM>(p, packs, st);
     if (packs <= 2048) return norm_launch<T, G, 4, NORM>(p, packs, st);
@@ -703,7 +759,7 @@ extern "C" int qnn_rms_norm(const void *x, int type, int64_t rows, int width, in
 extern "C" int qnn_i8_quantize(const void *x, int type, int64_t rows, int width, int64_t ldx, int8_t *codes, int64_t ldc, float *scales,
                                void *stream) {
     if (!g4_type_ok(type) || rows < 0 || width < 1) return QNN_E_ARG;
-    if (width > NORM_MAX_WIDTH || rows > ROWS_MAX) return QNN_E_RANGE;
+    if (width > CODES_MAX_WIDTH || rows > ROWS_MAX) return QNN_E_RANGE;
     if (rows == 0) return QNN_OK;
     int rc = check_real(x, type, ldx, width);
     if (rc == QNN_OK) rc = check_codes(codes, scales, ldc, width);
@@ -717,7 +773,7 @@ extern "C" int qnn_i8_quantize(const void *x, int type, int64_t rows, int width,
 extern "C" int qnn_i8_decode(const int8_t *codes, const float *scales, int64_t rows, int width, int64_t ldc, int type, void *out, int64_t ldo,
                              void *stream) {
     if (!g4_type_ok(type) || rows < 0 || width < 1) return QNN_E_ARG;
-    if (rows > ROWS_MAX) return QNN_E_RANGE;
+    if (width > CODES_MAX_WIDTH || rows > ROWS_MAX) return QNN_E_RANGE;
     if (rows == 0) return QNN_OK;
     int rc = check_codes(codes, scales, ldc, width);
     if (rc == QNN_OK) rc = check_real(out, type, ldo, width);

@@ -25,7 +25,7 @@ __host__ __device__ constexpr int choose_threads(int v) { return v <= 4 ? 1024 :
 __host__ __device__ constexpr int rank_warps(int experts) { return experts <= 256 ? 32 : experts <= 512 ? 16 : 8; }
 constexpr int MAX_RUNS = 148;                                 // of tokens, a block each
 constexpr int ALONE_TOKENS = 16;                              // up to so many make one run, whose block makes the plan as well
-constexpr int64_t ROUTE_MAX_SLOTS = (1ll << 31) - 1;
+constexpr int64_t ROUTE_MAX_SLOTS = (1ll << 30) - 1;         // (tokens past the last are counted in 31 bits)
 
 struct RouteParams {
     const void *logits;
@@ -488,7 +488,15 @@ __device__ __forceinline__ int route_token(const RouteParams &p, int64_t token, 
             near = lane < p.top - 1 ? expert >= 0 && (key < behind || (key == behind && mine > expert))
                                     : lane == p.top - 1 && mine >= 0 && p.type == QNN_F32 && ordered(__fadd_rn(key, 0.0f)) <= (best | LOW) && best > NO_KEY;
         }
-        if (__any_sync(0xffffffffu, near)) {
+        bool open = __any_sync(0xffffffffu, near);
+        if (open && !p.bias) {                                // equal logits whose lowest bits were not needed (all 0, say) are in order
+            load_row<V>(p.logits, p.type, token * p.ld, p.experts, l);
+            uint32_t cut = 0;
+#pragma unroll
+            for (int v = 0; v < V; ++v) cut |= __float_as_uint(l[v]) & LOW;
+            open = __any_sync(0xffffffffu, cut != 0);
+        }
+        if (open) {
             const int count = min(32, p.top + 8);
             take_sorted<V>(keys, p.top, count, mine, best);
             mine = order_in_64_bits<V>(p, token, mine, count, best > NO_KEY ? best | LOW : NO_KEY, margin, stay);

@@ -51,9 +51,9 @@ def norm(h, gain, eps):
     return h * gain[None, :] * rstd[:, None], rstd
 
 
-# A thread adds at most 33 squares in a row, warps and blocks 10 partial sums more; all are positive, so the sum is off by at most 43
+# A thread adds at most 64 squares in a row, warps and blocks 10 partial sums more; all are positive, so the sum is off by at most 74
 # roundings, its square root by half of them, and quotient, sum with eps, root and inverse by one each.
-RSTD_ROUNDINGS = 43 / 2 + 4
+RSTD_ROUNDINGS = 74 / 2 + 4
 Y_ROUNDINGS = RSTD_ROUNDINGS + 2
 
 
@@ -65,12 +65,12 @@ def norm_backward(dy, h, gain, rstd, dh):
 
 
 def norm_backward_bounds(dy, h, gain, rstd, dh, dtype):
-    """The mean adds at most 33 + 10 products of three factors, and is divided; then each element is rounded at every step.  A column of
+    """The mean adds at most 64 + 10 products of three factors, and is divided; then each element is rounded at every step.  A column of
     dgain adds `rows / 296` products, then 8 sums of warps or none, then 10 + 5 partial sums."""
     u, a = np.abs(h * rstd[:, None]), np.abs(dy * gain[None, :])
     mean = np.mean(a * u, axis=1, keepdims=True)
     dx, _ = norm_backward(dy, h, gain, rstd, dh)
-    off = rstd[:, None] * (3 * a + u * mean * (43 + 3 + 1 + 4)) * U32 + (np.abs(dx) + (0 if dh is None else np.abs(dh))) * U32
+    off = rstd[:, None] * (3 * a + u * mean * (74 + 3 + 1 + 4)) * U32 + (np.abs(dx) + (0 if dh is None else np.abs(dh))) * U32
     return off + rounding(np.abs(dx) + off, dtype), (np.abs(dy) * u).sum(0) * (h.shape[0] // 296 + 1 + 8 + 10 + 5 + 2) * U32
 
 

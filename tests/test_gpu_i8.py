@@ -43,7 +43,7 @@ def same(t, got, want):
 
 @pytest.mark.parametrize("dtype", ref.TYPES)
 @pytest.mark.parametrize("rows,k", [(1, 1), (1, 7), (3, 8), (5, 64), (4, 255), (2, 256), (9, 264), (7, 1000), (3, 1001), (2, 4096), (1, 8192),
-                                    (2, 8200), (400, 1032), (300, 129), (1, 16384), (2, 16383)])
+                                    (2, 8200), (400, 1032), (300, 129), (1, 16384), (2, 16383), (3, 16400), (2, 28672), (2, 28671), (1, 40000), (2, 131072), (1, 131071)])
 def test_quantize_and_decode(t, qnn, dtype, rows, k):
     rng = np.random.default_rng(rows * 7919 + k)
     x = t.from_numpy((rng.standard_normal((rows, k)) * np.exp(rng.standard_normal((rows, 1)) * 3)).astype(np.float32)).to(ref.torch_type(dtype)).to(DEV)
@@ -226,4 +226,4 @@ def test_refusals(t, qnn):
         with pytest.raises(ValueError):
             bad()
     with pytest.raises(qnn.QnnError):
-        qnn.i8_quantize(t.zeros((1, 16385), device=DEV))
+        qnn.i8_quantize(t.zeros((1, 131073), device=DEV))

@@ -58,7 +58,7 @@ def check_norm(t, qnn, x, gain, residual, dtype):
 
 
 SIZES = [(1, 1), (1, 8), (3, 64), (5, 100), (2, 256), (7, 264), (3, 1001), (300, 512), (1, 4096), (297, 2048), (2, 8192), (3, 8200), (1, 16384), (2, 16383),
-         (400, 333), (5, 1538)]
+         (400, 333), (5, 1538), (3, 16400), (2, 32768), (2, 32767)]
 
 
 @pytest.mark.parametrize("dtype", ref.TYPES)
@@ -215,7 +215,7 @@ def test_refusals(t, qnn):
         with pytest.raises(ValueError):
             bad()
     for bad in (lambda: qnn.rms_norm(x, gain, -1.0), lambda: qnn.rms_norm(x, gain, float("nan")),
-                lambda: qnn.rms_norm(t.zeros((1, 16385), device=DEV), t.ones(16385, device=DEV)),
+                lambda: qnn.rms_norm(t.zeros((1, 32769), device=DEV), t.ones(32769, device=DEV)),
                 lambda: qnn.rms_norm_backward(x, x, gain, rstd, workspace=t.zeros(8, dtype=t.uint8, device=DEV))):
         with pytest.raises(qnn.QnnError):
             bad()

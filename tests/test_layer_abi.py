@@ -40,7 +40,7 @@ def test_quantize_and_decode_refusals(qnn, p):
         assert call(**bad) == qnn.E_ARG, bad
     for bad in ({"codes": off(p, 8)}, {"ldc": 40}, {"ldc": 50}, {"x": off(p, 1)}, {"type": 0, "x": off(p, 2)}, {"scales": off(p, 2)}):
         assert call(**bad) == qnn.E_ALIGN, bad
-    assert call(width=16385, ldx=16385, ldc=16400) == qnn.E_RANGE and call(rows=1 << 31) == qnn.E_RANGE
+    assert call(width=131073, ldx=131073, ldc=131088) == qnn.E_RANGE and call(rows=1 << 31) == qnn.E_RANGE
     assert call(rows=0) == qnn.OK and call(rows=0, x=None, codes=None, scales=None) == qnn.OK
     call = caller(qnn.lib.qnn_i8_decode, "codes scales rows width ldc type out ldo stream", (p, p, 4, 40, 48, 1, p, 40, None))
     for bad in ({"codes": None}, {"scales": None}, {"out": None}, {"type": 9}, {"rows": -1}, {"width": 0}, {"ldc": 32}, {"ldo": 39}):
@@ -65,9 +65,10 @@ def test_gemm_refusals_and_plan(qnn, p):
     f = qnn.lib.qnn_i8_plan
     assert f(0, 8, 8, ctypes.byref(tile), ctypes.byref(ranks)) == qnn.E_ARG and f(1, 8, 8, None, ctypes.byref(ranks)) == qnn.E_ARG
     assert f(1, 8, 131072, ctypes.byref(tile), ctypes.byref(ranks)) == qnn.E_RANGE
-    for rows, n, k in [(1, 64, 1), (1, 8192, 8192), (16, 128, 100), (33, 4096, 4096), (100, 300, 200), (8192, 8192, 8192), (1 << 20, 128, 64)]:
+    for rows, n, k in [(1, 64, 1), (1, 8192, 8192), (16, 128, 100), (33, 4096, 4096), (100, 300, 200), (8192, 8192, 8192), (1 << 20, 128, 64), ((1 << 23) - 1, 16, 16), ((1 << 23) - 1, 1, 131071), (1 << 21, 65535 * 16, 1)]:
         tile, ranks = qnn.i8_plan(rows, n, k)
         assert tile in (16, 32, 64, 128, 256) and ranks in (0, 1, 2, 4, 8) and ranks <= -(-k // 128)      # every rank has a step
+        assert ranks == 0 or -(-rows // tile) <= 65535
     assert qnn.i8_plan(8192, 8192, 8192)[1] == 0 and qnn.i8_plan(1, 8192, 8192)[0] == 16
 
 
@@ -81,10 +82,10 @@ def test_norm_refusals(qnn, p):
     for bad in ({"x": off(p, 1)}, {"residual": off(p, 1)}, {"h": off(p, 1)}, {"y": off(p, 1)}, {"codes": off(p, 4)}, {"ldc": 44}, {"gain": off(p, 1)},
                 {"gain_type": 0, "gain": off(p, 2)}, {"rstd": off(p, 2)}, {"scales": off(p, 1)}):
         assert call(**bad) == qnn.E_ALIGN, bad
-    assert call(width=16385, ldx=16385) == qnn.E_RANGE and call(rows=1 << 31) == qnn.E_RANGE
+    assert call(width=32769, ldx=32769) == qnn.E_RANGE and call(rows=1 << 31) == qnn.E_RANGE
     assert call(rows=0) == qnn.OK and call(rows=0, x=None, y=None, codes=None, h=None) == qnn.OK and call(rows=0, gain=None) == qnn.E_ARG
     f = qnn.lib.qnn_rms_norm_backward_workspace
-    assert f(0, 40) == 0 and f(4, 0) == 0 and f(4, 16385) == 0 and f(1, 40) >= 160 and f(10 ** 6, 4096) % 256 == 0
+    assert f(0, 40) == 0 and f(4, 0) == 0 and f(4, 32769) == 0 and f(1, 40) >= 160 and f(10 ** 6, 4096) % 256 == 0
     need = f(4, 40)
     call = caller(qnn.lib.qnn_rms_norm_backward, "dy type rows width lddy h ldh gain gain_type rstd dh lddh dx lddx dgain ws ws_bytes stream",
                   (p, 1, 4, 40, 40, p, 40, p, 0, p, p, 40, p, 40, p, p, need, None))
@@ -97,7 +98,7 @@ def test_norm_refusals(qnn, p):
 
 def test_route_refusals(qnn, p):
     f = qnn.lib.qnn_route_workspace
-    assert f(0, 8, 2) == 0 and f(10, 8, 2) == 0 and f(10, 8, 9) == 0 and f(10, 1025, 2) == 0 and f(10 ** 6, 64, 33) == 0 and f(1 << 31, 8, 2) == 0
+    assert f(0, 8, 2) == 0 and f(10, 8, 2) == 0 and f(10, 8, 9) == 0 and f(10, 1025, 2) == 0 and f(10 ** 6, 64, 33) == 0 and f(1 << 29, 8, 2) == 0
     need = f(5000, 64, 4)
     assert need > 0 and need % 256 == 0
     call = caller(qnn.lib.qnn_route, "logits type tokens experts ld top flags bias groups top_groups factor mask chosen weights order place offsets ws ws_bytes stream",
@@ -111,7 +112,7 @@ def test_route_refusals(qnn, p):
                 {"offsets": off(p, 2)}, {"ws": off(p, 128)}):
         assert call(**bad) == qnn.E_ALIGN, bad
     assert call(factor=float("inf")) == qnn.E_SCALE and call(factor=float("nan")) == qnn.E_SCALE
-    assert call(tokens=1 << 30) == qnn.E_RANGE
+    assert call(tokens=1 << 28) == qnn.E_RANGE
     assert call(tokens=0, offsets=None, order=None, place=None) == qnn.OK
     call = caller(qnn.lib.qnn_route_backward, "dw logits type tokens experts ld top flags chosen factor out ldd stream",
                   (p, p, 0, 5, 64, 64, 4, 3, p, 1.0, p, 64, None))
@@ -120,7 +121,7 @@ def test_route_refusals(qnn, p):
         assert call(**bad) == qnn.E_ARG, bad
     for bad in ({"dw": off(p, 2)}, {"logits": off(p, 2)}, {"chosen": off(p, 2)}, {"out": off(p, 2)}):
         assert call(**bad) == qnn.E_ALIGN, bad
-    assert call(factor=float("nan")) == qnn.E_SCALE and call(tokens=1 << 30) == qnn.E_RANGE and call(tokens=0) == qnn.OK
+    assert call(factor=float("nan")) == qnn.E_SCALE and call(tokens=1 << 28) == qnn.E_RANGE and call(tokens=0) == qnn.OK
 
 
 # ------------------------------------------------------------------------------------------------ the plain forms, by hand
