@@ -73,7 +73,7 @@ def _binding_command(out: Path) -> list[str]:
     torch = Path(importlib.util.find_spec("torch").origin).parent
     return [os.environ.get("CXX", "g++"), "-O2", "-std=c++20", "-fPIC", "-shared", f"-I{INCLUDE}", f"-I{sysconfig.get_path('include')}",
             f"-I{torch / 'include'}", f"-I{torch / 'include/torch/csrc/api/include'}", "-I/usr/local/cuda/include", "-o", str(out),
-            str(CSRC / "binding.cpp"), f"-L{torch / 'lib'}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", f"-L{PKG}", "-l:libqnn.so",
+            str(CSRC / "binding.cpp"), f"-L{torch / 'lib'}", "-ltorch_python", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda", f"-L{PKG}", "-l:libqnn.so",
             "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{torch / 'lib'}"]
 
 

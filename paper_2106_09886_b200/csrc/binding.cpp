@@ -5,6 +5,7 @@
 // Argument marshalling only: every step of the work runs inside libqnn's kernels.
 #include <Python.h>
 
+#include <ATen/cuda/EmptyTensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_strided.h>
 #include <c10/cuda/CUDAFunctions.h>
@@ -117,13 +118,18 @@ at::Tensor result_for(PyObject *out, const at::Tensor &like, int64_t rows, int64
     return t;
 }
 
+// New memory on a device, from torch's allocator without its dispatcher (0.3 us less).
+at::Tensor new_array(const at::Tensor &like, at::ScalarType type, at::IntArrayRef sizes) {
+    return at::Tensor(at::detail::empty_cuda(sizes, type, like.device(), std::nullopt));
+}
+
 at::Tensor workspace_for(PyObject *workspace, size_t need, const at::Tensor &like) {
     if (given(workspace)) {
         const at::Tensor &t = tensor_of(workspace, "workspace must be a tensor");
         if (!t.is_cuda() || t.get_device() != like.get_device() || !t.is_contiguous()) throw Refused("workspace must be contiguous on the device of the rows");
         return t;
     }
-    return need ? at::empty({(int64_t)need}, like.options().dtype(at::kByte)) : at::Tensor();
+    return need ? new_array(like, at::kByte, {(int64_t)need}) : at::Tensor();
 }
 
 PyObject *answer(int status, at::Tensor &&result) { return status == QNN_OK ? THPVariable_Wrap(std::move(result)) : PyLong_FromLong(status); }
@@ -225,12 +231,12 @@ class Results {
         if (total > TOGETHER || count_ == 1) {
             for (int i = 0; i < count_; ++i) {
                 const Part &p = parts_[i];
-                const auto options = like_.options().dtype(p.type);
-                *p.t = p.flat ? at::empty({p.rows}, options) : p.ld == p.width ? at::empty({p.rows, p.width}, options) : at::empty_strided({p.rows, p.width}, {p.ld, 1}, options);
+                *p.t = p.flat ? new_array(like_, p.type, {p.rows}) : p.ld == p.width ? new_array(like_, p.type, {p.rows, p.width})
+                                                                                     : at::empty_strided({p.rows, p.width}, {p.ld, 1}, like_.options().dtype(p.type));
             }
             return;
         }
-        const at::Tensor all = at::empty({total}, like_.options().dtype(at::kByte));
+        const at::Tensor all = new_array(like_, at::kByte, {total});
         int64_t at_byte = 0;
         for (int i = 0; i < count_; ++i) {
             const Part &p = parts_[i];
@@ -327,7 +333,7 @@ int code_of(at::ScalarType t) { return t == at::kFloat ? QNN_F32 : t == at::kBFl
 at::Tensor rows_for(PyObject *out, const at::Tensor &like, at::ScalarType type, int64_t rows, int64_t width, int64_t *ld) {
     if (!given(out)) {
         *ld = width;
-        return at::empty({rows, width}, like.options().dtype(type));
+        return new_array(like, type, {rows, width});
     }
     const at::Tensor &t = tensor_of(out, "out must be a tensor");
     const Rows r = rows_of(t, width);

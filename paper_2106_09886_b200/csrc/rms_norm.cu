@@ -4,9 +4,11 @@
 //   h = round(x + residual)     rstd = 1 / sqrt(mean(h^2) + eps)     y = (h * gain) * rstd
 //   scale = max|y| / 127        code = rint(y / scale)
 //
-// Bound: HBM.  A row is read once and stays in registers, in its own type (h is rounded to it, so nothing is lost).  The order
-// (h * gain) * rstd makes max|y| = max|h * gain| * rstd exactly, rounding being monotone: the sum of squares and the largest
-// magnitude come out of one pass and one reduction, and the codes follow from the registers.
+// Bound: HBM.  A row is read once and stays in registers.  The order (h * gain) * rstd makes max|y| = max|h * gain| * rstd exactly,
+// rounding being monotone: the sum of squares and the largest magnitude come out of one pass and one reduction, and the codes follow
+// from the registers, a multiplication and a fused multiply-add each: a sum with 1.5 * 2^23 holds the nearest whole number in its low
+// byte.  (With a conversion, a clamp and a comparison for each code the kernel was bound by issue: 16384 x 4096 bf16 with a residual 125 us,
+// now 74, 6.3 TB/s; decoding them 29, 6.9 TB/s with the codes still in L2; 8192 x 4096 in a profile 37.7 us.)
 #include "real_rows.cuh"
 #include "tc_ptx.cuh"
 
@@ -376,7 +378,8 @@ int decode(const int8_t *codes, const float *scales, int64_t rows, int width, in
 
 // dx = rstd * a - h * rstd^3 * mean(a * h) + dh with a = dy * gain; dgain = sum over the rows of dy * h * rstd.
 // A block takes every gridDim.x-th row and keeps dgain of its columns in registers; the blocks' sums are added in a fixed order
-// by a second kernel, so results repeat bit for bit.
+// by a second kernel, so results repeat bit for bit.  Bound: HBM (8192 x 4096 bf16 with dh 49.7 us, 5.4 TB/s, 4 of them the second
+// kernel; loads into registers, two rows of an SM at a time, took 81).
 struct NormBackParams {
     const void *dy, *h, *gain, *dh;           // dh NULL: no gradient reaches h by another way
     const float *rstd;
