@@ -91,12 +91,12 @@ struct RowScale {
         inverse = finite ? __frcp_rn(scale) : 0.0f;
     }
     // rint(v / scale), the quotient rounded to fp32, as the low byte of a word; any byte where the scale is NaN.  The product with the
-    // inverse is off by at most 2^-23 of 127, so that only a quotient next to a half needs the division itself.  (|v| <= 127 scale:
-    // no clamp is needed.)
+    // inverse is off from it by at most three halves of 2^-23 times 127, so that only a quotient that near a half needs the division
+    // itself.  (One branch for a whole pack took 55 us for 16384 x 4096 bf16, one for each 49.  |v| <= 127 scale: no clamp is needed.)
     __device__ __forceinline__ uint32_t code_byte(float v) const {
         const float t = __fmul_rn(v, inverse);
         float r = __fadd_rn(t, TO_NEAREST);
-        if (fabsf(__fadd_rn(t, -__fadd_rn(r, -TO_NEAREST))) > 0.4999f) r = __fadd_rn(rintf(__fdiv_rn(v, scale)), TO_NEAREST);
+        if (fabsf(__fadd_rn(t, -__fadd_rn(r, -TO_NEAREST))) > 0.49997f) r = __fadd_rn(rintf(__fdiv_rn(v, scale)), TO_NEAREST);
         return __float_as_uint(r);
     }
     // Bytes of codes, zeros where the scale is NaN.

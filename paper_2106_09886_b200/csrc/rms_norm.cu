@@ -8,7 +8,7 @@
 // rounding being monotone: the sum of squares and the largest magnitude come out of one pass and one reduction, and the codes follow
 // from the registers, a multiplication and a fused multiply-add each: a sum with 1.5 * 2^23 holds the nearest whole number in its low
 // byte.  (With a conversion, a clamp and a comparison for each code the kernel was bound by issue: 16384 x 4096 bf16 with a residual 125 us,
-// now 74, 6.3 TB/s; decoding them 29, 6.9 TB/s with the codes still in L2; 8192 x 4096 in a profile 37.7 us.)
+// now 70, 6.7 TB/s; decoding them 32, 6.3 TB/s.)
 #include "real_rows.cuh"
 #include "tc_ptx.cuh"
 
