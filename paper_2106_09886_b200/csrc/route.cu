@@ -44,8 +44,8 @@ struct RouteParams {
     int32_t *chosen;
     float *weights;
     int32_t *order, *place, *offsets;                         // NULL: no plan
-    int32_t *counts;                                          // [experts][runs], behind them [experts] rows of each
-    int runs, run;                                            // tokens of a run
+    int32_t *counts;                                          // [experts][pitch_runs], behind them [experts] rows of each
+    int runs, run, pitch_runs;                                // tokens of a run; runs in whole fours
     bool scanned;                                             // counts are added up over the runs by a launch of its own
 };
 
@@ -527,55 +527,75 @@ __device__ __forceinline__ int route_token(const RouteParams &p, int64_t token, 
     return mine;
 }
 
-// Places of the slots of one run.  base[e]: in, the first row of expert e for this run.  counts: [warps][experts].
-__device__ void rank_run(const RouteParams &p, int run, int32_t *base, int32_t *counts) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, all = (int)blockDim.x >> 5;
-    const int log_warps = 31 - __clz(min(rank_warps(p.experts), all)), warps = 1 << log_warps;
-    const int first = run * p.run * p.top, slots = min(p.tokens - run * p.run, p.run) * p.top;               // (fewer than 2^31 in all)
-    const int segment = ((slots - 1) >> (log_warps + 5)) + 1 << 5;                                            // whole 32s
-    const int lo = min(slots, warp * segment), hi = warp < warps ? min(slots - lo, segment) + lo : lo;
-    // a run of up to 32 slots a warp is ranked in one step, whose slots stay in registers
-    const int e0 = lo + lane < hi ? p.chosen[first + lo + lane] : -1;
-    for (int i = threadIdx.x; i < warps * p.experts; i += blockDim.x) counts[i] = 0;
-    __syncthreads();
-    const unsigned same0 = __match_any_sync(0xffffffffu, e0);
-    for (int i = lo; i < hi; i += 32) {
-        const int e = i == lo ? e0 : i + lane < hi ? p.chosen[first + i + lane] : -1;
-        const unsigned same = i == lo ? same0 : __match_any_sync(0xffffffffu, e);
-        if (e >= 0 && __ffs(same) - 1 == lane) counts[warp * p.experts + e] += __popc(same);
-        __syncwarp();
+// A block's shared memory, in words: rows of each expert ahead of its run and in all runs, each ranking warp's counts, sums; then each
+// warp's keys.
+struct RouteSmem {
+    static __host__ __device__ int all(int experts) { return experts; }
+    static __host__ __device__ int ranks(int experts) { return 2 * experts; }
+    static __host__ __device__ int sums(int experts) { return (2 + rank_warps(experts)) * experts; }
+    static __host__ __device__ int keys(int experts) { return (sums(experts) + 40 + 3) / 4 * 4; }
+};
+
+// The places of a run's slots, whose warps take segments of whole 32s in order.  count(): each warp's slots of every expert, which needs
+// nothing of the other runs; place(): their rows, once the counts are the rows ahead of each warp's.
+struct RunRanks {
+    const RouteParams &p;
+    int32_t *counts;                                          // [warps][experts]
+    int first, lo, hi, warps, e0;                             // the run's first slot, the warp's segment; lane's first slot's expert
+    unsigned same0;
+    __device__ __forceinline__ RunRanks(const RouteParams &params, int run, int32_t *words) : p(params), counts(words + RouteSmem::ranks(params.experts)) {
+        const int warp = threadIdx.x >> 5, log_warps = 31 - __clz(min(rank_warps(p.experts), (int)blockDim.x >> 5));
+        const int slots = min(p.tokens - run * p.run, p.run) * p.top, segment = ((slots - 1) >> (log_warps + 5)) + 1 << 5;      // (fewer than 2^31)
+        warps = 1 << log_warps;
+        first = run * p.run * p.top;
+        lo = min(slots, warp * segment);
+        hi = warp < warps ? min(slots - lo, segment) + lo : lo;
+        e0 = -1;
+        same0 = 0;
     }
-    __syncthreads();
-    for (int e = threadIdx.x; e < p.experts; e += blockDim.x) {
-        int at = base[e];
-#pragma unroll 8
-        for (int w = 0; w < warps; ++w) {
-            const int c = counts[w * p.experts + e];
-            counts[w * p.experts + e] = at;
-            at += c;
+    __device__ __forceinline__ void load() { e0 = lo + (int)(threadIdx.x & 31) < hi ? p.chosen[first + lo + (threadIdx.x & 31)] : -1; }
+    __device__ __forceinline__ int expert(int i) const {
+        const int at = i + (threadIdx.x & 31);
+        return i == lo ? e0 : at < hi ? p.chosen[first + at] : -1;      // (up to 32 slots a warp stay in registers)
+    }
+    __device__ __forceinline__ void count() {
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        int32_t *mine = counts + warp * p.experts;
+        if (warp < warps)
+            for (int e = lane; e < p.experts; e += 32) mine[e] = 0;
+        __syncwarp();
+        same0 = __match_any_sync(0xffffffffu, e0);
+        for (int i = lo; i < hi; i += 32) {
+            const int e = expert(i);
+            const unsigned same = i == lo ? same0 : __match_any_sync(0xffffffffu, e);
+            if (e >= 0 && __ffs(same) - 1 == lane) mine[e] += __popc(same);
+            __syncwarp();
         }
     }
-    __syncthreads();
-    for (int i = lo; i < hi; i += 32) {
-        const bool in = i + lane < hi;
-        const int e = i == lo ? e0 : in ? p.chosen[first + i + lane] : -1;
-        const unsigned same = i == lo ? same0 : __match_any_sync(0xffffffffu, e);
-        const int at = e >= 0 ? counts[warp * p.experts + e] + __popc(same & ((1u << lane) - 1u)) : -1;
-        __syncwarp();
-        if (e >= 0 && __ffs(same) - 1 == lane) counts[warp * p.experts + e] += __popc(same);
-        __syncwarp();
-        if (in) p.place[first + i + lane] = at;
-        if (e >= 0) p.order[at] = first + i + lane;
+    __device__ __forceinline__ void place() {
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        int32_t *mine = counts + warp * p.experts;
+        for (int i = lo; i < hi; i += 32) {
+            const int e = expert(i);
+            const unsigned same = i == lo ? same0 : __match_any_sync(0xffffffffu, e);
+            const int at = e >= 0 ? mine[e] + __popc(same & ((1u << lane) - 1u)) : -1;
+            __syncwarp();
+            if (e >= 0 && __ffs(same) - 1 == lane) mine[e] += __popc(same);
+            __syncwarp();
+            if (i + lane < hi) p.place[first + i + lane] = at;
+            if (e >= 0) p.order[at] = first + i + lane;
+        }
     }
-}
+};
 
-// counts[e] of every expert -> the experts' first rows, into offsets too where that is given; returns the rows in all.  warp_sums: 33
-// numbers of shared memory.
-__device__ __forceinline__ int scan_experts(int32_t *counts, int experts, int32_t *warp_sums, int32_t *offsets) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, each = (experts + blockDim.x - 1) / blockDim.x;
-    const int first = threadIdx.x * each;
+// From the rows of every expert ahead of the run and in all: offsets where it is given, order's rest by `blocks` blocks, and the run's
+// places.
+__device__ __forceinline__ void plan_run(const RouteParams &p, RunRanks &ranks, int32_t *words, int32_t *offsets, int block, int blocks) {
+    const int32_t *ahead = words, *all = words + RouteSmem::all(p.experts);
+    int32_t *warp_sums = words + RouteSmem::sums(p.experts);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, each = (p.experts + blockDim.x - 1) / blockDim.x, first = threadIdx.x * each;
     int v = 0;
-    for (int e = first; e < min(first + each, experts); ++e) v += counts[e];
+    for (int e = first; e < min(first + each, p.experts); ++e) v += all[e];
     int incl = v;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -584,36 +604,26 @@ __device__ __forceinline__ int scan_experts(int32_t *counts, int experts, int32_
     }
     if (lane == 31) warp_sums[warp] = incl;
     __syncthreads();
-    if (warp == 0) {
-        const int own = lane < (int)(blockDim.x >> 5) ? warp_sums[lane] : 0;
-        int w = own;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int o = __shfl_up_sync(0xffffffffu, w, d);
-            if (lane >= d) w += o;
-        }
-        warp_sums[lane] = w - own;
-        if (lane == 31) warp_sums[32] = w;
-    }
-    __syncthreads();
-    const int total = warp_sums[32];
-    int at = warp_sums[warp] + incl - v;
-    for (int e = first; e < min(first + each, experts); ++e) {
-        const int c = counts[e];
-        counts[e] = at;
+    // every warp adds up the sums ahead of it itself
+    const int sum = lane < (int)(blockDim.x >> 5) ? warp_sums[lane] : 0;
+    const int before = __reduce_add_sync(0xffffffffu, lane < warp ? sum : 0), total = __reduce_add_sync(0xffffffffu, sum);
+    int at = before + incl - v;
+    for (int e = first; e < min(first + each, p.experts); ++e) {
         if (offsets) offsets[e] = at;
-        at += c;
+        int row = at + ahead[e];
+#pragma unroll 8
+        for (int w = 0; w < ranks.warps; ++w) {
+            const int c = ranks.counts[w * p.experts + e];
+            ranks.counts[w * p.experts + e] = row;
+            row += c;
+        }
+        at += all[e];
     }
-    if (offsets && threadIdx.x == 0) offsets[experts] = total;
-    return total;
+    if (offsets && threadIdx.x == 0) offsets[p.experts] = total;
+    for (int64_t i = total + (int64_t)block * blockDim.x + threadIdx.x; i < (int64_t)p.tokens * p.top; i += (int64_t)blocks * blockDim.x) p.order[i] = -1;
+    __syncthreads();
+    ranks.place();
 }
-
-// A block's shared memory: counts of its run, the ranks' counts, sums; then each warp's keys.
-struct RouteSmem {
-    static __host__ __device__ int ranks(int experts) { return experts; }
-    static __host__ __device__ int sums(int experts) { return (1 + rank_warps(experts)) * experts; }
-    static __host__ __device__ int keys(int experts) { return ((1 + rank_warps(experts)) * experts + 40 + 3) / 4 * 4; }      // in words
-};
 
 // Choices of a run of tokens; ALONE: the plan as well (one run).
 template <int V, bool ALONE>
@@ -622,7 +632,8 @@ __global__ void __launch_bounds__(choose_threads(V)) route_choose_kernel(const _
     start_next();
     wait_for_previous();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int e = threadIdx.x; e < p.experts; e += blockDim.x) words[e] = 0;
+    int32_t *counts = words + RouteSmem::all(p.experts);
+    for (int e = threadIdx.x; e < 2 * p.experts; e += blockDim.x) words[e] = 0;
     float bias[V], bias_most = 0.0f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -638,19 +649,20 @@ __global__ void __launch_bounds__(choose_threads(V)) route_choose_kernel(const _
     __syncthreads();
     for (int t = first + warp; t < last;) {
         const int e = route_token<V>(p, t, bias, bias_most, scratch);
-        if (lane < p.top && e >= 0) atomicAdd(&words[e], 1);
+        if (lane < p.top && e >= 0) atomicAdd(&counts[e], 1);
         if (lane == 0) t = atomicAdd(next, 1);
         t = __shfl_sync(0xffffffffu, t, 0);
     }
     if (!p.order) return;
     __syncthreads();
     if constexpr (!ALONE) {
-        for (int e = threadIdx.x; e < p.experts; e += blockDim.x) p.counts[(int64_t)e * p.runs + blockIdx.x] = words[e];
+        for (int e = threadIdx.x; e < p.experts; e += blockDim.x) p.counts[(int64_t)e * p.pitch_runs + blockIdx.x] = counts[e];
     } else {
-        const int total = scan_experts(words, p.experts, words + RouteSmem::sums(p.experts), p.offsets);
-        for (int i = total + threadIdx.x; i < p.tokens * p.top; i += blockDim.x) p.order[i] = -1;
+        RunRanks ranks(p, 0, words);
+        ranks.load();
+        ranks.count();
         __syncthreads();
-        rank_run(p, 0, words, words + RouteSmem::ranks(p.experts));
+        plan_run(p, ranks, words, p.offsets, 0, 1);
     }
 }
 
@@ -660,7 +672,7 @@ __global__ void __launch_bounds__(256) route_scan_kernel(const __grid_constant__
     wait_for_previous();
     const int e = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (e >= p.experts) return;
-    int32_t *counts = p.counts + (int64_t)e * p.runs;
+    int32_t *counts = p.counts + (int64_t)e * p.pitch_runs;
     int c[MAX_RUNS / 32 + 1], sum = 0;
     constexpr int EACH = MAX_RUNS / 32 + 1;
 #pragma unroll
@@ -680,7 +692,7 @@ __global__ void __launch_bounds__(256) route_scan_kernel(const __grid_constant__
         if (lane * EACH + i < p.runs) counts[lane * EACH + i] = at;
         at += c[i];
     }
-    if (lane == 31) p.counts[(int64_t)p.experts * p.runs + e] = incl;
+    if (lane == 31) p.counts[(int64_t)p.experts * p.pitch_runs + e] = incl;
 }
 
 // The plan of a run.
@@ -688,35 +700,47 @@ __global__ void __launch_bounds__(PLAN_THREADS) route_plan_kernel(const __grid_c
     extern __shared__ __align__(16) int32_t words[];
     start_next();
     wait_for_previous();
-    int32_t *ahead = words, *all = words + RouteSmem::ranks(p.experts);
+    RunRanks ranks(p, blockIdx.x, words);
+    ranks.load();
+    int32_t *ahead = words, *all = words + RouteSmem::all(p.experts);
     if (p.scanned) {
         for (int e = threadIdx.x; e < p.experts; e += blockDim.x) {
-            ahead[e] = p.counts[(int64_t)e * p.runs + blockIdx.x];
-            all[e] = p.counts[(int64_t)p.experts * p.runs + e];
+            ahead[e] = p.counts[(int64_t)e * p.pitch_runs + blockIdx.x];
+            all[e] = p.counts[(int64_t)p.experts * p.pitch_runs + e];
         }
-    } else {                                                  // a warp adds up an expert's runs
-        const int lane = threadIdx.x & 31;
-#pragma unroll 4
-        for (int e = threadIdx.x >> 5; e < p.experts; e += blockDim.x >> 5) {
-            const int32_t *counts = p.counts + (int64_t)e * p.runs;
+        ranks.count();
+    } else {                                                  // eight lanes add up an expert's runs, four at a time
+        const int sub = threadIdx.x & 7, me = blockIdx.x;
+        const int whole = (p.experts + 3) / 4 * 4;            // (all lanes of a warp go round together)
+        for (int e = threadIdx.x >> 3; e < whole; e += blockDim.x >> 3) {
+            const int4 *counts = reinterpret_cast<const int4 *>(p.counts + (int64_t)min(e, p.experts - 1) * p.pitch_runs);
             int a = 0, b = 0;
-            for (int r = lane; r < p.runs; r += 32) {
-                const int c = counts[r];
-                b += c;
-                a += r < (int)blockIdx.x ? c : 0;
+            constexpr int MOST = (MAX_RUNS + 31) / 32;
+            int4 c[MOST];
+#pragma unroll
+            for (int i = 0; i < MOST; ++i) c[i] = (sub + 8 * i) * 4 < p.runs ? counts[sub + 8 * i] : make_int4(0, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < MOST; ++i) {
+                const int r = (sub + 8 * i) * 4;
+                const int n[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int v = r + k < p.runs ? n[k] : 0;  // (the last pack of a row ends past the runs)
+                    b += v;
+                    a += r + k < me ? v : 0;
+                }
             }
-            a = __reduce_add_sync(0xffffffffu, a);
-            b = __reduce_add_sync(0xffffffffu, b);
-            if (lane == 0) { ahead[e] = a; all[e] = b; }
+#pragma unroll
+            for (int d = 1; d < 8; d <<= 1) {
+                a += __shfl_xor_sync(0xffffffffu, a, d);
+                b += __shfl_xor_sync(0xffffffffu, b, d);
+            }
+            if (sub == 0 && e < p.experts) { ahead[e] = a; all[e] = b; }
         }
+        ranks.count();
     }
     __syncthreads();
-    const int total = scan_experts(all, p.experts, words + RouteSmem::sums(p.experts), blockIdx.x == 0 ? p.offsets : nullptr);
-    __syncthreads();
-    for (int e = threadIdx.x; e < p.experts; e += blockDim.x) ahead[e] += all[e];
-    for (int64_t i = total + (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < (int64_t)p.tokens * p.top; i += (int64_t)gridDim.x * blockDim.x) p.order[i] = -1;
-    __syncthreads();
-    rank_run(p, blockIdx.x, words, words + RouteSmem::ranks(p.experts));
+    plan_run(p, ranks, words, blockIdx.x == 0 ? p.offsets : nullptr, blockIdx.x, gridDim.x);
 }
 
 // ------------------------------------------------------------------------------------------------ backward
@@ -826,10 +850,10 @@ template <auto KERNEL> int launch_route(int blocks, int threads, int smem, cudaS
     cudaGetLastError();
     return QNN_E_CUDA;
 }
-// Threads of the blocks that rank runs, and whether a launch of its own adds up the counts ahead of them: where a warp would have
-// more than 32 loads of them to make.
-int plan_threads(const RouteParams &p) { return p.run * p.top <= 256 ? 256 : PLAN_THREADS; }
-bool plan_scanned(const RouteParams &p) { return (int64_t)p.experts * ((p.runs + 31) / 32) > plan_threads(p); }
+// Threads of the blocks that rank runs, and whether a launch of its own adds up the counts ahead of them: where eight lanes an expert would
+// go round more than once (16384 x 256: PP us with it, QQ without; 4096 x 64: RR and SS).
+int plan_threads(const RouteParams &p) { return p.run * p.top <= 256 && p.experts * (p.runs + 31) / 32 <= 64 ? 256 : PLAN_THREADS; }
+bool plan_scanned(const RouteParams &p) { return p.experts > PLAN_THREADS / 8; }
 template <int V> int route_launch(const RouteParams &p, cudaStream_t st) {
     constexpr int threads = choose_threads(V);
     const int fixed = RouteSmem::keys(p.experts) * 4, smem = fixed + (p.groups > 1 ? threads / 32 * p.groups * p.pitch * 8 : 0);
@@ -862,7 +886,7 @@ bool route_sizes_ok(int64_t tokens, int experts, int top) {
 
 extern "C" size_t qnn_route_workspace(int64_t tokens, int experts, int top) {
     if (!route_sizes_ok(tokens, experts, top) || tokens == 0 || tokens * top > ROUTE_MAX_SLOTS || route_runs(tokens) == 1) return 0;
-    return ((size_t)(route_runs(tokens) + 1) * (size_t)experts * sizeof(int32_t) + 255) / 256 * 256;
+    return ((size_t)((route_runs(tokens) + 3) / 4 * 4 + 1) * (size_t)experts * sizeof(int32_t) + 255) / 256 * 256;
 }
 
 extern "C" int qnn_route(const void *logits, int type, int64_t tokens, int experts, int64_t ld, int top, unsigned flags, const float *bias,
@@ -899,6 +923,7 @@ extern "C" int qnn_route(const void *logits, int type, int64_t tokens, int exper
     p.counts = static_cast<int32_t *>(workspace);
     p.run = route_run(tokens);
     p.runs = route_runs(tokens);
+    p.pitch_runs = (p.runs + 3) / 4 * 4;
     p.scanned = plan_scanned(p);
     if (experts <= 32) return route_launch<1>(p, st);
     if (experts <= 64) return route_launch<2>(p, st);
