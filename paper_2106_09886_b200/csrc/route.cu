@@ -8,7 +8,7 @@
 //
 // Plan.  A counting sort in three launches: a block takes a run of tokens and counts its slots by expert; the counts are added up
 // over the runs (few of them: by the last launch); a block ranks the slots of its run.  Slots of an expert keep their order, and nothing depends on the order in
-// which blocks run.  Few tokens: one block does it all.
+// which blocks run.  Few tokens: one cluster does it all.
 //
 // Bound: for few tokens the launches and a token's chain of dependent steps (1 x 64 top 6 4.0 us in a replayed graph, 1 x 256 in groups
 // 5.2, 512 x 8 6.1); for many, issue: 16384 x 256 top 8 of four in eight groups take 40 us, some 1030 instructions a token (250 for any,
@@ -26,7 +26,7 @@ __host__ __device__ constexpr int choose_threads(int v) { return v <= 4 ? 1024 :
 // Warps that rank a run's slots, each with counts of its own.
 __host__ __device__ constexpr int rank_warps(int experts) { return experts <= 256 ? 32 : experts <= 512 ? 16 : 8; }
 constexpr int MAX_RUNS = 148;                                 // of tokens, a block each
-constexpr int ALONE_TOKENS = 16;                              // up to so many make one run, whose block makes the plan as well
+constexpr int ALONE_RUNS = 8;                                 // blocks of the cluster that few tokens are left to
 constexpr int64_t ROUTE_MAX_SLOTS = (1ll << 30) - 1;         // (tokens past the last are counted in 31 bits)
 
 struct RouteParams {
@@ -527,12 +527,13 @@ __device__ __forceinline__ int route_token(const RouteParams &p, int64_t token, 
     return mine;
 }
 
-// A block's shared memory, in words: rows of each expert ahead of its run and in all runs, each ranking warp's counts, sums; then each
-// warp's keys.
+// A block's shared memory, in words: rows of each expert ahead of its run, in all runs, and in its own; each ranking warp's counts, sums;
+// then each warp's keys.
 struct RouteSmem {
     static __host__ __device__ int all(int experts) { return experts; }
-    static __host__ __device__ int ranks(int experts) { return 2 * experts; }
-    static __host__ __device__ int sums(int experts) { return (2 + rank_warps(experts)) * experts; }
+    static __host__ __device__ int own(int experts) { return 2 * experts; }
+    static __host__ __device__ int ranks(int experts) { return 3 * experts; }
+    static __host__ __device__ int sums(int experts) { return (3 + rank_warps(experts)) * experts; }
     static __host__ __device__ int keys(int experts) { return (sums(experts) + 40 + 3) / 4 * 4; }
 };
 
@@ -545,7 +546,7 @@ struct RunRanks {
     unsigned same0;
     __device__ __forceinline__ RunRanks(const RouteParams &params, int run, int32_t *words) : p(params), counts(words + RouteSmem::ranks(params.experts)) {
         const int warp = threadIdx.x >> 5, log_warps = 31 - __clz(min(rank_warps(p.experts), (int)blockDim.x >> 5));
-        const int slots = min(p.tokens - run * p.run, p.run) * p.top, segment = ((slots - 1) >> (log_warps + 5)) + 1 << 5;      // (fewer than 2^31)
+        const int slots = max(0, min(p.tokens - run * p.run, p.run)) * p.top, segment = ((slots - 1) >> (log_warps + 5)) + 1 << 5;      // (fewer than 2^31)
         warps = 1 << log_warps;
         first = run * p.run * p.top;
         lo = min(slots, warp * segment);
@@ -625,15 +626,15 @@ __device__ __forceinline__ void plan_run(const RouteParams &p, RunRanks &ranks, 
     ranks.place();
 }
 
-// Choices of a run of tokens; ALONE: the plan as well (one run).
+// Choices of a run of tokens; ALONE: the plan as well, the runs being the blocks of one cluster, which read one another's counts.
 template <int V, bool ALONE>
 __global__ void __launch_bounds__(choose_threads(V)) route_choose_kernel(const __grid_constant__ RouteParams p) {
     extern __shared__ __align__(16) int32_t words[];
     start_next();
     wait_for_previous();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int32_t *counts = words + RouteSmem::all(p.experts);
-    for (int e = threadIdx.x; e < 2 * p.experts; e += blockDim.x) words[e] = 0;
+    int32_t *counts = words + RouteSmem::own(p.experts);
+    for (int e = threadIdx.x; e < p.experts; e += blockDim.x) counts[e] = 0;
     float bias[V], bias_most = 0.0f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -653,16 +654,38 @@ __global__ void __launch_bounds__(choose_threads(V)) route_choose_kernel(const _
         if (lane == 0) t = atomicAdd(next, 1);
         t = __shfl_sync(0xffffffffu, t, 0);
     }
-    if (!p.order) return;
-    __syncthreads();
+    if (!p.order) return;                                     // (for every block)
     if constexpr (!ALONE) {
+        __syncthreads();
         for (int e = threadIdx.x; e < p.experts; e += blockDim.x) p.counts[(int64_t)e * p.pitch_runs + blockIdx.x] = counts[e];
     } else {
-        RunRanks ranks(p, 0, words);
+        __syncthreads();
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        RunRanks ranks(p, blockIdx.x, words);
         ranks.load();
         ranks.count();
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        for (int e = threadIdx.x; e < p.experts; e += blockDim.x) {
+            int a = 0, b = 0;
+            const uint32_t mine = smem_u32(counts + e);
+#pragma unroll
+            for (int r = 0; r < ALONE_RUNS; ++r)
+                if (r < (int)gridDim.x) {
+                    uint32_t there;
+                    int c;
+                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(r));
+                    asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(c) : "r"(there) : "memory");
+                    b += c;
+                    a += r < (int)blockIdx.x ? c : 0;
+                }
+            words[e] = a;
+            words[RouteSmem::all(p.experts) + e] = b;
+        }
         __syncthreads();
-        plan_run(p, ranks, words, p.offsets, 0, 1);
+        asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // nobody leaves while its counts are read
+        plan_run(p, ranks, words, blockIdx.x == 0 ? p.offsets : nullptr, blockIdx.x, gridDim.x);
+        __syncwarp();
+        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     }
 }
 
@@ -826,47 +849,52 @@ __global__ void __launch_bounds__(256) route_back_kernel(const RouteBackParams p
 
 // ------------------------------------------------------------------------------------------------ host side
 
-// Runs of tokens: one for so few that the warps of a block take less time than a second launch (50 x 144 in groups: 12 us in one
-// block, 8 by runs), else as many as there are SMs, of at least eight tokens.  Sized for 148 SMs, so that workspace queries and
-// calls agree.
-int route_run(int64_t tokens) {
-    if (tokens <= ALONE_TOKENS) return ALONE_TOKENS;
-    const int64_t each = (tokens + MAX_RUNS - 1) / MAX_RUNS;
-    return (int)(each < 8 ? 8 : each);
+// Few tokens are left to one launch: a cluster of one to eight blocks, of eight tokens and more, the fewer the more work a token is.
+// (In a replayed graph and from Python: 100 x 64 top 6 5.2 and 5.4 us so, 6.4 and 7.2 in two launches; 512 x 8 7.9 and 8.1 so, 5.4
+// and 8.3 in two.)  Others make as
+// many runs as there are SMs, of at least eight tokens.  Sized for 148 SMs, so that workspace queries and calls agree.
+bool route_alone(int64_t tokens, int experts) { return tokens <= (experts <= 64 ? 256 : experts <= 128 ? 128 : 64); }
+int route_runs(int64_t tokens, int experts) {
+    if (route_alone(tokens, experts)) {
+        int runs = 1;
+        while (runs < ALONE_RUNS && runs * 8 < tokens) runs *= 2;
+        return runs;
+    }
+    const int64_t each = (tokens + MAX_RUNS - 1) / MAX_RUNS, run = each < 8 ? 8 : each;
+    return (int)((tokens + run - 1) / run);
 }
-int route_runs(int64_t tokens) { return (int)((tokens + route_run(tokens) - 1) / route_run(tokens)); }
 
-template <auto KERNEL> int launch_route(int blocks, int threads, int smem, cudaStream_t st, const RouteParams &p) {
+template <auto KERNEL> int launch_route(int blocks, int cluster, int threads, int smem, cudaStream_t st, const RouteParams &p) {
     if (smem > 48 * 1024 && !allow_shared_memory<KERNEL>(200 * 1024)) return QNN_E_CUDA;
-    LaunchAttrs attrs(1);
+    LaunchAttrs attrs(cluster);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(blocks);
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.attrs = attrs.a;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     if (cudaLaunchKernelEx(&cfg, KERNEL, p) == cudaSuccess) return QNN_OK;
     cudaGetLastError();
     return QNN_E_CUDA;
 }
 // Threads of the blocks that rank runs, and whether a launch of its own adds up the counts ahead of them: where eight lanes an expert would
-// go round more than once (16384 x 256: PP us with it, QQ without; 4096 x 64: RR and SS).
+// go round more than once (2000 x 256: 15.4 us with it, 17.4 without; 4096 x 64: 10.1 and 9.1).
 int plan_threads(const RouteParams &p) { return p.run * p.top <= 256 && p.experts * (p.runs + 31) / 32 <= 64 ? 256 : PLAN_THREADS; }
 bool plan_scanned(const RouteParams &p) { return p.experts > PLAN_THREADS / 8; }
 template <int V> int route_launch(const RouteParams &p, cudaStream_t st) {
     constexpr int threads = choose_threads(V);
     const int fixed = RouteSmem::keys(p.experts) * 4, smem = fixed + (p.groups > 1 ? threads / 32 * p.groups * p.pitch * 8 : 0);
-    if (p.runs == 1) {
+    if (route_alone(p.tokens, p.experts)) {
         // a warp for each token, and at least half a thread for each expert: barriers of idle warps take longer than their work
-        const int some = max(p.tokens, (p.experts + 63) / 64) * 32;
-        return launch_route<route_choose_kernel<V, true>>(1, some < threads ? some : threads, smem, st, p);
+        const int some = max(p.run, (p.experts + 63) / 64) * 32;
+        return launch_route<route_choose_kernel<V, true>>(p.runs, p.runs, some < threads ? some : threads, smem, st, p);
     }
     const int some = p.run * 32;
-    const int rc = launch_route<route_choose_kernel<V, false>>(p.runs, some < threads ? some : threads, smem, st, p);
+    const int rc = launch_route<route_choose_kernel<V, false>>(p.runs, 1, some < threads ? some : threads, smem, st, p);
     if (rc != QNN_OK || !p.order) return rc;
     const int scanned = p.scanned ? launch_early(route_scan_kernel, dim3((p.experts + 7) / 8), dim3(256), st, p) : QNN_OK;
-    return scanned != QNN_OK ? scanned : launch_route<route_plan_kernel>(p.runs, plan_threads(p), fixed, st, p);
+    return scanned != QNN_OK ? scanned : launch_route<route_plan_kernel>(p.runs, 1, plan_threads(p), fixed, st, p);
 }
 template <class T, int V> int back_launch(const RouteBackParams &p, cudaStream_t st) {
     const int64_t blocks = ((int64_t)p.tokens + 7) / 8;
@@ -885,8 +913,8 @@ bool route_sizes_ok(int64_t tokens, int experts, int top) {
 }  // namespace
 
 extern "C" size_t qnn_route_workspace(int64_t tokens, int experts, int top) {
-    if (!route_sizes_ok(tokens, experts, top) || tokens == 0 || tokens * top > ROUTE_MAX_SLOTS || route_runs(tokens) == 1) return 0;
-    return ((size_t)((route_runs(tokens) + 3) / 4 * 4 + 1) * (size_t)experts * sizeof(int32_t) + 255) / 256 * 256;
+    if (!route_sizes_ok(tokens, experts, top) || tokens * top > ROUTE_MAX_SLOTS || route_alone(tokens, experts)) return 0;
+    return ((size_t)((route_runs(tokens, experts) + 3) / 4 * 4 + 1) * (size_t)experts * sizeof(int32_t) + 255) / 256 * 256;
 }
 
 extern "C" int qnn_route(const void *logits, int type, int64_t tokens, int experts, int64_t ld, int top, unsigned flags, const float *bias,
@@ -921,8 +949,8 @@ extern "C" int qnn_route(const void *logits, int type, int64_t tokens, int exper
     p.factor = factor; p.mask = mask; p.chosen = chosen; p.weights = weights;
     p.order = order; p.place = place; p.offsets = offsets;
     p.counts = static_cast<int32_t *>(workspace);
-    p.run = route_run(tokens);
-    p.runs = route_runs(tokens);
+    p.runs = route_runs(tokens, experts);
+    p.run = (int)((tokens + p.runs - 1) / p.runs);
     p.pitch_runs = (p.runs + 3) / 4 * 4;
     p.scanned = plan_scanned(p);
     if (experts <= 32) return route_launch<1>(p, st);
