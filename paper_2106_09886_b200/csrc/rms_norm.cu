@@ -417,23 +417,32 @@ template <class T> struct BackPack {
     }
 };
 
-// Rows of up to 32 * NV packs, a warp each: no barrier but the last, which adds the warps' sums of the gain in order.
+// Rows of up to 32 * NV packs, a warp each: no barrier but the last, which adds the warps' sums of the gain in order.  A row stays in its
+// own type and is unpacked twice; with four packs a lane the gain is read again (from L1) for each row, so that all fits the registers.
 constexpr int BACK_WARPS = 8;
 template <class T, class G, int NV>
 __global__ void __launch_bounds__(BACK_WARPS * 32, 2) norm_back_warps_kernel(const NormBackParams p) {
-    __shared__ float all[BACK_WARPS][32 * NV * Octets<T>::V];
+    extern __shared__ float all[];                              // [BACK_WARPS][32 * NV * V]
     start_next();
     wait_for_previous();
-    constexpr int V = Octets<T>::V;
+    constexpr int V = Octets<T>::V, WIDE = 32 * NV * V;
     const int packs = p.width / V, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint4 zero = make_uint4(0, 0, 0, 0);
-    float g[NV][V], sum[NV][V];
+    float kept[NV > 2 ? 1 : NV][V], sum[NV][V];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        gain_of_pack<T, G>(p.gain, min(lane + 32 * j, packs - 1), g[j]);
+        if constexpr (NV <= 2) gain_of_pack<T, G>(p.gain, min(lane + 32 * j, packs - 1), kept[j]);
 #pragma unroll
         for (int e = 0; e < V; ++e) sum[j][e] = 0.0f;
     }
+    auto gain = [&](int j, float (&g)[V]) {
+        if constexpr (NV <= 2) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) g[e] = kept[j][e];
+        } else {
+            gain_of_pack<T, G>(p.gain, min(lane + 32 * j, packs - 1), g);
+        }
+    };
     for (int64_t row = (int64_t)blockIdx.x * BACK_WARPS + warp; row < p.rows; row += (int64_t)gridDim.x * BACK_WARPS) {
         const uint4 *dys = reinterpret_cast<const uint4 *>(static_cast<const T *>(p.dy) + row * p.lddy);
         const uint4 *hs = reinterpret_cast<const uint4 *>(static_cast<const T *>(p.h) + row * p.ldh);
@@ -449,26 +458,34 @@ __global__ void __launch_bounds__(BACK_WARPS * 32, 2) norm_back_warps_kernel(con
             dh[j] = p.dh && i < packs ? dhs[i] : zero;
         }
         float dot = 0.0f;
-        BackPack<T> b[NV];
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            b[j].get(dy[j], h[j], r);
-            b[j].add(g[j], dot, sum[j]);
+            BackPack<T> b;
+            float g[V];
+            b.get(dy[j], h[j], r);
+            gain(j, g);
+            b.add(g, dot, sum[j]);
         }
         const float mean = __fdiv_rn(warp_sum(dot), (float)p.width);
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-            if (lane + 32 * j < packs) dxs[lane + 32 * j] = b[j].result(g[j], mean, r, dh[j]);
+        for (int j = 0; j < NV; ++j) {
+            BackPack<T> b;
+            float g[V];
+            b.get(dy[j], h[j], r);
+            gain(j, g);
+            const uint4 out = b.result(g, mean, r, dh[j]);
+            if (lane + 32 * j < packs) dxs[lane + 32 * j] = out;
+        }
     }
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int e = 0; e < V; ++e) all[warp][(lane + 32 * j) * V + e] = sum[j][e];
+        for (int e = 0; e < V; ++e) all[warp * WIDE + (lane + 32 * j) * V + e] = sum[j][e];
     __syncthreads();
     for (int c = threadIdx.x; c < p.width; c += BACK_WARPS * 32) {
-        float s = all[0][c];
+        float s = all[c];
 #pragma unroll
-        for (int w = 1; w < BACK_WARPS; ++w) s = __fadd_rn(s, all[w][c]);
+        for (int w = 1; w < BACK_WARPS; ++w) s = __fadd_rn(s, all[w * WIDE + c]);
         p.sums[(int64_t)blockIdx.x * p.width + c] = s;
     }
 }
@@ -553,10 +570,64 @@ __global__ void __launch_bounds__(512) norm_back_kernel(const NormBackParams p, 
     }
 }
 
-// Rows that cannot be accessed in packs, element by element, NE of them a thread, blockDim.x apart.
+// The same for narrow rows that cannot be accessed in packs: NE elements a lane, 32 apart.
 template <class T, class G, int NE>
-__global__ void __launch_bounds__(512, NE <= 8 ? 2 : 1) norm_back_elements_kernel(const NormBackParams p) {
-    __shared__ float parts[2][16];
+__global__ void __launch_bounds__(BACK_WARPS * 32, 2) norm_back_warp_elements_kernel(const NormBackParams p) {
+    __shared__ float all[BACK_WARPS][32 * NE];
+    start_next();
+    wait_for_previous();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, width = p.width;
+    const G *gain = static_cast<const G *>(p.gain) + lane;
+    float g[NE], sum[NE];
+#pragma unroll
+    for (int j = 0; j < NE; ++j) {
+        g[j] = lane + 32 * j < width ? to_f32(gain[32 * j]) : 0.0f;
+        sum[j] = 0.0f;
+    }
+    for (int64_t row = (int64_t)blockIdx.x * BACK_WARPS + warp; row < p.rows; row += (int64_t)gridDim.x * BACK_WARPS) {
+        const T *dys = static_cast<const T *>(p.dy) + row * p.lddy + lane, *hs = static_cast<const T *>(p.h) + row * p.ldh + lane;
+        const T *dhs = static_cast<const T *>(p.dh) + row * p.lddh + lane;
+        T *dxs = static_cast<T *>(p.dx) + row * p.lddx + lane;
+        const float r = p.rstd[row];
+        const T zero = from_f32<T>(0.0f);
+        T dy[NE], h[NE], dh[NE];
+#pragma unroll
+        for (int j = 0; j < NE; ++j) {
+            const bool in = lane + 32 * j < width;
+            dy[j] = in ? dys[32 * j] : zero;
+            h[j] = in ? hs[32 * j] : zero;
+            dh[j] = in && p.dh ? dhs[32 * j] : zero;
+        }
+        float dot = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NE; ++j) {
+            const float d = to_f32(dy[j]), u = __fmul_rn(to_f32(h[j]), r);
+            dot = __fmaf_rn(__fmul_rn(d, g[j]), u, dot);
+            sum[j] = __fmaf_rn(d, u, sum[j]);
+        }
+        const float mean = __fdiv_rn(warp_sum(dot), (float)width);
+#pragma unroll
+        for (int j = 0; j < NE; ++j) {
+            const float u = __fmul_rn(to_f32(h[j]), r);
+            const float d = __fadd_rn(__fmul_rn(__fmaf_rn(-u, mean, __fmul_rn(to_f32(dy[j]), g[j])), r), to_f32(dh[j]));
+            if (lane + 32 * j < width) dxs[32 * j] = from_f32<T>(d);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NE; ++j) all[warp][lane + 32 * j] = sum[j];
+    __syncthreads();
+    for (int c = threadIdx.x; c < width; c += BACK_WARPS * 32) {
+        float s = all[0][c];
+#pragma unroll
+        for (int w = 1; w < BACK_WARPS; ++w) s = __fadd_rn(s, all[w][c]);
+        p.sums[(int64_t)blockIdx.x * width + c] = s;
+    }
+}
+
+// Wider rows that cannot be accessed in packs, element by element, NE of them a thread, blockDim.x apart; ROWS rows for each barrier.
+template <class T, class G, int NE, int ROWS>
+__global__ void __launch_bounds__(ROWS > 1 ? 256 : 512, NE <= 8 ? 2 : 1) norm_back_elements_kernel(const NormBackParams p) {
+    __shared__ float parts[2][ROWS][16];
     start_next();
     wait_for_previous();
     const int step = blockDim.x, width = p.width, first = threadIdx.x;
@@ -569,36 +640,50 @@ __global__ void __launch_bounds__(512, NE <= 8 ? 2 : 1) norm_back_elements_kerne
         sum[j] = 0.0f;
     }
     int side = 0;
-    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, side ^= 1) {
-        const T *dys = static_cast<const T *>(p.dy) + row * p.lddy + first, *hs = static_cast<const T *>(p.h) + row * p.ldh + first;
-        const T *dhs = static_cast<const T *>(p.dh) + row * p.lddh + first;
-        T *dxs = static_cast<T *>(p.dx) + row * p.lddx + first;
-        const float r = p.rstd[row];
+    for (int64_t row = blockIdx.x; row < p.rows; row += ROWS * (int64_t)gridDim.x, side ^= 1) {
         const T zero = from_f32<T>(0.0f);
-        T dy[NE], h[NE], dh[NE];
+        T dy[ROWS][NE], h[ROWS][NE], dh[ROWS][NE];
+        float r[ROWS];
 #pragma unroll
-        for (int j = 0; j < NE; ++j) {
-            const bool in = first + j * step < width;
-            dy[j] = in ? dys[j * step] : zero;
-            h[j] = in ? hs[j * step] : zero;
-            dh[j] = in && p.dh ? dhs[j * step] : zero;
-        }
-        float dot = 0.0f;
+        for (int k = 0; k < ROWS; ++k) {                        // (rows past the last are rows of zeros, and not stored)
+            const int64_t at = row + k * (int64_t)gridDim.x;
+            const bool there = at < p.rows;
+            const T *dys = static_cast<const T *>(p.dy) + at * p.lddy + first, *hs = static_cast<const T *>(p.h) + at * p.ldh + first;
+            const T *dhs = static_cast<const T *>(p.dh) + at * p.lddh + first;
+            r[k] = there ? p.rstd[at] : 0.0f;
 #pragma unroll
-        for (int j = 0; j < NE; ++j) {
-            const float d = to_f32(dy[j]), u = __fmul_rn(to_f32(h[j]), r);
-            dot = __fmaf_rn(__fmul_rn(d, g[j]), u, dot);
-            sum[j] = __fmaf_rn(d, u, sum[j]);
+            for (int j = 0; j < NE; ++j) {
+                const bool in = there && first + j * step < width;
+                dy[k][j] = in ? dys[j * step] : zero;
+                h[k][j] = in ? hs[j * step] : zero;
+                dh[k][j] = in && p.dh ? dhs[j * step] : zero;
+            }
         }
-        dot = warp_sum(dot);
-        if (lane == 0) parts[side][warp] = dot;                 // (two sides: the next row's sums do not wait for this one's readers)
+        float dot[ROWS];
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            dot[k] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < NE; ++j) {
+                const float d = to_f32(dy[k][j]), u = __fmul_rn(to_f32(h[k][j]), r[k]);
+                dot[k] = __fmaf_rn(__fmul_rn(d, g[j]), u, dot[k]);
+                sum[j] = __fmaf_rn(d, u, sum[j]);
+            }
+            dot[k] = warp_sum(dot[k]);
+            if (lane == 0) parts[side][k][warp] = dot[k];       // (two sides: the next rows' sums do not wait for these ones' readers)
+        }
         __syncthreads();
-        const float mean = __fdiv_rn(warp_sum(lane < warps ? parts[side][lane] : 0.0f), (float)width);
 #pragma unroll
-        for (int j = 0; j < NE; ++j) {
-            const float u = __fmul_rn(to_f32(h[j]), r);
-            const float d = __fadd_rn(__fmul_rn(__fmaf_rn(-u, mean, __fmul_rn(to_f32(dy[j]), g[j])), r), to_f32(dh[j]));
-            if (first + j * step < width) dxs[j * step] = from_f32<T>(d);
+        for (int k = 0; k < ROWS; ++k) {
+            const int64_t at = row + k * (int64_t)gridDim.x;
+            const float mean = __fdiv_rn(warp_sum(lane < warps ? parts[side][k][lane] : 0.0f), (float)width);
+            T *dxs = static_cast<T *>(p.dx) + at * p.lddx + first;
+#pragma unroll
+            for (int j = 0; j < NE; ++j) {
+                const float u = __fmul_rn(to_f32(h[k][j]), r[k]);
+                const float d = __fadd_rn(__fmul_rn(__fmaf_rn(-u, mean, __fmul_rn(to_f32(dy[k][j]), g[j])), r[k]), to_f32(dh[k][j]));
+                if (at < p.rows && first + j * step < width) dxs[j * step] = from_f32<T>(d);
+            }
         }
     }
 #pragma unroll
@@ -644,7 +729,7 @@ __global__ void __launch_bounds__(512) norm_back_any_kernel(const NormBackParams
     for (int i = threadIdx.x; i < p.width; i += blockDim.x) p.sums[(int64_t)blockIdx.x * p.width + i] = sums[i];
 }
 
-// dgain[c] = sum over `parts` rows of sums.  A thread adds every 32nd of them, with all loads under way; 32 threads a column, whose sums
+// dgain[c] = sum over `parts` rows of sums.  A thread adds every 32nd of them, with twelve loads under way; 32 threads a column, whose sums
 // are added in order.
 constexpr int BACK_PARTS = 296;
 __global__ void __launch_bounds__(1024) norm_gain_kernel(const float *sums, int parts, int width, float *dgain) {
@@ -652,15 +737,14 @@ __global__ void __launch_bounds__(1024) norm_gain_kernel(const float *sums, int 
     start_next();
     wait_for_previous();
     const int c = blockIdx.x * 32 + threadIdx.x;
-    constexpr int EACH = (BACK_PARTS + 31) / 32;
-    float v[EACH], sum = 0.0f;
+    float sum = 0.0f;
+    for (int q0 = threadIdx.y; q0 < parts; q0 += 32 * 12) {
+        float v[12];
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        const int q = threadIdx.y + 32 * i;
-        v[i] = c < width && q < parts ? sums[(int64_t)q * width + c] : 0.0f;
+        for (int i = 0; i < 12; ++i) v[i] = c < width && q0 + 32 * i < parts ? sums[(int64_t)(q0 + 32 * i) * width + c] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 12; ++i) sum = __fadd_rn(sum, v[i]);
     }
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) sum = __fadd_rn(sum, v[i]);
     part[threadIdx.y][threadIdx.x] = sum;
     __syncthreads();
     const float total = warp_sum(part[threadIdx.x][threadIdx.y]);         // warp y takes column y
@@ -688,11 +772,21 @@ int back_launch(const NormBackParams &p, int packs, cudaStream_t st) {
 }
 template <class T, class G, int NV>
 int back_warps_launch(const NormBackParams &p, cudaStream_t st) {
-    return launch_early(norm_back_warps_kernel<T, G, NV>, dim3(back_blocks(p.rows)), dim3(BACK_WARPS * 32), st, p);
+    LaunchAttrs attrs(1);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(back_blocks(p.rows));
+    cfg.blockDim = dim3(BACK_WARPS * 32);
+    cfg.dynamicSmemBytes = BACK_WARPS * 32 * NV * Octets<T>::V * sizeof(float);      // (at most 32 KB)
+    cfg.stream = st;
+    cfg.attrs = attrs.a;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, norm_back_warps_kernel<T, G, NV>, p) == cudaSuccess) return QNN_OK;
+    cudaGetLastError();
+    return QNN_E_CUDA;
 }
-template <class T, class G, int NE>
+template <class T, class G, int NE, int ROWS>
 int back_elements_launch(const NormBackParams &p, cudaStream_t st) {
-    return launch_early(norm_back_elements_kernel<T, G, NE>, dim3(back_blocks(p.rows)), dim3(whole_warps((p.width + NE - 1) / NE)), st, p);
+    return launch_early(norm_back_elements_kernel<T, G, NE, ROWS>, dim3(back_blocks(p.rows)), dim3(whole_warps((p.width + NE - 1) / NE)), st, p);
 }
 template <class T, class G>
 int back_any_launch(const NormBackParams &p, cudaStream_t st) {
@@ -714,12 +808,14 @@ template <class T, class G>
 int back_typed(const NormBackParams &p, bool vec, float *dgain, cudaStream_t st) {
     const int packs = p.width / (16 / (int)sizeof(T));
     int rc;
-    if (!vec && p.width <= 4096) rc = back_elements_launch<T, G, 8>(p, st);
-    else if (!vec && p.width <= 8192) rc = back_elements_launch<T, G, 16>(p, st);
+    if (!vec && p.width <= 512) rc = launch_early(norm_back_warp_elements_kernel<T, G, 16>, dim3(back_blocks(p.rows)), dim3(BACK_WARPS * 32), st, p);
+    else if (!vec && p.width <= 4096) rc = p.width <= 2048 ? back_elements_launch<T, G, 8, 2>(p, st) : back_elements_launch<T, G, 8, 1>(p, st);
+    else if (!vec && p.width <= 8192) rc = back_elements_launch<T, G, 16, 1>(p, st);
     else if (!vec || packs > 2048) rc = back_any_launch<T, G>(p, st);
     else if (packs <= 32) rc = back_warps_launch<T, G, 1>(p, st);
     else if (packs <= 64) rc = back_warps_launch<T, G, 2>(p, st);
-    else if (packs <= 128) rc = back_launch<T, G, 1>(p, packs, st);
+    else if (packs <= 128) rc = back_warps_launch<T, G, 4>(p, st);
+    else if (packs <= 256) rc = back_launch<T, G, 1>(p, packs, st);
     else if (packs <= 1024) rc = back_launch<T, G, 2>(p, packs, st);
     else rc = back_launch<T, G, 4>(p, packs, st);
     if (rc != QNN_OK) return rc;

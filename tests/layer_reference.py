@@ -66,12 +66,12 @@ def norm_backward(dy, h, gain, rstd, dh):
 
 def norm_backward_bounds(dy, h, gain, rstd, dh, dtype):
     """The mean adds at most 64 + 10 products of three factors, and is divided; then each element is rounded at every step.  A column of
-    dgain adds `rows / 296` products, then 8 sums of warps or none, then 10 + 5 partial sums."""
+    dgain adds `rows / 296` products or fewer, then 8 sums of warps or none, then up to 37 + 5 partial sums."""
     u, a = np.abs(h * rstd[:, None]), np.abs(dy * gain[None, :])
     mean = np.mean(a * u, axis=1, keepdims=True)
     dx, _ = norm_backward(dy, h, gain, rstd, dh)
     off = rstd[:, None] * (3 * a + u * mean * (74 + 3 + 1 + 4)) * U32 + (np.abs(dx) + (0 if dh is None else np.abs(dh))) * U32
-    return off + rounding(np.abs(dx) + off, dtype), (np.abs(dy) * u).sum(0) * (h.shape[0] // 296 + 1 + 8 + 10 + 5 + 2) * U32
+    return off + rounding(np.abs(dx) + off, dtype), (np.abs(dy) * u).sum(0) * (h.shape[0] // 296 + 1 + 8 + 37 + 5 + 2) * U32
 
 
 # ------------------------------------------------------------------------------------------------ routing
