@@ -378,7 +378,7 @@ int decode(const int8_t *codes, const float *scales, int64_t rows, int width, in
 
 // dx = rstd * a - h * rstd^3 * mean(a * h) + dh with a = dy * gain; dgain = sum over the rows of dy * h * rstd.
 // A block takes every gridDim.x-th row and keeps dgain of its columns in registers; the blocks' sums are added in a fixed order
-// by a second kernel, so results repeat bit for bit.  Bound: HBM (8192 x 4096 bf16 with dh 49.7 us, 5.4 TB/s, 4 of them the second
+// by a second kernel, so results repeat bit for bit.  Bound: HBM (8192 x 4096 bf16 with dh 50 us, 5.4 TB/s, 4 of them the second
 // kernel; loads into registers, two rows of an SM at a time, took 81).
 struct NormBackParams {
     const void *dy, *h, *gain, *dh;           // dh NULL: no gradient reaches h by another way
