@@ -7,12 +7,13 @@
 // in 64 bits.  The choice is therefore that of 64-bit scores, at the cost of fp32 ones.
 //
 // Plan.  A counting sort in three launches: a block takes a run of tokens and counts its slots by expert; the counts are added up
-// over the runs (few of them: by the last launch); a block ranks the slots of its run.  Slots of an expert keep their order, and nothing depends on the order in
-// which blocks run.  Few tokens: one cluster does it all.
+// over the runs (few experts: by the last launch); a block ranks the slots of its run.  Slots of an expert keep their order, and
+// nothing depends on the order in which blocks run.  Few tokens: one cluster does it all.
 //
 // Bound: for few tokens the launches and a token's chain of dependent steps (1 x 64 top 6 4.2 us in a replayed graph, 1 x 256 in groups
-// 5.8, 512 x 8 5.4); for many, issue: 16384 x 256 top 8 of four in eight groups take 40 us (28 for the choice), some 1030 instructions a token (250 for any,
-// 27 for each 32 experts, 26 for each choice, 18 for each 32 scores with a bias, 230 for the groups), 74 % of the slots.
+// 5.8, 512 x 8 5.4); for many, issue: 16384 x 256 top 8 of four in eight groups take 40 us (28 for the choice), some 1030
+// instructions a token (250 for any, 27 for each 32 experts, 26 for each choice, 18 for each 32 scores with a bias, 230 for the
+// groups), 74 % of the slots.
 #include "real_rows.cuh"
 #include "tc_ptx.cuh"
 
@@ -21,7 +22,7 @@ namespace {
 constexpr int ROUTE_MAX_EXPERTS = 1024, ROUTE_MAX_TOP = 32, ROUTE_MAX_GROUPS = 32;
 constexpr int PLAN_THREADS = 1024;
 // Threads of a block whose lanes hold V experts each: V numbers of four kinds have to fit the registers (256 experts in groups, one token:
-// 5.2 us with 512 threads of 128 registers, 5.8 with 1024 of 64; 16384 tokens: the same).
+// half a microsecond less with 512 threads of 128 registers than with 1024 of 64; 16384 tokens: the same).
 __host__ __device__ constexpr int choose_threads(int v) { return v <= 4 ? 1024 : 512; }
 // Warps that rank a run's slots, each with counts of its own.
 __host__ __device__ constexpr int rank_warps(int experts) { return experts <= 256 ? 32 : experts <= 512 ? 16 : 8; }
@@ -851,8 +852,8 @@ __global__ void __launch_bounds__(256) route_back_kernel(const RouteBackParams p
 
 // Few tokens are left to one launch: a cluster of one to eight blocks, of eight tokens and more, the fewer the more work a token is.
 // (In a replayed graph and from Python: 100 x 64 top 6 5.2 and 5.4 us so, 6.4 and 7.2 in two launches; 512 x 8 7.9 and 8.1 so, 5.4
-// and 8.3 in two.)  Others make as
-// many runs as there are SMs, of at least eight tokens.  Sized for 148 SMs, so that workspace queries and calls agree.
+// and 8.3 in two.)  Others make as many runs as there are SMs, of at least eight tokens.  Sized for 148 SMs, so that workspace
+// queries and calls agree.
 bool route_alone(int64_t tokens, int experts) { return tokens <= (experts <= 64 ? 256 : experts <= 128 ? 128 : 64); }
 int route_runs(int64_t tokens, int experts) {
     if (route_alone(tokens, experts)) {

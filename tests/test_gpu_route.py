@@ -179,6 +179,26 @@ def test_many_tokens(t, qnn):
     assert t.equal(want.indices.int(), r.experts)
 
 
+@pytest.mark.parametrize("experts,top", [(5, 2), (64, 6), (100, 8), (200, 4), (600, 3)])
+def test_every_split_of_few_tokens(t, qnn, experts, top):
+    """One block, clusters of two to eight whose last blocks have fewer tokens or none, and the two and three launches beyond: against a
+    stable sort."""
+    g = t.Generator(device=DEV).manual_seed(experts)
+    for tokens in (1, 2, 7, 8, 9, 15, 16, 17, 18, 25, 31, 33, 34, 41, 49, 57, 63, 64, 65, 66, 73, 97, 100, 121, 127, 128, 129, 200, 255, 256, 257, 300, 1000):
+        l = t.randn((tokens, experts), device=DEV, generator=g)
+        mask = t.rand(tokens, device=DEV, generator=g) < 0.9
+        r = qnn.route(l, top, mask=mask)
+        assert t.equal(r.experts, t.where(mask.view(-1, 1), l.topk(top, 1).indices.int(), -1))
+        flat = r.experts.reshape(-1).long()
+        key = t.where(flat < 0, experts, flat)
+        rows = int((flat >= 0).sum())
+        assert t.equal(r.offsets.long(), t.cat([t.zeros(1, dtype=t.int64, device=DEV), t.bincount(key, minlength=experts + 1)[:experts].cumsum(0)]))
+        assert t.equal(r.order[:rows].long(), key.sort(stable=True).indices[:rows]) and bool((r.order[rows:] == -1).all())
+        place = t.full((tokens * top,), -1, dtype=t.int32, device=DEV)
+        place[r.order[:rows].long()] = t.arange(rows, dtype=t.int32, device=DEV)
+        assert t.equal(r.place.reshape(-1), place)
+
+
 # ------------------------------------------------------------------------------------------------ backward
 
 @pytest.mark.parametrize("dtype", ref.TYPES)
