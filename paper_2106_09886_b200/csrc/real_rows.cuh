@@ -83,21 +83,28 @@ __device__ __forceinline__ float max_or_nan(float a, float b) {
 // A row's scale from its largest magnitude m: m / 127, at least the smallest normal number, so that 1 / scale is finite and a row
 // of zeros decodes to zeros.  NaN for a row that holds an infinity or NaN.
 constexpr float TO_NEAREST = 12582912.0f;          // 1.5 * 2^23: a sum with it holds the nearest whole number in its low bits
+//
+// A code is rint(y / scale), the quotient rounded to fp32, and comes without a division: q0 = y * inverse, corrected by its residual,
+// q = q0 + (y - q0 * scale) * inverse.  Only where y / scale is next to a border, half a step of fp32 off a half H, could q fall on the
+// border's other side.  With scale = S * 2^a, 2^23 < S < 2^24 (all is exact for S = 2^23), y and H * scale are multiples of 2^(a-1), so that
+// a quotient lies j / 2S steps off its border with a whole j, never 0.  There q0, whose product is off by 0.993 steps before it is rounded, is
+// one of the border's two neighbours and the residual is exact; the inverse, off by S * 2^-48 (relative), makes the sum off by
+// (S + j) * 2^-49 steps at most: less than j / 2S, as S * (S + j) < j * 2^48.  (Farther off, from j = 7, it is off by 3 * 2^-24 steps at most.)
+// The residual has to be a normal number: rows of small scales are raised by a power of two, which changes no quotient.  |y| <= 127 scale:
+// no clamp is needed.
 struct RowScale {
-    float scale, inverse;
+    float scale, up, raised, inverse;              // up: 1, or what small scales are raised by; raised = scale * up; inverse of that
     __device__ __forceinline__ explicit RowScale(float m) {
         const bool finite = m <= 3.402823466e38f;
         scale = finite ? fmaxf(__fdiv_rn(m, 127.0f), 1.17549435e-38f) : __int_as_float(0x7FC00000);
-        inverse = finite ? __frcp_rn(scale) : 0.0f;
+        up = scale < 8.67361738e-19f ? 1.8446744e19f : 1.0f;        // 2^-60, 2^64
+        raised = __fmul_rn(scale, up);
+        inverse = finite ? __frcp_rn(raised) : 0.0f;
     }
-    // rint(v / scale), the quotient rounded to fp32, as the low byte of a word; any byte where the scale is NaN.  The product with the
-    // inverse is off from it by at most three halves of 2^-23 times 127, so that only a quotient that near a half needs the division
-    // itself.  (One branch for a whole pack took 55 us for 16384 x 4096 bf16, one for each 49.  |v| <= 127 scale: no clamp is needed.)
-    __device__ __forceinline__ uint32_t code_byte(float v) const {
-        const float t = __fmul_rn(v, inverse);
-        float r = __fadd_rn(t, TO_NEAREST);
-        if (fabsf(__fadd_rn(t, -__fadd_rn(r, -TO_NEAREST))) > 0.49997f) r = __fadd_rn(rintf(__fdiv_rn(v, scale)), TO_NEAREST);
-        return __float_as_uint(r);
+    // The code of y as the low byte of a word; any byte where the scale is NaN.
+    __device__ __forceinline__ uint32_t code(float y) const {
+        const float a = __fmul_rn(y, up), q = __fmul_rn(a, inverse), r = __fmaf_rn(-q, raised, a);
+        return __float_as_uint(__fadd_rn(__fmaf_rn(r, inverse, q), TO_NEAREST));
     }
     // Bytes of codes, zeros where the scale is NaN.
     __device__ __forceinline__ uint32_t word(uint32_t a, uint32_t b, uint32_t c, uint32_t d) const {

@@ -6,9 +6,11 @@
 //
 // Bound: HBM.  A row is read once and stays in registers.  The order (h * gain) * rstd makes max|y| = max|h * gain| * rstd exactly,
 // rounding being monotone: the sum of squares and the largest magnitude come out of one pass and one reduction, and the codes follow
-// from the registers, a multiplication and a fused multiply-add each: a sum with 1.5 * 2^23 holds the nearest whole number in its low
-// byte.  (With a conversion, a clamp and a comparison for each code the kernel was bound by issue: 16384 x 4096 bf16 with a residual 125 us,
-// now 70, 6.7 TB/s; decoding them 32, 6.3 TB/s.)
+// from the registers by a few multiplications and fused multiply-adds each, without a branch (RowScale): a sum with 1.5 * 2^23 holds
+// the nearest whole number in its low byte.
+// 16384 x 4096 bf16 with a residual take 73 us (470 MB, some of the writes still in L2 at the end), the quantiser of as many 45, decoding 32.
+// With a conversion, a clamp and a comparison for each code the norm took 125; with codes by two bounds of the product, and those that
+// the bounds leave open by division out of line, 91; with the product alone, whose codes are not always the quotient's, 72.
 #include "real_rows.cuh"
 #include "tc_ptx.cuh"
 
@@ -144,7 +146,7 @@ __global__ void __launch_bounds__(NV == 1 ? 1024 : 512, NV == 2 ? 2 : 1) norm_ro
             const int i = threadIdx.x + j * step;
             uint32_t c[V];
 #pragma unroll
-            for (int e = 0; e < V; ++e) c[e] = NORM ? __float_as_uint(__fmaf_rn(__fmul_rn(v[j][e], rstd), s.inverse, TO_NEAREST)) : s.code_byte(v[j][e]);
+            for (int e = 0; e < V; ++e) c[e] = s.code(NORM ? __fmul_rn(v[j][e], rstd) : v[j][e]);
             if (i < packs) {
                 if constexpr (V == 8)
                     reinterpret_cast<uint2 *>(codes)[i] = make_uint2(s.word(c[0], c[1], c[2], c[3]), s.word(c[4], c[5], c[6], c[7]));
@@ -210,7 +212,7 @@ __global__ void __launch_bounds__(512, NE <= 16 ? 2 : 1) norm_elements_kernel(co
         int8_t *codes = p.codes + row * p.ldc + first;
 #pragma unroll
         for (int j = 0; j < NE; ++j) {
-            const uint32_t c = NORM ? __float_as_uint(__fmaf_rn(__fmul_rn(v[j], rstd), s.inverse, TO_NEAREST)) : s.code_byte(v[j]);
+            const uint32_t c = s.code(NORM ? __fmul_rn(v[j], rstd) : v[j]);
             if (first + j * step < width) codes[j * step] = (int8_t)(s.inverse != 0.0f ? c : 0u);
         }
     }
@@ -266,7 +268,7 @@ __global__ void __launch_bounds__(1024) norm_wide_kernel(const NormParams p) {
         float a = to_f32(x[i]);
         if constexpr (NORM) a = __fmul_rn(__fmul_rn(a, to_f32(gain[i])), rstd);
         if (NORM && p.y) y[i] = from_f32<T>(a);
-        if (coded) codes[i] = (int8_t)(s.inverse != 0.0f ? (NORM ? __float_as_uint(__fmaf_rn(a, s.inverse, TO_NEAREST)) : s.code_byte(a)) : 0u);
+        if (coded) codes[i] = (int8_t)(s.inverse != 0.0f ? s.code(a) : 0u);
     }
 }
 
