@@ -443,7 +443,8 @@ int qnn_rms_norm_backward(const void *dy, int type, int64_t rows, int width, int
  * qnn_route_workspace(...) bytes (0: it may be NULL), needed with a plan only.
  *
  * Backward: dlogits [tokens][ldd] of `type`, fully written, from dweights fp32 [tokens][top], the logits and the choice (experts
- * outside 0 .. experts - 1 count as none).  flags and factor as in the call; the bias has no part in it.
+ * outside 0 .. experts - 1 count as none).  flags and factor as in the call; the bias has no part in it.  A token without an expert
+ * (padding, say) gets zeros, whatever its logits and dweights hold.
  */
 #define QNN_ROUTE_SIGMOID 1u
 #define QNN_ROUTE_RENORMALISE 2u

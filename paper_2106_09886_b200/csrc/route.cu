@@ -798,6 +798,8 @@ __global__ void __launch_bounds__(256) route_back_kernel(const RouteBackParams p
         const float dw = e >= 0 ? __fmul_rn(p.dweights[token * p.top + lane], p.factor) : 0.0f;
         float g = 0.0f, rest = 0.0f;                          // dl at the chosen expert; of every expert, times its score
         float l[V], scale = 0.0f;
+        // a token without an expert has a gradient of zeros, whatever its logits hold
+        const bool dense = !p.renormalise && !p.sigmoid && __any_sync(0xffffffffu, e >= 0);
         if (p.renormalise) {
             const float high = warp_most(x);
             float u = 0.0f;
@@ -812,7 +814,7 @@ __global__ void __launch_bounds__(256) route_back_kernel(const RouteBackParams p
             if (p.sigmoid && e >= 0) g = __fdiv_rn(g, __fadd_rn(1.0f, expf(x)));                 // 1 - s
         } else if (p.sigmoid) {
             if (e >= 0) g = __fmul_rn(dw, __fmul_rn(__fdiv_rn(1.0f, __fadd_rn(1.0f, expf(-x))), __fdiv_rn(1.0f, __fadd_rn(1.0f, expf(x)))));
-        } else {
+        } else if (dense) {
             load_row<V>(p.logits, p.type, token * p.ld, p.experts, l);
             float most = __int_as_float(0xFF800000), sum = 0.0f;
 #pragma unroll
@@ -830,7 +832,6 @@ __global__ void __launch_bounds__(256) route_back_kernel(const RouteBackParams p
             g = __fmul_rn(dw, s);
             rest = warp_add(g);
         }
-        const bool dense = !p.renormalise && !p.sigmoid;
         T *out = static_cast<T *>(p.dlogits) + token * p.ldd;
         float d[V];
 #pragma unroll
