@@ -911,11 +911,12 @@ template <class T> int back_typed(const RouteBackParams &p, cudaStream_t st) {
 bool route_sizes_ok(int64_t tokens, int experts, int top) {
     return tokens >= 0 && experts >= 1 && experts <= ROUTE_MAX_EXPERTS && top >= 1 && top <= experts && top <= ROUTE_MAX_TOP;
 }
+bool route_slots_ok(int64_t tokens, int top) { return tokens <= ROUTE_MAX_SLOTS / top; }      // (tokens * top could wrap around)
 
 }  // namespace
 
 extern "C" size_t qnn_route_workspace(int64_t tokens, int experts, int top) {
-    if (!route_sizes_ok(tokens, experts, top) || tokens * top > ROUTE_MAX_SLOTS || route_alone(tokens, experts)) return 0;
+    if (!route_sizes_ok(tokens, experts, top) || !route_slots_ok(tokens, top) || route_alone(tokens, experts)) return 0;
     return ((size_t)((route_runs(tokens, experts) + 3) / 4 * 4 + 1) * (size_t)experts * sizeof(int32_t) + 255) / 256 * 256;
 }
 
@@ -927,7 +928,7 @@ extern "C" int qnn_route(const void *logits, int type, int64_t tokens, int exper
         (groups > 1 && (flags & QNN_ROUTE_GROUPS_BY_TWO) && experts / groups < 2))
         return QNN_E_ARG;
     if (!(fabsf(factor) <= 3.0e38f)) return QNN_E_SCALE;
-    if (tokens * top > ROUTE_MAX_SLOTS) return QNN_E_RANGE;
+    if (!route_slots_ok(tokens, top)) return QNN_E_RANGE;
     if (!qnn_aligned(bias, 4) || !qnn_aligned(order, 4) || !qnn_aligned(place, 4) || !qnn_aligned(offsets, 4)) return QNN_E_ALIGN;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (tokens == 0)
@@ -967,7 +968,7 @@ extern "C" int qnn_route_backward(const float *dweights, const void *logits, int
                                   unsigned flags, const int32_t *chosen, float factor, void *dlogits, int64_t ldd, void *stream) {
     if (!g4_type_ok(type) || !route_sizes_ok(tokens, experts, top) || ld < experts || ldd < experts || flags > 7u) return QNN_E_ARG;
     if (!(fabsf(factor) <= 3.0e38f)) return QNN_E_SCALE;
-    if (tokens * top > ROUTE_MAX_SLOTS) return QNN_E_RANGE;
+    if (!route_slots_ok(tokens, top)) return QNN_E_RANGE;
     if (tokens == 0) return QNN_OK;
     if (!dweights || !logits || !chosen || !dlogits) return QNN_E_ARG;
     if (!qnn_aligned(logits, g4_type_bytes(type)) || !qnn_aligned(dlogits, g4_type_bytes(type)) || !qnn_aligned(dweights, 4) || !qnn_aligned(chosen, 4))
