@@ -426,7 +426,8 @@ int qnn_rms_norm_backward(const void *dy, int type, int64_t rows, int width, int
  *   scores   s = softmax(l), or 1 / (1 + exp(-l)) with QNN_ROUTE_SIGMOID
  *   keys     s + bias where a bias is given (it decides the choice alone and has no gradient), else l itself (s grows with it)
  *   groups   experts lie in `groups` equal groups; the top_groups groups of the largest key (QNN_ROUTE_GROUPS_BY_TWO: of the largest
- *            sum of two keys; without a bias, of two scores) stay, ties to the lowest group
+ *            sum of two keys; without a bias, of two scores) stay, ties to the lowest group.  Experts that are not to be chosen count as
+ *            -infinity: by two, a group with fewer than two others comes behind all that have them
  *   choice   the `top` largest keys, in that order, ties to the lowest expert.  Decisions are those of scores in 64 bits.
  *   weights  factor * s of the chosen, QNN_ROUTE_RENORMALISE: factor * s / (sum of the chosen s); in fp32
  * An expert whose logit or bias is -infinity (or whose bias is NaN) is not chosen; where fewer than `top` are left, the rest of

@@ -145,6 +145,16 @@ template <class K> __device__ __forceinline__ unsigned best_groups(const RoutePa
     return stay;
 }
 
+// The sum of a group's two largest keys; -infinity where there are not two.  A sum of fp32 keys may be beyond fp32: it becomes the largest
+// finite number there, near enough to others' for 64 bits to decide.
+__device__ __forceinline__ double sum_of_two(double first, double second) {
+    return second > __longlong_as_double(0xFFF0000000000000ll) ? first + second : second;
+}
+__device__ __forceinline__ float sum_of_two(float first, float second) {
+    const float most = 3.402823466e38f, inf = __int_as_float(0x7F800000), sum = fmaxf(__fadd_rn(first, second), -most);
+    return second > -inf ? (first < inf ? fminf(sum, most) : sum) : second;
+}
+
 // The worth of lane >> log_lanes' group: its largest number, or the sum of its two largest.  worth: -infinity where an expert is not to
 // be chosen.  By way of shared memory, for groups of any size.
 template <class K, int V>
@@ -174,7 +184,7 @@ __device__ __forceinline__ K group_worth(const RouteParams &p, const K (&worth)[
         second = low > second ? low : second;
         first = high;
     }
-    return p.by_sums ? first + second : first;
+    return p.by_sums ? sum_of_two(first, second) : first;
 }
 // The same for groups of 32 experts: register v of the lanes holds group v, as ordered numbers.  The two largest of every group by
 // one exchange that halves the registers at each of its first steps: lane l ends up with group l / (32 / V), where group_worth has it.
@@ -204,7 +214,7 @@ template <int V> __device__ __forceinline__ float whole_group_worth(const RouteP
             first[0] = max(first[0], b);
         }
     }
-    return p.by_sums ? __fadd_rn(from_ordered(first[0]), from_ordered(second[0])) : from_ordered(first[0]);
+    return p.by_sums ? sum_of_two(from_ordered(first[0]), from_ordered(second[0])) : from_ordered(first[0]);
 }
 // Lanes whose group is at bit group << log_lanes of a warp's mask.
 __device__ __forceinline__ bool holds_group(const RouteParams &p) {
