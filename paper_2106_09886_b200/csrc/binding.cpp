@@ -10,6 +10,7 @@
 #include <ATen/ops/empty_strided.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/GradMode.h>
 #include <c10/core/TensorImpl.h>
 #include <torch/csrc/Dtype.h>
@@ -41,10 +42,13 @@ int type_of(const at::Tensor &t) {
     }
 }
 
-// These calls record no gradients: an operand that requires one, while they are recorded, would lose it without a word.
+// These calls record no gradients: an operand that requires one, while they are recorded, would lose it without a word, and so would one that
+// carries a forward-mode tangent.
 void check_no_graph(const at::Tensor &t) {
     if (t.requires_grad() && c10::GradMode::is_enabled())
         throw Refused("these calls record no gradients: detach tensors that require grad, or call under torch.no_grad()");
+    if (t._fw_grad(0).defined() && c10::AutogradState::get_tls_state().get_fw_grad_mode())
+        throw Refused("these calls carry no forward-mode tangents: pass the primal alone");
 }
 
 struct Rows {

@@ -488,7 +488,8 @@ def g4_plan(product: str, dtype: torch.dtype, rows: int, experts: int, n: int, k
 class I8Rows(NamedTuple):
     """Rows in 8 bits (tokens, or output features of a weight matrix): scales[r] * codes[r, i].  Rows of codes start on 16 bytes; the
     calls that make them lay them out so.  Like the calls on 4-bit weights, those on rows in 8 bits, the norm and the routing are
-    not joined to torch's autograd and refuse operands that require grad while gradients are recorded."""
+    not joined to torch's autograd and refuse operands that require grad while gradients are recorded, or carry a forward-mode
+    tangent."""
     codes: torch.Tensor      # int8 [rows, k], rows a multiple of 16 bytes apart
     scales: torch.Tensor     # fp32 [rows]
 
