@@ -407,6 +407,8 @@ int qnn_i8_plan(int64_t rows, int n, int k, int *tile, int *ranks);
  *   codes, scales   out, optional: the rows y, before any rounding to `type`, in 8 bits as above.  One of y and codes is given.
  *   rstd       out, optional fp32 [rows], for the backward products
  * eps >= 0 (with 0 a row of zeros gives NaN); width at most 32768; alignment and rows = 0 as above.
+ * A row's results do not depend on the rows beside it, nor on their number; whether every array's rows (and the gain) start on 16 bytes decides
+ * the order in which its squares are added, and with it rstd's last bits.
  *
  * Backward, given dy = dC/dy (through codes: straight through) and, optional, dh = what reaches h by another way:
  *   dx = rstd * (dy * gain - u * mean(dy * gain * u)) + dh with u = h * rstd     (also the residual's gradient)

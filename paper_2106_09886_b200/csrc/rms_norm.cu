@@ -40,17 +40,31 @@ __device__ __forceinline__ float warp_max(float v) {
     return v;
 }
 
-// Over the threads of a row: blockDim.x of them, whole warps.
-template <bool SUM> __device__ __forceinline__ void block_sum_and_max(float &sum, float &most, float (*parts)[32]) {
-    if constexpr (SUM) sum = warp_sum(sum);
+// Over the threads of a row: blockDim.x of them, whole warps.  With two sums a thread, of packs blockDim.x apart, the warps' are added as if
+// each pack had a thread of its own, so that a row's bits do not depend on which form its call takes: the warp's lower lanes end up
+// with its first sum and the upper ones with its second, as warp_sum has them.
+template <bool SUM, int SUMS> __device__ __forceinline__ void block_sum_and_max(float (&sums)[SUMS], float &most, float (*parts)[32]) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    float sum = sums[0];
+    if constexpr (SUM && SUMS == 2) {
+        const float other = __shfl_xor_sync(0xffffffffu, lane < 16 ? sums[1] : sums[0], 16);
+        sum = __fadd_rn(lane < 16 ? sums[0] : sums[1], other);
+#pragma unroll
+        for (int d = 8; d; d >>= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xffffffffu, sum, d));
+    } else if constexpr (SUM) {
+        sum = warp_sum(sum);
+    }
     most = warp_max(most);
     if (blockDim.x > 32) {
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-        if (lane == 0) { parts[0][warp] = sum; parts[1][warp] = most; }
+        if (SUMS == 2 ? (lane & 15) == 0 : lane == 0) parts[0][(lane >> 4) * warps + warp] = sum;
+        if (lane == 0) parts[1][warp] = most;
         __syncthreads();
-        if constexpr (SUM) sum = warp_sum(lane < warps ? parts[0][lane] : 0.0f);
+        if constexpr (SUM) sum = warp_sum(lane < SUMS * warps ? parts[0][lane] : 0.0f);
         most = warp_max(lane < warps ? parts[1][lane] : 0.0f);
+    } else if constexpr (SUM && SUMS == 2) {
+        sum = __fadd_rn(sum, __shfl_xor_sync(0xffffffffu, sum, 16));
     }
+    sums[0] = sum;
 }
 __device__ __forceinline__ float norm_factor(float sum, const NormParams &p) {
     return __frcp_rn(__fsqrt_rn(__fadd_rn(__fdiv_rn(sum, (float)p.width), p.eps)));
@@ -103,9 +117,11 @@ __global__ void __launch_bounds__(NV == 1 ? 1024 : 512, NV == 2 ? 2 : 1) norm_ro
             if (i < packs) out[i] = h[j];
         }
     }
-    float v[NV][V], sum = 0.0f, most = 0.0f;
+    constexpr int SUMS = NV == 2 ? 2 : 1;                           // (NV is 1 or 2 by the number of rows)
+    float v[NV][V], sums[SUMS] = {}, most = 0.0f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
+        float &sum = sums[j % SUMS];
         O::get(h[j], v[j]);
         if constexpr (NORM) {
             float g[V];
@@ -119,10 +135,10 @@ __global__ void __launch_bounds__(NV == 1 ? 1024 : 512, NV == 2 ? 2 : 1) norm_ro
 #pragma unroll
         for (int e = 0; e < V; ++e) most = max_or_nan(most, fabsf(v[j][e]));
     }
-    block_sum_and_max<NORM>(sum, most, parts);
+    block_sum_and_max<NORM>(sums, most, parts);
     float rstd = 1.0f;
     if constexpr (NORM) {
-        rstd = norm_factor(sum, p);
+        rstd = norm_factor(sums[0], p);
         if (p.rstd && threadIdx.x == 0) p.rstd[row] = rstd;
         most = __fmul_rn(most, rstd);
         if (p.y) {
@@ -170,7 +186,8 @@ __global__ void __launch_bounds__(512, NE <= 16 ? 2 : 1) norm_elements_kernel(co
     const T *x = static_cast<const T *>(p.x) + row * p.ldx + first;
     const G *gain = static_cast<const G *>(p.gain) + first;
     T h[NE], r[NE];
-    float v[NE], sum = 0.0f, most = 0.0f;
+    float v[NE], sums[1] = {}, most = 0.0f;
+    float &sum = sums[0];
 #pragma unroll
     for (int j = 0; j < NE; ++j) h[j] = first + j * step < width ? x[j * step] : from_f32<T>(0.0f);
     if (NORM && p.residual) {
@@ -193,7 +210,7 @@ __global__ void __launch_bounds__(512, NE <= 16 ? 2 : 1) norm_elements_kernel(co
         }
         most = max_or_nan(most, fabsf(v[j]));
     }
-    block_sum_and_max<NORM>(sum, most, parts);
+    block_sum_and_max<NORM>(sums, most, parts);
     float rstd = 1.0f;
     if constexpr (NORM) {
         rstd = norm_factor(sum, p);
@@ -227,7 +244,8 @@ __global__ void __launch_bounds__(1024) norm_wide_kernel(const NormParams p) {
     const int64_t row = blockIdx.x;
     const T *x = static_cast<const T *>(p.x) + row * p.ldx;
     const G *gain = static_cast<const G *>(p.gain);
-    float sum = 0.0f, most = 0.0f;
+    float sums[1] = {}, most = 0.0f;
+    float &sum = sums[0];
     if (NORM && p.residual) {
         const T *res = static_cast<const T *>(p.residual) + row * p.ldr;
         T *h = static_cast<T *>(p.h) + row * p.ldh;
@@ -251,7 +269,7 @@ __global__ void __launch_bounds__(1024) norm_wide_kernel(const NormParams p) {
             most = max_or_nan(most, fabsf(a));
         }
     }
-    block_sum_and_max<NORM>(sum, most, parts);
+    block_sum_and_max<NORM>(sums, most, parts);
     float rstd = 1.0f;
     if constexpr (NORM) {
         rstd = norm_factor(sum, p);
