@@ -1,15 +1,11 @@
-// Rows of real numbers as the row-wise kernels (rms_norm.cu, route.cu, i8_gemm.cu) see them: element types, packs of elements
-// that move in one access, and the code of a value in 8 bits.
+// Rows of real numbers as the row-wise kernels (rms_norm.cu, route.cu, i8_gemm.cu) see them: element types, 16 bytes of them in one
+// access, and the code of a value in 8 bits.
 #pragma once
 #include <type_traits>
 #include "g4_format.cuh"
 
 constexpr int64_t ROWS_MAX = (1ll << 31) - 1;      // rows of a call
 
-// N elements that are read and written in one access.
-template <class T, int N> struct alignas(N * sizeof(T)) Pack {
-    T e[N];
-};
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
