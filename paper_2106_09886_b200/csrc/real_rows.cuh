@@ -97,9 +97,11 @@ struct RowScale {
         raised = __fmul_rn(scale, up);
         inverse = finite ? __frcp_rn(raised) : 0.0f;
     }
-    // The code of y as the low byte of a word; any byte where the scale is NaN.
-    __device__ __forceinline__ uint32_t code(float y) const {
-        const float a = __fmul_rn(y, up), q = __fmul_rn(a, inverse), r = __fmaf_rn(-q, raised, a);
+    // The code of y as the low byte of a word; any byte where the scale is NaN.  RAISED: whether the row is one that has to be raised (a
+    // multiplication more for each code, so that rows take their own side of a branch).
+    __device__ __forceinline__ bool is_raised() const { return up != 1.0f; }
+    template <bool RAISED> __device__ __forceinline__ uint32_t code(float y) const {
+        const float a = RAISED ? __fmul_rn(y, up) : y, q = __fmul_rn(a, inverse), r = __fmaf_rn(-q, raised, a);
         return __float_as_uint(__fadd_rn(__fmaf_rn(r, inverse, q), TO_NEAREST));
     }
     // Bytes of codes, zeros where the scale is NaN.

@@ -8,7 +8,7 @@
 // rounding being monotone: the sum of squares and the largest magnitude come out of one pass and one reduction, and the codes follow
 // from the registers by a few multiplications and fused multiply-adds each, without a branch (RowScale): a sum with 1.5 * 2^23 holds
 // the nearest whole number in its low byte.
-// 16384 x 4096 bf16 with a residual take 73 us (470 MB, some of the writes still in L2 at the end), the quantiser of as many 45, decoding 32.
+// 16384 x 4096 bf16 with a residual take 73 us (470 MB, some of the writes still in L2 at the end), the quantiser of as many 44, decoding 32.
 // With a conversion, a clamp and a comparison for each code the norm took 125; with codes by two bounds of the product, and those that
 // the bounds leave open by division out of line, 91; with the product alone, whose codes are not always the quotient's, 72.
 #include "real_rows.cuh"
@@ -34,11 +34,8 @@ __device__ __forceinline__ float warp_sum(float v) {
     for (int d = 16; d; d >>= 1) v = __fadd_rn(v, __shfl_xor_sync(0xffffffffu, v, d));
     return v;
 }
-__device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-    for (int d = 16; d; d >>= 1) v = max_or_nan(v, __shfl_xor_sync(0xffffffffu, v, d));
-    return v;
-}
+// Of magnitudes: their bits are in the numbers' order, NaN's beyond infinity's.
+__device__ __forceinline__ float warp_max(float v) { return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v))); }
 
 // Over the threads of a row: blockDim.x of them, whole warps.  With two sums a thread, of packs blockDim.x apart, the warps' are added as if
 // each pack had a thread of its own, so that a row's bits do not depend on which form its call takes: the warp's lower lanes end up
@@ -86,7 +83,7 @@ template <class T> __device__ __forceinline__ uint4 add_pack(uint4 a, uint4 b) {
 // A row by `blockDim.x` threads (y: rows of a block, more than one for rows of a single warp).  Each thread holds NV packs of 16
 // bytes, as products with the gain.  NORM = false: codes of the rows themselves.
 template <class T, class G, int NV, bool NORM>
-__global__ void __launch_bounds__(NV == 1 ? 1024 : 512, NV == 2 ? 2 : 1) norm_rows_kernel(const NormParams p) {
+__global__ void __launch_bounds__(NV == 1 ? 1024 : 512, NV == 2 ? 3 : 1) norm_rows_kernel(const NormParams p) {
     __shared__ float parts[2][32];
     start_next();
     wait_for_previous();
@@ -157,19 +154,23 @@ __global__ void __launch_bounds__(NV == 1 ? 1024 : 512, NV == 2 ? 2 : 1) norm_ro
         const RowScale s(most);
         if (threadIdx.x == 0) p.scales[row] = s.scale;
         uint32_t *codes = reinterpret_cast<uint32_t *>(p.codes + row * p.ldc);
+        auto encode = [&](auto raised) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int i = threadIdx.x + j * step;
-            uint32_t c[V];
+            for (int j = 0; j < NV; ++j) {
+                const int i = threadIdx.x + j * step;
+                uint32_t c[V];
 #pragma unroll
-            for (int e = 0; e < V; ++e) c[e] = s.code(NORM ? __fmul_rn(v[j][e], rstd) : v[j][e]);
-            if (i < packs) {
-                if constexpr (V == 8)
-                    reinterpret_cast<uint2 *>(codes)[i] = make_uint2(s.word(c[0], c[1], c[2], c[3]), s.word(c[4], c[5], c[6], c[7]));
-                else
-                    codes[i] = s.word(c[0], c[1], c[2], c[3]);
+                for (int e = 0; e < V; ++e) c[e] = s.code<raised>(NORM ? __fmul_rn(v[j][e], rstd) : v[j][e]);
+                if (i < packs) {
+                    if constexpr (V == 8)
+                        reinterpret_cast<uint2 *>(codes)[i] = make_uint2(s.word(c[0], c[1], c[2], c[3]), s.word(c[4], c[5], c[6], c[7]));
+                    else
+                        codes[i] = s.word(c[0], c[1], c[2], c[3]);
+                }
             }
-        }
+        };
+        if (s.is_raised()) encode(std::true_type());
+        else encode(std::false_type());
     }
 }
 
@@ -227,11 +228,15 @@ __global__ void __launch_bounds__(512, NE <= 16 ? 2 : 1) norm_elements_kernel(co
         const RowScale s(most);
         if (threadIdx.x == 0) p.scales[row] = s.scale;
         int8_t *codes = p.codes + row * p.ldc + first;
+        auto encode = [&](auto raised) {
 #pragma unroll
-        for (int j = 0; j < NE; ++j) {
-            const uint32_t c = s.code(NORM ? __fmul_rn(v[j], rstd) : v[j]);
-            if (first + j * step < width) codes[j * step] = (int8_t)(s.inverse != 0.0f ? c : 0u);
-        }
+            for (int j = 0; j < NE; ++j) {
+                const uint32_t c = s.code<raised>(NORM ? __fmul_rn(v[j], rstd) : v[j]);
+                if (first + j * step < width) codes[j * step] = (int8_t)(s.inverse != 0.0f ? c : 0u);
+            }
+        };
+        if (s.is_raised()) encode(std::true_type());
+        else encode(std::false_type());
     }
 }
 
@@ -286,7 +291,7 @@ __global__ void __launch_bounds__(1024) norm_wide_kernel(const NormParams p) {
         float a = to_f32(x[i]);
         if constexpr (NORM) a = __fmul_rn(__fmul_rn(a, to_f32(gain[i])), rstd);
         if (NORM && p.y) y[i] = from_f32<T>(a);
-        if (coded) codes[i] = (int8_t)(s.inverse != 0.0f ? s.code(a) : 0u);
+        if (coded) codes[i] = (int8_t)(s.inverse != 0.0f ? s.code<true>(a) : 0u);
     }
 }
 
