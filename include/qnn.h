@@ -414,6 +414,7 @@ int qnn_i8_plan(int64_t rows, int n, int k, int *tile, int *ranks);
  *   dx = rstd * (dy * gain - u * mean(dy * gain * u)) + dh with u = h * rstd     (also the residual's gradient)
  *   dgain = sum over the rows of dy * u, fp32 [width], added in a fixed order; zeros for rows = 0
  * dx may be dy or dh.  workspace: device scratch owned by the caller, 256-byte aligned, qnn_rms_norm_backward_workspace(...) bytes.
+ * Waits inside its kernels are bounded and reported by qnn_tensor_path_status: where one ran out, dx and dgain are not complete.
  */
 int qnn_rms_norm(const void *x, int type, int64_t rows, int width, int64_t ldx, const void *residual, int64_t ldr, const void *gain,
                  int gain_type, float eps, void *h, int64_t ldh, void *y, int64_t ldy, int8_t *codes, int64_t ldc, float *scales,

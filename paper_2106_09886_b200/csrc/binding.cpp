@@ -1,7 +1,7 @@
-// Tensor arguments of the calls of a decoding step (4-bit weights, rows in 8 bits, norms, routing) -> the C ABI (include/qnn.h): checks, the result's allocation on the current
-// stream, and the call, in one step from Python.  A step of decoding makes these calls for every layer with microseconds of
-// work each; through ctypes the marshalling alone took longer than the small ones run (a call with a new result 10.7 us, of which
-// 2.9 the launch, and 4.5 here; with a result given 8.9 and 3.4).
+// Tensor arguments of the calls of a decoding step (4-bit weights, rows in 8 bits, norms, routing) -> the C ABI (include/qnn.h):
+// checks, the result's allocation on the current stream, and the call, in one step from Python.  A step of decoding makes these
+// calls for every layer with microseconds of work each; through ctypes the marshalling alone took longer than the small ones run
+// (a call with a new result 10.7 us, of which 2.9 the launch, and 4.5 here; with a result given 8.9 and 3.4).
 // Argument marshalling only: every step of the work runs inside libqnn's kernels.
 #include <Python.h>
 
@@ -222,7 +222,8 @@ float float_of(PyObject *o) {
 void *pointer(const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
 
 // The results of one call.  Small ones lie in one allocation, each on 16 bytes: an allocation takes half a microsecond, and a decoding
-// step's results are small.  Large ones have their own, so that none keeps another's memory alive.
+// step's results are small.  One that is kept then keeps the others' memory too, 256 KB at most, and one that is saved is saved with
+// all of it (both: clone it).  Larger ones have allocations of their own.
 class Results {
   public:
     Results(const at::Tensor &like) : like_(like) {}
@@ -537,7 +538,7 @@ PyMethodDef methods[] = {
     {"route", (PyCFunction)(void (*)(void))entry<route, 9>, METH_FASTCALL, nullptr},
     {"route_backward", (PyCFunction)(void (*)(void))entry<route_backward, 6>, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "tensor arguments of the 4-bit-weight calls", -1, methods, nullptr, nullptr, nullptr, nullptr};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "tensor arguments of the calls of a decoding step", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 

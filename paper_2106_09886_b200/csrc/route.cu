@@ -11,9 +11,8 @@
 // nothing depends on the order in which blocks run.  Few tokens: one cluster does it all.
 //
 // Bound: for few tokens the launches and a token's chain of dependent steps (1 x 64 top 6 4.2 us in a replayed graph, 1 x 256 in groups
-// 5.8, 512 x 8 5.4); for many, issue: 16384 x 256 top 8 of four in eight groups take 40 us (28 for the choice), some 1030
-// instructions a token (250 for any, 27 for each 32 experts, 26 for each choice, 18 for each 32 scores with a bias, 230 for the
-// groups), 74 % of the slots.
+// 5.8, 512 x 8 5.4); for many, each warp's own chain: 16384 x 256 top 8 of four in eight groups take 40 us, 28 of them the choice, whose 1100
+// instructions a token fill 55 % of the issue slots, 16 warps an SM waiting on their own results most of the rest.
 #include "real_rows.cuh"
 #include "tc_ptx.cuh"
 

@@ -402,7 +402,7 @@ class G4Weights(NamedTuple):
 
     The calls on them are not joined to torch's autograd: their backward products are calls of their own.  Rows (and alpha, and
     results) that require grad are refused while gradients are recorded; inside an autograd.Function or torch.no_grad() they
-    are not.  Packing takes weights that require grad: codes have no gradient, and the straight-through one goes to the
+    are not.  Ones that carry a forward-mode tangent are refused.  Packing takes weights that require grad: codes have no gradient, and the straight-through one goes to the
     weights that were packed."""
     codes: torch.Tensor      # int32 [experts, ceil(n/128), ceil(k/128), 4, 128, 4]
     scales: torch.Tensor     # uint8 [experts, ceil(n/128), ceil(k/128), 128 // group, 128], 1-4-3 floats
@@ -489,7 +489,8 @@ class I8Rows(NamedTuple):
     """Rows in 8 bits (tokens, or output features of a weight matrix): scales[r] * codes[r, i].  Rows of codes start on 16 bytes; the
     calls that make them lay them out so.  Like the calls on 4-bit weights, those on rows in 8 bits, the norm and the routing are
     not joined to torch's autograd and refuse operands that require grad while gradients are recorded, or carry a forward-mode
-    tangent."""
+    tangent.  Results of one such call that are 256 KB together or less lie in one allocation: keep or save a clone of one where
+    the others' memory is not to be kept or saved with it."""
     codes: torch.Tensor      # int8 [rows, k], rows a multiple of 16 bytes apart
     scales: torch.Tensor     # fp32 [rows]
 
